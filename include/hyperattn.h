@@ -394,6 +394,83 @@ int hyperattn_forward_alg2(const void* Q, const void* K, const void* V, void* ou
                            const ha_shape* shape, const ha_params* params, const ha_alg2_options* options,
                            void* workspace, size_t workspace_bytes, void* stream);
 
+/* Strides of [rows][heads][d] in elements; the d values of a row are consecutive. */
+typedef struct {
+  int64_t row, head;
+} ha_strides;
+
+/* ------------------------------------------------------------------------
+ * A paged cache of K and V in 4 bits, for decoding behind a long prompt.
+ *
+ * Numbers: OCP MX FP4, the 4-bit type that gfx950 converts in one instruction.  32 consecutive channels of a row share a scale 2^(byte - 127)
+ * (E8M0; byte 255: NaN), and a value is a code (E2M1: 0, 1/2, 1, 3/2, 2, 3, 4, 6 and their negatives) times it, exact in bf16.  A
+ * writer takes the smallest scale of 2^-125 ... 2^125 with max |x| <= 6 scale (numbers past 6 * 2^125 count as that) and rounds to the nearest value,
+ * ties to the even code: a number is off by at most max |x| / 3, in the r.m.s. 0.115 of that of normal ones.  32 channels with an Inf or NaN are NaN.
+ * Readers take any byte; values below 2^-126 may count as zeros in attention.
+ *
+ * cache: uint8 [n_pages][Hk][page * (d + d / 16)], 16-byte aligned, n_pages * page < 2^31; page: tokens of a page, 16, 32, 64, 128 or 256.
+ * A page's block of a head (token t, channel c = 32 g + c'):
+ *   K codes  d / 2 bytes a token: 32-bit word (c' / 8) * (d / 32) + g holds the codes of eight channels, channel c in nibble c' % 8
+ *   V codes  for four tokens 4 u ... 4 u + 3 together d / 8 pieces of 16 bytes, a 32-bit word per token: d = 128: word c' / 2, byte g, d = 64: word
+ *            c' / 4, byte 2 g + c' / 2 % 2; the even channel in the low nibble
+ *   K scales d / 32 bytes a token, then V scales d / 32 bytes a token
+ * Slot i of the cache is token i % page of page i / page.
+ *
+ * ha_cache4_write: row i of K and V ([rows][Hk][d] of dtype, strides as above: kv[0] of K, kv[1] of V; NULL: contiguous) to slot slots[i]; rows
+ * whose slot lies outside the cache are left out.  Slots given must differ; where two rows name one slot it holds a mixture of both, and no
+ * other slot is touched.  ha_cache4_read: the rows of these slots back (exact in both types; rows of slots outside the cache: zeros),
+ * for a prefix whose pages are used again. */
+typedef struct {
+  int32_t n_pages, page, Hk, d;
+} ha_cache4;
+
+size_t ha_cache4_bytes(const ha_cache4* cache); /* 0 if it is not a valid one */
+int ha_cache4_write(const void* K, const void* V, const int32_t* slots, void* cache, const ha_cache4* shape, int32_t rows,
+                    int32_t dtype, const ha_strides* kv, void* stream);
+int ha_cache4_read(const void* cache, const int32_t* slots, void* K, void* V, const ha_cache4* shape, int32_t rows, int32_t dtype,
+                   const ha_strides* kv, void* stream);
+
+/* Attention over the cache: the queries of the last q_len tokens of every sequence (1: a decoding step; more: drafted tokens that are
+ * verified together).  Q, out: [n_seq * q_len][Hq][d] of dtype, row s * q_len + i the query of token lens[s] - q_len + i, which sees tokens 0 ... lens[s] -
+ * q_len + i; strides qo[0], qo[1] (NULL: contiguous).  lse: float [Hq][n_seq * q_len].  Token t of sequence s lies in page block_table[s][t / page]
+ * (device int32 [n_seq][max_blocks]).  lens (device int32) are taken within [0, max_blocks * page]; tokens of a page number outside [0, n_pages) count
+ * as absent.  A query that sees nothing has out 0 and lse -inf.  What lies in a page behind a sequence's last token counts for nothing.
+ * Products as in exact_attn_forward: bf16 queries on the matrix cores; fp32 queries split in three, to fp32 accuracy of the cached values.
+ * 1 <= q_len <= 64, n_seq <= 2^16, n_seq * q_len * Hq <= 2^22, Hq * q_len <= 2^15, Hq % Hk == 0, n_seq * max_blocks <= 2^30, max_blocks * page < 2^31.
+ * workspace: device, 256-byte aligned, >= ha_cache4_attn_workspace_bytes(); nothing in it is kept.  Two calls may overlap only with
+ * different workspaces.  Same inputs, same bits. */
+typedef struct {
+  int32_t n_seq, q_len, Hq;
+  int32_t dtype; /* ha_dtype of Q and out */
+  int32_t max_blocks;
+} ha_cache4_query;
+
+int ha_cache4_attn(const void* Q, const void* cache, const int32_t* block_table, const int32_t* lens, void* out, float* lse,
+                   const ha_cache4* shape, const ha_cache4_query* query, const ha_strides* qo, void* workspace,
+                   size_t workspace_bytes, void* stream);
+size_t ha_cache4_attn_workspace_bytes(const ha_cache4* shape, const ha_cache4_query* query); /* 0 if not valid */
+
+/* Block tables and slots, on the GPU from the sequences' lengths: one launch before a step's rows are written.
+ *   lens[s]   tokens that sequence s holds, in pages block_table[s][0 ... ceil(lens / page) - 1]
+ *   add[s]    >= 0: rows that the step appends to it; < 0: it has ended, its pages are free again
+ *   free_pages, free_count   a stack: free_pages[0 ... *free_count - 1]
+ * Pages of sequences that end are put on top of the stack, in order; then every sequence, in order, takes the pages that its new
+ * rows need from the top, into its row of block_table.  A sequence whose rows do not fit max_blocks, `rows` or, counted up to it, the free pages gets
+ * none, unless it needs none: its length stays, and its rows have no slots.
+ *   lens_out[s]     the length after the step (0: ended)
+ *   cu_seqlens[s]   rows of the step before sequence s, [n_seq + 1]: as exact_attn_packed_forward takes them
+ *   slots[i]        slot of row i, i < rows, as ha_cache4_write takes them; -1: none (also behind the last sequence)
+ *   free_count_out  free pages left, free_pages[0 ... *free_count_out - 1]
+ * block_table and free_pages are changed in place; nothing else may overlap.  All device int32.  lens are taken within [0, max_blocks * page].
+ * n_seq <= 8192, rows <= 2^26, n_seq * max_blocks <= 2^30, page as above, n_pages * page < 2^31. */
+typedef struct {
+  int32_t n_seq, max_blocks, page, n_pages, rows;
+} ha_page_plan_shape;
+
+int ha_page_plan(const int32_t* lens, const int32_t* add, int32_t* block_table, int32_t* free_pages, const int32_t* free_count,
+                 int32_t* lens_out, int32_t* cu_seqlens, int32_t* slots, int32_t* free_count_out, const ha_page_plan_shape* shape,
+                 void* stream);
+
 /* Measurement aids (no passage of the paper: they serve the roofline report).
  * Both run on `stream`, time themselves with events and WAIT for the stream;
  * `buf` is caller-owned device memory that they overwrite.

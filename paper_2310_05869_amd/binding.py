@@ -57,6 +57,22 @@ class HyperAttnError(RuntimeError):
         super().__init__(f"{where}: {strerror(status)} (status {status})")
 
 
+class HaStrides(ctypes.Structure):
+    _fields_ = [("row", c_int64), ("head", c_int64)]
+
+
+class HaCache4(ctypes.Structure):
+    _fields_ = [(k, c_int32) for k in ("n_pages", "page", "Hk", "d")]
+
+
+class HaCache4Query(ctypes.Structure):
+    _fields_ = [(k, c_int32) for k in ("n_seq", "q_len", "Hq", "dtype", "max_blocks")]
+
+
+class HaPagePlanShape(ctypes.Structure):
+    _fields_ = [(k, c_int32) for k in ("n_seq", "max_blocks", "page", "n_pages", "rows")]
+
+
 _SIGNATURES = {
     "ha_workspace_layout": (c_int, [POINTER(HaShape), POINTER(HaParams), POINTER(HaWsLayout)]),
     "ha_workspace_bytes": (c_size_t, [POINTER(HaShape), POINTER(HaParams)]),
@@ -96,6 +112,12 @@ _SIGNATURES = {
     "ha_alg2_workspace_bytes": (c_size_t, [POINTER(HaShape), POINTER(HaParams)]),
     "hyperattn_forward_alg2": (c_int, [c_void_p] * 5 + [POINTER(HaShape), POINTER(HaParams), POINTER(HaAlg2Options),
                                                        c_void_p, c_size_t, c_void_p]),
+    "ha_cache4_bytes": (c_size_t, [POINTER(HaCache4)]),
+    "ha_cache4_write": (c_int, [c_void_p] * 4 + [POINTER(HaCache4), c_int32, c_int32, POINTER(HaStrides), c_void_p]),
+    "ha_cache4_read": (c_int, [c_void_p] * 4 + [POINTER(HaCache4), c_int32, c_int32, POINTER(HaStrides), c_void_p]),
+    "ha_cache4_attn": (c_int, [c_void_p] * 6 + [POINTER(HaCache4), POINTER(HaCache4Query), POINTER(HaStrides), c_void_p, c_size_t, c_void_p]),
+    "ha_cache4_attn_workspace_bytes": (c_size_t, [POINTER(HaCache4), POINTER(HaCache4Query)]),
+    "ha_page_plan": (c_int, [c_void_p] * 9 + [POINTER(HaPagePlanShape), c_void_p]),
     "ha_measure_mfma_rate": (c_int, [c_void_p, c_size_t, c_int32, POINTER(c_float), c_void_p]),
     "ha_measure_hbm_rate": (c_int, [c_void_p, c_size_t, POINTER(c_float), POINTER(c_float), c_void_p]),
     "ha_issue_probe_count": (c_int32, []),
@@ -706,3 +728,159 @@ def alg2_workspace_views(workspace, shape: HaShape, params: HaParams):
             "vnorm_w": view(lay.vnorm_w, BH * fwd.n_cov, torch.float64, (BH, fwd.n_cov)),
             "vnorm_samples": view(lay.vnorm_samples, BH * nodes * m, torch.int32, (BH, nodes, m)),
             "vnorm_logw": view(lay.vnorm_logw, BH * nodes * m, torch.float32, (BH, nodes, m))}
+
+
+# ---------------------------------------------------------------- paged 4-bit cache
+# Rows [rows, heads, d] may be slices of a larger tensor: their strides go along.  These calls run on the current device: a launch for another one's
+# tensors is refused here.
+def _stream_for(stream, like):
+    """The stream's handle; `like` and the stream have to be on the current device."""
+    torch = _torch()
+    here = torch.cuda.current_device()
+    if like.device.index != here:
+        raise ValueError(f"tensors are on {like.device}, the current device is cuda:{here}")
+    if stream is not None and stream.device.index != here:
+        raise ValueError(f"the stream is on {stream.device}, the current device is cuda:{here}")
+    return _stream(stream)
+
+
+def _empty(stream, shape, dtype, like):
+    """Memory for a call's results or scratch: from the pool of the stream that the call runs on."""
+    torch = _torch()
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=like.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=like.device)
+
+
+def _rows(t, name, shape, dtype, like):
+    """Strides of a [rows, heads, d] tensor whose rows are whole."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    _expect(t, name, shape, dtype, like)
+    row, head, one = t.stride()
+    if one != 1:
+        raise ValueError(f"the last dimension of {name} must be contiguous, its stride is {one}")
+    return HaStrides(row if shape[0] > 1 else shape[1] * shape[2], head if shape[1] > 1 else shape[2])
+
+
+def _ints(t, name, shape, like):
+    _expect(t, name, shape, _torch().int32, like)
+    return _dev(t, name)
+
+
+def _cache4(cache, page, d=None):
+    """The cache's shape: uint8 [n_pages, Hk, page * (d + d / 16)]."""
+    torch = _torch()
+    if cache.dtype != torch.uint8 or cache.dim() != 3:
+        raise TypeError(f"cache must be uint8 [n_pages, Hk, page * (d + d / 16)], got {cache.dtype} {tuple(cache.shape)}")
+    n_pages, Hk, nbytes = cache.shape
+    of_page = nbytes // page * 16 // 17 if page > 0 else 0
+    if of_page not in (64, 128) or of_page * 17 // 16 * page != nbytes or (d is not None and d != of_page):
+        raise ValueError(f"cache has shape {tuple(cache.shape)}, expected [n_pages, Hk, {page} * (d + d / 16)] with d = {'64 or 128' if d is None else d}")
+    return HaCache4(n_pages, page, Hk, of_page)
+
+
+def ha_cache4_bytes(n_pages, page, Hk, d) -> int:
+    return int(lib().ha_cache4_bytes(ctypes.byref(HaCache4(n_pages, page, Hk, d))))
+
+
+def alloc_cache4(n_pages, page, Hk, d, device="cuda"):
+    """A cache of n_pages pages of `page` tokens, uint8 [n_pages, Hk, page * (d + d / 16)]; its contents are what was there."""
+    if ha_cache4_bytes(max(n_pages, 1), page, Hk, d) == 0:
+        raise HyperAttnError(-3, "alloc_cache4")
+    return _torch().empty((n_pages, Hk, page * (d + d // 16)), dtype=_torch().uint8, device=device)
+
+
+def ha_cache4_write(K, V, slots, cache, page, stream=None):
+    """Rows of K and V ([rows, Hk, d], bf16 or fp32; strided as they lie) into the cache's slots (int32 [rows]; outside the cache: left out)."""
+    if K.dim() != 3:
+        raise ValueError(f"K has shape {tuple(K.shape)}, expected [rows, Hk, d]")
+    rows, Hk, d = K.shape
+    shape = _cache4(cache, page, d)
+    if shape.Hk != Hk:
+        raise ValueError(f"K has {Hk} heads, the cache {shape.Hk}")
+    kv = (HaStrides * 2)(_rows(K, "K", K.shape, K.dtype, cache), _rows(V, "V", K.shape, K.dtype, cache))
+    _check(lib().ha_cache4_write(K.data_ptr(), V.data_ptr(), _ints(slots, "slots", (rows,), cache), _dev(cache, "cache"), ctypes.byref(shape), rows,
+                                 _dtype_code(K), kv, _stream_for(stream, cache)), "ha_cache4_write")
+
+
+def ha_cache4_read(cache, slots, page, dtype=None, K=None, V=None, stream=None):
+    """K, V ([rows, Hk, d]): the rows of the slots (int32 [rows]) as the cache holds them; of slots outside it: zeros."""
+    torch = _torch()
+    shape = _cache4(cache, page)
+    rows = slots.shape[0]
+    if K is not None:
+        dtype = K.dtype
+    elif V is not None:
+        dtype = V.dtype
+    elif dtype is None:
+        dtype = torch.bfloat16
+    full = (rows, shape.Hk, shape.d)
+    handle = _stream_for(stream, cache)
+    K = _empty(stream, full, dtype, cache) if K is None else K
+    V = _empty(stream, full, dtype, cache) if V is None else V
+    kv = (HaStrides * 2)(_rows(K, "K", full, dtype, cache), _rows(V, "V", full, dtype, cache))
+    _check(lib().ha_cache4_read(_dev(cache, "cache"), _ints(slots, "slots", (rows,), cache), K.data_ptr(), V.data_ptr(), ctypes.byref(shape), rows,
+                                _dtype_code(K), kv, handle), "ha_cache4_read")
+    return K, V
+
+
+def ha_cache4_attn_workspace_bytes(cache, page, n_seq, q_len, Hq, max_blocks, dtype=None) -> int:
+    code = HA_BF16 if dtype is None else _dtype_code(_torch().empty((), dtype=dtype))
+    return int(lib().ha_cache4_attn_workspace_bytes(ctypes.byref(_cache4(cache, page)), ctypes.byref(HaCache4Query(n_seq, q_len, Hq, code, max_blocks))))
+
+
+def ha_cache4_attn(Q, cache, block_table, lens, page, q_len=1, out=None, lse=None, workspace=None, stream=None):
+    """out, lse: attention of the last q_len tokens of every sequence over its pages.  Q [n_seq * q_len, Hq, d] (bf16 or fp32; strided as it lies),
+    block_table int32 [n_seq, max_blocks], lens int32 [n_seq], the tokens that the cache holds of a sequence, those of the queries among them.
+    lse: float32 [Hq, n_seq * q_len]."""
+    torch = _torch()
+    if Q.dim() != 3:
+        raise ValueError(f"Q has shape {tuple(Q.shape)}, expected [n_seq * q_len, Hq, d]")
+    rows, Hq, d = Q.shape
+    shape = _cache4(cache, page, d)
+    if block_table.dim() != 2 or rows != block_table.shape[0] * q_len:
+        raise ValueError(f"Q has {rows} rows, the block table {tuple(block_table.shape)}, q_len is {q_len}")
+    n_seq, max_blocks = block_table.shape
+    query = HaCache4Query(n_seq, q_len, Hq, _dtype_code(Q), max_blocks)
+    handle = _stream_for(stream, cache)
+    if out is None:
+        out = _empty(stream, (rows, Hq, d), Q.dtype, Q)
+    if lse is None:
+        lse = _empty(stream, (Hq, rows), torch.float32, Q)
+    _expect_f32(cache, (Hq, rows), lse=lse)
+    qo = (HaStrides * 2)(_rows(Q, "Q", Q.shape, Q.dtype, cache), _rows(out, "out", Q.shape, Q.dtype, cache))
+    if workspace is None:
+        workspace = _empty(stream, (int(lib().ha_cache4_attn_workspace_bytes(ctypes.byref(shape), ctypes.byref(query))),), torch.uint8, Q)
+    _check(lib().ha_cache4_attn(Q.data_ptr(), _dev(cache, "cache"), _ints(block_table, "block_table", block_table.shape, cache),
+                                _ints(lens, "lens", (n_seq,), cache), out.data_ptr(), _dev(lse, "lse"), ctypes.byref(shape), ctypes.byref(query), qo,
+                                _dev(workspace, "workspace"), workspace.numel(), handle), "ha_cache4_attn")
+    return out, lse
+
+
+def ha_page_plan(lens, add, block_table, free_pages, free_count, page, rows=None, lens_out=None, cu_seqlens=None, slots=None, free_count_out=None,
+                 stream=None):
+    """(lens_out, cu_seqlens, slots, free_count_out): pages for the rows that a step appends to its sequences (add int32 [n_seq]; < 0: the sequence has ended
+    and its pages are free again).  lens int32 [n_seq]; block_table int32 [n_seq, max_blocks] and free_pages int32 [n_pages] change in place; free_count
+    int32 [1].  rows: how many slots there are (or `slots` int32 [rows] itself)."""
+    torch = _torch()
+    if block_table.dim() != 2 or free_pages.dim() != 1:
+        raise ValueError(f"block_table has shape {tuple(block_table.shape)}, expected [n_seq, max_blocks]; free_pages {tuple(free_pages.shape)}, expected [n_pages]")
+    n_seq, max_blocks = block_table.shape
+    if slots is None and rows is None:
+        raise ValueError("ha_page_plan needs rows or slots")
+    rows = slots.shape[0] if slots is not None else rows
+    i32, handle = torch.int32, _stream_for(stream, block_table)
+    lens_out = _empty(stream, (n_seq,), i32, lens) if lens_out is None else lens_out
+    cu_seqlens = _empty(stream, (n_seq + 1,), i32, lens) if cu_seqlens is None else cu_seqlens
+    slots = _empty(stream, (rows,), i32, lens) if slots is None else slots
+    free_count_out = _empty(stream, (1,), i32, lens) if free_count_out is None else free_count_out
+    like = block_table
+    shape = HaPagePlanShape(n_seq, max_blocks, page, free_pages.shape[0], rows)
+    _check(lib().ha_page_plan(_ints(lens, "lens", (n_seq,), like), _ints(add, "add", (n_seq,), like), _ints(block_table, "block_table", block_table.shape, like),
+                              _ints(free_pages, "free_pages", free_pages.shape, like), _ints(free_count, "free_count", (1,), like),
+                              _ints(lens_out, "lens_out", (n_seq,), like), _ints(cu_seqlens, "cu_seqlens", (n_seq + 1,), like),
+                              _ints(slots, "slots", (rows,), like), _ints(free_count_out, "free_count_out", (1,), like), ctypes.byref(shape), handle),
+           "ha_page_plan")
+    return lens_out, cu_seqlens, slots, free_count_out

@@ -19,7 +19,8 @@ BUILD = os.path.join(CSRC, "_build")
 LIB = os.path.join(HERE, "libhyperattn.so")
 
 SOURCES = ["api.hip", "lsh_hash.hip", "lsh_hash_mfma.hip", "seg_sort.hip", "stage_kernels.hip", "attn_mfma.hip", "attn_f32.hip",
-           "calib.hip", "attn_bwd_mfma.hip", "attn_bwd_f32.hip", "bwd_kernels.hip", "alg2_kernels.hip", "alg2_mfma.hip"]
+           "calib.hip", "attn_bwd_mfma.hip", "attn_bwd_f32.hip", "bwd_kernels.hip", "alg2_kernels.hip", "alg2_mfma.hip",
+           "page_plan.hip", "cache4_rows.hip", "cache4_attn.hip", "cache_api.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -40,13 +40,6 @@ namespace ha {
 
 static size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Tensors and float arrays are accessed 16 bytes at a time; index arrays 4 bytes at a time.
-static bool misaligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
-template <typename... P>
-static bool any_misaligned16(P... ptrs) { return (misaligned(ptrs, 16) || ...); }
-template <typename... P>
-static bool any_misaligned4(P... ptrs) { return (misaligned(ptrs, 4) || ...); }
-
 static int make_geometry(const ha_shape* sh, const ha_params* p, Geometry* g) {
   if (!sh || !p) return HA_ERR_NULL;
   if (sh->dtype != HA_BF16 && sh->dtype != HA_FP32) return HA_ERR_DTYPE;

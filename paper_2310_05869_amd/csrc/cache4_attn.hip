@@ -1,0 +1,488 @@
+// Attention of each sequence's last tokens over its pages of the 4-bit cache (ha_cache4_attn).
+//
+// One pass over the keys with a running reference and sum of the softmax.  What bounds it is the cache's bytes: a query row costs four flops per cached
+// value that 4.25 bits are read for, so a wave keeps 16 query rows (the query heads of one key head, times the tokens of the call) and turns
+// codes into bf16 operands in registers, never through LDS:
+//   * S^T = K Q^T by v_mfma_f32_16x16x32_bf16: tokens run along M, query rows along N, and one product takes one group of 32 channels.  K's words lie
+//     as that operand wants them; v_cvt_scalef32_pk_bf16_fp4 makes two bf16 values of a byte, scale included, and the values are exact.
+//   * the accumulators, exponentiated, are the B operand of O^T += V^T P^T: a lane's eight contraction elements are its four tokens of
+//     two runs of 16, which is how V's words lie.  A conversion yields two channels of one token, two byte permutations make two tokens of
+//     one channel each of two such.
+// So per 16 tokens of d = 128 and lane: 32 conversions, 16 permutations, 20 for scales, and some 20 for the softmax, against 2176 bytes.
+//
+// Split: the tokens of all sequences, in units of 64 (one wave's step), are one line, cut into `parts` equal runs, a workgroup of four waves each per key
+// head and tile of 16 query rows: however unlike the sequences' lengths are, every workgroup has the same to read.  The waves of a workgroup take the
+// units of a sequence in turn and merge through LDS; a sequence that lies in one workgroup is finished there, the others' parts go to the
+// workspace and are joined by a second launch.
+#include "attn_common.h"
+#include "cache4_common.h"
+
+namespace ha {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kCWaves = 4, kCThreads = 64 * kCWaves;
+constexpr int kUnit = 64;        // tokens of a wave's step
+constexpr int kTilesPerUnit = 4; // of 16 tokens
+constexpr int kCRows = 16;       // query rows of a workgroup
+
+// Units of all sequences before s (exclusive), found by one wave: lane l sums a run of sequences.
+__device__ inline int seq_len(const CacheAttnArgs& a, int s) { return min(max(a.lens[s], 0), a.max_blocks << a.c.log_page); }
+__device__ inline int seq_units(const CacheAttnArgs& a, int s) { return (seq_len(a, s) + kUnit - 1) / kUnit; }
+
+// The total of units and, for unit `u` of the line (u < total), its sequence and the units before that sequence.  Wave-uniform results.
+__device__ inline int units_total(const CacheAttnArgs& a, int lane, int* before) {
+  const int each = (a.n_seq + 63) / 64, s0 = min(a.n_seq, lane * each), s1 = min(a.n_seq, s0 + each);
+  int sum = 0;
+  for (int s = s0; s < s1; ++s) sum += seq_units(a, s);
+  int inc = sum;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int up = __shfl_up(inc, o);
+    if (lane >= o) inc += up;
+  }
+  *before = inc - sum;
+  return __builtin_amdgcn_readfirstlane(__shfl(inc, 63));
+}
+__device__ inline int find_unit(const CacheAttnArgs& a, int lane, int before, int u, int* seq_first) {
+  const int each = (a.n_seq + 63) / 64;
+  // the last lane whose run starts at or before u (runs without units start where the next one does)
+  const unsigned long long le = __ballot(before <= u);
+  const int run = 63 - __builtin_clzll(le);
+  int at = __builtin_amdgcn_readfirstlane(__shfl(before, run));
+  int s = run * each;
+  for (; s < a.n_seq - 1; ++s) {
+    const int n = seq_units(a, s);
+    if (u < at + n) break;
+    at += n;
+  }
+  *seq_first = at;
+  return __builtin_amdgcn_readfirstlane(s);
+}
+
+// 16 tokens' raw words
+template <int D>
+struct RawTile {
+  uint32_t k[D / 32];
+  uint32_t v[4];        // a token's word each
+  uint32_t ks;          // the token's scales, a byte per group
+  uint32_t vs[D == 128 ? 4 : 2];  // of the lane's four tokens
+};
+
+template <int SPLIT>
+struct Weights {
+  uint32_t w[SPLIT][4];  // eight tokens in bf16: parts of each weight, the largest first
+};
+
+// SPLIT: parts of a query number and of a weight: 1 for bf16 queries, 3 for fp32 ones (24 bits); cached values have one.
+template <int D, int SPLIT>
+__global__ __launch_bounds__(kCThreads, SPLIT == 1 ? 3 : 2) void cache4_attn_kernel(CacheAttnArgs a) {
+  constexpr int G = D / 32;     // groups of channels, products per score
+  constexpr int MT = D / 16;    // tiles of 16 channels of the output
+  constexpr bool F32 = SPLIT > 1;
+  __shared__ float merge_o[kCWaves][kCRows][D + 4];
+  __shared__ float merge_m[kCWaves][kCRows], merge_l[kCWaves][kCRows];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, kq = lane >> 4;
+  const int hk = blockIdx.y % a.c.Hk, tile = blockIdx.y / a.c.Hk;
+
+  int before;
+  const int total = units_total(a, lane, &before);
+  const int part = blockIdx.x, parts = min(a.parts, total);  // (none of them empty: those of a sequence are joined from its first to its last)
+  if (part >= parts) return;
+  const int u0 = (int)((int64_t)total * part / parts), u1 = (int)((int64_t)total * (part + 1) / parts);
+  int seq_first;
+  int s = find_unit(a, lane, before, u0, &seq_first);
+
+  const int row = tile * kCRows + r;                   // query row within the key head
+  const int row_use = row < a.rows ? row : 0;
+  const int q_tok = row_use / a.group, q_head = hk * a.group + row_use % a.group;
+
+  const int64_t page_bytes = (int64_t)a.c.Hk * a.c.block_bytes();
+  const unsigned char* head_base = a.cache + (int64_t)hk * a.c.block_bytes();
+  const int log_page = a.c.log_page, in_page = a.c.page - 1;
+
+  int u = u0;
+  while (u < u1) {
+    const int len = seq_len(a, s);
+    const int n_units = (len + kUnit - 1) / kUnit;
+    const int first = u - seq_first, last = min(u1 - seq_first, n_units);  // units of the sequence that are this workgroup's
+    const int32_t* blocks = a.table + (int64_t)s * a.max_blocks;
+    const int last_block = (len - 1) >> log_page;
+
+    bf16x8 q[SPLIT][G];
+    {
+      const int64_t at = ((int64_t)s * a.q_len + q_tok) * a.q.row + (int64_t)q_head * a.q.head + 8 * kq;
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        if constexpr (!F32) {
+          q[0][g] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(a.Q) + at + 32 * g));
+        } else {
+          const f32x4* p = reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(a.Q) + at + 32 * g);
+          const f32x4 x0 = p[0], x1 = p[1];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            float x = 0.5f * (i < 4 ? x0[i % 4] : x1[i % 4]);  // (at half: rounding the first part up leaves the largest finite)
+#pragma unroll
+            for (int z = 0; z < SPLIT; ++z) {
+              q[z][g][i] = (__bf16)x;
+              x -= (float)q[z][g][i];
+            }
+          }
+        }
+      }
+    }
+    const int limit = len - a.q_len + 1 + q_tok;  // tokens that the lane's row sees
+    const int all_see = len - a.q_len + 1;        // that every row sees
+
+    RawTile<D> raw[kTilesPerUnit];
+    int page_of[kTilesPerUnit];
+    auto find_pages = [&](int unit) {
+#pragma unroll
+      for (int t = 0; t < kTilesPerUnit; ++t) page_of[t] = blocks[min((unit * kUnit + 16 * t) >> log_page, last_block)];
+    };
+    auto tile_base = [&](int unit, int t, bool* there) {  // the page's block, and whether the page exists
+      const int p = __builtin_amdgcn_readfirstlane(page_of[t]);
+      *there = (unsigned)p < (unsigned)a.c.n_pages;
+      return head_base + (int64_t)(*there ? p : 0) * page_bytes;
+    };
+    auto load_k = [&](int unit) {
+#pragma unroll
+      for (int t = 0; t < kTilesPerUnit; ++t) {
+        bool there;
+        const unsigned char* b = tile_base(unit, t, &there);
+        const int tok = (unit * kUnit + 16 * t) & in_page;
+        const unsigned char* kp = b + (tok + r) * (D / 2) + kq * (D / 8);
+        if constexpr (D == 128) {
+          const u32x4 w = *reinterpret_cast<const u32x4*>(kp);
+#pragma unroll
+          for (int g = 0; g < G; ++g) raw[t].k[g] = w[g];
+          raw[t].ks = *reinterpret_cast<const uint32_t*>(b + a.c.k_scale_at() + (tok + r) * 4);
+        } else {
+          const u32x2 w = *reinterpret_cast<const u32x2*>(kp);
+#pragma unroll
+          for (int g = 0; g < G; ++g) raw[t].k[g] = w[g];
+          raw[t].ks = *reinterpret_cast<const uint16_t*>(b + a.c.k_scale_at() + (tok + r) * 2);
+        }
+      }
+    };
+    auto load_v = [&](int unit) {
+#pragma unroll
+      for (int t = 0; t < kTilesPerUnit; ++t) {
+        bool there;
+        const unsigned char* b = tile_base(unit, t, &there);
+        const int tok = (unit * kUnit + 16 * t) & in_page;
+        const u32x4 w = *reinterpret_cast<const u32x4*>(b + a.c.v_at() + ((tok >> 2) + kq) * (D * 2) + (D == 128 ? r : r >> 1) * 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) raw[t].v[i] = w[i];
+        if constexpr (D == 128) {
+          const u32x4 sc = *reinterpret_cast<const u32x4*>(b + a.c.v_scale_at() + (tok + 4 * kq) * 4);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) raw[t].vs[i] = sc[i];
+        } else {
+          const u32x2 sc = *reinterpret_cast<const u32x2*>(b + a.c.v_scale_at() + (tok + 4 * kq) * 2);
+          raw[t].vs[0] = sc[0];
+          raw[t].vs[1] = sc[1];
+        }
+      }
+    };
+
+    f32x4 o[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) o[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    // reference of the exponentials, moved (and the sums rescaled) where a row's scores exceed it by more than 8; log2 domain for bf16
+    // queries, natural for fp32 ones; l: this lane's share of the row sum
+    float m = -INFINITY, l = 0.f;
+    constexpr float unit_of = F32 ? 2.f : kLog2e;
+
+    int unit = first + wave;
+    if (unit < last) {
+      find_pages(unit);
+      load_k(unit);
+      load_v(unit);
+    }
+    for (; unit < last; unit += kCWaves) {
+      const int next = unit + kCWaves;
+      const bool more = next < last;
+      bool there[kTilesPerUnit];
+#pragma unroll
+      for (int t = 0; t < kTilesPerUnit; ++t) there[t] = (unsigned)__builtin_amdgcn_readfirstlane(page_of[t]) < (unsigned)a.c.n_pages;
+      if (more) find_pages(next);
+
+      // ---- scores ----
+      f32x4 c[kTilesPerUnit];
+#pragma unroll
+      for (int t = 0; t < kTilesPerUnit; ++t) {
+        c[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          const float sc = __uint_as_float(g < 3 ? raw[t].ks << (23 - 8 * g) : raw[t].ks >> 1);  // (the exponent alone counts)
+          const uint32_t w = raw[t].k[g];
+          u32x4 f;
+          f[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc, 0));
+          f[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc, 1));
+          f[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc, 2));
+          f[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc, 3));
+#pragma unroll
+          for (int z = SPLIT - 1; z >= 0; --z)
+            c[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), q[z][g], c[t], 0, 0, 0);
+        }
+      }
+      if (more) load_k(next);
+
+      // ---- masks: tokens behind the row's own, behind the sequence, of pages that are not there ----
+      const int base = unit * kUnit;
+      bool special = base + kUnit > all_see;
+#pragma unroll
+      for (int t = 0; t < kTilesPerUnit; ++t) special = special || !there[t];
+      if (special) {
+#pragma unroll
+        for (int t = 0; t < kTilesPerUnit; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int tok = base + 16 * t + 4 * kq + i;
+            if (!there[t] || tok >= limit) c[t][i] = -INFINITY;
+            if (!there[t] || tok >= len) {  // whatever lies there: weight 0 times a NaN would be NaN
+              raw[t].v[i] = 0;
+              if (D == 128) raw[t].vs[i % (D / 32)] = 0;
+              else raw[t].vs[i / 2] &= i & 1 ? 0x0000ffffu : 0xffff0000u;
+            }
+          }
+      }
+
+      // ---- weights ----
+      float mx = fmaxf(fmaxf(c[0][0], c[0][1]), fmaxf(c[0][2], c[0][3]));
+#pragma unroll
+      for (int t = 1; t < kTilesPerUnit; ++t) mx = fmaxf(mx, fmaxf(fmaxf(c[t][0], c[t][1]), fmaxf(c[t][2], c[t][3])));
+      mx *= unit_of;
+      if (__any(mx > m + (F32 ? 5.5f : 8.f))) {
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float m_new = fmaxf(m, mx), ref = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = F32 ? expf(m - ref) : __builtin_amdgcn_exp2f(m - ref);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) o[i] *= alpha;
+        l *= alpha;
+        m = m_new;
+      }
+      const float ref = m == -INFINITY ? 0.f : m;
+      Weights<SPLIT> p[kTilesPerUnit / 2];
+#pragma unroll
+      for (int t = 0; t < kTilesPerUnit; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+          float x0, x1;
+          if constexpr (F32) {
+            x0 = exp_split(__builtin_fmaf(c[t][i], unit_of, -ref));
+            x1 = exp_split(__builtin_fmaf(c[t][i + 1], unit_of, -ref));
+          } else {
+            x0 = __builtin_amdgcn_exp2f(__builtin_fmaf(c[t][i], unit_of, -ref));
+            x1 = __builtin_amdgcn_exp2f(__builtin_fmaf(c[t][i + 1], unit_of, -ref));
+          }
+          l += x0 + x1;
+#pragma unroll
+          for (int z = 0; z < SPLIT; ++z) {
+            const uint32_t w = pack_bf16x2(x0, x1);
+            p[t / 2].w[z][2 * (t % 2) + i / 2] = w;
+            if (z + 1 < SPLIT) {
+              x0 -= __uint_as_float(w << 16);
+              x1 -= __uint_as_float(w & 0xffff0000u);
+            }
+          }
+        }
+
+      // ---- O^T += V^T P^T, two runs of 16 tokens at a time ----
+#pragma unroll
+      for (int pr = 0; pr < kTilesPerUnit / 2; ++pr) {
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          u32x4 f[2];  // the group's even and odd channels of the lane, eight tokens each
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            const RawTile<D>& t = raw[2 * pr + half];
+            uint32_t x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              float sc;
+              uint32_t b;
+              if constexpr (D == 128) {
+                sc = __uint_as_float(g < 3 ? t.vs[i] << (23 - 8 * g) : t.vs[i] >> 1);
+                if (g == 0) b = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(t.v[i], sc, 0));
+                else if (g == 1) b = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(t.v[i], sc, 1));
+                else if (g == 2) b = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(t.v[i], sc, 2));
+                else b = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(t.v[i], sc, 3));
+              } else {
+                const int byte = 2 * (i & 1) + g;   // of the word with the scales of tokens i & ~1 and behind
+                sc = __uint_as_float(byte < 3 ? t.vs[i / 2] << (23 - 8 * byte) : t.vs[i / 2] >> 1);
+                const uint32_t w = t.v[i] >> (8 * (r & 1));
+                if (g == 0) b = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc, 0));
+                else b = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc, 2));
+              }
+              x[i] = b;
+            }
+            f[0][2 * half] = __builtin_amdgcn_perm(x[1], x[0], 0x05040100u);
+            f[0][2 * half + 1] = __builtin_amdgcn_perm(x[3], x[2], 0x05040100u);
+            f[1][2 * half] = __builtin_amdgcn_perm(x[1], x[0], 0x07060302u);
+            f[1][2 * half + 1] = __builtin_amdgcn_perm(x[3], x[2], 0x07060302u);
+          }
+#pragma unroll
+          for (int e = 0; e < 2; ++e)
+#pragma unroll
+            for (int z = SPLIT - 1; z >= 0; --z) {
+              const u32x4 w = {p[pr].w[z][0], p[pr].w[z][1], p[pr].w[z][2], p[pr].w[z][3]};
+              o[2 * g + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f[e]), __builtin_bit_cast(bf16x8, w), o[2 * g + e], 0, 0, 0);
+            }
+        }
+      }
+      if (more) load_v(next);
+    }
+
+    // ---- the waves' sums through LDS.  Lane (r, kq), register i of o[2 g + e]: query row r, channel 32 g + 8 kq + 2 i + e ----
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (kq == 0) {
+      merge_m[wave][r] = m;
+      merge_l[wave][r] = l;
+    }
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      float* at = &merge_o[wave][r][32 * g + 8 * kq];
+      *reinterpret_cast<f32x4*>(at) = (f32x4){o[2 * g][0], o[2 * g + 1][0], o[2 * g][1], o[2 * g + 1][1]};
+      *reinterpret_cast<f32x4*>(at + 4) = (f32x4){o[2 * g][2], o[2 * g + 1][2], o[2 * g][3], o[2 * g + 1][3]};
+    }
+    __syncthreads();
+    const bool whole = first == 0 && last == n_units;
+    constexpr int LPR = D / 4;
+    for (int idx = threadIdx.x; idx < kCRows * LPR; idx += kCThreads) {
+      const int rr = idx / LPR, ch = (idx % LPR) * 4;
+      const int rw = tile * kCRows + rr;
+      if (rw >= a.rows) break;
+      float top = merge_m[0][rr];
+#pragma unroll
+      for (int w = 1; w < kCWaves; ++w) top = fmaxf(top, merge_m[w][rr]);
+      const float ref = top == -INFINITY ? 0.f : top;
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+      float sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < kCWaves; ++w) {
+        const float wt = F32 ? expf(merge_m[w][rr] - ref) : __builtin_amdgcn_exp2f(merge_m[w][rr] - ref);
+        sum += wt * merge_l[w][rr];
+        acc += wt * *reinterpret_cast<const f32x4*>(&merge_o[w][rr][ch]);
+      }
+      if (whole) {
+        const bool empty = sum == 0.f;
+        const float inv = empty ? 0.f : 1.f / sum;
+        acc *= inv;
+        const int64_t orow = (int64_t)s * a.q_len + rw / a.group;
+        const int head = hk * a.group + rw % a.group;
+        const int64_t at = orow * a.o.row + (int64_t)head * a.o.head + ch;
+        if constexpr (F32) *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.out) + at) = acc;
+        else *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(a.out) + at) = (u32x2){pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3])};
+        if (ch == 0)
+          a.lse[(int64_t)head * a.n_seq * a.q_len + orow] = empty ? -INFINITY : F32 ? top + logf(sum) : (top + log2f(sum)) * kLn2;
+      } else {
+        const int64_t slot = ((int64_t)blockIdx.y * (a.parts + a.n_seq) + part + s) * kCRows + rr;
+        *reinterpret_cast<f32x4*>(a.part_o + slot * D + ch) = acc;
+        if (ch == 0) {
+          a.part_ml[2 * slot] = top;
+          a.part_ml[2 * slot + 1] = sum;
+        }
+      }
+    }
+    if (blockIdx.y == 0 && threadIdx.x == 0) {
+      if (first == 0) a.span[2 * s] = part;
+      if (last == n_units) a.span[2 * s + 1] = part;
+    }
+    u = seq_first + last;
+    if (u >= u1) break;
+    __syncthreads();
+    seq_first += n_units;
+    do ++s;
+    while (seq_units(a, s) == 0);  // (a unit follows)
+  }
+}
+
+// Joins the parts of a query row, or writes the result of one that sees nothing: a workgroup per row.
+template <int D, int SPLIT>
+__global__ __launch_bounds__(kCThreads) void cache4_join_kernel(CacheAttnArgs a) {
+  constexpr bool F32 = SPLIT > 1;
+  constexpr int LPR = D / 4, PAR = kCThreads / LPR;  // lanes per row, parts at a time
+  __shared__ f32x4 sum_o[PAR][LPR];
+  __shared__ float sum_l[PAR], sum_m[PAR];
+  const int s = blockIdx.x, hq = blockIdx.y % a.Hq, tok = blockIdx.y / a.Hq;
+  const int len = seq_len(a, s);
+  const int hk = hq / a.group, row = tok * a.group + hq % a.group, tile = row / kCRows, rr = row % kCRows;
+  const int64_t orow = (int64_t)s * a.q_len + tok;
+  const int lane = threadIdx.x % LPR, at_part = threadIdx.x / LPR, ch = lane * 4;
+  int p0 = 0, p1 = -1;
+  if (len > 0) {
+    p0 = a.span[2 * s];
+    p1 = a.span[2 * s + 1];
+    if (p0 == p1) return;  // finished where its tokens were read
+  }
+  const int64_t slot0 = ((int64_t)(tile * a.c.Hk + hk) * (a.parts + a.n_seq) + s) * kCRows + rr;
+  float m = -INFINITY, l = 0.f;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int p = p0 + at_part; p <= p1; p += PAR) {
+    const int64_t slot = slot0 + (int64_t)p * kCRows;
+    const float pm = a.part_ml[2 * slot], pl = a.part_ml[2 * slot + 1];
+    const f32x4 v = *reinterpret_cast<const f32x4*>(a.part_o + slot * D + ch);
+    const float top = fmaxf(m, pm), ref = top == -INFINITY ? 0.f : top;
+    const float w0 = F32 ? expf(m - ref) : __builtin_amdgcn_exp2f(m - ref), w1 = F32 ? expf(pm - ref) : __builtin_amdgcn_exp2f(pm - ref);
+    acc = acc * w0 + v * w1;
+    l = l * w0 + pl * w1;
+    m = top;
+  }
+  sum_o[at_part][lane] = acc;
+  if (lane == 0) {
+    sum_m[at_part] = m;
+    sum_l[at_part] = l;
+  }
+  __syncthreads();
+  if (at_part != 0) return;
+  float top = m;
+#pragma unroll
+  for (int i = 1; i < PAR; ++i) top = fmaxf(top, sum_m[i]);
+  const float ref = top == -INFINITY ? 0.f : top;
+  acc = (f32x4){0.f, 0.f, 0.f, 0.f};
+  l = 0.f;
+#pragma unroll
+  for (int i = 0; i < PAR; ++i) {
+    const float w = F32 ? expf(sum_m[i] - ref) : __builtin_amdgcn_exp2f(sum_m[i] - ref);
+    acc += w * sum_o[i][lane];
+    l += w * sum_l[i];
+  }
+  const bool empty = l == 0.f;
+  acc *= empty ? 0.f : 1.f / l;
+  const int64_t at = orow * a.o.row + (int64_t)hq * a.o.head + ch;
+  if constexpr (F32) *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.out) + at) = acc;
+  else *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(a.out) + at) = (u32x2){pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3])};
+  if (lane == 0) a.lse[(int64_t)hq * a.n_seq * a.q_len + orow] = empty ? -INFINITY : F32 ? top + logf(l) : (top + log2f(l)) * kLn2;
+}
+
+// Workgroups that share a key head's tokens: three fit a CU, 768 the chip at once.
+int cache4_parts(int Hk, int tiles) {
+  const int heads = Hk * tiles;
+  return heads >= 768 ? 1 : 768 / heads;
+}
+
+template <int D, int SPLIT>
+static int launch_attn_form(const CacheAttnArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL((cache4_attn_kernel<D, SPLIT>), dim3((unsigned)a.parts, (unsigned)(a.c.Hk * a.tiles)), dim3(kCThreads), 0, st, a);
+  const int rc = check_launch();
+  if (rc != HA_OK) return rc;
+  hipLaunchKernelGGL((cache4_join_kernel<D, SPLIT>), dim3((unsigned)a.n_seq, (unsigned)(a.Hq * a.q_len)), dim3(kCThreads), 0, st, a);
+  return check_launch();
+}
+
+int launch_cache4_attn(const CacheAttnArgs& a, int dtype, hipStream_t st) {
+  if (a.c.d == 128) return dtype == HA_BF16 ? launch_attn_form<128, 1>(a, st) : launch_attn_form<128, 3>(a, st);
+  return dtype == HA_BF16 ? launch_attn_form<64, 1>(a, st) : launch_attn_form<64, 3>(a, st);
+}
+
+}  // namespace ha

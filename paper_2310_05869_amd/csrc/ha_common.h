@@ -186,6 +186,13 @@ int launch_merge_unpermute(const float* o_b, const float* lse_b, const float* o_
                            const int32_t* perm_q, void* out, float* lse, int groups, int n, int d, int dtype,
                            hipStream_t st);
 
+// Tensors and float arrays are accessed 16 bytes at a time; index arrays 4 bytes at a time.
+inline bool misaligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) != 0; }
+template <typename... P>
+inline bool any_misaligned16(P... ptrs) { return (misaligned(ptrs, 16) || ...); }
+template <typename... P>
+inline bool any_misaligned4(P... ptrs) { return (misaligned(ptrs, 4) || ...); }
+
 inline int check_launch() { return hipGetLastError() == hipSuccess ? HA_OK : HA_ERR_LAUNCH; }
 
 // Lets kernel `fn` use up to 160 KiB of dynamic LDS on the current device.  The
