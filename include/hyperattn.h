@@ -394,10 +394,44 @@ int hyperattn_forward_alg2(const void* Q, const void* K, const void* V, void* ou
                            const ha_shape* shape, const ha_params* params, const ha_alg2_options* options,
                            void* workspace, size_t workspace_bytes, void* stream);
 
-/* Strides of [rows][heads][d] in elements; the d values of a row are consecutive. */
+/* ------------------------------------------------------------------------
+ * Packed sequences: exact attention (as exact_attn_forward / exact_attn_backward) over sequences of different lengths that lie
+ * one behind the other in one batch of rows, with grouped heads.  Sequence s owns rows [cu_seqlens[s], cu_seqlens[s + 1]) of all
+ * tensors; a row sees the keys of its own sequence, causal: those up to itself.  Query head h reads key head h / (Hq / Hk); dK and
+ * dV are summed over the query heads of a group.
+ *
+ * Tensors are [rows][heads][d] with the strides given (elements; the d values of a row are consecutive), so that slices of one
+ * projection's output are taken as they lie; strides == NULL: contiguous.  Strides are multiples of 16 bytes; row strides are
+ * at least d and at most 2^22, and so are head strides of what is written at least d.  lse: float [Hq][rows], out_f32: float [rows][Hq][d] contiguous (bf16 tensors; may be NULL).
+ * cu_seqlens: device int32 [n_seq + 1], not decreasing, within [0, rows]; values that are not so are clamped where they are read, and
+ * no access leaves the tensors.  Rows of no sequence are not read and not written: a batch may be padded at its end.
+ * A sequence may be empty.  A key row past its query's sequence counts for nothing, whatever it holds; an Inf or NaN in V reaches, as 0 times
+ * itself, also earlier rows of its own sequence that lie in the same tile of 64 rows.
+ * rows <= 2^24, rows * Hq <= 2^27, n_seq * Hq <= 2^22, Hq % Hk == 0, Hq <= 1024; d in {64, 128}.
+ * exact_attn_packed_backward: out, lse and out_f32 as exact_attn_packed_forward wrote them; workspace: device, 256-byte aligned, >=
+ * exact_attn_packed_backward_workspace_bytes(); nothing in it is kept.  Sums in a fixed order: same inputs, same bits. */
 typedef struct {
   int64_t row, head;
 } ha_strides;
+
+typedef struct {
+  int32_t n_seq, rows, Hq, Hk, d;
+  int32_t dtype; /* ha_dtype */
+  int32_t causal;
+} ha_packed;
+
+typedef struct {
+  ha_strides q, k, v, out;       /* the forward takes these four */
+  ha_strides d_out, dq, dk, dv;
+} ha_packed_strides;
+
+int exact_attn_packed_forward(const void* Q, const void* K, const void* V, const int32_t* cu_seqlens, void* out, float* lse,
+                              float* out_f32, const ha_packed* shape, const ha_packed_strides* strides, void* stream);
+int exact_attn_packed_backward(const void* Q, const void* K, const void* V, const int32_t* cu_seqlens, const void* out,
+                               const float* out_f32, const float* lse, const void* d_out, void* dQ, void* dK, void* dV,
+                               const ha_packed* shape, const ha_packed_strides* strides, void* workspace, size_t workspace_bytes,
+                               void* stream);
+size_t exact_attn_packed_backward_workspace_bytes(const ha_packed* shape);
 
 /* ------------------------------------------------------------------------
  * A paged cache of K and V in 4 bits, for decoding behind a long prompt.

@@ -61,6 +61,14 @@ class HaStrides(ctypes.Structure):
     _fields_ = [("row", c_int64), ("head", c_int64)]
 
 
+class HaPacked(ctypes.Structure):
+    _fields_ = [(k, c_int32) for k in ("n_seq", "rows", "Hq", "Hk", "d", "dtype", "causal")]
+
+
+class HaPackedStrides(ctypes.Structure):
+    _fields_ = [(k, HaStrides) for k in ("q", "k", "v", "out", "d_out", "dq", "dk", "dv")]
+
+
 class HaCache4(ctypes.Structure):
     _fields_ = [(k, c_int32) for k in ("n_pages", "page", "Hk", "d")]
 
@@ -112,6 +120,9 @@ _SIGNATURES = {
     "ha_alg2_workspace_bytes": (c_size_t, [POINTER(HaShape), POINTER(HaParams)]),
     "hyperattn_forward_alg2": (c_int, [c_void_p] * 5 + [POINTER(HaShape), POINTER(HaParams), POINTER(HaAlg2Options),
                                                        c_void_p, c_size_t, c_void_p]),
+    "exact_attn_packed_forward": (c_int, [c_void_p] * 7 + [POINTER(HaPacked), POINTER(HaPackedStrides), c_void_p]),
+    "exact_attn_packed_backward": (c_int, [c_void_p] * 11 + [POINTER(HaPacked), POINTER(HaPackedStrides), c_void_p, c_size_t, c_void_p]),
+    "exact_attn_packed_backward_workspace_bytes": (c_size_t, [POINTER(HaPacked)]),
     "ha_cache4_bytes": (c_size_t, [POINTER(HaCache4)]),
     "ha_cache4_write": (c_int, [c_void_p] * 4 + [POINTER(HaCache4), c_int32, c_int32, POINTER(HaStrides), c_void_p]),
     "ha_cache4_read": (c_int, [c_void_p] * 4 + [POINTER(HaCache4), c_int32, c_int32, POINTER(HaStrides), c_void_p]),
@@ -730,7 +741,7 @@ def alg2_workspace_views(workspace, shape: HaShape, params: HaParams):
             "vnorm_logw": view(lay.vnorm_logw, BH * nodes * m, torch.float32, (BH, nodes, m))}
 
 
-# ---------------------------------------------------------------- paged 4-bit cache
+# ---------------------------------------------------------------- packed sequences
 # Rows [rows, heads, d] may be slices of a larger tensor: their strides go along.  These calls run on the current device: a launch for another one's
 # tensors is refused here.
 def _stream_for(stream, like):
@@ -769,6 +780,72 @@ def _ints(t, name, shape, like):
     return _dev(t, name)
 
 
+def _packed_shape(Q, K, V, cu_seqlens, causal):
+    for name, t in (("Q", Q), ("K", K), ("V", V)):
+        if t.dim() != 3:
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected [rows, heads, d]")
+    rows, Hq, d = Q.shape
+    Hk = K.shape[1]
+    if cu_seqlens.dim() != 1 or cu_seqlens.shape[0] < 1:
+        raise ValueError(f"cu_seqlens has shape {tuple(cu_seqlens.shape)}, expected [n_seq + 1]")
+    return HaPacked(cu_seqlens.shape[0] - 1, rows, Hq, Hk, d, _dtype_code(Q), int(bool(causal)))
+
+
+def exact_attn_packed_forward(Q, K, V, cu_seqlens, causal=False, out=None, lse=None, stream=None, out_f32=None):
+    """out, lse: exact attention over sequences that lie one behind the other: rows cu_seqlens[s] to cu_seqlens[s + 1] (int32 [n_seq + 1]) are
+    sequence s.  Q [rows, Hq, d], K and V [rows, Hk, d] (bf16 or fp32; strided as they lie), Hq a multiple of Hk: query head h reads key head
+    h // (Hq // Hk).  lse: float32 [Hq, rows].  Rows of no sequence are left as they were.  out_f32 (float32 [rows, Hq, d]; bf16 tensors), if given,
+    receives the output before its rounding: pass it on to exact_attn_packed_backward."""
+    torch = _torch()
+    shape = _packed_shape(Q, K, V, cu_seqlens, causal)
+    rows, Hq, d = Q.shape
+    handle = _stream_for(stream, Q)
+    out = _empty(stream, (rows, Hq, d), Q.dtype, Q) if out is None else out
+    lse = _empty(stream, (Hq, rows), torch.float32, Q) if lse is None else lse
+    _expect_f32(Q, (Hq, rows), lse=lse)
+    _expect_f32(Q, (rows, Hq, d), out_f32=out_f32)
+    kv = (rows, shape.Hk, d)
+    strides = HaPackedStrides(_rows(Q, "Q", Q.shape, Q.dtype, Q), _rows(K, "K", kv, Q.dtype, Q), _rows(V, "V", kv, Q.dtype, Q),
+                              _rows(out, "out", Q.shape, Q.dtype, Q))
+    _check(lib().exact_attn_packed_forward(Q.data_ptr(), K.data_ptr(), V.data_ptr(), _ints(cu_seqlens, "cu_seqlens", cu_seqlens.shape, Q),
+                                           out.data_ptr(), _dev(lse, "lse"), None if out_f32 is None else _dev(out_f32, "out_f32"),
+                                           ctypes.byref(shape), ctypes.byref(strides), handle), "exact_attn_packed_forward")
+    return out, lse
+
+
+def exact_attn_packed_backward_workspace_bytes(rows, n_seq, Hq, Hk, d, dtype=None) -> int:
+    code = HA_BF16 if dtype is None else _dtype_code(_torch().empty((), dtype=dtype))
+    return int(lib().exact_attn_packed_backward_workspace_bytes(ctypes.byref(HaPacked(n_seq, rows, Hq, Hk, d, code, 0))))
+
+
+def exact_attn_packed_backward(Q, K, V, cu_seqlens, out, lse, d_out, causal=False, workspace=None, grads=None, stream=None, out_f32=None):
+    """dQ, dK, dV of sum(out * d_out); out, lse and out_f32 as exact_attn_packed_forward wrote them.  Rows of no sequence are left as they were (zeros,
+    where this call allocates the gradients)."""
+    torch = _torch()
+    shape = _packed_shape(Q, K, V, cu_seqlens, causal)
+    rows, Hq, d = Q.shape
+    kv = (rows, shape.Hk, d)
+    handle = _stream_for(stream, Q)
+    if grads is None:
+        grads = tuple(_empty(stream, s, Q.dtype, Q) for s in (Q.shape, kv, kv))
+        with torch.cuda.stream(stream):   # (None: the current one)
+            for t in grads:
+                t.zero_()
+    dQ, dK, dV = grads
+    _expect_f32(Q, (Hq, rows), lse=lse)
+    _expect_f32(Q, (rows, Hq, d), out_f32=out_f32)
+    if workspace is None:
+        workspace = _empty(stream, (int(lib().exact_attn_packed_backward_workspace_bytes(ctypes.byref(shape))),), torch.uint8, Q)
+    strides = HaPackedStrides(*(_rows(t, name, s, Q.dtype, Q) for t, name, s in (
+        (Q, "Q", Q.shape), (K, "K", kv), (V, "V", kv), (out, "out", Q.shape), (d_out, "d_out", Q.shape), (dQ, "dQ", Q.shape), (dK, "dK", kv), (dV, "dV", kv))))
+    _check(lib().exact_attn_packed_backward(Q.data_ptr(), K.data_ptr(), V.data_ptr(), _ints(cu_seqlens, "cu_seqlens", cu_seqlens.shape, Q),
+                                            out.data_ptr(), None if out_f32 is None else _dev(out_f32, "out_f32"), _dev(lse, "lse"), d_out.data_ptr(),
+                                            dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), ctypes.byref(shape), ctypes.byref(strides),
+                                            _dev(workspace, "workspace"), workspace.numel(), handle), "exact_attn_packed_backward")
+    return dQ, dK, dV
+
+
+# ---------------------------------------------------------------- paged 4-bit cache
 def _cache4(cache, page, d=None):
     """The cache's shape: uint8 [n_pages, Hk, page * (d + d / 16)]."""
     torch = _torch()

@@ -634,6 +634,49 @@ static void fill_alg2_layout(const Geometry& g, const ha_ws_layout& fwd, ha_alg2
   l->total_bytes = off;
 }
 
+
+// Checks of a packed call; fills g and the packed rows of *a but its pointers.
+static int packed_geometry(const ha_packed* sh, const ha_packed_strides* st, bool backward, AttnArgs* a) {
+  if (!sh) return HA_ERR_NULL;
+  if (sh->dtype != HA_BF16 && sh->dtype != HA_FP32) return HA_ERR_DTYPE;
+  if (sh->n_seq < 0 || sh->rows < 0 || sh->Hk < 1 || sh->Hq < 1 || sh->Hq > 1024 || sh->Hq % sh->Hk != 0) return HA_ERR_SHAPE;
+  if ((sh->d != 64 && sh->d != 128) || sh->rows > (1 << 24) || (int64_t)sh->rows * sh->Hq > (1ll << 27) || (int64_t)sh->n_seq * sh->Hq > (1ll << 22))
+    return HA_ERR_SHAPE;
+  a->g.n = sh->rows;
+  a->g.BH = sh->Hq;
+  a->g.d = sh->d;
+  a->g.dtype = sh->dtype;
+  a->g.b = 1;
+  a->g.causal = 1;  // (no node: the backward's sampled keys are none)
+  a->exact_causal = sh->causal ? 1 : 0;
+  PackedRows& p = a->pk;
+  p.n_seq = sh->n_seq;
+  p.rows = sh->rows;
+  p.Hq = sh->Hq;
+  p.Hk = sh->Hk;
+  p.group = sh->Hq / sh->Hk;
+  p.splits = packed_splits(packed_slots<128>(p) * sh->Hk, p.group);
+  const auto strides = [&](const ha_strides* s, int heads, bool written, RowStrides* out) { return row_strides(s, heads, sh->d, sh->dtype, written, out); };
+  int rc = strides(st ? &st->q : nullptr, sh->Hq, false, &p.q);
+  if (rc == HA_OK) rc = strides(st ? &st->k : nullptr, sh->Hk, false, &p.k);
+  if (rc == HA_OK) rc = strides(st ? &st->v : nullptr, sh->Hk, false, &p.v);
+  if (rc == HA_OK) rc = strides(st ? &st->out : nullptr, sh->Hq, !backward, &p.o);
+  if (rc == HA_OK && backward) rc = strides(st ? &st->d_out : nullptr, sh->Hq, false, &p.d_o);
+  return rc;
+}
+
+struct PackedSpace {
+  size_t part1, part2, total;
+};
+static PackedSpace packed_space(const PackedRows& p, int d) {
+  const size_t part = p.splits > 1 ? align256((size_t)p.splits * p.rows * p.Hk * d * 4) : 0;
+  PackedSpace s;
+  s.part1 = align256((size_t)p.rows * p.Hq * 4);  // delta comes first
+  s.part2 = s.part1 + part;
+  s.total = s.part2 + part;
+  return s;
+}
+
 }  // namespace ha
 
 using namespace ha;
@@ -1030,6 +1073,78 @@ int exact_attn_backward(const void* Q, const void* K, const void* V, const void*
   a.fin1 = dK;
   a.fin2 = dV;
   return launch_attn_bwd(a, kBwdDkvExact, st);
+}
+
+int exact_attn_packed_forward(const void* Q, const void* K, const void* V, const int32_t* cu_seqlens, void* out, float* lse,
+                              float* out_f32, const ha_packed* shape, const ha_packed_strides* strides, void* stream) {
+  AttnArgs a{};
+  const int rc = packed_geometry(shape, strides, false, &a);
+  if (rc != HA_OK) return rc;
+  if (out_f32 && shape->dtype != HA_BF16) return HA_ERR_DTYPE;
+  if (shape->rows == 0 || shape->n_seq == 0) return HA_OK;
+  if (!Q || !K || !V || !cu_seqlens || !out || !lse) return HA_ERR_NULL;
+  if (any_misaligned16(Q, K, V, out, out_f32) || any_misaligned4(lse, cu_seqlens)) return HA_ERR_ALIGN;
+  a.Q = Q;
+  a.K = K;
+  a.V = V;
+  a.pk.cu = cu_seqlens;
+  a.out = out;
+  a.lse = lse;
+  a.out_f32 = out_f32;
+  return run_attention(a, kModePacked, (hipStream_t)stream);
+}
+
+int exact_attn_packed_backward(const void* Q, const void* K, const void* V, const int32_t* cu_seqlens, const void* out,
+                               const float* out_f32, const float* lse, const void* d_out, void* dQ, void* dK, void* dV,
+                               const ha_packed* shape, const ha_packed_strides* strides, void* workspace, size_t workspace_bytes,
+                               void* stream) {
+  BwdArgs a{};
+  int rc = packed_geometry(shape, strides, true, &a.f);
+  if (rc != HA_OK) return rc;
+  RowStrides dq, dk, dv;
+  rc = row_strides(strides ? &strides->dq : nullptr, shape->Hq, shape->d, shape->dtype, true, &dq);
+  if (rc == HA_OK) rc = row_strides(strides ? &strides->dk : nullptr, shape->Hk, shape->d, shape->dtype, true, &dk);
+  if (rc == HA_OK) rc = row_strides(strides ? &strides->dv : nullptr, shape->Hk, shape->d, shape->dtype, true, &dv);
+  if (rc != HA_OK) return rc;
+  if (out_f32 && shape->dtype != HA_BF16) return HA_ERR_DTYPE;
+  if (shape->rows == 0 || shape->n_seq == 0) return HA_OK;
+  if (!Q || !K || !V || !cu_seqlens || !out || !lse || !d_out || !dQ || !dK || !dV || !workspace) return HA_ERR_NULL;
+  if (any_misaligned16(Q, K, V, out, out_f32, d_out, dQ, dK, dV) || any_misaligned4(lse, cu_seqlens)) return HA_ERR_ALIGN;
+  PackedRows& p = a.f.pk;
+  const PackedSpace sp = packed_space(p, shape->d);
+  if (workspace_bytes < sp.total || ((uintptr_t)workspace & 255) != 0) return HA_ERR_WORKSPACE;
+  hipStream_t st = (hipStream_t)stream;
+  unsigned char* w = (unsigned char*)workspace;
+  a.f.Q = Q;
+  a.f.K = K;
+  a.f.V = V;
+  p.cu = cu_seqlens;
+  a.dO = d_out;
+  a.lse = lse;
+  a.delta = (float*)w;
+  a.delta_out = (float*)w;
+  a.O = out;
+  a.O32 = out_f32;
+  a.fin1 = dQ;
+  p.fin1 = dq;
+  rc = launch_attn_bwd(a, kBwdDqPacked, st);
+  if (rc != HA_OK) return rc;
+  a.fin1 = dK;
+  a.fin2 = dV;
+  p.fin1 = dk;
+  p.fin2 = dv;
+  if (p.splits > 1) {
+    a.out1 = (float*)(w + sp.part1);
+    a.out2 = (float*)(w + sp.part2);
+  }
+  rc = launch_attn_bwd(a, kBwdDkvPacked, st);
+  if (rc != HA_OK || p.splits == 1) return rc;
+  return launch_packed_sum(p, a.out1, a.out2, dK, dV, shape->d, shape->dtype, st);
+}
+
+size_t exact_attn_packed_backward_workspace_bytes(const ha_packed* shape) {
+  AttnArgs a{};
+  return packed_geometry(shape, nullptr, true, &a) == HA_OK ? packed_space(a.pk, shape->d).total : 0;
 }
 
 size_t exact_attn_backward_workspace_bytes(const ha_shape* sh) {

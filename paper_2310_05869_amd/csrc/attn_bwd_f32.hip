@@ -78,8 +78,10 @@ struct F32BwdLds {
 // wg: the workgroup's number among the pass's wgs.
 template <int D, int MODE, int RG, int KW, bool FINAL>
 __device__ __forceinline__ void bwd_f32_pass(const BwdArgs& a, const int wg, const int wgs, unsigned char* smem) {
-  constexpr bool kDq = (MODE == kBwdDqNode || MODE == kBwdDqExact);
-  constexpr bool kExact = (MODE == kBwdDqExact || MODE == kBwdDkvExact);
+  constexpr bool kPacked = MODE == kBwdDqPacked || MODE == kBwdDkvPacked, kHeads = MODE == kBwdDkvPacked;
+  constexpr bool kDqExact = MODE == kBwdDqExact || MODE == kBwdDqPacked, kDkvExact = MODE == kBwdDkvExact || MODE == kBwdDkvPacked;
+  constexpr bool kDq = MODE == kBwdDqNode || kDqExact;
+  constexpr bool kExact = kDqExact || kDkvExact;
   constexpr bool kSorted = (MODE == kBwdDkvBlock || MODE == kBwdDkvSamp);
   constexpr bool kHits = FINAL && MODE == kBwdDkvBlock;  // sampled keys' sums added here
   constexpr int NW = RG * KW, kFBT = 64 * NW;
@@ -107,13 +109,27 @@ __device__ __forceinline__ void bwd_f32_pass(const BwdArgs& a, const int wg, con
   BwdWork b = decode_bwd_work<kRT, MODE>(a, kExact ? wg : logical_block(wg, wgs), wgs);
   const TileWork& w = b.w;
 
+  if (kPacked && w.rows_valid <= 0) return;
+
   const int64_t hs = f.q_bh_stride;
-  const float* Qh = reinterpret_cast<const float*>(f.Q) + (int64_t)w.bh * hs;
-  const float* Kh = reinterpret_cast<const float*>(f.K) + (int64_t)w.bh * hs;
-  const float* Vh = reinterpret_cast<const float*>(f.V) + (int64_t)w.bh * hs;
-  const float* Gh = reinterpret_cast<const float*>(a.dO) + (int64_t)w.bh * hs;
-  const float* lse_h = a.lse + (int64_t)w.bh * g.n;
-  const float* del_h = a.delta + (int64_t)w.bh * g.n;
+  const float* Qh = reinterpret_cast<const float*>(f.Q) + (kPacked ? (int64_t)b.seq_start * f.pk.q.row + (int64_t)w.bh * f.pk.q.head : (int64_t)w.bh * hs);
+  const float* Kh = reinterpret_cast<const float*>(f.K);
+  const float* Vh = reinterpret_cast<const float*>(f.V);
+  const float* Gh = reinterpret_cast<const float*>(a.dO) + (kPacked ? (int64_t)b.seq_start * f.pk.d_o.row + (int64_t)w.bh * f.pk.d_o.head : (int64_t)w.bh * hs);
+  if constexpr (kPacked) {
+    const int kv = w.bh / f.pk.group;
+    Kh += (int64_t)b.seq_start * f.pk.k.row + (int64_t)kv * f.pk.k.head;
+    Vh += (int64_t)b.seq_start * f.pk.v.row + (int64_t)kv * f.pk.v.head;
+  } else {
+    Kh += (int64_t)w.bh * hs;
+    Vh += (int64_t)w.bh * hs;
+  }
+  const int64_t lse_at = kPacked ? (int64_t)w.bh * f.pk.rows + b.seq_start : (int64_t)w.bh * g.n;
+  const float* lse_h = a.lse + lse_at;
+  const float* del_h = a.delta + lse_at;
+  // elements from one row to the next of the R rows, bytes of the T rows
+  const int64_t x_row = !kPacked ? D : kDq ? f.pk.q.row : f.pk.k.row, a_row = !kPacked ? D : kDq ? f.pk.d_o.row : f.pk.v.row;
+  const int y_row = 4 * (!kPacked ? D : (int)(kDq ? f.pk.k.row : f.pk.q.row)), b_row = 4 * (!kPacked ? D : (int)(kDq ? f.pk.v.row : f.pk.d_o.row));
   const float* Xh = kDq ? Qh : Kh;   // R rows: operand of the scores
   const float* Ah = kDq ? Gh : Vh;   // R rows: operand of dP
   const float* Yh = kDq ? Kh : Qh;   // T rows: operand of the scores and of dQ / dK
@@ -130,9 +146,9 @@ __device__ __forceinline__ void bwd_f32_pass(const BwdArgs& a, const int wg, con
     f32x4 x[2 * KS];
 #pragma unroll
     for (int j = 0; j < 2 * KS; ++j) {
-      const int64_t at = (int64_t)r_row * D + 16 * (j / 2) + 8 * h + 4 * (j % 2);
-      if (kShared) x[j] = *reinterpret_cast<const f32x4*>(Xh + at);
-      av[j] = *reinterpret_cast<const f32x4*>(Ah + at);
+      const int col = 16 * (j / 2) + 8 * h + 4 * (j % 2);
+      if (kShared) x[j] = *reinterpret_cast<const f32x4*>(Xh + r_row * x_row + col);
+      av[j] = *reinterpret_cast<const f32x4*>(Ah + r_row * a_row + col);
     }
     if constexpr (kShared) {
 #pragma unroll
@@ -149,9 +165,11 @@ __device__ __forceinline__ void bwd_f32_pass(const BwdArgs& a, const int wg, con
       for (int i = tid; i < 32 * T::PPR; i += kFBT) {
         const int r = i / T::PPR, piece = i % T::PPR;
         int blk;
-        const int64_t at = (int64_t)bwd_r_row<MODE>(a, b, r < w.rows_valid ? r : 0, &blk) * D + piece * 8;
-        const f32x4 x0 = *reinterpret_cast<const f32x4*>(Xh + at), x1 = *reinterpret_cast<const f32x4*>(Xh + at + 4);
-        const f32x4 a0 = *reinterpret_cast<const f32x4*>(Ah + at), a1 = *reinterpret_cast<const f32x4*>(Ah + at + 4);
+        const int rr = bwd_r_row<MODE>(a, b, r < w.rows_valid ? r : 0, &blk);
+        const float* xp = Xh + rr * x_row + piece * 8;
+        const float* ap = Ah + rr * a_row + piece * 8;
+        const f32x4 x0 = *reinterpret_cast<const f32x4*>(xp), x1 = *reinterpret_cast<const f32x4*>(xp + 4);
+        const f32x4 a0 = *reinterpret_cast<const f32x4*>(ap), a1 = *reinterpret_cast<const f32x4*>(ap + 4);
         T::store(ytile, r, piece, x0, x1);
         T::store(btile, r, piece, a0, a1);
       }
@@ -161,7 +179,8 @@ __device__ __forceinline__ void bwd_f32_pass(const BwdArgs& a, const int wg, con
       if (a.delta_out == nullptr) {
         del_r = del_h[r_row];
       } else {
-        const float* Oh = reinterpret_cast<const float*>(a.O) + ((int64_t)w.bh * g.n + r_row) * D + 8 * h;
+        const float* Oh = reinterpret_cast<const float*>(a.O) +
+                          (kPacked ? (int64_t)(b.seq_start + r_row) * f.pk.o.row + (int64_t)w.bh * f.pk.o.head : ((int64_t)w.bh * g.n + r_row) * D) + 8 * h;
         f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < 2 * KS; ++j) {
@@ -171,7 +190,7 @@ __device__ __forceinline__ void bwd_f32_pass(const BwdArgs& a, const int wg, con
         }
         del_r = (s[0] + s[1]) + (s[2] + s[3]);
         del_r += __shfl_xor(del_r, 32);
-        if (h == 0 && kw == 0 && r_in_tile < w.rows_valid) a.delta_out[(int64_t)w.bh * g.n + r_row] = del_r;
+        if (h == 0 && kw == 0 && r_in_tile < w.rows_valid) a.delta_out[lse_at + r_row] = del_r;
       }
     }
   }
@@ -195,10 +214,11 @@ __device__ __forceinline__ void bwd_f32_pass(const BwdArgs& a, const int wg, con
   }
   const float nat_bias = ((MODE == kBwdDqNode || MODE == kBwdDkvSamp) && g.m > 0) ? logf((float)w.nr.s / (float)g.m) : 0.f;
   // tiles of the workgroup; in causal passes a wave leaves out those that lie wholly on its masked side
-  const int tiles = (nT + kFTT - 1) / kFTT;
+  // (packed dK / dV: the query heads' tiles one behind the other, tph of each; kt_lo counts within a head)
+  const int tph = (nT + kFTT - 1) / kFTT, tiles = kHeads ? b.heads * tph : tph;
   int kt_lo = 0, kt_hi = tiles;
-  if (MODE == kBwdDqExact && f.exact_causal) kt_hi = min(kt_hi, (w.q0 - w.k0 + grp * 32 + 31) / kFTT + 1);
-  if (MODE == kBwdDkvExact && f.exact_causal) kt_lo = grp;  // T starts at the workgroup's first key
+  if (kDqExact && f.exact_causal) kt_hi = min(kt_hi, (w.q0 - w.k0 + grp * 32 + 31) / kFTT + 1);
+  if (kDkvExact && f.exact_causal) kt_lo = grp;  // T starts at the workgroup's first key
 
   // ---- tile movers.  Shared tiles: a thread fetches pieces of eight floats, splits them and puts them into its way's tiles ----
   // (exact passes: rows past the T rows' end read as zeros and are masked)
@@ -208,28 +228,43 @@ __device__ __forceinline__ void bwd_f32_pass(const BwdArgs& a, const int wg, con
   const __amdgpu_buffer_rsrc_t brsrc = __builtin_amdgcn_make_buffer_rsrc((void*)Bh, 0, (int)bytes, 0x00020000);
   const __amdgpu_buffer_rsrc_t lrsrc = __builtin_amdgcn_make_buffer_rsrc((void*)lse_h, 0, (kExact ? w.k1 : g.n) * 4, 0x00020000);
   const __amdgpu_buffer_rsrc_t drsrc = __builtin_amdgcn_make_buffer_rsrc((void*)del_h, 0, (kExact ? w.k1 : g.n) * 4, 0x00020000);
+  // packed passes: descriptors per tile, which end with the T rows; rows count from the tile's first
+  auto head_of = [&](int kt) { return kHeads ? (int)((unsigned)kt / (unsigned)tph) : 0; };
+  auto tile_rsrc = [&](const __amdgpu_buffer_rsrc_t& whole, const void* base, int64_t head_bytes, int row_bytes, int kt) {
+    if constexpr (!kPacked) return whole;
+    const int head = head_of(kt), row = w.k0 + (kt - head * tph) * kFTT;
+    const uint64_t at = (uint64_t)base + head * head_bytes + (int64_t)row * row_bytes;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)at), hi = __builtin_amdgcn_readfirstlane((uint32_t)(at >> 32));
+    return __builtin_amdgcn_make_buffer_rsrc((void*)((uint64_t)hi << 32 | lo), 0, __builtin_amdgcn_readfirstlane(max(0, min(kFTT, w.k1 - row)) * row_bytes), 0x00020000);
+  };
+  auto y_tile = [&](int kt) { return tile_rsrc(yrsrc, Yh, kHeads ? f.pk.q.head * 4 : 0, y_row, kt); };
+  auto b_tile = [&](int kt) { return tile_rsrc(brsrc, Bh, kHeads ? f.pk.d_o.head * 4 : 0, b_row, kt); };
+  auto l_tile = [&](int kt) { return tile_rsrc(lrsrc, lse_h, (int64_t)f.pk.rows * 4, 4, kt); };
+  auto d_tile = [&](int kt) { return tile_rsrc(drsrc, del_h, (int64_t)f.pk.rows * 4, 4, kt); };
   int trow[NP];  // rows of the tile that is fetched next
   auto find_rows = [&](int kt) {
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       const int tp = kt * kFTT + (wtid + i * 64 * RG) / T::PPR;
-      if (kExact) trow[i] = w.k0 + tp;
+      if (kPacked) trow[i] = (wtid + i * 64 * RG) / T::PPR;
+      else if (kExact) trow[i] = w.k0 + tp;
       else trow[i] = kSorted ? tperm[min(tp, nT - 1)] : list[min(tp, nT - 1)];
     }
   };
   f32x4 ys[NP][2], bs[NP][2];
   float sl[NP], sd[NP];  // dK / dV passes: L and delta of the row
-  auto fetch = [&]() {
+  auto fetch = [&](int kt) {
+    const __amdgpu_buffer_rsrc_t yr = y_tile(kt), br = b_tile(kt);
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      const int off = trow[i] * (D * 4) + (wtid + i * 64 * RG) % T::PPR * 32;
-      ys[i][0] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(yrsrc, off, 0, 0));
-      ys[i][1] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(yrsrc, off + 16, 0, 0));
-      bs[i][0] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(brsrc, off, 0, 0));
-      bs[i][1] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(brsrc, off + 16, 0, 0));
+      const int piece = (wtid + i * 64 * RG) % T::PPR * 32, off = trow[i] * y_row + piece, boff = trow[i] * b_row + piece;
+      ys[i][0] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(yr, off, 0, 0));
+      ys[i][1] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(yr, off + 16, 0, 0));
+      bs[i][0] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(br, boff, 0, 0));
+      bs[i][1] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(br, boff + 16, 0, 0));
       if (!kDq) {
-        sl[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(lrsrc, trow[i] * 4, 0, 0));
-        sd[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(drsrc, trow[i] * 4, 0, 0));
+        sl[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(l_tile(kt), trow[i] * 4, 0, 0));
+        sd[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(d_tile(kt), trow[i] * 4, 0, 0));
       }
     }
   };
@@ -250,38 +285,38 @@ __device__ __forceinline__ void bwd_f32_pass(const BwdArgs& a, const int wg, con
   int row = 0;
   float scl = 0.f, scd = 0.f;  // dK / dV of sorted rows: L and delta of the T row this lane holds
   f32x4 yf[kShared ? 1 : 2 * KS];
-  auto load_rows = [&](const __amdgpu_buffer_rsrc_t& rsrc, int of, f32x4 (&v)[kShared ? 1 : 2 * KS]) {
+  auto load_rows = [&](const __amdgpu_buffer_rsrc_t& rsrc, int row_bytes, int of, f32x4 (&v)[kShared ? 1 : 2 * KS]) {
     if constexpr (!kShared) {
 #pragma unroll
       for (int j = 0; j < 2 * KS; ++j)
-        v[j] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, of * (D * 4) + 32 * h + 16 * (j % 2), 64 * (j / 2), 0));
+        v[j] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, of * row_bytes + 32 * h + 16 * (j % 2), 64 * (j / 2), 0));
     }
   };
   auto fetch_own = [&](int kt) {
     const int tp = min(kt * kFTT + lq, nT - 1);
-    row = kExact ? w.k0 + kt * kFTT + lq : kSorted ? tperm[tp] : list[tp];
-    load_rows(yrsrc, row, yf);
+    row = kPacked ? lq : kExact ? w.k0 + kt * kFTT + lq : kSorted ? tperm[tp] : list[tp];
+    load_rows(y_tile(kt), y_row, row, yf);
     if (!kDq && !kExact) {
       scl = lse_h[row];
       scd = del_h[row];
     }
   };
   auto of_elem = [&](auto v, int i) { return __shfl(v, 8 * (i / 4) + 4 * h + (i % 4)); };
-  auto load_cols = [&](const __amdgpu_buffer_rsrc_t& rsrc, int of, int kt, auto& v, int i0, int count) {
+  auto load_cols = [&](const __amdgpu_buffer_rsrc_t& rsrc, int row_bytes, int of, int kt, auto& v, int i0, int count) {
     // Consecutive rows.  All of the row is in the lane's offset: the bounds check covers it, not the scalar one.  One
     // running offset (opaque, or the compiler keeps one register per eight rows across the loop): 241.3 us where constants of
     // one offset take 245.6 (4 heads, n = 4096 in causal blocks of 1024, forward + backward).
     if (kExact) {
-      int off = (w.k0 + kt * kFTT + 8 * (i0 / 4) + 4 * h) * (D * 4) + 4 * lq;
+      int off = ((kPacked ? 0 : w.k0 + kt * kFTT) + 8 * (i0 / 4) + 4 * h) * row_bytes + 4 * lq;
 #pragma unroll
       for (int i = i0; i < i0 + count; ++i) {
         if (i % 4 == 0 && i > i0) {
-          off += 8 * (D * 4);
+          off += 8 * row_bytes;
           asm volatile("" : "+v"(off));
         }
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
-          v[i][dt] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rsrc, off + (i % 4) * (D * 4) + 128 * dt, 0, 0));
+          v[i][dt] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rsrc, off + (i % 4) * row_bytes + 128 * dt, 0, 0));
       }
       return;
     }
@@ -312,7 +347,7 @@ __device__ __forceinline__ void bwd_f32_pass(const BwdArgs& a, const int wg, con
     if constexpr (kShared) {
       if (!BOUND && kw < tiles) {
         find_rows(kw);
-        fetch();
+        fetch(kw);
         if (!kExact) find_rows(kw + KW);
       }
     } else if (!BOUND && kt_lo + kw < kt_hi) {
@@ -325,16 +360,16 @@ __device__ __forceinline__ void bwd_f32_pass(const BwdArgs& a, const int wg, con
         if (kt >= KW) __syncthreads();  // the tiles before are read no more
         if (BOUND && kt < tiles) {
           find_rows(kt);
-          fetch();
+          fetch(kt);
         }
         if (kt < tiles) store();
         __syncthreads();
         if (!BOUND && kt + KW < tiles) {
           if (kExact) find_rows(kt + KW);
-          fetch();
+          fetch(kt + KW);
           if (!kExact) find_rows(kt + 2 * KW);
         }
-        if (kt < kt_lo || kt >= kt_hi) continue;
+        if (kt - head_of(kt) * (kHeads ? tph : 0) < kt_lo || kt >= kt_hi) continue;
       } else if (BOUND) {
         fetch_own(kt);
       }
@@ -342,15 +377,15 @@ __device__ __forceinline__ void bwd_f32_pass(const BwdArgs& a, const int wg, con
       if (!kDq && (kShared || kExact)) {
 #pragma unroll
         for (int q4 = 0; q4 < 4; ++q4) {
-          const int at = (w.k0 + kt * kFTT + 8 * q4 + 4 * h) * 4;
-          l4[q4] = kShared ? *reinterpret_cast<const f32x4*>(sc + 8 * q4 + 4 * h) : __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(lrsrc, at, 0, 0));
-          d4[q4] = kShared ? *reinterpret_cast<const f32x4*>(sc + kFTT + 8 * q4 + 4 * h) : __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(drsrc, at, 0, 0));
+          const int at = ((kPacked ? 0 : w.k0 + kt * kFTT) + 8 * q4 + 4 * h) * 4;
+          l4[q4] = kShared ? *reinterpret_cast<const f32x4*>(sc + 8 * q4 + 4 * h) : __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(l_tile(kt), at, 0, 0));
+          d4[q4] = kShared ? *reinterpret_cast<const f32x4*>(sc + kFTT + 8 * q4 + 4 * h) : __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(d_tile(kt), at, 0, 0));
         }
       }
       const int row_c = row;
       const float scl_c = scl, scd_c = scd;
       f32x4 bf[kShared ? 1 : 2 * KS];
-      if (!kShared) load_rows(brsrc, row_c, bf);
+      if (!kShared) load_rows(b_tile(kt), b_row, row_c, bf);
 
       f32x16 c, e;
       {
@@ -369,7 +404,7 @@ __device__ __forceinline__ void bwd_f32_pass(const BwdArgs& a, const int wg, con
         split_sum<BOUND>(c, small);
       }
       float tv[kShared ? 1 : 16][DT];
-      if constexpr (!kShared && !(kDq && kKeepY)) load_cols(kDq ? yrsrc : brsrc, row_c, kt, tv, 0, 16);
+      if constexpr (!kShared && !(kDq && kKeepY)) load_cols(kDq ? y_tile(kt) : b_tile(kt), kDq ? y_row : b_row, row_c, kt, tv, 0, 16);
       {
         f32x16 small;
 #pragma unroll
@@ -383,11 +418,11 @@ __device__ __forceinline__ void bwd_f32_pass(const BwdArgs& a, const int wg, con
       }
 
       // masks, on the tiles that have any: in the sampled-key pass the keys differ by lane
-      const int tbase = kt * kFTT;
+      const int tbase = (kt - head_of(kt) * (kHeads ? tph : 0)) * kFTT;
       bool special = tbase + kFTT > nT;
       if (MODE == kBwdDqNode) special = special || (tbase < nb && tbase + kFTT > nb);
-      if (MODE == kBwdDqExact && f.exact_causal) special = special || (w.k0 + tbase + kFTT - 1 > w.q0 + grp * 32);
-      if (MODE == kBwdDkvExact && f.exact_causal) special = special || (w.k0 + tbase < w.q0 + grp * 32 + 31);
+      if (kDqExact && f.exact_causal) special = special || (w.k0 + tbase + kFTT - 1 > w.q0 + grp * 32);
+      if (kDkvExact && f.exact_causal) special = special || (w.k0 + tbase < w.q0 + grp * 32 + 31);
       if (MODE == kBwdDkvSamp) {
         const int mlo = blk_r * g.b - (b.chunk_start + tbase);
         special = special || __any(mlo < kFTT && mlo + g.b > 0);
@@ -402,8 +437,8 @@ __device__ __forceinline__ void bwd_f32_pass(const BwdArgs& a, const int wg, con
           if (MODE == kBwdDqNode && tbase < nb && tpos >= nb) c[i] += nat_bias * (1.f / kSplitScore);
           // queries of the key's own block: factor 1 - M of Algorithm 2
           if (MODE == kBwdDkvSamp) masked = masked || (unsigned)(b.chunk_start + tpos - blk_r * g.b) < (unsigned)g.b;
-          if (MODE == kBwdDqExact && f.exact_causal) masked = masked || (w.k0 + tpos > r_row);   // keys after the query
-          if (MODE == kBwdDkvExact && f.exact_causal) masked = masked || (w.k0 + tpos < r_row);  // queries before the key
+          if (kDqExact && f.exact_causal) masked = masked || (w.k0 + tpos > r_row);   // keys after the query
+          if (kDkvExact && f.exact_causal) masked = masked || (w.k0 + tpos < r_row);  // queries before the key
           if (masked) c[i] = -INFINITY;
           if (kExact && !kDq && masked) {  // (a piece of four values can end past the head's last row)
             l4[i / 4][i % 4] = 0.f;
@@ -435,7 +470,7 @@ __device__ __forceinline__ void bwd_f32_pass(const BwdArgs& a, const int wg, con
         // Y^T dS from the wave's own tile, or from the caches: the rows arrive while the dV products run
         float yv[kKeepY || kDq ? 1 : 16][DT];
         if constexpr (!kDq) {
-          if constexpr (!kKeepY) load_cols(yrsrc, row_c, kt, yv, 0, 16);
+          if constexpr (!kKeepY) load_cols(y_tile(kt), y_row, row_c, kt, yv, 0, 16);
 #pragma unroll
           for (int hf = 0; hf < 2; ++hf) ps[hf] = split8([&](int i) { return c[8 * hf + i]; });
           split_tile_products<DT, kSumEach, BOUND>([&](int dt, int hf) { return split8_raw([&](int i) { return tv[8 * hf + i][dt]; }); }, ps, acc2);
@@ -484,7 +519,7 @@ __device__ __forceinline__ void bwd_f32_pass(const BwdArgs& a, const int wg, con
   constexpr int RS = L::ROW;
   float* rows_lds = reinterpret_cast<float*>(smem);
   const int64_t srow0 = (int64_t)w.bh * bwd_chunks_per_node(g, a.chunk, 0) * g.m;  // sample 0's sums (kHits)
-  auto write_out = [&](const auto& acc, float* node_dst, const float* samp, float* fin, const float* lvl) {
+  auto write_out = [&](const auto& acc, float* node_dst, const float* samp, float* fin, const float* lvl, const RowStrides& fs) {
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -499,6 +534,14 @@ __device__ __forceinline__ void bwd_f32_pass(const BwdArgs& a, const int wg, con
       f32x4 v = *reinterpret_cast<const f32x4*>(src);
 #pragma unroll
       for (int k = 1; k < KW; ++k) v += *reinterpret_cast<const f32x4*>(src + k * kRT * RS);
+      if constexpr (kPacked) {
+        const int64_t row = (int64_t)b.seq_start + w.q0 + r;
+        const int head = kHeads ? w.bh / f.pk.group : w.bh;
+        float* to = kHeads && node_dst != nullptr ? node_dst + (((int64_t)b.chunk_start * f.pk.rows + row) * f.pk.Hk + head) * D + col
+                                                  : fin + row * fs.row + (int64_t)head * fs.head + col;
+        *reinterpret_cast<f32x4*>(to) = v;
+        continue;
+      }
       if (kHits && samp != nullptr) {
         const int j = sh.first[r];
         const f32x4 sv = *reinterpret_cast<const f32x4*>(samp + (srow0 + (j != kNoSample ? j : 0)) * D + col);
@@ -519,10 +562,10 @@ __device__ __forceinline__ void bwd_f32_pass(const BwdArgs& a, const int wg, con
       *reinterpret_cast<f32x4*>((kExact || FINAL ? fin : node_dst) + out_row * D + col) = v;
     }
   };
-  write_out(acc1, a.out1, a.samp1, reinterpret_cast<float*>(a.fin1), a.lvl1);
+  write_out(acc1, a.out1, a.samp1, reinterpret_cast<float*>(a.fin1), a.lvl1, f.pk.fin1);
   if constexpr (!kDq) {
     __syncthreads();  // the rows of the other gradient are read no more
-    write_out(acc2, a.out2, a.samp2, reinterpret_cast<float*>(a.fin2), a.lvl2);
+    write_out(acc2, a.out2, a.samp2, reinterpret_cast<float*>(a.fin2), a.lvl2, f.pk.fin2);
   }
 }
 
@@ -578,7 +621,16 @@ static int launch_bwd_f32_form(const BwdArgs& args, int grid, hipStream_t st) {
 }
 
 template <int D, int MODE, int RG, int KW>
-static int launch_bwd_f32_one(const BwdArgs& a, hipStream_t st) {
+static int launch_bwd_f32_one(const BwdArgs& args, hipStream_t st) {
+  if constexpr (MODE == kBwdDqPacked || MODE == kBwdDkvPacked) {
+    BwdArgs a = args;
+    const int64_t slots = packed_slots<32 * RG>(a.f.pk), wgs = slots * (MODE == kBwdDqPacked ? a.f.pk.Hq : a.f.pk.Hk * a.f.pk.splits);
+    if (wgs > kMaxLaunch) return HA_ERR_SHAPE;
+    a.f.pk.slots = (int32_t)slots;
+    set_packed_divs(a.f, MODE == kBwdDqPacked ? a.f.pk.group : a.f.pk.splits);
+    return launch_bwd_f32_form<D, MODE, RG, KW, false>(a, (int)wgs, st);
+  }
+  const BwdArgs& a = args;
   const int64_t grid = bwd_grid<32 * RG>(a, MODE);
   if (grid <= 0) return HA_OK;
   if (grid > kMaxGrid) return HA_ERR_SHAPE;
@@ -707,8 +759,23 @@ static int launch_bwd_f32_d(const BwdArgs& a, int mode, hipStream_t st) {
   }
 }
 
+// Packed sequences: the same, by the average length and an upper bound of the workgroups.
+template <int D, int MODE>
+static int launch_bwd_f32_packed(const BwdArgs& a, hipStream_t st) {
+  const PackedRows& p = a.f.pk;
+  const int64_t avg = p.rows / (p.n_seq > 0 ? p.n_seq : 1), per = MODE == kBwdDqPacked ? p.Hq : p.Hk * p.splits;
+  const int64_t grid = packed_slots<128>(p) * per;
+  if constexpr (D == 64)
+    if (avg >= 512 && packed_slots<32>(p) * per <= (!a.f.exact_causal ? 256 : avg < 2048 ? 384 : 512)) return launch_bwd_f32_one<D, MODE, 1, 8>(a, st);
+  const int64_t enough = a.f.exact_causal ? (D == 64 ? 512 : 1024) : D == 128 ? 208 : 256;
+  const bool fits = 3 * ((avg + 127) / 128 * 128) <= 4 * avg;
+  return fits && grid >= enough ? launch_bwd_f32_one<D, MODE, 4, 1>(a, st) : launch_bwd_f32_one<D, MODE, 1, 4>(a, st);
+}
+
 int launch_attn_bwd_f32(const BwdArgs& a, int mode, hipStream_t st) {
   if (a.f.g.dtype != HA_FP32) return HA_ERR_DTYPE;
+  if (mode == kBwdDqPacked) return a.f.g.d == 128 ? launch_bwd_f32_packed<128, kBwdDqPacked>(a, st) : launch_bwd_f32_packed<64, kBwdDqPacked>(a, st);
+  if (mode == kBwdDkvPacked) return a.f.g.d == 128 ? launch_bwd_f32_packed<128, kBwdDkvPacked>(a, st) : launch_bwd_f32_packed<64, kBwdDkvPacked>(a, st);
   if (a.f.g.d == 128) return launch_bwd_f32_d<128>(a, mode, st);
   if (a.f.g.d == 64) return launch_bwd_f32_d<64>(a, mode, st);
   return HA_ERR_SHAPE;

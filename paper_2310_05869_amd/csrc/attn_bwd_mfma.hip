@@ -113,6 +113,13 @@ __device__ inline void dma_1k(const __amdgpu_buffer_rsrc_t& rsrc, uint32_t lds_a
   asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(lds_at), "v"(voff), "s"(rsrc) : "memory");
 }
 
+// A descriptor of memory that is the same for all lanes, where the compiler does not see that by itself
+__device__ inline __amdgpu_buffer_rsrc_t uniform_rsrc(const void* p, int bytes) {
+  const uint64_t at = (uint64_t)p;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)at), hi = __builtin_amdgcn_readfirstlane((uint32_t)(at >> 32));
+  return __builtin_amdgcn_make_buffer_rsrc((void*)((uint64_t)hi << 32 | lo), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
+}
+
 // Waves per SIMD that the compiler is asked for.
 constexpr int bwd_waves_per_simd(int d, int mode) { return d == 64 && mode == kBwdDkvSamp ? 3 : 2; }
 
@@ -124,8 +131,10 @@ template <int D, int MODE, bool FINAL, int NG, bool FOUR>
 __global__ __launch_bounds__(kBNT * NG, FOUR ? 4 : bwd_waves_per_simd(D, MODE)) void attn_bwd_kernel(BwdArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   using L = BwdLds<D>;
-  constexpr bool kDq = (MODE == kBwdDqNode || MODE == kBwdDqExact);
-  constexpr bool kExact = (MODE == kBwdDqExact || MODE == kBwdDkvExact);
+  constexpr bool kPacked = MODE == kBwdDqPacked || MODE == kBwdDkvPacked;
+  constexpr bool kDqExact = MODE == kBwdDqExact || MODE == kBwdDqPacked, kDkvExact = MODE == kBwdDkvExact || MODE == kBwdDkvPacked;
+  constexpr bool kDq = MODE == kBwdDqNode || kDqExact;
+  constexpr bool kExact = kDqExact || kDkvExact;
   constexpr bool kSorted = (MODE == kBwdDkvBlock || MODE == kBwdDkvSamp);  // T rows = a run of sorted query positions
   constexpr bool kHits = FINAL && MODE == kBwdDkvBlock;  // sampled keys' sums added here
   constexpr int KS = D / 16;
@@ -151,13 +160,27 @@ __global__ __launch_bounds__(kBNT * NG, FOUR ? 4 : bwd_waves_per_simd(D, MODE)) 
   const BwdWork b = decode_bwd_work<kRT, MODE>(a, kExact ? (int)blockIdx.x : logical_block(blockIdx.x, gridDim.x), (int)gridDim.x);
   const TileWork& w = b.w;
 
+  if (kPacked && w.rows_valid <= 0) return;
+
   const int64_t hs = f.q_bh_stride;
-  const uint16_t* Qh = reinterpret_cast<const uint16_t*>(f.Q) + (int64_t)w.bh * hs;
-  const uint16_t* Kh = reinterpret_cast<const uint16_t*>(f.K) + (int64_t)w.bh * hs;
-  const uint16_t* Vh = reinterpret_cast<const uint16_t*>(f.V) + (int64_t)w.bh * hs;
-  const uint16_t* Gh = reinterpret_cast<const uint16_t*>(a.dO) + (int64_t)w.bh * hs;
-  const float* lse_h = a.lse + (int64_t)w.bh * g.n;
-  const float* del_h = a.delta + (int64_t)w.bh * g.n;
+  const uint16_t* Qh = reinterpret_cast<const uint16_t*>(f.Q) + (kPacked ? (int64_t)b.seq_start * f.pk.q.row + (int64_t)w.bh * f.pk.q.head : (int64_t)w.bh * hs);
+  const uint16_t* Kh = reinterpret_cast<const uint16_t*>(f.K);
+  const uint16_t* Vh = reinterpret_cast<const uint16_t*>(f.V);
+  const uint16_t* Gh = reinterpret_cast<const uint16_t*>(a.dO) + (kPacked ? (int64_t)b.seq_start * f.pk.d_o.row + (int64_t)w.bh * f.pk.d_o.head : (int64_t)w.bh * hs);
+  if constexpr (kPacked) {
+    const int kv = w.bh / f.pk.group;
+    Kh += (int64_t)b.seq_start * f.pk.k.row + (int64_t)kv * f.pk.k.head;
+    Vh += (int64_t)b.seq_start * f.pk.v.row + (int64_t)kv * f.pk.v.head;
+  } else {
+    Kh += (int64_t)w.bh * hs;
+    Vh += (int64_t)w.bh * hs;
+  }
+  const int64_t lse_at = kPacked ? (int64_t)w.bh * f.pk.rows + b.seq_start : (int64_t)w.bh * g.n;
+  const float* lse_h = a.lse + lse_at;
+  const float* del_h = a.delta + lse_at;
+  // elements from one row to the next, of the four operands
+  const int64_t x_row = !kPacked ? D : kDq ? f.pk.q.row : f.pk.k.row, a_row = !kPacked ? D : kDq ? f.pk.d_o.row : f.pk.v.row;
+  const int y_row = !kPacked ? D : (int)(kDq ? f.pk.k.row : f.pk.q.row), b_row = !kPacked ? D : (int)(kDq ? f.pk.v.row : f.pk.d_o.row);
   const uint16_t* Xh = kDq ? Qh : Kh;   // R rows: x operand of the scores
   const uint16_t* Ah = kDq ? Gh : Vh;   // R rows: operand of dP
   const uint16_t* Yh = kDq ? Kh : Qh;   // T rows: y operand of the scores
@@ -181,8 +204,8 @@ __global__ __launch_bounds__(kBNT * NG, FOUR ? 4 : bwd_waves_per_simd(D, MODE)) 
   const int t_first = kSorted ? tperm[min(tid, nsorted - 1)] : 0;
   bf16x8 xreg[KS], areg[KS];
   {
-    const u32x4* xp = reinterpret_cast<const u32x4*>(Xh + (int64_t)r_row * D + 8 * h);
-    const u32x4* ap = reinterpret_cast<const u32x4*>(Ah + (int64_t)r_row * D + 8 * h);
+    const u32x4* xp = reinterpret_cast<const u32x4*>(Xh + r_row * x_row + 8 * h);
+    const u32x4* ap = reinterpret_cast<const u32x4*>(Ah + r_row * a_row + 8 * h);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
       xreg[ks] = __builtin_bit_cast(bf16x8, xp[2 * ks]);
@@ -201,7 +224,10 @@ __global__ __launch_bounds__(kBNT * NG, FOUR ? 4 : bwd_waves_per_simd(D, MODE)) 
   } else {
     nT = max(0, w.k1 - w.k0);
   }
-  const int ntiles = (nT + NG * kTT - 1) / (NG * kTT);  // of the group; its tile kt is tile NG kt + grp of the T rows
+  // tiles of the group; its tile kt is tile NG kt + grp of the T rows (packed dK / dV: of the query heads' T rows, one head behind the other)
+  constexpr bool kHeads = MODE == kBwdDkvPacked;
+  const int tph = (nT + kTT - 1) / kTT, all_tiles = kHeads ? b.heads * tph : tph;
+  const int ntiles = (all_tiles + NG - 1) / NG;
   const float bias2 = ((MODE == kBwdDqNode || MODE == kBwdDkvSamp) && g.m > 0) ? log2f((float)w.nr.s / (float)g.m) : 0.f;
   const float nat_bias = bias2 * kLn2;
 
@@ -216,7 +242,47 @@ __global__ __launch_bounds__(kBNT * NG, FOUR ? 4 : bwd_waves_per_simd(D, MODE)) 
   const int dcol = ((lane % CPR) ^ L::swz(drow)) * 16;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)bufs + 1024 * wave_s;
   float sc_l = 0.f, sc_d = 0.f;
+  // packed dK / dV: place of a group's next tile among the heads' T rows, stepped by NG
+  struct HeadTile {
+    int head, t;
+  };
+  auto to_head = [&](HeadTile& p) {
+    while (p.t >= tph) {
+      p.t -= tph;
+      ++p.head;
+    }
+  };
+  HeadTile req{0, grp}, cur{0, grp};
   auto request_tile = [&](int kt) {
+    if constexpr (kPacked) {
+      if (NG == 2 && NG * kt + grp >= all_tiles) return;
+      int t0 = (NG * kt + grp) * kTT, head = 0;
+      if constexpr (kHeads) {
+        to_head(req);
+        t0 = req.t * kTT;
+        head = req.head;
+        req.t += NG;
+      }
+      const int first = w.k0 + t0, last = nT - 1 - t0;  // the tile's first row; its last one there (past it that one again, masked)
+      if (!kDq && tid < kTT) {
+        const int64_t row = (int64_t)head * f.pk.rows + first + min(tid, last);
+        sc_l = lse_h[row];
+        sc_d = del_h[row];
+      }
+      const uint16_t* yp = Yh + (int64_t)first * y_row + (kHeads ? head * f.pk.q.head : 0);
+      const uint16_t* bp = Bh + (int64_t)first * b_row + (kHeads ? head * f.pk.d_o.head : 0);
+      const int span = min(kTT, last + 1);
+      const __amdgpu_buffer_rsrc_t ys = uniform_rsrc(yp, span * y_row * 2);
+      const __amdgpu_buffer_rsrc_t bs = uniform_rsrc(bp, span * b_row * 2);
+      const uint32_t at = lds0 + (kt & 1) * L::BUF;
+#pragma unroll
+      for (int ii = 0; ii < NDMA; ++ii) {
+        const int row = min(4 * RPI * ii + drow, last);
+        dma_1k(ys, at + 4096 * ii, row * (y_row * 2) + dcol);
+        dma_1k(bs, at + L::TILE + 4096 * ii, row * (b_row * 2) + dcol);
+      }
+      return;
+    }
     const int t0 = (NG * kt + grp) * kTT;
     if (NG == 2 && t0 >= nT) return;  // (the other group has the last tile)
     if (!kDq && tid < kTT) {
@@ -276,7 +342,8 @@ __global__ __launch_bounds__(kBNT * NG, FOUR ? 4 : bwd_waves_per_simd(D, MODE)) 
       // The lane's half of the row.  A launch of its own read dO once more.  Forward + backward, with it -> without (MI355X, us):
       // 12 heads, n = 16384, d = 64 217 -> 209; n = 32768, d = 128 820 -> 805; 2 heads, n = 4096 74.4 -> 73.8; exact, 12 heads, n =
       // 5000, d = 128 375 -> 373.
-      const int64_t at = ((int64_t)w.bh * g.n + r_row) * D + 8 * h;
+      const int64_t row32 = kPacked ? ((int64_t)(b.seq_start + r_row) * f.pk.Hq + w.bh) : (int64_t)w.bh * g.n + r_row;
+      const int64_t at = row32 * D + 8 * h;
       f32x4 s = {0.f, 0.f, 0.f, 0.f};
       auto add = [&](int ks, f32x4 o0, f32x4 o1) {
         const u32x4 dv = __builtin_bit_cast(u32x4, areg[ks]);
@@ -299,16 +366,17 @@ __global__ __launch_bounds__(kBNT * NG, FOUR ? 4 : bwd_waves_per_simd(D, MODE)) 
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) add(ks, o[2 * ks], o[2 * ks + 1]);
       } else {
+        const int64_t at16 = kPacked ? (int64_t)(b.seq_start + r_row) * f.pk.o.row + (int64_t)w.bh * f.pk.o.head + 8 * h : at;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
-          const u32x4 ob = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(a.O) + at + 16 * ks);
+          const u32x4 ob = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(a.O) + at16 + 16 * ks);
           add(ks, (f32x4){__uint_as_float(ob[0] << 16), __uint_as_float(ob[0] & 0xFFFF0000u), __uint_as_float(ob[1] << 16), __uint_as_float(ob[1] & 0xFFFF0000u)},
               (f32x4){__uint_as_float(ob[2] << 16), __uint_as_float(ob[2] & 0xFFFF0000u), __uint_as_float(ob[3] << 16), __uint_as_float(ob[3] & 0xFFFF0000u)});
         }
       }
       del_r = (s[0] + s[1]) + (s[2] + s[3]);
       del_r += __shfl_xor(del_r, 32);
-      if (h == 0 && grp == 0 && r_in_tile < w.rows_valid) a.delta_out[(int64_t)w.bh * g.n + r_row] = del_r;
+      if (h == 0 && grp == 0 && r_in_tile < w.rows_valid) a.delta_out[lse_at + r_row] = del_r;
     }
   }
 
@@ -333,21 +401,28 @@ __global__ __launch_bounds__(kBNT * NG, FOUR ? 4 : bwd_waves_per_simd(D, MODE)) 
     // the sampled key's own block, factor 1 - M of Algorithm 2).
     // Whether the tile has any is known from scalars, except in the sampled-key pass, whose keys differ by lane;
     // the limits themselves are formed inside the branch, so that they hold no registers across the products.
-    const int tbase = (NG * kt + grp) * kTT;
+    int tbase = (NG * kt + grp) * kTT;
+    bool mine = NG == 1 || tbase < nT;
+    if constexpr (kHeads) {
+      mine = NG == 1 || NG * kt + grp < all_tiles;
+      to_head(cur);
+      tbase = cur.t * kTT;
+      cur.t += NG;
+    }
     float nl2_t = nl2_r;
     if (MODE == kBwdDqNode && tbase >= nb) nl2_t += bias2;
     const int r_first = w.q0 + 32 * wave_s;   // exact passes: the wave's first R row
     bool special = tbase + kTT > nT;
     if (MODE == kBwdDqNode) special = special || (tbase < nb && tbase + kTT > nb);
-    if (MODE == kBwdDqExact && f.exact_causal) special = special || (w.k0 + tbase + kTT - 1 > r_first);
-    if (MODE == kBwdDkvExact && f.exact_causal) special = special || (w.k0 + tbase < r_first + 31);
+    if (kDqExact && f.exact_causal) special = special || (w.k0 + tbase + kTT - 1 > r_first);
+    if (kDkvExact && f.exact_causal) special = special || (w.k0 + tbase < r_first + 31);
     if (MODE == kBwdDkvSamp) {
       const int mlo = blk_r * g.b - (b.chunk_start + tbase);
       special = special || __any(mlo < kTT && mlo + g.b > 0);
     }
 
     // one 32-row half of the tile at a time: S^T = Y X^T and dP^T = Bt A^T, then P^T / dS^T
-    if (NG == 1 || tbase < nT)
+    if (mine)
 #pragma unroll
     for (int sub = 0; sub < 2; ++sub) {
       // dK / dV passes start the sums at bias - L and -delta of the T rows, straight from LDS; in the dQ passes,
@@ -393,8 +468,8 @@ __global__ __launch_bounds__(kBNT * NG, FOUR ? 4 : bwd_waves_per_simd(D, MODE)) 
       if constexpr (kPrio) __builtin_amdgcn_s_setprio(0);
       if (special) {  // rare tiles, behind a branch: folded into the weights' code the tests would double it
         int hi2 = nT - tbase - 4 * h, lo2 = 0;
-        if (MODE == kBwdDqExact && f.exact_causal) hi2 = min(hi2, r_row - w.k0 - tbase + 1 - 4 * h);
-        if (MODE == kBwdDkvExact && f.exact_causal) lo2 = r_row - w.k0 - tbase - 4 * h;
+        if (kDqExact && f.exact_causal) hi2 = min(hi2, r_row - w.k0 - tbase + 1 - 4 * h);
+        if (kDkvExact && f.exact_causal) lo2 = r_row - w.k0 - tbase - 4 * h;
         const int mlo2 = blk_r * g.b - (b.chunk_start + tbase) - 4 * h;
         const int nb2 = (tbase < nb ? nb : 0x40000000) - tbase - 4 * h;  // a tile past nb has its bias already
 #pragma unroll
@@ -402,7 +477,7 @@ __global__ __launch_bounds__(kBNT * NG, FOUR ? 4 : bwd_waves_per_simd(D, MODE)) 
           const int ko = 32 * sub + 8 * (i / 4) + (i % 4);
           if (MODE == kBwdDqNode && ko >= nb2) cs[i] += nat_bias;
           bool msk = ko >= hi2;
-          if (MODE == kBwdDkvExact) msk = msk || (ko < lo2);
+          if (kDkvExact) msk = msk || (ko < lo2);
           if (MODE == kBwdDkvSamp) msk = msk || ((unsigned)(ko - mlo2) < (unsigned)g.b);
           if (msk) cs[i] = -INFINITY;
         }
@@ -485,7 +560,7 @@ __global__ __launch_bounds__(kBNT * NG, FOUR ? 4 : bwd_waves_per_simd(D, MODE)) 
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
   };
-  auto write_out = [&](const auto& acc, float* dst32, const float* samp, uint16_t* dst16, const float* lvl) {
+  auto write_out = [&](const auto& acc, float* dst32, const float* samp, uint16_t* dst16, const float* lvl, const RowStrides& fin) {
     // ---- epilogue: the wave's 32 rows leave through an LDS transpose as whole rows.
     // Node passes write or add fp32 rows into the accumulated rows (unmasked problems: write the final gradient).
     // Exact passes (the base case of Algorithm 4) write the final gradient in the tensors' dtype, after
@@ -503,7 +578,7 @@ __global__ __launch_bounds__(kBNT * NG, FOUR ? 4 : bwd_waves_per_simd(D, MODE)) 
     if (h == 0) {  // (the row's index is fetched again: kept across the loop it would cost registers)
       int r = wave * 32 + lq, blk;
       asm volatile("" : "+v"(r));
-      ep_rows[lq] = r < w.rows_valid ? bwd_out_row<MODE>(a, b, r, bwd_r_row<MODE>(a, b, r, &blk)) : (int64_t)-1;
+      ep_rows[lq] = r >= w.rows_valid ? (int64_t)-1 : kPacked ? (int64_t)b.seq_start + w.q0 + r : bwd_out_row<MODE>(a, b, r, bwd_r_row<MODE>(a, b, r, &blk));
     }
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
@@ -582,6 +657,30 @@ __global__ __launch_bounds__(kBNT * NG, FOUR ? 4 : bwd_waves_per_simd(D, MODE)) 
       }
       return;
     }
+    if constexpr (kPacked) {
+      const int head = kHeads ? w.bh / f.pk.group : w.bh;
+      if (kHeads && dst32 != nullptr) {  // a part of the group's heads: fp32 rows that are added up by a launch of their own
+        constexpr int CH = D / 4, IT = 32 / NG * CH / 64;
+#pragma unroll
+        for (int it = 0; it < IT; ++it) {
+          const int idx = lane + 64 * it, row = row0 + idx / CH, ch = idx % CH;
+          const int64_t r = ep_rows[row];
+          const f32x4 v = sums_at(row, ch * 16);
+          if (r >= 0) *reinterpret_cast<f32x4*>(dst32 + (((int64_t)b.chunk_start * f.pk.rows + r) * f.pk.Hk + head) * D + ch * 4) = v;
+        }
+        return;
+      }
+      constexpr int CH = D / 8, IT = 32 / NG * CH / 64;
+#pragma unroll
+      for (int it = 0; it < IT; ++it) {
+        const int idx = lane + 64 * it, row = row0 + idx / CH, ch = idx % CH;
+        const int64_t r = ep_rows[row];
+        const f32x4 v0 = sums_at(row, ch * 32), v1 = sums_at(row, ch * 32 + 16);
+        const u32x4 pk = {pack_bf16x2(v0.x, v0.y), pack_bf16x2(v0.z, v0.w), pack_bf16x2(v1.x, v1.y), pack_bf16x2(v1.z, v1.w)};
+        if (r >= 0) __builtin_nontemporal_store(pk, reinterpret_cast<u32x4*>(dst16 + r * fin.row + (int64_t)head * fin.head + ch * 8));
+      }
+      return;
+    }
     // the 32 rows of a wave lie in one n_min block: the node passes hold all of them or none
     const int i0 = w.q0 + 32 * __builtin_amdgcn_readfirstlane(wave);
     const bool fold = kExact && lvl != nullptr && node_levels_hold(g, i0, kDq, g.levels);
@@ -632,10 +731,10 @@ __global__ __launch_bounds__(kBNT * NG, FOUR ? 4 : bwd_waves_per_simd(D, MODE)) 
       if (r64[it] >= 0) __builtin_nontemporal_store(pk, reinterpret_cast<u32x4*>(dst16 + r64[it] * D + ch * 8));
     }
   };
-  write_out(acc1, a.out1, a.samp1, reinterpret_cast<uint16_t*>(a.fin1), a.lvl1);
+  write_out(acc1, a.out1, a.samp1, reinterpret_cast<uint16_t*>(a.fin1), a.lvl1, f.pk.fin1);
   if constexpr (!kDq) {
     staged();  // (one group: a wave rewrites only its own staging area, which its own reads above have left)
-    write_out(acc2, a.out2, a.samp2, reinterpret_cast<uint16_t*>(a.fin2), a.lvl2);
+    write_out(acc2, a.out2, a.samp2, reinterpret_cast<uint16_t*>(a.fin2), a.lvl2, f.pk.fin2);
   }
 }
 
@@ -644,6 +743,7 @@ static int launch_bwd_form(const BwdArgs& args, int grid, hipStream_t st) {
   BwdArgs a = args;
   if (MODE == kBwdDqNode || MODE == kBwdDkvBlock) set_node_divs<kRT>(a.f);
   if (MODE == kBwdDqExact || MODE == kBwdDkvExact) set_exact_divs<kRT>(a.f);
+  if (MODE == kBwdDqPacked || MODE == kBwdDkvPacked) set_packed_divs(a.f, MODE == kBwdDqPacked ? a.f.pk.group : a.f.pk.splits);
   a.f.exact_lpt = NG == 2;
   const size_t lds = bwd_lds_bytes<D, NG>(a, MODE);
   static std::atomic<uint64_t> lds_set{0};  // per instantiation: devices on which the LDS limit is raised
@@ -703,13 +803,24 @@ static int launch_bwd_d(const BwdArgs& a, int mode, int grid, hipStream_t st) {
     case kBwdDkvBlock: return launch_bwd_one<D, kBwdDkvBlock>(a, grid, st);
     case kBwdDkvSamp: return launch_bwd_one<D, kBwdDkvSamp>(a, grid, st);
     case kBwdDkvExact: return launch_bwd_one<D, kBwdDkvExact>(a, grid, st);
+    case kBwdDqPacked: return launch_bwd_one<D, kBwdDqPacked>(a, grid, st);
+    case kBwdDkvPacked: return launch_bwd_one<D, kBwdDkvPacked>(a, grid, st);
     default: return HA_ERR_SHAPE;
   }
 }
 
-int launch_attn_bwd_mfma(const BwdArgs& a, int mode, hipStream_t st) {
+int launch_attn_bwd_mfma(const BwdArgs& args, int mode, hipStream_t st) {
+  BwdArgs a = args;
   if (a.f.g.dtype != HA_BF16) return HA_ERR_DTYPE;
-  const int64_t grid64 = bwd_grid<kRT>(a, mode);
+  int64_t grid64;
+  if (mode == kBwdDqPacked || mode == kBwdDkvPacked) {
+    const int64_t slots = packed_slots<kRT>(a.f.pk);
+    grid64 = slots * (mode == kBwdDqPacked ? a.f.pk.Hq : a.f.pk.Hk * a.f.pk.splits);
+    if (grid64 > kMaxLaunch) return HA_ERR_SHAPE;
+    a.f.pk.slots = (int32_t)slots;
+  } else {
+    grid64 = bwd_grid<kRT>(a, mode);
+  }
   if (grid64 > kMaxGrid) return HA_ERR_SHAPE;
   const int grid = (int)grid64;
   if (a.f.g.d == 128) return launch_bwd_d<128>(a, mode, grid, st);

@@ -164,6 +164,86 @@ __host__ __device__ inline int64_t exact_grid(const AttnArgs& a) {
   return (int64_t)a.g.BH * nblk * tpb;
 }
 
+// Packed sequences.  Tiles of QT rows of a sequence, counted over all sequences without a pass over them: sequence s gets the numbers from
+// floor(cu[s] / QT) + s on.  It has at most floor(cu[s + 1] / QT) - floor(cu[s] / QT) + 1 tiles, so the ranges do not meet, the sequence of a number
+// is found by bisection, and at most n_seq numbers, whose workgroups end at once, have no tile.  The host needs no lengths.
+template <int QT>
+inline int64_t packed_slots(const PackedRows& p) { return (int64_t)p.rows / QT + p.n_seq; }
+
+__device__ inline int packed_start(const PackedRows& p, int s) { return min(max(p.cu[s], 0), p.rows); }
+
+struct PackedTile {
+  int start, len;  // the sequence's rows
+  int tile;        // of QT rows within it; >= tiles(len): none
+};
+
+// 64 probes at a time: two round trips for up to 4096 sequences
+template <int QT>
+__device__ inline PackedTile packed_tile(const PackedRows& p, int slot) {
+  const int lane = __lane_id();
+  int lo = 0, n = p.n_seq;
+  while (n > 1) {
+    const int step = (n + 63) >> 6, at = lo + lane * step;
+    const bool in = lane * step < n;
+    const bool le = in && packed_start(p, in ? at : lo) / QT + at <= slot;
+    const unsigned long long bal = __ballot(le);
+    const int i = bal ? 63 - __builtin_clzll(bal) : 0;
+    lo += i * step;
+    n = min(step, n - i * step);
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  PackedTile t;
+  t.start = __builtin_amdgcn_readfirstlane(packed_start(p, lo));
+  t.len = __builtin_amdgcn_readfirstlane(max(packed_start(p, lo + 1), t.start)) - t.start;
+  t.tile = slot - (t.start / QT + lo);
+  return t;
+}
+
+// Order of a packed launch's workgroups: the tiles in order of the sequences, the heads that share K and V beside each other and on one XCD, whose L2 then
+// holds the sequence's rows of few key heads.  Where the key heads are a multiple of 8, every XCD has the tiles of its own ones.
+struct PackedPlace {
+  int slot, kv, sub;  // tile number, key head, and which of `per` workgroups of it
+};
+inline void set_packed_divs(AttnArgs& a, int per) {  // per: workgroups of a key head's tile (query heads, or splits of dK / dV)
+  a.div_tpb = make_fast_div(per);
+  a.div_tpl = make_fast_div((int64_t)a.pk.slots * per);
+  a.div_unit = make_fast_div((int64_t)a.pk.Hk * per);
+}
+__device__ inline PackedPlace packed_place(const AttnArgs& a, int wg) {
+  const int Hk = a.pk.Hk, per = (int)a.div_tpb.d;
+  PackedPlace p;
+  if ((Hk & 7) == 0) {
+    const int xcd = wg & 7, j = wg >> 3;
+    const int k = a.div_tpl.div(j), rest = j - k * (int)a.div_tpl.d;
+    p.kv = 8 * k + xcd;
+    p.slot = a.div_tpb.div(rest);
+    p.sub = rest - p.slot * per;
+  } else {
+    p.slot = a.div_unit.div(wg);
+    int h = wg - p.slot * (int)a.div_unit.d;
+    if (((Hk * per) & 7) == 0) h = (h & 7) * ((Hk * per) >> 3) + (h >> 3);
+    p.kv = a.div_tpb.div(h);
+    p.sub = h - p.kv * per;
+  }
+  return p;
+}
+
+// w.bh: the query head.  Rows are counted from the sequence's start; causal tiles come last rows, the most keys, first.
+template <int QT>
+__device__ inline TileWork decode_packed_tile(const AttnArgs& a, int wg, int* start) {
+  TileWork w{};
+  const PackedPlace p = packed_place(a, wg);
+  const PackedTile t = packed_tile<QT>(a.pk, p.slot);
+  *start = t.start;
+  w.bh = p.kv * a.pk.group + p.sub;
+  const int tiles = (t.len + QT - 1) / QT;
+  if (t.tile < 0 || t.tile >= tiles) return w;
+  w.q0 = (tiles - 1 - t.tile) * QT;
+  w.rows_valid = min(QT, t.len - w.q0);
+  w.k1 = a.exact_causal ? w.q0 + w.rows_valid : t.len;
+  return w;
+}
+
 constexpr int64_t kMaxGrid = 0x7fffffff;  // workgroup ids are decoded as 32-bit integers
 
 // The first index values a thread contributes to the key list (block key `tid`, sample `tid` and

@@ -47,7 +47,7 @@ struct F32Lds {
 // What the loop keeps in front of the tiles: the key list, and behind it the rows drawn by value norm with their weights and the waves'
 // masked sums.
 __host__ __device__ inline size_t f32_list_bytes(int b, int m, int mode) {
-  if (mode == kModeExact) return 0;
+  if (mode == kModeExact || mode == kModePacked) return 0;
   const size_t list = (size_t)(((b + m + 63) & ~63) + 64) * 4 + 64;
   const size_t cap = mode == kModeCap || mode == kModeValue ? 4 * 32 * 2 * 4 : 0;
   const size_t drawn = mode == kModeValue ? 2 * (size_t)((m + 63) & ~63) * 4 : 0;
@@ -108,6 +108,7 @@ __global__ __launch_bounds__(64 * f32_waves(KW), D == 128 && KW < 4 ? 1 : D == 6
   constexpr int kQT = 32 * RG;
   using T = SplitTile<D>;
   constexpr bool kValue = MODE == kModeValue, kCap = MODE == kModeCap || kValue, kNode = MODE == kModeNode || kCap;
+  constexpr bool kPacked = MODE == kModePacked, kExact = MODE == kModeExact || kPacked;
   constexpr int KJ = D / 8;    // 16-byte pieces of a row per lane
   constexpr int KS = D / 16;   // steps of a score's product
   constexpr int DT = D / 32;
@@ -122,6 +123,7 @@ __global__ __launch_bounds__(64 * f32_waves(KW), D == 128 && KW < 4 ? 1 : D == 6
 
   const int bid = a.wg_first + (kNode ? logical_block(blockIdx.x, gridDim.x) : (int)blockIdx.x);
   TileWork w;
+  int seq_start = 0;  // packed mode: the sequence's first row, from which all others count
   int nb, nkeys;
   int32_t* qrows = reinterpret_cast<int32_t*>(smem + (SORT ? f32_qrows_at<D, KW>(a.g) : 0));
   unsigned char* tiles_at = smem + f32_list_bytes(a.g.b, a.g.m, MODE);
@@ -136,7 +138,12 @@ __global__ __launch_bounds__(64 * f32_waves(KW), D == 128 && KW < 4 ? 1 : D == 6
     w = decode_node_tile<kQT>(a, bid);
     nkeys = build_key_list<kFNT, kCap>(a, w, list, scratch, &nb, key_list_fetch<kFNT>(a, w));
   } else {
-    w = decode_exact_tile<kQT>(a, bid);
+    if constexpr (kPacked) {
+      w = decode_packed_tile<kQT>(a, bid, &seq_start);
+      if (w.rows_valid <= 0) return;
+    } else {
+      w = decode_exact_tile<kQT>(a, bid);
+    }
     nkeys = max(0, w.k1 - w.k0);
     nb = 0x7fffffff;
   }
@@ -144,7 +151,7 @@ __global__ __launch_bounds__(64 * f32_waves(KW), D == 128 && KW < 4 ? 1 : D == 6
   // causal: a wave ends with the tile that holds its own last row.  Tiles wholly behind its rows are not only idle work:
   // weight 0 times a V that is Inf or NaN is NaN.
   int wg_tiles = ntiles;  // of the workgroup
-  if (MODE == kModeExact && a.exact_causal) ntiles = min(ntiles, (w.q0 - w.k0) / kFKT + grp + 1);
+  if (kExact && a.exact_causal) ntiles = min(ntiles, (w.q0 - w.k0) / kFKT + grp + 1);
   // value mode: the rows drawn by value norm, all m of them for every block, follow in tiles of their own
   const int vt0 = ntiles, drawn_at = (((a.g.b + a.g.m + 63) & ~63) + 64) + ((a.g.m + 63) & ~63);
   float* drawn_w = reinterpret_cast<float*>(list + drawn_at);  // -log(m p); -inf past the end
@@ -160,9 +167,21 @@ __global__ __launch_bounds__(64 * f32_waves(KW), D == 128 && KW < 4 ? 1 : D == 6
   }
   const float nat_bias = (kNode && a.g.m > 0) ? logf((float)w.nr.s / (float)a.g.m) : 0.f;
 
-  const float* Qh = reinterpret_cast<const float*>(a.Q) + (int64_t)w.bh * a.q_bh_stride;
-  const float* Kh = reinterpret_cast<const float*>(a.K) + (int64_t)w.bh * a.k_bh_stride;
-  const float* Vh = reinterpret_cast<const float*>(a.V) + (int64_t)w.bh * a.k_bh_stride;
+  const float* Qh = reinterpret_cast<const float*>(a.Q);
+  const float* Kh = reinterpret_cast<const float*>(a.K);
+  const float* Vh = reinterpret_cast<const float*>(a.V);
+  if constexpr (kPacked) {
+    const int kv = w.bh / a.pk.group;
+    Qh += (int64_t)seq_start * a.pk.q.row + (int64_t)w.bh * a.pk.q.head;
+    Kh += (int64_t)seq_start * a.pk.k.row + (int64_t)kv * a.pk.k.head;
+    Vh += (int64_t)seq_start * a.pk.v.row + (int64_t)kv * a.pk.v.head;
+  } else {
+    Qh += (int64_t)w.bh * a.q_bh_stride;
+    Kh += (int64_t)w.bh * a.k_bh_stride;
+    Vh += (int64_t)w.bh * a.k_bh_stride;
+  }
+  const int64_t q_row = kPacked ? a.pk.q.row : (int64_t)D;
+  const int k_row = kPacked ? (int)a.pk.k.row * 4 : D * 4, v_row = kPacked ? (int)a.pk.v.row * 4 : D * 4;  // bytes from one row to the next
   const int r_in_tile = grp * 32 + lq;
   const int r_use = r_in_tile < w.rows_valid ? r_in_tile : 0;
   int qrow, q_global = 0;
@@ -180,14 +199,14 @@ __global__ __launch_bounds__(64 * f32_waves(KW), D == 128 && KW < 4 ? 1 : D == 6
   if constexpr (kShared) {
     f32x4 qf[KJ];
 #pragma unroll
-    for (int j = 0; j < KJ; ++j) qf[j] = *reinterpret_cast<const f32x4*>(Qh + (int64_t)qrow * D + 16 * (j / 2) + 8 * h + 4 * (j % 2));
+    for (int j = 0; j < KJ; ++j) qf[j] = *reinterpret_cast<const f32x4*>(Qh + qrow * q_row + 16 * (j / 2) + 8 * h + 4 * (j % 2));
 #pragma unroll
     for (int s = 0; s < KS; ++s) q[s] = split8_raw([&](int e) { return qf[2 * s + e / 4][e % 4]; });
   } else {
     for (int i = tid; i < 32 * T::PPR; i += kFNT) {
       const int r = i / T::PPR, piece = i % T::PPR, ru = r < w.rows_valid ? r : 0;
       const int row = SORT ? qrows[ru] : kNode && a.perm_q ? a.perm_q[w.seg_off + w.p0 + ru] : kNode ? w.nr.q_start + w.p0 + ru : w.q0 + ru;
-      const f32x4* at = reinterpret_cast<const f32x4*>(Qh + (int64_t)row * D + piece * 8);
+      const f32x4* at = reinterpret_cast<const f32x4*>(Qh + row * q_row + piece * 8);
       T::store(tiles_at, r, piece, at[0], at[1]);
     }
   }
@@ -196,31 +215,40 @@ __global__ __launch_bounds__(64 * f32_waves(KW), D == 128 && KW < 4 ? 1 : D == 6
   const uint32_t bytes = (uint32_t)(kNode ? a.g.n : w.k1) * (uint32_t)(D * 4);
   const __amdgpu_buffer_rsrc_t krsrc = __builtin_amdgcn_make_buffer_rsrc((void*)Kh, 0, (int)bytes, 0x00020000);
   const __amdgpu_buffer_rsrc_t vrsrc = __builtin_amdgcn_make_buffer_rsrc((void*)Vh, 0, (int)bytes, 0x00020000);
+  // packed mode: a descriptor per tile, which ends with the workgroup's keys; rows count from the tile's first
+  auto tile_rsrc = [&](const __amdgpu_buffer_rsrc_t& whole, const float* head, int row_bytes, int kt) {
+    if constexpr (!kPacked) return whole;
+    const int row = kt * kFKT;
+    return __builtin_amdgcn_make_buffer_rsrc((void*)(reinterpret_cast<const unsigned char*>(head) + (int64_t)row * row_bytes), 0,
+                                             max(0, min(kFKT, w.k1 - row)) * row_bytes, 0x00020000);
+  };
   f32x4 kf[kShared ? 1 : KJ];
   auto load_k = [&](int kt, int j0 = 0, int j1 = D / 8) {
     if constexpr (kShared) return;
-    const int row = kNode ? list[kt * kFKT + lq] : w.k0 + kt * kFKT + lq;
+    const int row = kNode ? list[kt * kFKT + lq] : kPacked ? lq : w.k0 + kt * kFKT + lq;
+    const __amdgpu_buffer_rsrc_t rsrc = tile_rsrc(krsrc, Kh, k_row, kt);
     if constexpr (FAR) {  // (every row of the list exists)
 #pragma unroll
       for (int j = j0; j < j1; ++j) kf[kShared ? 0 : j] = *reinterpret_cast<const f32x4*>(Kh + (int64_t)row * D + 16 * (j / 2) + 8 * h + 4 * (j % 2));
       return;
     }
-    const int off = row * (D * 4) + 32 * h;
+    const int off = row * k_row + 32 * h;
 #pragma unroll
     for (int j = j0; j < j1; ++j)
-      kf[kShared ? 0 : j] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(krsrc, off + 16 * (j % 2), 64 * (j / 2), 0));
+      kf[kShared ? 0 : j] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, off + 16 * (j % 2), 64 * (j / 2), 0));
   };
   // V rows of the tile, columns 32 dt + lq for dt in [dt0, dt0 + DTA): element i of a lane is key
   // 8 (i / 4) + 4 h + i % 4, the key of accumulator register i
   auto load_v = [&](int kt, int dt0, float (&v)[kShared ? 1 : 16][DTA]) {
     if constexpr (kShared) return;
+    const __amdgpu_buffer_rsrc_t rsrc = tile_rsrc(vrsrc, Vh, v_row, kt);
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       i32x4 rows;
       if (kNode) {
         rows = *reinterpret_cast<const i32x4*>(list + kt * kFKT + 8 * g + 4 * h);
       } else {
-        const int r0 = w.k0 + kt * kFKT + 8 * g + 4 * h;
+        const int r0 = (kPacked ? 0 : w.k0 + kt * kFKT) + 8 * g + 4 * h;
         rows = (i32x4){r0, r0 + 1, r0 + 2, r0 + 3};
       }
 #pragma unroll
@@ -228,7 +256,7 @@ __global__ __launch_bounds__(64 * f32_waves(KW), D == 128 && KW < 4 ? 1 : D == 6
 #pragma unroll
         for (int dt = 0; dt < DTA; ++dt)
           v[kShared ? 0 : 4 * g + z][dt] = FAR ? Vh[(int64_t)rows[z] * D + 32 * (dt0 + dt) + lq]
-                                 : __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(vrsrc, rows[z] * (D * 4) + 4 * lq,
+                                 : __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rsrc, rows[z] * v_row + 4 * lq,
                                                                                        128 * (dt0 + dt), 0));
     }
   };
@@ -240,15 +268,17 @@ __global__ __launch_bounds__(64 * f32_waves(KW), D == 128 && KW < 4 ? 1 : D == 6
   unsigned char* vtile = ktile + T::BYTES;
   f32x4 ks[NP][2], vs[NP][2];
   auto fetch = [&](int kt) {
+    const __amdgpu_buffer_rsrc_t kr = tile_rsrc(krsrc, Kh, k_row, kt), vr = tile_rsrc(vrsrc, Vh, v_row, kt);
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       const int r = (wtid + i * 64 * RG) / T::PPR, piece = (wtid + i * 64 * RG) % T::PPR;
-      const int off = (kNode ? list[kt * kFKT + r] : w.k0 + kt * kFKT + r) * (D * 4) + piece * 32;
-      ks[i][0] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(krsrc, off, 0, 0));
-      ks[i][1] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(krsrc, off + 16, 0, 0));
+      const int row = kNode ? list[kt * kFKT + r] : kPacked ? r : w.k0 + kt * kFKT + r;
+      const int off = row * k_row + piece * 32, voff = row * v_row + piece * 32;
+      ks[i][0] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(kr, off, 0, 0));
+      ks[i][1] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(kr, off + 16, 0, 0));
       if (kValue && kt < vt0) continue;
-      vs[i][0] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(vrsrc, off, 0, 0));
-      vs[i][1] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(vrsrc, off + 16, 0, 0));
+      vs[i][0] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(vr, voff, 0, 0));
+      vs[i][1] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(vr, voff + 16, 0, 0));
     }
   };
   auto store = [&](int kt) {
@@ -392,10 +422,10 @@ __global__ __launch_bounds__(64 * f32_waves(KW), D == 128 && KW < 4 ? 1 : D == 6
         }
       }
       const bool plain = kCap || base + kFKT <= min(nkeys, nb) &&
-                         !(MODE == kModeExact && a.exact_causal && w.k0 + base + kFKT - 1 > w.q0 + grp * 32);
+                         !(kExact && a.exact_causal && w.k0 + base + kFKT - 1 > w.q0 + grp * 32);
       if (!plain) {
         int lim = nkeys;
-        if (MODE == kModeExact && a.exact_causal) lim = min(lim, q_global - w.k0 + 1);
+        if (kExact && a.exact_causal) lim = min(lim, q_global - w.k0 + 1);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int pos = base + 8 * (i / 4) + 4 * h + (i % 4);
@@ -573,6 +603,12 @@ __global__ __launch_bounds__(64 * f32_waves(KW), D == 128 && KW < 4 ? 1 : D == 6
       }
       lse = Lm;
     }
+    if constexpr (kPacked) {
+      const int64_t row = (int64_t)seq_start + w.q0 + r;
+      *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.out) + row * a.pk.o.row + (int64_t)w.bh * a.pk.o.head + col) = acc;
+      if (col == 0) a.lse[(int64_t)w.bh * a.pk.rows + row] = lse;
+      continue;
+    }
     if (a.out != nullptr) *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.out) + dest.out_row * D + col) = acc;
     if (a.lse != nullptr && col == 0) a.lse[dest.out_row] = lse;
   }
@@ -582,10 +618,19 @@ template <int D, int MODE, int KW, bool FAR = false, bool SORT = false>
 static int launch_f32_one(const AttnArgs& args, hipStream_t st) {
   constexpr int kQT = 32 * (f32_waves(KW) / KW), NT = 64 * f32_waves(KW);
   AttnArgs a = args;
-  if (MODE != kModeExact) set_node_divs<kQT>(a);
-  else set_exact_divs<kQT>(a);
+  int64_t grid;
+  if constexpr (MODE == kModePacked) {
+    const int64_t slots = packed_slots<kQT>(a.pk);
+    grid = slots * a.pk.Hq;
+    if (grid > kMaxLaunch) return HA_ERR_SHAPE;
+    a.pk.slots = (int32_t)slots;
+    set_packed_divs(a, a.pk.group);
+  } else {
+    if (MODE != kModeExact) set_node_divs<kQT>(a);
+    else set_exact_divs<kQT>(a);
+    grid = MODE != kModeExact ? node_grid<kQT>(a.g) : exact_grid<kQT>(a);
+  }
   a.exact_lpt = KW == 8;
-  const int64_t grid = MODE != kModeExact ? node_grid<kQT>(a.g) : exact_grid<kQT>(a);
   if (grid <= 0) return HA_OK;
   if (grid > kMaxGrid) return HA_ERR_SHAPE;
   const size_t lds = SORT ? f32_qrows_at<D, KW>(a.g) + kQT * 4 : f32_lds_bytes<D, KW>(a.g.b, a.g.m, MODE);
@@ -689,9 +734,22 @@ static int launch_f32_mode(const AttnArgs& a, hipStream_t st) {
   return launch_f32_one<D, MODE, 4>(a, st);
 }
 
+// Packed sequences: the same, by the average length and an upper bound of the workgroups.
+template <int D>
+static int launch_f32_packed(const AttnArgs& a, hipStream_t st) {
+  const int64_t avg = a.pk.rows / (a.pk.n_seq > 0 ? a.pk.n_seq : 1);
+  if (avg >= 512 && packed_slots<32>(a.pk) * a.pk.Hq <= (!a.exact_causal ? 256 : avg < 2048 ? 384 : 512)) return launch_f32_one<D, kModePacked, 8>(a, st);
+  const int kw = f32_ways(D, (int)avg, packed_slots<128>(a.pk) * a.pk.Hq, a.exact_causal);
+  if (kw == 1) return launch_f32_one<D, kModePacked, 1>(a, st);
+  if constexpr (D == 64)
+    if (kw == 2) return launch_f32_one<D, kModePacked, 2>(a, st);
+  return launch_f32_one<D, kModePacked, 4>(a, st);
+}
+
 int launch_attn_f32(const AttnArgs& a, int mode, hipStream_t st) {
   if (a.g.dtype != HA_FP32) return HA_ERR_DTYPE;
   if (a.g.d != 64 && a.g.d != 128) return HA_ERR_SHAPE;
+  if (mode == kModePacked) return a.g.d == 128 ? launch_f32_packed<128>(a, st) : launch_f32_packed<64>(a, st);
   if (mode == kModeNode) return a.g.d == 128 ? launch_f32_mode<128, kModeNode>(a, st) : launch_f32_mode<64, kModeNode>(a, st);
   if (mode == kModeCap) return a.g.d == 128 ? launch_f32_mode<128, kModeCap>(a, st) : launch_f32_mode<64, kModeCap>(a, st);
   if (mode == kModeValue) return a.g.d == 128 ? launch_f32_mode<128, kModeValue>(a, st) : launch_f32_mode<64, kModeValue>(a, st);

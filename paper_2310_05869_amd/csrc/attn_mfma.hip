@@ -13,6 +13,8 @@
 //               and the n_min base case of Algorithm 4, whose epilogue also
 //               folds in the per-level partial results of the recursion
 //               (row sum = D_21 + D_C22 at every split).
+//   packed mode exact mode over packed sequences: a tile of rows of one sequence against that sequence's keys, rows of all
+//               tensors at the caller's strides, query heads in groups that share a key head.
 //
 // Tiling (wave64, v_mfma_f32_32x32x16_bf16):
 //   * 4 waves per workgroup, 32 queries per wave, 64 keys per step.
@@ -65,7 +67,7 @@ __host__ __device__ inline int list_capacity(int b, int m) { return ((b + m + 63
 template <int D>
 __host__ __device__ inline size_t mfma_lds_bytes(int b, int m, int mode) {
   size_t s = 2 * (size_t)Lds<D>::BUF + 64;  // + wave counters
-  if (mode != kModeExact) s += (size_t)list_capacity(b, m) * 4;
+  if (mode != kModeExact && mode != kModePacked) s += (size_t)list_capacity(b, m) * 4;
   return s;
 }
 
@@ -96,6 +98,7 @@ __global__ __launch_bounds__(64 * NW * NG, (D == 64 && NW == 4 && NG == 1) ? 3 :
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   constexpr bool kCap = MODE == kModeCap;
   constexpr bool kNode = MODE == kModeNode || kCap;
+  constexpr bool kPacked = MODE == kModePacked, kExact = MODE == kModeExact || kPacked;
   constexpr int kQT = 32 * NW;  // queries per workgroup
   constexpr int kNT = 64 * NW;  // threads of a group
   using L = Lds<D>;
@@ -126,12 +129,27 @@ __global__ __launch_bounds__(64 * NW * NG, (D == 64 && NW == 4 && NG == 1) ? 3 :
 
   const int bid = (kCap ? a.wg_first : 0) + (kNode ? logical_block(blockIdx.x, gridDim.x) : (int)blockIdx.x);
   TileWork w;
+  int seq_start = 0;  // packed mode: the sequence's first row, from which all others count
   if (kNode) w = decode_node_tile<kQT>(a, bid);
+  else if (kPacked) w = decode_packed_tile<kQT>(a, bid, &seq_start);
   else w = decode_exact_tile<kQT>(a, bid);
+  if (kPacked && w.rows_valid <= 0) return;
 
-  const uint16_t* Qh = reinterpret_cast<const uint16_t*>(a.Q) + (int64_t)w.bh * a.q_bh_stride;
-  const uint16_t* Kh = reinterpret_cast<const uint16_t*>(a.K) + (int64_t)w.bh * a.k_bh_stride;
-  const uint16_t* Vh = reinterpret_cast<const uint16_t*>(a.V) + (int64_t)w.bh * a.k_bh_stride;
+  const uint16_t* Qh = reinterpret_cast<const uint16_t*>(a.Q);
+  const uint16_t* Kh = reinterpret_cast<const uint16_t*>(a.K);
+  const uint16_t* Vh = reinterpret_cast<const uint16_t*>(a.V);
+  if constexpr (kPacked) {
+    const int kv = w.bh / a.pk.group;
+    Qh += (int64_t)seq_start * a.pk.q.row + (int64_t)w.bh * a.pk.q.head;
+    Kh += (int64_t)seq_start * a.pk.k.row + (int64_t)kv * a.pk.k.head;
+    Vh += (int64_t)seq_start * a.pk.v.row + (int64_t)kv * a.pk.v.head;
+  } else {
+    Qh += (int64_t)w.bh * a.q_bh_stride;
+    Kh += (int64_t)w.bh * a.k_bh_stride;
+    Vh += (int64_t)w.bh * a.k_bh_stride;
+  }
+  // bytes from one row to the next (packed: at most 2^23, and tiles have descriptors of their own)
+  const int k_row = kPacked ? (int)a.pk.k.row * 2 : D * 2, v_row = kPacked ? (int)a.pk.v.row * 2 : D * 2;
 
   // ---- this lane's query row: B operand of S^T = K Q^T, kept in registers.
   // Node mode: the key list's first index values and the row's own index (through P_Q) travel
@@ -169,11 +187,11 @@ __global__ __launch_bounds__(64 * NW * NG, (D == 64 && NW == 4 && NG == 1) ? 3 :
     q_global = w.q0 + r_in_tile;
     qrow_load = dest.valid ? q_global : w.q0;
     dest.row_in_head = q_global;
-    dest.out_row = (int64_t)w.bh * (a.out_bh_stride / D) + q_global;
+    dest.out_row = kPacked ? (int64_t)seq_start + q_global : (int64_t)w.bh * (a.out_bh_stride / D) + q_global;
   }
   bf16x8 qreg[KS];
   {
-    const u32x4* qp = reinterpret_cast<const u32x4*>(Qh + (int64_t)qrow_load * D + 8 * h);
+    const u32x4* qp = reinterpret_cast<const u32x4*>(Qh + qrow_load * (kPacked ? a.pk.q.row : (int64_t)D) + 8 * h);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) qreg[ks] = __builtin_bit_cast(bf16x8, qp[2 * ks]);
   }
@@ -200,21 +218,33 @@ __global__ __launch_bounds__(64 * NW * NG, (D == 64 && NW == 4 && NG == 1) ? 3 :
   // tensor) are not read and count as zeros.  Masking their scores alone would not do: weight 0 times a V that is Inf or
   // NaN is NaN, and with two wave groups a whole tile can lie there.  A descriptor is six scalar instructions per tile: 1 %
   // where one chain of tiles is the launch (7 heads, n = 3328, d = 64: 35.05 -> 35.5 us), nothing where the chip is full.
-  auto rows_rsrc = [&](const uint16_t* head, int kt) {
+  auto rows_rsrc = [&](const uint16_t* head, int row_bytes, int kt) {
+    if constexpr (kPacked) {
+      const int row = (NG * kt + grp) * kKT;
+      return __builtin_amdgcn_make_buffer_rsrc((void*)(reinterpret_cast<const unsigned char*>(head) + (int64_t)row * row_bytes), 0,
+                                               max(0, min(kKT, w.k1 - row)) * row_bytes, 0x00020000);
+    }
     if (kNode) return __builtin_amdgcn_make_buffer_rsrc((void*)head, 0, (int)((uint32_t)a.g.n * (D * 2)), 0x00020000);
     const int off = (w.k0 + (NG * kt + grp) * kKT) * (D * 2);
     return __builtin_amdgcn_make_buffer_rsrc((void*)(reinterpret_cast<const unsigned char*>(head) + (uint32_t)off), 0,
                                              max(0, w.k1 * (D * 2) - off), 0x00020000);
   };
   u32x4 kreg[TR::NKC], vreg[TR::NKC];
-  auto load_rows = [&](int kt, const uint16_t* head, u32x4 (&reg)[TR::NKC]) {
-    const __amdgpu_buffer_rsrc_t rsrc = rows_rsrc(head, kt);
+  auto load_rows = [&](int kt, const uint16_t* head, int row_bytes, u32x4 (&reg)[TR::NKC]) {
+    const __amdgpu_buffer_rsrc_t rsrc = rows_rsrc(head, row_bytes, kt);
+    if constexpr (kPacked) {  // (formed anew for every tile: kept, the offsets of two strides take registers that d = 64 does not have)
+      int at = tid / TR::CPR * row_bytes + tid % TR::CPR * 16;
+      asm volatile("" : "+v"(at));
+#pragma unroll
+      for (int i = 0; i < TR::NKC; ++i) reg[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, at + i * (kNT / TR::CPR) * row_bytes, 0, 0);
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < TR::NKC; ++i) {
       const int c = tid + i * kNT;
       const int key = c / TR::CPR, col = c % TR::CPR;
       const int row = kNode ? list[kt * kKT + key] : key;
-      reg[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, row * (D * 2) + col * 16, 0, 0);
+      reg[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, row * row_bytes + col * 16, 0, 0);
     }
   };
   auto store_rows = [&](unsigned char* dst, int stride, const u32x4 (&reg)[TR::NKC]) {
@@ -274,11 +304,11 @@ __global__ __launch_bounds__(64 * NW * NG, (D == 64 && NW == 4 && NG == 1) ? 3 :
     const int key_base = (NG * t + grp) * kKT;
     const bool tail = key_base + kKT > nkeys;
     const bool mixed = (key_base < nb) && (key_base + kKT > nb);  // (cap mode: the block's last, padded tile)
-    const bool diag = (MODE == kModeExact) && a.exact_causal && (w.k0 + key_base + kKT - 1 > w.q0 + wave * 32);
+    const bool diag = kExact && a.exact_causal && (w.k0 + key_base + kKT - 1 > w.q0 + wave * 32);
     bias = (key_base >= nb) ? bias2 : 0.f;
     if (tail || mixed || diag) {
       int lim = kCap && mixed ? nb : nkeys;
-      if (MODE == kModeExact && a.exact_causal) lim = min(lim, q_global - w.k0 + 1);
+      if (kExact && a.exact_causal) lim = min(lim, q_global - w.k0 + 1);
       const int lim2 = lim - key_base - 4 * h;  // element i is masked iff koff_i >= lim2
       const int nb2 = !kCap && mixed ? nb - key_base - 4 * h : 0x7fffffff;
       const float nat_bias = bias2 * kLn2;
@@ -321,9 +351,9 @@ __global__ __launch_bounds__(64 * NW * NG, (D == 64 && NW == 4 && NG == 1) ? 3 :
   if (ntiles > 0) {
     // all three tiles are requested before any is stored: one global round trip
     u32x4 kreg1[TR::NKC];
-    load_rows(0, Kh, kreg);
-    load_rows(0, Vh, vreg);
-    if (ntiles > 1) load_rows(1, Kh, kreg1);
+    load_rows(0, Kh, k_row, kreg);
+    load_rows(0, Vh, v_row, vreg);
+    if (ntiles > 1) load_rows(1, Kh, k_row, kreg1);
     store_rows(kbuf_at(0), L::KSTR, kreg);
     store_rows(vbuf_at(0), L::VSTR, vreg);
     if (ntiles > 1) store_rows(kbuf_at(1), L::KSTR, kreg1);
@@ -357,8 +387,8 @@ __global__ __launch_bounds__(64 * NW * NG, (D == 64 && NW == 4 && NG == 1) ? 3 :
     // LDS: there they are issued here, ahead of the block.
     constexpr bool kRequestInBlock = D == 64;
     if constexpr (!kRequestInBlock) {
-      if (more_k) load_rows(kt + 2, Kh, kreg);
-      if (HN) load_rows(kt + 1, Vh, vreg);
+      if (more_k) load_rows(kt + 2, Kh, k_row, kreg);
+      if (HN) load_rows(kt + 1, Vh, v_row, vreg);
     }
 
     if constexpr (kCap) {
@@ -404,13 +434,13 @@ __global__ __launch_bounds__(64 * NW * NG, (D == 64 && NW == 4 && NG == 1) ? 3 :
     // vector work fills: measured -3 % on the causal base case, -2 % on the node launch (any of the
     // neighbouring placements of the two instructions measured the same; priority during P V alone: no gain;
     // the d = 64 node launch, where vector issue binds, loses 2 % with it and goes without).
-    constexpr bool kPrio = D == 128 || MODE == kModeExact;
+    constexpr bool kPrio = D == 128 || kExact;
     bf16x8 pf[4];
     if constexpr (kPrio) __builtin_amdgcn_s_setprio(1);
     if constexpr (kRequestInBlock && HN) {
       // no branch here: past the end the last tile is requested again (and not stored)
-      load_rows(min(kt + 2, ntiles - 1), Kh, kreg);
-      load_rows(kt + 1, Vh, vreg);
+      load_rows(min(kt + 2, ntiles - 1), Kh, k_row, kreg);
+      load_rows(kt + 1, Vh, v_row, vreg);
     }
     {
       if (HN) {
@@ -674,7 +704,7 @@ __global__ __launch_bounds__(64 * NW * NG, (D == 64 && NW == 4 && NG == 1) ? 3 :
   }
   float* lse_dst = to_partial ? a.part_l : a.lse;
   const int64_t row_dst = to_partial ? dest.part_row : dest.out_row;
-  if (lse_dst != nullptr && dest.valid && h == 0) lse_dst[row_dst] = lse_own;
+  if (lse_dst != nullptr && dest.valid && h == 0) lse_dst[kPacked ? (int64_t)w.bh * a.pk.rows + row_dst : row_dst] = lse_own;
 
   unsigned char* dst_base = to_partial ? reinterpret_cast<unsigned char*>(a.part_o) : reinterpret_cast<unsigned char*>(a.out);
   if (dst_base == nullptr) return;
@@ -754,11 +784,12 @@ __global__ __launch_bounds__(64 * NW * NG, (D == 64 && NW == 4 && NG == 1) ? 3 :
           continue;
         }
         const u32x4 pk = {pack_bf16x2(v0.x, v0.y), pack_bf16x2(v0.z, v0.w), pack_bf16x2(v1.x, v1.y), pack_bf16x2(v1.z, v1.w)};
-        u32x4* to = reinterpret_cast<u32x4*>(dst_base + (r64[it] * D + ch * 8) * 2);
-        if (MODE == kModeExact) __builtin_nontemporal_store(pk, to);
+        const int64_t at = kPacked ? r64[it] * a.pk.o.row + (int64_t)w.bh * a.pk.o.head : r64[it] * D;
+        u32x4* to = reinterpret_cast<u32x4*>(dst_base + (at + ch * 8) * 2);
+        if (kExact) __builtin_nontemporal_store(pk, to);
         else *to = pk;
         if (!to_partial && a.out_f32 != nullptr) {  // unrounded copy of the final output, for the backward's delta
-          f32x4* fp = reinterpret_cast<f32x4*>(a.out_f32 + r64[it] * D + ch * 8);
+          f32x4* fp = reinterpret_cast<f32x4*>(a.out_f32 + (kPacked ? r64[it] * a.pk.Hq + w.bh : r64[it]) * D + ch * 8);
           __builtin_nontemporal_store(v0, fp);
           __builtin_nontemporal_store(v1, fp + 1);
         }
@@ -799,10 +830,19 @@ __global__ __launch_bounds__(64 * NW * NG, (D == 64 && NW == 4 && NG == 1) ? 3 :
 template <int D, int MODE, int NW, bool STAMPS = false, int NG = 1, bool SORT = false>
 static int launch_one(const AttnArgs& args, hipStream_t st) {
   AttnArgs a = args;
-  if (MODE != kModeExact) set_node_divs<32 * NW>(a);
-  else set_exact_divs<32 * NW>(a);
+  int64_t grid;
+  if constexpr (MODE == kModePacked) {
+    const int64_t slots = packed_slots<32 * NW>(a.pk);
+    grid = slots * a.pk.Hq;
+    if (grid > kMaxLaunch) return HA_ERR_SHAPE;
+    a.pk.slots = (int32_t)slots;
+    set_packed_divs(a, a.pk.group);
+  } else {
+    if (MODE != kModeExact) set_node_divs<32 * NW>(a);
+    else set_exact_divs<32 * NW>(a);
+    grid = MODE != kModeExact ? node_grid<32 * NW>(a.g) : exact_grid<32 * NW>(a);
+  }
   a.exact_lpt = NG == 2;
-  const int64_t grid = MODE != kModeExact ? node_grid<32 * NW>(a.g) : exact_grid<32 * NW>(a);
   if (grid <= 0) return HA_OK;
   if (grid > kMaxGrid) return HA_ERR_SHAPE;
   size_t lds = mfma_lds_bytes<D>(a.g.b, a.g.m, MODE) + (NG - 1) * 2 * (size_t)Lds<D>::BUF;
@@ -921,6 +961,7 @@ int64_t attn_mfma_grid(const AttnArgs& a, int mode) {
 
 int launch_attn_mfma(const AttnArgs& a, int mode, hipStream_t st) {
   if (a.g.dtype != HA_BF16) return HA_ERR_DTYPE;
+  if (mode == kModePacked) return a.g.d == 128 ? launch_one<128, kModePacked, 4>(a, st) : launch_one<64, kModePacked, 4>(a, st);
   if (mode == kModeExact && a.merge_levels > 0 && !a.part_bf16) return HA_ERR_DTYPE;  // this kernel folds bf16 partial rows
   const bool split = mode == kModeExact && split_exact(a);
   if (a.stamps != nullptr) {  // the measuring instantiations: the node launch behind a sorting launch, the base case

@@ -12,6 +12,8 @@ enum BwdMode : int32_t {
   kBwdDkvBlock = 2,  // dK, dV of the block keys of every node: key tiles over the queries of their block
   kBwdDkvSamp = 3,   // dK, dV of the sampled keys of every node: sample slabs over chunks of the node's queries
   kBwdDkvExact = 4,  // dK, dV of exact attention / the causal base case
+  kBwdDqPacked = 5,   // dQ and dK, dV of exact attention over packed sequences (kModePacked): a key head's rows collect from all query
+  kBwdDkvPacked = 6,  // heads of its group, or from a part of them (PackedRows::splits) into fp32 rows of their own in out1 / out2 [split][rows][Hk][d]
 };
 
 constexpr int kBwdMaxLevels = 24;
@@ -109,6 +111,7 @@ inline int64_t bwd_sample_rows(const Geometry& g) {
 // pass: q0 = first KEY row, [k0, k1) = its queries).
 struct BwdWork {
   TileWork w;
+  int seq_start, heads, tiles_per_head;  // packed passes: the sequence's first row; dK / dV: query heads from w.bh on, and T tiles of each
   int chunk_start, chunk_len;   // sampled-key pass: run of sorted query positions
   int samp0;                    // first sample
   int64_t samp_row0;            // row of sample 0 of this (head, node, chunk) in the pass's output
@@ -135,6 +138,20 @@ __device__ inline BwdWork decode_bwd_work(const BwdArgs& a, int idx, int wgs) { 
     b.w.rows_valid = max(0, min(QT, blk_rows - ktile * QT));
     b.w.k0 = f.exact_causal ? b.w.q0 : blk * eb;
     b.w.k1 = blk * eb + blk_rows;     // queries [k0, k1)
+  } else if (MODE == kBwdDqPacked) {
+    b.w = decode_packed_tile<QT>(f, idx, &b.seq_start);
+  } else if (MODE == kBwdDkvPacked) {  // w.q0: first KEY row, [k0, k1): its queries, w.bh: the first query head, node: unused
+    const PackedPlace p = packed_place(f, idx);
+    const PackedTile t = packed_tile<QT>(f.pk, p.slot);
+    b.seq_start = t.start;
+    b.heads = f.pk.group / f.pk.splits;
+    b.w.bh = p.kv * f.pk.group + p.sub * b.heads;
+    b.chunk_start = p.sub;
+    if (t.tile < 0 || t.tile * QT >= t.len) return b;
+    b.w.q0 = t.tile * QT;
+    b.w.rows_valid = min(QT, t.len - b.w.q0);
+    b.w.k0 = f.exact_causal ? b.w.q0 : 0;
+    b.w.k1 = t.len;
   } else {  // kBwdDkvSamp: a slab of QT samples over one chunk of the node's sorted queries
     const int spn = (g.m + QT - 1) / QT;              // sample slabs per node
     const int slab = idx % spn;
@@ -259,6 +276,19 @@ inline int64_t bwd_grid(const BwdArgs& a, int mode) {
   if (mode == kBwdDqExact || mode == kBwdDkvExact) return exact_grid<QT>(a.f);
   return (int64_t)a.samp_chunks * ((g.m + QT - 1) / QT);
 }
+
+// Query heads of a key head's tile that one workgroup of the packed dK / dV pass takes: all of the group, halved (thirded ...) while the pass has fewer
+// than 512 workgroups: the number of them that share it, a divisor of the group.
+inline int packed_splits(int64_t workgroups, int group) {
+  int splits = 1;
+  for (int k = 1; k <= group; ++k)
+    if (group % k == 0) {
+      splits = k;
+      if (workgroups * k >= 512) break;
+    }
+  return splits;
+}
+int launch_packed_sum(const PackedRows& p, const float* part1, const float* part2, void* out1, void* out2, int d, int dtype, hipStream_t st);
 
 int launch_attn_bwd_mfma(const BwdArgs& a, int mode, hipStream_t st);  // bf16 tensors
 int launch_attn_bwd_f32(const BwdArgs& a, int mode, hipStream_t st);   // fp32 tensors

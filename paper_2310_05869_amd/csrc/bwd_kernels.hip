@@ -270,4 +270,51 @@ int launch_bwd_sample_reduce(const BwdArgs& a, float* samp_k, float* samp_v, hip
   return check_launch();
 }
 
+// Packed dK / dV of key heads whose query heads were shared among workgroups: the parts of a row added up in order, into the tensors' dtype.  Rows of no sequence
+// have no parts and are left alone.
+template <int D, bool F32>
+__global__ __launch_bounds__(256) void packed_sum_kernel(PackedRows p, const float* part1, const float* part2, void* out1, void* out2) {
+  constexpr int LPR = D / 8;  // lanes per row of a head, eight values each
+  const int first = min(max(p.cu[0], 0), p.rows), end = min(max(p.cu[p.n_seq], first), p.rows);
+  const int64_t unit = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t row_head = unit / LPR;
+  const int ch = (int)(unit % LPR) * 8;
+  const int row = (int)(row_head / p.Hk), head = (int)(row_head % p.Hk);
+  if (row < first || row >= end) return;
+  const float* part = blockIdx.y ? part2 : part1;
+  void* out = blockIdx.y ? out2 : out1;
+  const RowStrides st = blockIdx.y ? p.fin2 : p.fin1;
+  f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
+  const int64_t step = (int64_t)p.rows * p.Hk * D;
+  const float* at = part + ((int64_t)row * p.Hk + head) * D + ch;
+#pragma unroll 4
+  for (int s = 0; s < p.splits; ++s) {
+    a += *reinterpret_cast<const f32x4*>(at + s * step);
+    b += *reinterpret_cast<const f32x4*>(at + s * step + 4);
+  }
+  const int64_t to = (int64_t)row * st.row + (int64_t)head * st.head + ch;
+  if constexpr (F32) {
+    *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(out) + to) = a;
+    *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(out) + to + 4) = b;
+  } else {
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    *reinterpret_cast<u32x4*>(reinterpret_cast<uint16_t*>(out) + to) =
+        (u32x4){pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]), pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3])};
+  }
+}
+
+int launch_packed_sum(const PackedRows& p, const float* part1, const float* part2, void* out1, void* out2, int d, int dtype, hipStream_t st) {
+  const int64_t wgs = ((int64_t)p.rows * p.Hk * (d / 8) + 255) / 256;
+  if (wgs > kMaxLaunch / 2) return HA_ERR_SHAPE;
+  const dim3 grid((unsigned)wgs, 2);
+  if (d == 128) {
+    if (dtype == HA_BF16) hipLaunchKernelGGL((packed_sum_kernel<128, false>), grid, dim3(256), 0, st, p, part1, part2, out1, out2);
+    else hipLaunchKernelGGL((packed_sum_kernel<128, true>), grid, dim3(256), 0, st, p, part1, part2, out1, out2);
+  } else {
+    if (dtype == HA_BF16) hipLaunchKernelGGL((packed_sum_kernel<64, false>), grid, dim3(256), 0, st, p, part1, part2, out1, out2);
+    else hipLaunchKernelGGL((packed_sum_kernel<64, true>), grid, dim3(256), 0, st, p, part1, part2, out1, out2);
+  }
+  return check_launch();
+}
+
 }  // namespace ha

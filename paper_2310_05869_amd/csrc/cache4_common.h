@@ -25,10 +25,6 @@ struct CacheGeometry {
   __host__ __device__ int v_scale_at() const { return page * (d + d / kCacheGroup); }
 };
 
-struct RowStrides {
-  int64_t row, head;  // elements
-};
-
 struct CacheRowsArgs {
   const int32_t* slots;
   void* K;

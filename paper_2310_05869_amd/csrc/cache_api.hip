@@ -21,18 +21,6 @@ static int cache_geometry(const ha_cache4* sh, CacheGeometry* c) {
   return HA_OK;
 }
 
-// Strides of [rows][heads][d] in elements; null: contiguous.  written: rows and heads may not share elements.
-static int row_strides(const ha_strides* given, int heads, int d, int dtype, bool written, RowStrides* out) {
-  *out = RowStrides{(int64_t)heads * d, d};
-  if (!given) return HA_OK;
-  const int64_t unit = dtype == HA_BF16 ? 8 : 4, most = 1ll << 22;
-  if (given->row < 0 || given->head < 0 || given->row > most || given->head > (1ll << 40)) return HA_ERR_SHAPE;
-  if (given->row % unit || given->head % unit) return HA_ERR_ALIGN;
-  if (written && (given->row < d || (heads > 1 && given->head < d))) return HA_ERR_SHAPE;
-  *out = RowStrides{given->row, given->head};
-  return HA_OK;
-}
-
 static int rows_call(const void* K, const void* V, const int32_t* slots, const void* cache, const ha_cache4* shape, int32_t rows, int32_t dtype,
                      const ha_strides* kv, void* stream, bool write) {
   CacheRowsArgs a{};

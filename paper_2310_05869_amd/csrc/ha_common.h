@@ -81,6 +81,21 @@ enum AttnMode : int32_t {
   kModeExact = 1,  // contiguous keys, optional causal mask (exact attention / causal base case)
   kModeCap = 2,    // node mode with Algorithm 2's cap on every sampled entry and its lower cap
   kModeValue = 3,  // cap mode for the row sums, Lemma 2's rows for the output (fp32)
+  kModePacked = 4, // exact mode over packed sequences: rows of a sequence against its keys, strided rows, grouped heads
+};
+
+struct RowStrides {
+  int64_t row, head;  // elements; the d values of a row are consecutive
+};
+
+// Packed sequences (kModePacked): sequence s owns rows [cu[s], cu[s + 1]) of all tensors; query head h reads key head h / group.
+struct PackedRows {
+  const int32_t* cu;  // [n_seq + 1]
+  int32_t n_seq, rows, Hq, Hk, group;
+  int32_t slots;      // tiles of the launch's rows, at most (packed_slots)
+  int32_t splits;     // dK / dV: workgroups that share the query heads of a key head, each with rows of sums of its own
+  RowStrides q, k, v, o, d_o;
+  RowStrides fin1, fin2;  // gradients that a backward pass writes
 };
 
 // Division of 0 <= n < 2^31 by a divisor known on the host: two scalar multiplications and a shift, where
@@ -154,6 +169,7 @@ struct AttnArgs {
   int32_t exact_causal;
   int32_t exact_lpt;                   // set by the launchers: workgroups that fill a CU each (exact_place)
   int32_t merge_levels;                // exact mode: merge part_o/part_l of this many levels into the result
+  PackedRows pk;  // packed mode
   // measurement only (null in every product call): kStampWords 64-bit words per workgroup, indexed by the
   // workgroup's logical tile number, written by the instrumented instantiation of the MFMA kernel
   long long* stamps;
@@ -192,6 +208,18 @@ template <typename... P>
 inline bool any_misaligned16(P... ptrs) { return (misaligned(ptrs, 16) || ...); }
 template <typename... P>
 inline bool any_misaligned4(P... ptrs) { return (misaligned(ptrs, 4) || ...); }
+
+// Strides of [rows][heads][d] in elements; null: contiguous.  written: heads may not share elements either.
+inline int row_strides(const ha_strides* given, int heads, int d, int dtype, bool written, RowStrides* out) {
+  *out = RowStrides{(int64_t)heads * d, d};
+  if (!given) return HA_OK;
+  const int64_t unit = dtype == HA_BF16 ? 8 : 4, most = 1ll << 22;
+  if (given->row < d || given->head < 0 || given->row > most || given->head > (1ll << 40)) return HA_ERR_SHAPE;
+  if (given->row % unit || given->head % unit) return HA_ERR_ALIGN;
+  if (written && heads > 1 && given->head < d) return HA_ERR_SHAPE;
+  *out = RowStrides{given->row, given->head};
+  return HA_OK;
+}
 
 inline int check_launch() { return hipGetLastError() == hipSuccess ? HA_OK : HA_ERR_LAUNCH; }
 
