@@ -233,9 +233,7 @@ __device__ __forceinline__ void bwd_f32_pass(const BwdArgs& a, const int wg, con
   auto tile_rsrc = [&](const __amdgpu_buffer_rsrc_t& whole, const void* base, int64_t head_bytes, int row_bytes, int kt) {
     if constexpr (!kPacked) return whole;
     const int head = head_of(kt), row = w.k0 + (kt - head * tph) * kFTT;
-    const uint64_t at = (uint64_t)base + head * head_bytes + (int64_t)row * row_bytes;
-    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)at), hi = __builtin_amdgcn_readfirstlane((uint32_t)(at >> 32));
-    return __builtin_amdgcn_make_buffer_rsrc((void*)((uint64_t)hi << 32 | lo), 0, __builtin_amdgcn_readfirstlane(max(0, min(kFTT, w.k1 - row)) * row_bytes), 0x00020000);
+    return uniform_rsrc(reinterpret_cast<const unsigned char*>(base) + head * head_bytes + (int64_t)row * row_bytes, max(0, min(kFTT, w.k1 - row)) * row_bytes);
   };
   auto y_tile = [&](int kt) { return tile_rsrc(yrsrc, Yh, kHeads ? f.pk.q.head * 4 : 0, y_row, kt); };
   auto b_tile = [&](int kt) { return tile_rsrc(brsrc, Bh, kHeads ? f.pk.d_o.head * 4 : 0, b_row, kt); };

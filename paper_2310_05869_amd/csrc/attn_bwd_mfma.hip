@@ -113,13 +113,6 @@ __device__ inline void dma_1k(const __amdgpu_buffer_rsrc_t& rsrc, uint32_t lds_a
   asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(lds_at), "v"(voff), "s"(rsrc) : "memory");
 }
 
-// A descriptor of memory that is the same for all lanes, where the compiler does not see that by itself
-__device__ inline __amdgpu_buffer_rsrc_t uniform_rsrc(const void* p, int bytes) {
-  const uint64_t at = (uint64_t)p;
-  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)at), hi = __builtin_amdgcn_readfirstlane((uint32_t)(at >> 32));
-  return __builtin_amdgcn_make_buffer_rsrc((void*)((uint64_t)hi << 32 | lo), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
-}
-
 // Waves per SIMD that the compiler is asked for.
 constexpr int bwd_waves_per_simd(int d, int mode) { return d == 64 && mode == kBwdDkvSamp ? 3 : 2; }
 

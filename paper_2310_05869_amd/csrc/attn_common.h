@@ -164,39 +164,131 @@ __host__ __device__ inline int64_t exact_grid(const AttnArgs& a) {
   return (int64_t)a.g.BH * nblk * tpb;
 }
 
-// Packed sequences.  Tiles of QT rows of a sequence, counted over all sequences without a pass over them: sequence s gets the numbers from
-// floor(cu[s] / QT) + s on.  It has at most floor(cu[s + 1] / QT) - floor(cu[s] / QT) + 1 tiles, so the ranges do not meet, the sequence of a number
-// is found by bisection, and at most n_seq numbers, whose workgroups end at once, have no tile.  The host needs no lengths.
+// Packed sequences: which tile of QT rows of which sequence a workgroup takes.  The host knows no lengths, so a launch has a number per tile that there can be,
+// packed_slots, and every wave finds its own.  With c_s = ceil(len_s / QT) tiles in sequence s:
+//   up to 256 sequences: the numbers go through the tiles by the work that they have, the most first, over all sequences.  A causal tile of level
+//     t, the t-th of its sequence (dK / dV: the t-th from its end), has t + 1 tiles of keys (queries); sum_s max(0, c_s - t) tiles have at least level t,
+//     so a number's level is found by bisection of that sum, one lane per sequence, and within the level its sequence by a ballot.  Unmasked,
+//     likewise, by the sequences' lengths.
+//   more: tiles in order of the sequences; s has the numbers from floor(cu[s] / QT) + s on.  It has at most floor(cu[s + 1] / QT) - floor(cu[s] / QT) + 1
+//     tiles, so the ranges do not meet, and the sequence of a number is found by bisection of cu, 64 probes at a time.
+// At most n_seq numbers have no tile; their workgroups end at once.
 template <int QT>
 inline int64_t packed_slots(const PackedRows& p) { return (int64_t)p.rows / QT + p.n_seq; }
 
 __device__ inline int packed_start(const PackedRows& p, int s) { return min(max(p.cu[s], 0), p.rows); }
 
+// Sum or maximum over the wave, in all lanes
+template <bool MAX>
+__device__ inline int wave_total(int x) {
+  auto step = [&](int y) { x = MAX ? max(x, y) : x + y; };  // (lanes without a source get 0: all values here are >= 0)
+  step(__builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true));  // row_shr:1, 2, 4, 8
+  step(__builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true));
+  step(__builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true));
+  step(__builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true));
+  step(__builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, true));  // row_bcast:15 into rows 1 and 3
+  step(__builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, true));  // row_bcast:31 into rows 2 and 3
+  return __builtin_amdgcn_readlane(x, 63);
+}
+
+enum PackedOrder : int { kTilesLate = 0, kTilesEarly = 1, kTilesAlike = 2 };  // which tiles of a sequence have the most work
+
 struct PackedTile {
   int start, len;  // the sequence's rows
-  int tile;        // of QT rows within it; >= tiles(len): none
+  int tile;        // of QT rows within it; < 0: none
 };
 
-// 64 probes at a time: two round trips for up to 4096 sequences
 template <int QT>
-__device__ inline PackedTile packed_tile(const PackedRows& p, int slot) {
+__device__ inline PackedTile find_packed_tile(const PackedRows& p, int slot, int order) {
   const int lane = __lane_id();
-  int lo = 0, n = p.n_seq;
-  while (n > 1) {
-    const int step = (n + 63) >> 6, at = lo + lane * step;
-    const bool in = lane * step < n;
-    const bool le = in && packed_start(p, in ? at : lo) / QT + at <= slot;
-    const unsigned long long bal = __ballot(le);
-    const int i = bal ? 63 - __builtin_clzll(bal) : 0;
-    lo += i * step;
-    n = min(step, n - i * step);
+  PackedTile t{0, 0, -1};
+  if (p.n_seq > 256) {
+    int lo = 0, n = p.n_seq;
+    while (n > 1) {
+      const int step = (n + 63) >> 6, at = lo + lane * step;
+      const bool in = lane * step < n;
+      const bool le = in && packed_start(p, in ? at : lo) / QT + at <= slot;
+      const unsigned long long bal = __ballot(le);
+      const int i = bal ? 63 - __builtin_clzll(bal) : 0;
+      lo += i * step;
+      n = min(step, n - i * step);
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    t.start = __builtin_amdgcn_readfirstlane(packed_start(p, lo));
+    t.len = __builtin_amdgcn_readfirstlane(max(packed_start(p, lo + 1), t.start)) - t.start;
+    const int tiles = (t.len + QT - 1) / QT, i = slot - (t.start / QT + lo);
+    t.tile = i < 0 || i >= tiles ? -1 : order == kTilesLate ? tiles - 1 - i : i;
+    return t;
   }
-  lo = __builtin_amdgcn_readfirstlane(lo);
-  PackedTile t;
-  t.start = __builtin_amdgcn_readfirstlane(packed_start(p, lo));
-  t.len = __builtin_amdgcn_readfirstlane(max(packed_start(p, lo + 1), t.start)) - t.start;
-  t.tile = slot - (t.start / QT + lo);
+  int start[4], len[4], c[4], most = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const int s = 64 * j + lane;
+    start[j] = len[j] = 0;
+    if (64 * j < p.n_seq) {
+      const int at = min(s, p.n_seq - 1);
+      start[j] = packed_start(p, at);
+      len[j] = s < p.n_seq ? max(packed_start(p, at + 1) - start[j], 0) : 0;
+    }
+    c[j] = (len[j] + QT - 1) / QT;
+    most = max(most, c[j]);
+  }
+  most = wave_total<true>(most);
+  const bool alike = order == kTilesAlike;
+  // tiles of level x and above; alike: of sequences with at least x tiles
+  auto above = [&](int x) {
+    int n = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) n += alike ? (c[j] >= x ? c[j] : 0) : max(0, c[j] - x);
+    return wave_total<false>(n);
+  };
+  int lo = alike ? 1 : 0, hi = most + (alike ? 1 : 0);  // above(lo) > slot >= above(hi)
+  if (most == 0 || above(lo) <= slot) return t;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (above(mid) > slot) lo = mid;
+    else hi = mid;
+  }
+  int k = slot - above(lo + 1);       // within the level
+  int tile = 0;
+  if (alike) {
+    tile = k % lo;
+    k /= lo;
+  }
+  int done = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const bool here = alike ? c[j] == lo : c[j] > lo;
+    const unsigned long long bal = __ballot(here);
+    const int n = __popcll(bal);
+    if (!done && k < n) {
+      const bool me = here && __popcll(bal & ((1ull << lane) - 1ull)) == k;
+      const int l = __builtin_ctzll(__ballot(me));
+      t.start = __builtin_amdgcn_readlane(start[j], l);
+      t.len = __builtin_amdgcn_readlane(len[j], l);
+      t.tile = alike ? tile : order == kTilesLate ? lo : __builtin_amdgcn_readlane(c[j], l) - 1 - lo;
+      done = 1;
+    }
+    k -= n;
+  }
   return t;
+}
+
+template <int QT>
+__device__ inline PackedTile packed_tile(const PackedRows& p, int slot, int order) {
+  PackedTile t = find_packed_tile<QT>(p, slot, order);
+  t.start = __builtin_amdgcn_readfirstlane(t.start);
+  t.len = __builtin_amdgcn_readfirstlane(t.len);
+  t.tile = __builtin_amdgcn_readfirstlane(t.tile);
+  return t;
+}
+
+// A buffer descriptor of memory that is the same for all lanes, where the compiler does not see that by itself and would loop over the lanes at every load:
+// packed tiles' (forward, d = 64, 16 sequences of up to 2048, 16 heads: 51 -> 38 us; fp32, 9 of up to 700, 6 heads: 32 -> 21).
+__device__ inline __amdgpu_buffer_rsrc_t uniform_rsrc(const void* p, int bytes) {
+  const uint64_t at = (uint64_t)p;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)at), hi = __builtin_amdgcn_readfirstlane((uint32_t)(at >> 32));
+  return __builtin_amdgcn_make_buffer_rsrc((void*)((uint64_t)hi << 32 | lo), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
 }
 
 // Order of a packed launch's workgroups: the tiles in order of the sequences, the heads that share K and V beside each other and on one XCD, whose L2 then
@@ -228,17 +320,16 @@ __device__ inline PackedPlace packed_place(const AttnArgs& a, int wg) {
   return p;
 }
 
-// w.bh: the query head.  Rows are counted from the sequence's start; causal tiles come last rows, the most keys, first.
+// w.bh: the query head.  Rows are counted from the sequence's start.
 template <int QT>
 __device__ inline TileWork decode_packed_tile(const AttnArgs& a, int wg, int* start) {
   TileWork w{};
   const PackedPlace p = packed_place(a, wg);
-  const PackedTile t = packed_tile<QT>(a.pk, p.slot);
+  const PackedTile t = packed_tile<QT>(a.pk, p.slot, a.exact_causal ? kTilesLate : kTilesAlike);
   *start = t.start;
   w.bh = p.kv * a.pk.group + p.sub;
-  const int tiles = (t.len + QT - 1) / QT;
-  if (t.tile < 0 || t.tile >= tiles) return w;
-  w.q0 = (tiles - 1 - t.tile) * QT;
+  if (t.tile < 0) return w;
+  w.q0 = t.tile * QT;
   w.rows_valid = min(QT, t.len - w.q0);
   w.k1 = a.exact_causal ? w.q0 + w.rows_valid : t.len;
   return w;

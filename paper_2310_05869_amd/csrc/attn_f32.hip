@@ -219,8 +219,7 @@ __global__ __launch_bounds__(64 * f32_waves(KW), D == 128 && KW < 4 ? 1 : D == 6
   auto tile_rsrc = [&](const __amdgpu_buffer_rsrc_t& whole, const float* head, int row_bytes, int kt) {
     if constexpr (!kPacked) return whole;
     const int row = kt * kFKT;
-    return __builtin_amdgcn_make_buffer_rsrc((void*)(reinterpret_cast<const unsigned char*>(head) + (int64_t)row * row_bytes), 0,
-                                             max(0, min(kFKT, w.k1 - row)) * row_bytes, 0x00020000);
+    return uniform_rsrc(reinterpret_cast<const unsigned char*>(head) + (int64_t)row * row_bytes, max(0, min(kFKT, w.k1 - row)) * row_bytes);
   };
   f32x4 kf[kShared ? 1 : KJ];
   auto load_k = [&](int kt, int j0 = 0, int j1 = D / 8) {

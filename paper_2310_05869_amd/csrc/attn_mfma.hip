@@ -221,8 +221,7 @@ __global__ __launch_bounds__(64 * NW * NG, (D == 64 && NW == 4 && NG == 1) ? 3 :
   auto rows_rsrc = [&](const uint16_t* head, int row_bytes, int kt) {
     if constexpr (kPacked) {
       const int row = (NG * kt + grp) * kKT;
-      return __builtin_amdgcn_make_buffer_rsrc((void*)(reinterpret_cast<const unsigned char*>(head) + (int64_t)row * row_bytes), 0,
-                                               max(0, min(kKT, w.k1 - row)) * row_bytes, 0x00020000);
+      return uniform_rsrc(reinterpret_cast<const unsigned char*>(head) + (int64_t)row * row_bytes, max(0, min(kKT, w.k1 - row)) * row_bytes);
     }
     if (kNode) return __builtin_amdgcn_make_buffer_rsrc((void*)head, 0, (int)((uint32_t)a.g.n * (D * 2)), 0x00020000);
     const int off = (w.k0 + (NG * kt + grp) * kKT) * (D * 2);

@@ -142,12 +142,12 @@ __device__ inline BwdWork decode_bwd_work(const BwdArgs& a, int idx, int wgs) { 
     b.w = decode_packed_tile<QT>(f, idx, &b.seq_start);
   } else if (MODE == kBwdDkvPacked) {  // w.q0: first KEY row, [k0, k1): its queries, w.bh: the first query head, node: unused
     const PackedPlace p = packed_place(f, idx);
-    const PackedTile t = packed_tile<QT>(f.pk, p.slot);
+    const PackedTile t = packed_tile<QT>(f.pk, p.slot, f.exact_causal ? kTilesEarly : kTilesAlike);
     b.seq_start = t.start;
     b.heads = f.pk.group / f.pk.splits;
     b.w.bh = p.kv * f.pk.group + p.sub * b.heads;
     b.chunk_start = p.sub;
-    if (t.tile < 0 || t.tile * QT >= t.len) return b;
+    if (t.tile < 0) return b;
     b.w.q0 = t.tile * QT;
     b.w.rows_valid = min(QT, t.len - b.w.q0);
     b.w.k0 = f.exact_causal ? b.w.q0 : 0;
