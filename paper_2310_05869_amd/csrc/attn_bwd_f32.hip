@@ -757,15 +757,17 @@ static int launch_bwd_f32_d(const BwdArgs& a, int mode, hipStream_t st) {
   }
 }
 
-// Packed sequences: the same, by the average length and an upper bound of the workgroups.
+// Packed sequences: the same, by the average length and an upper bound of the workgroups.  Forward and backward with dQ / dK and dV of one way, of four (MI355X, us;
+// workgroups of 128 rows at most): d = 64: 12 heads, 6 of up to 3000 (576) dQ 845, 810, dK / dV 845, 692; 16 heads, 8 of 500 (624) 206, 221 and 206, 201; d = 128: 16 and 4
+// heads, 3 of up to 2500 (560) 1277, 1363 and 1322, 1362; eight ways: d = 64, 4 heads, 5 of up to 900 (groups of 32 rows: 172) 95.2 -> 91.3 and 86.6
 template <int D, int MODE>
 static int launch_bwd_f32_packed(const BwdArgs& a, hipStream_t st) {
   const PackedRows& p = a.f.pk;
   const int64_t avg = p.rows / (p.n_seq > 0 ? p.n_seq : 1), per = MODE == kBwdDqPacked ? p.Hq : p.Hk * p.splits;
   const int64_t grid = packed_slots<128>(p) * per;
   if constexpr (D == 64)
-    if (avg >= 512 && packed_slots<32>(p) * per <= (!a.f.exact_causal ? 256 : avg < 2048 ? 384 : 512)) return launch_bwd_f32_one<D, MODE, 1, 8>(a, st);
-  const int64_t enough = a.f.exact_causal ? (D == 64 ? 512 : 1024) : D == 128 ? 208 : 256;
+    if (avg >= 128 && packed_slots<32>(p) * per <= (!a.f.exact_causal || avg < 512 ? 256 : avg < 2048 ? 384 : 512)) return launch_bwd_f32_one<D, MODE, 1, 8>(a, st);
+  const int64_t enough = a.f.exact_causal ? (D == 128 ? 544 : MODE == kBwdDqPacked ? 600 : 1024) : D == 128 ? 208 : 256;
   const bool fits = 3 * ((avg + 127) / 128 * 128) <= 4 * avg;
   return fits && grid >= enough ? launch_bwd_f32_one<D, MODE, 4, 1>(a, st) : launch_bwd_f32_one<D, MODE, 1, 4>(a, st);
 }

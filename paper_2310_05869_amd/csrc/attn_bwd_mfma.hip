@@ -779,6 +779,8 @@ static bool bwd_four_workgroups(int grid) { return grid > 768; }
 template <int D, int MODE>
 static int launch_bwd_one(const BwdArgs& a, int grid, hipStream_t st) {
   if (grid <= 0) return HA_OK;
+  if constexpr (MODE == kBwdDqPacked || MODE == kBwdDkvPacked)
+    if (packed_two_groups(a.f.pk, grid, a.f.exact_causal)) return launch_bwd_form<D, MODE, false, 2>(a, grid, st);
   if constexpr (MODE == kBwdDqExact || MODE == kBwdDkvExact)
     if (split_bwd_exact(a, grid)) return launch_bwd_form<D, MODE, false, 2>(a, grid, st);
   if constexpr (D == 64 && MODE == kBwdDqExact)

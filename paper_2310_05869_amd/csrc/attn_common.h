@@ -291,6 +291,18 @@ __device__ inline __amdgpu_buffer_rsrc_t uniform_rsrc(const void* p, int bytes) 
   return __builtin_amdgcn_make_buffer_rsrc((void*)((uint64_t)hi << 32 | lo), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00020000);
 }
 
+// Packed launches of few workgroups, whose longest chain of tiles bounds them: two groups of four waves share it, as in exact launches (bf16 kernels).
+// The host knows the average length alone.  One group -> two, forward and backward together with the forward, dQ or dK / dV of two groups (MI355X, us; [average
+// length, workgroups of that pass at most]): forward: 8 heads, 2048 tokens [2048, 136] 173 -> 167, 8192 [8192, 520] 465 -> 437, 10 of up to 2048 [449, 360] 184 -> 177; 12
+// heads, 8 of up to 512 [511, 468] 50.6 -> 54.1; 16 heads, 12 of up to 4096 [625, 1120] 370 -> 382; 8 heads, 30 of up to 300 [88, 400] 62.7 -> 68.1;
+// dQ: 173 -> 166, 465 -> 437, 184 -> 174, 50.6 -> 55.2, 370 -> 381, 62.7 -> 69.6; dK / dV: 173 -> 160, 465 -> 424, 184 -> 170, 50.6 -> 53.4, 370 -> 320 [625, 560], 62.7 -> 65.1;
+// unmasked, 12 heads, 6 of up to 2048 [634, 420]: 225 -> 238, 240, 244
+inline bool packed_two_groups(const PackedRows& p, int64_t workgroups, bool causal) {
+  const int64_t avg = p.n_seq > 0 ? p.rows / p.n_seq : 0;
+  if (!causal) return avg >= 512 && workgroups <= 256;
+  return avg >= 320 && workgroups <= (avg < 1024 ? 384 : 576);
+}
+
 // Order of a packed launch's workgroups: the tiles in order of the sequences, the heads that share K and V beside each other and on one XCD, whose L2 then
 // holds the sequence's rows of few key heads.  Where the key heads are a multiple of 8, every XCD has the tiles of its own ones.
 struct PackedPlace {

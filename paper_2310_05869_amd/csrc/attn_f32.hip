@@ -733,11 +733,12 @@ static int launch_f32_mode(const AttnArgs& a, hipStream_t st) {
   return launch_f32_one<D, MODE, 4>(a, st);
 }
 
-// Packed sequences: the same, by the average length and an upper bound of the workgroups.
+// Packed sequences: the same, by the average length and an upper bound of the workgroups; eight ways also wherever the chip holds all workgroups at once,
+// whose longest sequence is unknown (forward and backward, four -> eight: 4 heads, 5 of up to 900, d = 64 95.2 -> 92.9, 4 of up to 800, d = 128 142 -> 136).
 template <int D>
 static int launch_f32_packed(const AttnArgs& a, hipStream_t st) {
-  const int64_t avg = a.pk.rows / (a.pk.n_seq > 0 ? a.pk.n_seq : 1);
-  if (avg >= 512 && packed_slots<32>(a.pk) * a.pk.Hq <= (!a.exact_causal ? 256 : avg < 2048 ? 384 : 512)) return launch_f32_one<D, kModePacked, 8>(a, st);
+  const int64_t avg = a.pk.rows / (a.pk.n_seq > 0 ? a.pk.n_seq : 1), groups = packed_slots<32>(a.pk) * a.pk.Hq;
+  if (avg >= 128 && groups <= (!a.exact_causal || avg < 512 ? 256 : avg < 2048 ? 384 : 512)) return launch_f32_one<D, kModePacked, 8>(a, st);
   const int kw = f32_ways(D, (int)avg, packed_slots<128>(a.pk) * a.pk.Hq, a.exact_causal);
   if (kw == 1) return launch_f32_one<D, kModePacked, 1>(a, st);
   if constexpr (D == 64)

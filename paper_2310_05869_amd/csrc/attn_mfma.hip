@@ -960,7 +960,11 @@ int64_t attn_mfma_grid(const AttnArgs& a, int mode) {
 
 int launch_attn_mfma(const AttnArgs& a, int mode, hipStream_t st) {
   if (a.g.dtype != HA_BF16) return HA_ERR_DTYPE;
-  if (mode == kModePacked) return a.g.d == 128 ? launch_one<128, kModePacked, 4>(a, st) : launch_one<64, kModePacked, 4>(a, st);
+  if (mode == kModePacked) {
+    const bool two = packed_two_groups(a.pk, packed_slots<128>(a.pk) * a.pk.Hq, a.exact_causal);
+    if (a.g.d == 128) return two ? launch_one<128, kModePacked, 4, false, 2>(a, st) : launch_one<128, kModePacked, 4>(a, st);
+    return two ? launch_one<64, kModePacked, 4, false, 2>(a, st) : launch_one<64, kModePacked, 4>(a, st);
+  }
   if (mode == kModeExact && a.merge_levels > 0 && !a.part_bf16) return HA_ERR_DTYPE;  // this kernel folds bf16 partial rows
   const bool split = mode == kModeExact && split_exact(a);
   if (a.stamps != nullptr) {  // the measuring instantiations: the node launch behind a sorting launch, the base case

@@ -277,14 +277,17 @@ inline int64_t bwd_grid(const BwdArgs& a, int mode) {
   return (int64_t)a.samp_chunks * ((g.m + QT - 1) / QT);
 }
 
-// Query heads of a key head's tile that one workgroup of the packed dK / dV pass takes: all of the group, halved (thirded ...) while the pass has fewer
-// than 512 workgroups: the number of them that share it, a divisor of the group.
-inline int packed_splits(int64_t workgroups, int group) {
+// How many workgroups of the packed dK / dV pass share the query heads of a key head's tile, a divisor of the group: enough of them for the chip, counted in tiles
+// of 128 rows; each has fp32 rows of its own, which a launch of their own adds up.  The fp32 passes have four times as many workgroups where they are few.
+// Forward and backward (MI355X, us), at least 256 / 512 / 1024 workgroups: bf16: 16 and 4 heads, d = 64: 12 of up to 4096 538 / 370 / 310, 20 of up to 8192, d = 128 -
+// / 4046 / 4014; 16 and 2, 2 of 6000 967 / 771 / 736; 32 and 8, d = 128, 4 of 1024 268 / 249 / 258; fp32: 16 and 8, 8 of 500 177 / 206 / 206; 16 and 4, d = 128, 3 of up
+// to 2500 1320 / 1368 / 1365
+inline int packed_splits(int64_t workgroups, int group, int dtype) {
   int splits = 1;
   for (int k = 1; k <= group; ++k)
     if (group % k == 0) {
       splits = k;
-      if (workgroups * k >= 512) break;
+      if (workgroups * k >= (dtype == HA_BF16 ? 1024 : 256)) break;
     }
   return splits;
 }

@@ -137,12 +137,13 @@ def test_packed_forward_and_backward(ha, torch, case, dtype, causal):
         assert torch.equal(got[name], again[name]), name
 
 
-def test_many_workgroups_and_no_split(ha, torch):
-    """Enough tiles that one workgroup takes a key head's query heads together, and key heads in eights."""
+@pytest.mark.parametrize("lens,Hq,Hk,split", [([900, 1300, 1100, 128, 600, 777] * 2, 16, 8, True), ([1024] * 7 + [700], 32, 16, False)])
+def test_many_workgroups(ha, torch, lens, Hq, Hk, split):
+    """Key heads in eights, and enough tiles that one bf16 workgroup takes a key head's query heads together."""
     rng = np.random.default_rng(50)
-    lens, Hq, Hk, d = [900, 1300, 1100, 128, 600, 777] * 2, 16, 8, 64
+    d = 64
     cu = np.concatenate([[0], np.cumsum(lens)])
-    assert ha.exact_attn_packed_backward_workspace_bytes(int(cu[-1]), len(lens), Hq, Hk, d) < int(cu[-1]) * Hq * 4 + 512
+    assert (ha.exact_attn_packed_backward_workspace_bytes(int(cu[-1]), len(lens), Hq, Hk, d) > int(cu[-1]) * Hq * 4 + 512) == split
     c = torch.from_numpy(cu.astype(np.int32)).cuda()
     for dtype in ("bf16", "fp32"):
         Q, K, V, dO = inputs(torch, rng, int(cu[-1]), Hq, Hk, d, dtype, True)
