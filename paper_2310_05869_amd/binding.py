@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from ctypes import POINTER, c_char_p, c_float, c_int, c_int32, c_int64, c_size_t, c_uint64, c_void_p
 
 import numpy as np
@@ -57,30 +58,6 @@ class HyperAttnError(RuntimeError):
         super().__init__(f"{where}: {strerror(status)} (status {status})")
 
 
-class HaStrides(ctypes.Structure):
-    _fields_ = [("row", c_int64), ("head", c_int64)]
-
-
-class HaPacked(ctypes.Structure):
-    _fields_ = [(k, c_int32) for k in ("n_seq", "rows", "Hq", "Hk", "d", "dtype", "causal")]
-
-
-class HaPackedStrides(ctypes.Structure):
-    _fields_ = [(k, HaStrides) for k in ("q", "k", "v", "out", "d_out", "dq", "dk", "dv")]
-
-
-class HaCache4(ctypes.Structure):
-    _fields_ = [(k, c_int32) for k in ("n_pages", "page", "Hk", "d")]
-
-
-class HaCache4Query(ctypes.Structure):
-    _fields_ = [(k, c_int32) for k in ("n_seq", "q_len", "Hq", "dtype", "max_blocks")]
-
-
-class HaPagePlanShape(ctypes.Structure):
-    _fields_ = [(k, c_int32) for k in ("n_seq", "max_blocks", "page", "n_pages", "rows")]
-
-
 _SIGNATURES = {
     "ha_workspace_layout": (c_int, [POINTER(HaShape), POINTER(HaParams), POINTER(HaWsLayout)]),
     "ha_workspace_bytes": (c_size_t, [POINTER(HaShape), POINTER(HaParams)]),
@@ -120,15 +97,15 @@ _SIGNATURES = {
     "ha_alg2_workspace_bytes": (c_size_t, [POINTER(HaShape), POINTER(HaParams)]),
     "hyperattn_forward_alg2": (c_int, [c_void_p] * 5 + [POINTER(HaShape), POINTER(HaParams), POINTER(HaAlg2Options),
                                                        c_void_p, c_size_t, c_void_p]),
-    "exact_attn_packed_forward": (c_int, [c_void_p] * 7 + [POINTER(HaPacked), POINTER(HaPackedStrides), c_void_p]),
-    "exact_attn_packed_backward": (c_int, [c_void_p] * 11 + [POINTER(HaPacked), POINTER(HaPackedStrides), c_void_p, c_size_t, c_void_p]),
-    "exact_attn_packed_backward_workspace_bytes": (c_size_t, [POINTER(HaPacked)]),
-    "ha_cache4_bytes": (c_size_t, [POINTER(HaCache4)]),
-    "ha_cache4_write": (c_int, [c_void_p] * 4 + [POINTER(HaCache4), c_int32, c_int32, POINTER(HaStrides), c_void_p]),
-    "ha_cache4_read": (c_int, [c_void_p] * 4 + [POINTER(HaCache4), c_int32, c_int32, POINTER(HaStrides), c_void_p]),
-    "ha_cache4_attn": (c_int, [c_void_p] * 6 + [POINTER(HaCache4), POINTER(HaCache4Query), POINTER(HaStrides), c_void_p, c_size_t, c_void_p]),
-    "ha_cache4_attn_workspace_bytes": (c_size_t, [POINTER(HaCache4), POINTER(HaCache4Query)]),
-    "ha_page_plan": (c_int, [c_void_p] * 9 + [POINTER(HaPagePlanShape), c_void_p]),
+    "exact_attn_packed_forward": (c_int, [c_void_p] * 7 + [c_void_p, c_void_p, c_void_p]),
+    "exact_attn_packed_backward": (c_int, [c_void_p] * 11 + [c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "exact_attn_packed_backward_workspace_bytes": (c_size_t, [c_void_p]),
+    "ha_cache4_bytes": (c_size_t, [c_void_p]),
+    "ha_cache4_write": (c_int, [c_void_p] * 4 + [c_void_p, c_int32, c_int32, c_void_p, c_void_p]),
+    "ha_cache4_read": (c_int, [c_void_p] * 4 + [c_void_p, c_int32, c_int32, c_void_p, c_void_p]),
+    "ha_cache4_attn": (c_int, [c_void_p] * 6 + [c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "ha_cache4_attn_workspace_bytes": (c_size_t, [c_void_p, c_void_p]),
+    "ha_page_plan": (c_int, [c_void_p] * 9 + [c_void_p, c_void_p]),
     "ha_measure_mfma_rate": (c_int, [c_void_p, c_size_t, c_int32, POINTER(c_float), c_void_p]),
     "ha_measure_hbm_rate": (c_int, [c_void_p, c_size_t, POINTER(c_float), POINTER(c_float), c_void_p]),
     "ha_issue_probe_count": (c_int32, []),
@@ -742,17 +719,58 @@ def alg2_workspace_views(workspace, shape: HaShape, params: HaParams):
 
 
 # ---------------------------------------------------------------- packed sequences
-# Rows [rows, heads, d] may be slices of a larger tensor: their strides go along.  These calls run on the current device: a launch for another one's
-# tensors is refused here.
-def _stream_for(stream, like):
-    """The stream's handle; `like` and the stream have to be on the current device."""
+# Rows [rows, heads, d] may be slices of a larger tensor: their strides go along.  These calls run on the current device: tensors or a stream of another one
+# are refused here.  A tensor that fits costs four comparisons, and the sizes of a call go to the library as packed bytes: host time of a decoding
+# step's calls, whose kernels take 3 to 9 us (MI355X; structures of ctypes, devices compared as objects -> this): two calls for rows 17.4 -> 13.0 us, a plan
+# 10.7 -> 7.6, attention over pages 13.9 -> 9.7, over packed prompts 11.7 -> 9.3.
+_PACKED = struct.Struct("7i")
+_PACKED_STRIDES = struct.Struct("16q")
+_STRIDES2 = struct.Struct("4q")
+_CACHE4 = struct.Struct("4i")
+_FIVE = struct.Struct("5i")  # ha_cache4_query, ha_page_plan_shape
+
+
+def _here(t, name, stream):
+    """(device, stream handle) of a call on the current device, where t has to be."""
     torch = _torch()
-    here = torch.cuda.current_device()
-    if like.device.index != here:
-        raise ValueError(f"tensors are on {like.device}, the current device is cuda:{here}")
-    if stream is not None and stream.device.index != here:
+    dev, here = t.get_device(), torch.cuda.current_device()
+    if dev != here:
+        if dev < 0:
+            raise ValueError(f"{name} must be a device tensor")
+        raise ValueError(f"{name} is on cuda:{dev}, the current device is cuda:{here}")
+    if stream is None:
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        return dev, torch.cuda.current_stream().cuda_stream if raw is None else raw(dev)
+    if stream.device.index != here:
         raise ValueError(f"the stream is on {stream.device}, the current device is cuda:{here}")
-    return _stream(stream)
+    return dev, stream.cuda_stream
+
+
+def _misfit(t, name, shape, dtype, dev):
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, expected cuda:{dev}")
+    raise ValueError(f"{name} must be contiguous")
+
+
+def _whole(t, name, shape, dtype, dev):
+    """Address of a contiguous tensor."""
+    if t.shape == shape and t.dtype is dtype and t.get_device() == dev and t.is_contiguous():
+        return t.data_ptr()
+    return _misfit(t, name, shape, dtype, dev)
+
+
+def _rows(t, name, shape, dtype, dev):
+    """(row, head) strides of a [rows, heads, d] tensor whose rows are whole."""
+    if not (t.shape == shape and t.dtype is dtype and t.get_device() == dev):
+        _misfit(t, name, shape, dtype, dev)
+    row, head, one = t.stride()
+    if one != 1:
+        raise ValueError(f"the last dimension of {name} must be contiguous, its stride is {one}")
+    return row if shape[0] > 1 else shape[1] * shape[2], head if shape[1] > 1 else shape[2]
 
 
 def _empty(stream, shape, dtype, like):
@@ -764,31 +782,14 @@ def _empty(stream, shape, dtype, like):
         return torch.empty(shape, dtype=dtype, device=like.device)
 
 
-def _rows(t, name, shape, dtype, like):
-    """Strides of a [rows, heads, d] tensor whose rows are whole."""
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a device tensor")
-    _expect(t, name, shape, dtype, like)
-    row, head, one = t.stride()
-    if one != 1:
-        raise ValueError(f"the last dimension of {name} must be contiguous, its stride is {one}")
-    return HaStrides(row if shape[0] > 1 else shape[1] * shape[2], head if shape[1] > 1 else shape[2])
-
-
-def _ints(t, name, shape, like):
-    _expect(t, name, shape, _torch().int32, like)
-    return _dev(t, name)
-
-
-def _packed_shape(Q, K, V, cu_seqlens, causal):
-    for name, t in (("Q", Q), ("K", K), ("V", V)):
-        if t.dim() != 3:
-            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected [rows, heads, d]")
-    rows, Hq, d = Q.shape
-    Hk = K.shape[1]
+def _packed_call(Q, K, cu_seqlens, causal):
+    if Q.dim() != 3 or K.dim() != 3:
+        raise ValueError(f"Q and K have shapes {tuple(Q.shape)} and {tuple(K.shape)}, expected [rows, heads, d]")
     if cu_seqlens.dim() != 1 or cu_seqlens.shape[0] < 1:
         raise ValueError(f"cu_seqlens has shape {tuple(cu_seqlens.shape)}, expected [n_seq + 1]")
-    return HaPacked(cu_seqlens.shape[0] - 1, rows, Hq, Hk, d, _dtype_code(Q), int(bool(causal)))
+    rows, Hq, d = Q.shape
+    Hk = K.shape[1]
+    return rows, Hq, Hk, d, _PACKED.pack(cu_seqlens.shape[0] - 1, rows, Hq, Hk, d, _dtype_code(Q), 1 if causal else 0)
 
 
 def exact_attn_packed_forward(Q, K, V, cu_seqlens, causal=False, out=None, lse=None, stream=None, out_f32=None):
@@ -797,69 +798,69 @@ def exact_attn_packed_forward(Q, K, V, cu_seqlens, causal=False, out=None, lse=N
     h // (Hq // Hk).  lse: float32 [Hq, rows].  Rows of no sequence are left as they were.  out_f32 (float32 [rows, Hq, d]; bf16 tensors), if given,
     receives the output before its rounding: pass it on to exact_attn_packed_backward."""
     torch = _torch()
-    shape = _packed_shape(Q, K, V, cu_seqlens, causal)
-    rows, Hq, d = Q.shape
-    handle = _stream_for(stream, Q)
-    out = _empty(stream, (rows, Hq, d), Q.dtype, Q) if out is None else out
-    lse = _empty(stream, (Hq, rows), torch.float32, Q) if lse is None else lse
-    _expect_f32(Q, (Hq, rows), lse=lse)
-    _expect_f32(Q, (rows, Hq, d), out_f32=out_f32)
-    kv = (rows, shape.Hk, d)
-    strides = HaPackedStrides(_rows(Q, "Q", Q.shape, Q.dtype, Q), _rows(K, "K", kv, Q.dtype, Q), _rows(V, "V", kv, Q.dtype, Q),
-                              _rows(out, "out", Q.shape, Q.dtype, Q))
-    _check(lib().exact_attn_packed_forward(Q.data_ptr(), K.data_ptr(), V.data_ptr(), _ints(cu_seqlens, "cu_seqlens", cu_seqlens.shape, Q),
-                                           out.data_ptr(), _dev(lse, "lse"), None if out_f32 is None else _dev(out_f32, "out_f32"),
-                                           ctypes.byref(shape), ctypes.byref(strides), handle), "exact_attn_packed_forward")
+    rows, Hq, Hk, d, shape = _packed_call(Q, K, cu_seqlens, causal)
+    dt, f32 = Q.dtype, torch.float32
+    dev, handle = _here(Q, "Q", stream)
+    full, kv = (rows, Hq, d), (rows, Hk, d)
+    if out is None:
+        out = _empty(stream, full, dt, Q)
+    if lse is None:
+        lse = _empty(stream, (Hq, rows), f32, Q)
+    strides = _PACKED_STRIDES.pack(*_rows(Q, "Q", full, dt, dev), *_rows(K, "K", kv, dt, dev), *_rows(V, "V", kv, dt, dev), *_rows(out, "out", full, dt, dev),
+                                   0, 0, 0, 0, 0, 0, 0, 0)
+    _check(lib().exact_attn_packed_forward(Q.data_ptr(), K.data_ptr(), V.data_ptr(), _whole(cu_seqlens, "cu_seqlens", cu_seqlens.shape, torch.int32, dev),
+                                           out.data_ptr(), _whole(lse, "lse", (Hq, rows), f32, dev),
+                                           None if out_f32 is None else _whole(out_f32, "out_f32", full, f32, dev), shape, strides, handle),
+           "exact_attn_packed_forward")
     return out, lse
 
 
 def exact_attn_packed_backward_workspace_bytes(rows, n_seq, Hq, Hk, d, dtype=None) -> int:
     code = HA_BF16 if dtype is None else _dtype_code(_torch().empty((), dtype=dtype))
-    return int(lib().exact_attn_packed_backward_workspace_bytes(ctypes.byref(HaPacked(n_seq, rows, Hq, Hk, d, code, 0))))
+    return int(lib().exact_attn_packed_backward_workspace_bytes(_PACKED.pack(n_seq, rows, Hq, Hk, d, code, 0)))
 
 
 def exact_attn_packed_backward(Q, K, V, cu_seqlens, out, lse, d_out, causal=False, workspace=None, grads=None, stream=None, out_f32=None):
     """dQ, dK, dV of sum(out * d_out); out, lse and out_f32 as exact_attn_packed_forward wrote them.  Rows of no sequence are left as they were (zeros,
     where this call allocates the gradients)."""
     torch = _torch()
-    shape = _packed_shape(Q, K, V, cu_seqlens, causal)
-    rows, Hq, d = Q.shape
-    kv = (rows, shape.Hk, d)
-    handle = _stream_for(stream, Q)
+    rows, Hq, Hk, d, shape = _packed_call(Q, K, cu_seqlens, causal)
+    dt, f32 = Q.dtype, torch.float32
+    dev, handle = _here(Q, "Q", stream)
+    full, kv = (rows, Hq, d), (rows, Hk, d)
     if grads is None:
-        grads = tuple(_empty(stream, s, Q.dtype, Q) for s in (Q.shape, kv, kv))
+        grads = tuple(_empty(stream, s, dt, Q) for s in (full, kv, kv))
         with torch.cuda.stream(stream):   # (None: the current one)
             for t in grads:
                 t.zero_()
     dQ, dK, dV = grads
-    _expect_f32(Q, (Hq, rows), lse=lse)
-    _expect_f32(Q, (rows, Hq, d), out_f32=out_f32)
     if workspace is None:
-        workspace = _empty(stream, (int(lib().exact_attn_packed_backward_workspace_bytes(ctypes.byref(shape))),), torch.uint8, Q)
-    strides = HaPackedStrides(*(_rows(t, name, s, Q.dtype, Q) for t, name, s in (
-        (Q, "Q", Q.shape), (K, "K", kv), (V, "V", kv), (out, "out", Q.shape), (d_out, "d_out", Q.shape), (dQ, "dQ", Q.shape), (dK, "dK", kv), (dV, "dV", kv))))
-    _check(lib().exact_attn_packed_backward(Q.data_ptr(), K.data_ptr(), V.data_ptr(), _ints(cu_seqlens, "cu_seqlens", cu_seqlens.shape, Q),
-                                            out.data_ptr(), None if out_f32 is None else _dev(out_f32, "out_f32"), _dev(lse, "lse"), d_out.data_ptr(),
-                                            dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), ctypes.byref(shape), ctypes.byref(strides),
-                                            _dev(workspace, "workspace"), workspace.numel(), handle), "exact_attn_packed_backward")
+        workspace = _empty(stream, (int(lib().exact_attn_packed_backward_workspace_bytes(shape)),), torch.uint8, Q)
+    strides = _PACKED_STRIDES.pack(*_rows(Q, "Q", full, dt, dev), *_rows(K, "K", kv, dt, dev), *_rows(V, "V", kv, dt, dev), *_rows(out, "out", full, dt, dev),
+                                   *_rows(d_out, "d_out", full, dt, dev), *_rows(dQ, "dQ", full, dt, dev), *_rows(dK, "dK", kv, dt, dev),
+                                   *_rows(dV, "dV", kv, dt, dev))
+    _check(lib().exact_attn_packed_backward(Q.data_ptr(), K.data_ptr(), V.data_ptr(), _whole(cu_seqlens, "cu_seqlens", cu_seqlens.shape, torch.int32, dev),
+                                            out.data_ptr(), None if out_f32 is None else _whole(out_f32, "out_f32", full, f32, dev),
+                                            _whole(lse, "lse", (Hq, rows), f32, dev), d_out.data_ptr(), dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), shape,
+                                            strides, _whole(workspace, "workspace", workspace.shape, torch.uint8, dev), workspace.numel(), handle),
+           "exact_attn_packed_backward")
     return dQ, dK, dV
 
 
 # ---------------------------------------------------------------- paged 4-bit cache
 def _cache4(cache, page, d=None):
-    """The cache's shape: uint8 [n_pages, Hk, page * (d + d / 16)]."""
-    torch = _torch()
-    if cache.dtype != torch.uint8 or cache.dim() != 3:
+    """(n_pages, page, Hk, d) of a cache uint8 [n_pages, Hk, page * (d + d / 16)]."""
+    if cache.dtype is not _torch().uint8 or cache.dim() != 3:
         raise TypeError(f"cache must be uint8 [n_pages, Hk, page * (d + d / 16)], got {cache.dtype} {tuple(cache.shape)}")
     n_pages, Hk, nbytes = cache.shape
-    of_page = nbytes // page * 16 // 17 if page > 0 else 0
-    if of_page not in (64, 128) or of_page * 17 // 16 * page != nbytes or (d is not None and d != of_page):
+    of_page = d if d is not None else nbytes // page * 16 // 17 if page > 0 else 0
+    if of_page not in (64, 128) or of_page * 17 // 16 * page != nbytes:
         raise ValueError(f"cache has shape {tuple(cache.shape)}, expected [n_pages, Hk, {page} * (d + d / 16)] with d = {'64 or 128' if d is None else d}")
-    return HaCache4(n_pages, page, Hk, of_page)
+    return n_pages, page, Hk, of_page
 
 
 def ha_cache4_bytes(n_pages, page, Hk, d) -> int:
-    return int(lib().ha_cache4_bytes(ctypes.byref(HaCache4(n_pages, page, Hk, d))))
+    return int(lib().ha_cache4_bytes(_CACHE4.pack(n_pages, page, Hk, d)))
 
 
 def alloc_cache4(n_pages, page, Hk, d, device="cuda"):
@@ -871,21 +872,25 @@ def alloc_cache4(n_pages, page, Hk, d, device="cuda"):
 
 def ha_cache4_write(K, V, slots, cache, page, stream=None):
     """Rows of K and V ([rows, Hk, d], bf16 or fp32; strided as they lie) into the cache's slots (int32 [rows]; outside the cache: left out)."""
+    torch = _torch()
     if K.dim() != 3:
         raise ValueError(f"K has shape {tuple(K.shape)}, expected [rows, Hk, d]")
-    rows, Hk, d = K.shape
-    shape = _cache4(cache, page, d)
-    if shape.Hk != Hk:
-        raise ValueError(f"K has {Hk} heads, the cache {shape.Hk}")
-    kv = (HaStrides * 2)(_rows(K, "K", K.shape, K.dtype, cache), _rows(V, "V", K.shape, K.dtype, cache))
-    _check(lib().ha_cache4_write(K.data_ptr(), V.data_ptr(), _ints(slots, "slots", (rows,), cache), _dev(cache, "cache"), ctypes.byref(shape), rows,
-                                 _dtype_code(K), kv, _stream_for(stream, cache)), "ha_cache4_write")
+    rows, Hk, d = full = tuple(K.shape)
+    sizes = _cache4(cache, page, d)
+    if sizes[2] != Hk:
+        raise ValueError(f"K has {Hk} heads, the cache {sizes[2]}")
+    dt = K.dtype
+    dev, handle = _here(cache, "cache", stream)
+    kv = _STRIDES2.pack(*_rows(K, "K", full, dt, dev), *_rows(V, "V", full, dt, dev))
+    _check(lib().ha_cache4_write(K.data_ptr(), V.data_ptr(), _whole(slots, "slots", (rows,), torch.int32, dev),
+                                 _whole(cache, "cache", cache.shape, torch.uint8, dev), _CACHE4.pack(*sizes), rows, _dtype_code(K), kv, handle),
+           "ha_cache4_write")
 
 
 def ha_cache4_read(cache, slots, page, dtype=None, K=None, V=None, stream=None):
     """K, V ([rows, Hk, d]): the rows of the slots (int32 [rows]) as the cache holds them; of slots outside it: zeros."""
     torch = _torch()
-    shape = _cache4(cache, page)
+    sizes = _cache4(cache, page)
     rows = slots.shape[0]
     if K is not None:
         dtype = K.dtype
@@ -893,19 +898,21 @@ def ha_cache4_read(cache, slots, page, dtype=None, K=None, V=None, stream=None):
         dtype = V.dtype
     elif dtype is None:
         dtype = torch.bfloat16
-    full = (rows, shape.Hk, shape.d)
-    handle = _stream_for(stream, cache)
-    K = _empty(stream, full, dtype, cache) if K is None else K
-    V = _empty(stream, full, dtype, cache) if V is None else V
-    kv = (HaStrides * 2)(_rows(K, "K", full, dtype, cache), _rows(V, "V", full, dtype, cache))
-    _check(lib().ha_cache4_read(_dev(cache, "cache"), _ints(slots, "slots", (rows,), cache), K.data_ptr(), V.data_ptr(), ctypes.byref(shape), rows,
-                                _dtype_code(K), kv, handle), "ha_cache4_read")
+    full = (rows, sizes[2], sizes[3])
+    dev, handle = _here(cache, "cache", stream)
+    if K is None:
+        K = _empty(stream, full, dtype, cache)
+    if V is None:
+        V = _empty(stream, full, dtype, cache)
+    kv = _STRIDES2.pack(*_rows(K, "K", full, dtype, dev), *_rows(V, "V", full, dtype, dev))
+    _check(lib().ha_cache4_read(_whole(cache, "cache", cache.shape, torch.uint8, dev), _whole(slots, "slots", (rows,), torch.int32, dev), K.data_ptr(),
+                                V.data_ptr(), _CACHE4.pack(*sizes), rows, _dtype_code(K), kv, handle), "ha_cache4_read")
     return K, V
 
 
 def ha_cache4_attn_workspace_bytes(cache, page, n_seq, q_len, Hq, max_blocks, dtype=None) -> int:
     code = HA_BF16 if dtype is None else _dtype_code(_torch().empty((), dtype=dtype))
-    return int(lib().ha_cache4_attn_workspace_bytes(ctypes.byref(_cache4(cache, page)), ctypes.byref(HaCache4Query(n_seq, q_len, Hq, code, max_blocks))))
+    return int(lib().ha_cache4_attn_workspace_bytes(_CACHE4.pack(*_cache4(cache, page)), _FIVE.pack(n_seq, q_len, Hq, code, max_blocks)))
 
 
 def ha_cache4_attn(Q, cache, block_table, lens, page, q_len=1, out=None, lse=None, workspace=None, stream=None):
@@ -915,24 +922,25 @@ def ha_cache4_attn(Q, cache, block_table, lens, page, q_len=1, out=None, lse=Non
     torch = _torch()
     if Q.dim() != 3:
         raise ValueError(f"Q has shape {tuple(Q.shape)}, expected [n_seq * q_len, Hq, d]")
-    rows, Hq, d = Q.shape
-    shape = _cache4(cache, page, d)
+    rows, Hq, d = full = tuple(Q.shape)
+    sizes = _CACHE4.pack(*_cache4(cache, page, d))
     if block_table.dim() != 2 or rows != block_table.shape[0] * q_len:
         raise ValueError(f"Q has {rows} rows, the block table {tuple(block_table.shape)}, q_len is {q_len}")
     n_seq, max_blocks = block_table.shape
-    query = HaCache4Query(n_seq, q_len, Hq, _dtype_code(Q), max_blocks)
-    handle = _stream_for(stream, cache)
+    dt, i32 = Q.dtype, torch.int32
+    query = _FIVE.pack(n_seq, q_len, Hq, _dtype_code(Q), max_blocks)
+    dev, handle = _here(cache, "cache", stream)
     if out is None:
-        out = _empty(stream, (rows, Hq, d), Q.dtype, Q)
+        out = _empty(stream, full, dt, Q)
     if lse is None:
         lse = _empty(stream, (Hq, rows), torch.float32, Q)
-    _expect_f32(cache, (Hq, rows), lse=lse)
-    qo = (HaStrides * 2)(_rows(Q, "Q", Q.shape, Q.dtype, cache), _rows(out, "out", Q.shape, Q.dtype, cache))
+    qo = _STRIDES2.pack(*_rows(Q, "Q", full, dt, dev), *_rows(out, "out", full, dt, dev))
     if workspace is None:
-        workspace = _empty(stream, (int(lib().ha_cache4_attn_workspace_bytes(ctypes.byref(shape), ctypes.byref(query))),), torch.uint8, Q)
-    _check(lib().ha_cache4_attn(Q.data_ptr(), _dev(cache, "cache"), _ints(block_table, "block_table", block_table.shape, cache),
-                                _ints(lens, "lens", (n_seq,), cache), out.data_ptr(), _dev(lse, "lse"), ctypes.byref(shape), ctypes.byref(query), qo,
-                                _dev(workspace, "workspace"), workspace.numel(), handle), "ha_cache4_attn")
+        workspace = _empty(stream, (int(lib().ha_cache4_attn_workspace_bytes(sizes, query)),), torch.uint8, Q)
+    _check(lib().ha_cache4_attn(Q.data_ptr(), _whole(cache, "cache", cache.shape, torch.uint8, dev),
+                                _whole(block_table, "block_table", block_table.shape, i32, dev), _whole(lens, "lens", (n_seq,), i32, dev), out.data_ptr(),
+                                _whole(lse, "lse", (Hq, rows), torch.float32, dev), sizes, query, qo,
+                                _whole(workspace, "workspace", workspace.shape, torch.uint8, dev), workspace.numel(), handle), "ha_cache4_attn")
     return out, lse
 
 
@@ -941,23 +949,28 @@ def ha_page_plan(lens, add, block_table, free_pages, free_count, page, rows=None
     """(lens_out, cu_seqlens, slots, free_count_out): pages for the rows that a step appends to its sequences (add int32 [n_seq]; < 0: the sequence has ended
     and its pages are free again).  lens int32 [n_seq]; block_table int32 [n_seq, max_blocks] and free_pages int32 [n_pages] change in place; free_count
     int32 [1].  rows: how many slots there are (or `slots` int32 [rows] itself)."""
-    torch = _torch()
+    i32 = _torch().int32
     if block_table.dim() != 2 or free_pages.dim() != 1:
         raise ValueError(f"block_table has shape {tuple(block_table.shape)}, expected [n_seq, max_blocks]; free_pages {tuple(free_pages.shape)}, expected [n_pages]")
     n_seq, max_blocks = block_table.shape
-    if slots is None and rows is None:
+    if slots is not None:
+        rows = slots.shape[0]
+    elif rows is None:
         raise ValueError("ha_page_plan needs rows or slots")
-    rows = slots.shape[0] if slots is not None else rows
-    i32, handle = torch.int32, _stream_for(stream, block_table)
-    lens_out = _empty(stream, (n_seq,), i32, lens) if lens_out is None else lens_out
-    cu_seqlens = _empty(stream, (n_seq + 1,), i32, lens) if cu_seqlens is None else cu_seqlens
-    slots = _empty(stream, (rows,), i32, lens) if slots is None else slots
-    free_count_out = _empty(stream, (1,), i32, lens) if free_count_out is None else free_count_out
-    like = block_table
-    shape = HaPagePlanShape(n_seq, max_blocks, page, free_pages.shape[0], rows)
-    _check(lib().ha_page_plan(_ints(lens, "lens", (n_seq,), like), _ints(add, "add", (n_seq,), like), _ints(block_table, "block_table", block_table.shape, like),
-                              _ints(free_pages, "free_pages", free_pages.shape, like), _ints(free_count, "free_count", (1,), like),
-                              _ints(lens_out, "lens_out", (n_seq,), like), _ints(cu_seqlens, "cu_seqlens", (n_seq + 1,), like),
-                              _ints(slots, "slots", (rows,), like), _ints(free_count_out, "free_count_out", (1,), like), ctypes.byref(shape), handle),
+    dev, handle = _here(block_table, "block_table", stream)
+    if lens_out is None:
+        lens_out = _empty(stream, (n_seq,), i32, lens)
+    if cu_seqlens is None:
+        cu_seqlens = _empty(stream, (n_seq + 1,), i32, lens)
+    if slots is None:
+        slots = _empty(stream, (rows,), i32, lens)
+    if free_count_out is None:
+        free_count_out = _empty(stream, (1,), i32, lens)
+    n_pages = free_pages.shape[0]
+    _check(lib().ha_page_plan(_whole(lens, "lens", (n_seq,), i32, dev), _whole(add, "add", (n_seq,), i32, dev),
+                              _whole(block_table, "block_table", (n_seq, max_blocks), i32, dev), _whole(free_pages, "free_pages", (n_pages,), i32, dev),
+                              _whole(free_count, "free_count", (1,), i32, dev), _whole(lens_out, "lens_out", (n_seq,), i32, dev),
+                              _whole(cu_seqlens, "cu_seqlens", (n_seq + 1,), i32, dev), _whole(slots, "slots", (rows,), i32, dev),
+                              _whole(free_count_out, "free_count_out", (1,), i32, dev), _FIVE.pack(n_seq, max_blocks, page, n_pages, rows), handle),
            "ha_page_plan")
     return lens_out, cu_seqlens, slots, free_count_out
