@@ -25,7 +25,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kCWaves = 4, kCThreads = 64 * kCWaves;
+constexpr int kJoinThreads = 256;
 constexpr int kUnit = 64;        // tokens of a wave's step
 constexpr int kTilesPerUnit = 4; // of 16 tokens
 constexpr int kCRows = 16;       // query rows of a workgroup
@@ -33,12 +33,19 @@ constexpr int kCRows = 16;       // query rows of a workgroup
 // Units of all sequences before s (exclusive), found by one wave: lane l sums a run of sequences.
 __device__ inline int seq_len(const CacheAttnArgs& a, int s) { return min(max(a.lens[s], 0), a.max_blocks << a.c.log_page); }
 __device__ inline int seq_units(const CacheAttnArgs& a, int s) { return (seq_len(a, s) + kUnit - 1) / kUnit; }
+// What a sequence takes of the line: its units and what its start and its end cost a workgroup, in units.  (0 / 2 / 4 / 8: 64 sequences of up to 16384 tokens,
+// three queries each, 54 / 51 / 45 / 42 us; 256 of up to 8192 94 / 76 / 69 / 68; lengths alike +-0.)
+constexpr int kSeqCost = 8;
+__device__ inline int seq_cost(const CacheAttnArgs& a, int s) {
+  const int n = seq_units(a, s);
+  return n > 0 ? n + kSeqCost : 0;
+}
 
-// The total of units and, for unit `u` of the line (u < total), its sequence and the units before that sequence.  Wave-uniform results.
-__device__ inline int units_total(const CacheAttnArgs& a, int lane, int* before) {
+// The line's length, and *before: what precedes the lane's run of sequences.  Wave-uniform results.
+__device__ inline int line_total(const CacheAttnArgs& a, int lane, int* before) {
   const int each = (a.n_seq + 63) / 64, s0 = min(a.n_seq, lane * each), s1 = min(a.n_seq, s0 + each);
   int sum = 0;
-  for (int s = s0; s < s1; ++s) sum += seq_units(a, s);
+  for (int s = s0; s < s1; ++s) sum += seq_cost(a, s);
   int inc = sum;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -48,7 +55,8 @@ __device__ inline int units_total(const CacheAttnArgs& a, int lane, int* before)
   *before = inc - sum;
   return __builtin_amdgcn_readfirstlane(__shfl(inc, 63));
 }
-__device__ inline int find_unit(const CacheAttnArgs& a, int lane, int before, int u, int* seq_first) {
+// The sequence at place u of the line (u < total), and where it begins
+__device__ inline int find_place(const CacheAttnArgs& a, int lane, int before, int u, int* seq_first) {
   const int each = (a.n_seq + 63) / 64;
   // the last lane whose run starts at or before u (runs without units start where the next one does)
   const unsigned long long le = __ballot(before <= u);
@@ -56,7 +64,7 @@ __device__ inline int find_unit(const CacheAttnArgs& a, int lane, int before, in
   int at = __builtin_amdgcn_readfirstlane(__shfl(before, run));
   int s = run * each;
   for (; s < a.n_seq - 1; ++s) {
-    const int n = seq_units(a, s);
+    const int n = seq_cost(a, s);
     if (u < at + n) break;
     at += n;
   }
@@ -68,7 +76,7 @@ __device__ inline int find_unit(const CacheAttnArgs& a, int lane, int before, in
 template <int D>
 struct RawTile {
   uint32_t k[D / 32];
-  uint32_t v[4];        // a token's word each
+  u32x4 v;              // a token's word each
   uint32_t ks;          // the token's scales, a byte per group
   uint32_t vs[D == 128 ? 4 : 2];  // of the lane's four tokens
 };
@@ -79,8 +87,10 @@ struct Weights {
 };
 
 // SPLIT: parts of a query number and of a weight: 1 for bf16 queries, 3 for fp32 ones (24 bits); cached values have one.
-template <int D, int SPLIT>
-__global__ __launch_bounds__(kCThreads, SPLIT == 1 ? 3 : 2) void cache4_attn_kernel(CacheAttnArgs a) {
+// NW waves.  WHOLE: a workgroup per sequence, which it finishes (small tables: no second launch).
+template <int D, int SPLIT, int NW, bool WHOLE>
+__global__ __launch_bounds__(64 * NW, SPLIT == 1 && NW == 4 ? 3 : 2) void cache4_attn_kernel(CacheAttnArgs a) {
+  constexpr int kCWaves = NW, kCThreads = 64 * NW;
   constexpr int G = D / 32;     // groups of channels, products per score
   constexpr int MT = D / 16;    // tiles of 16 channels of the output
   constexpr bool F32 = SPLIT > 1;
@@ -91,13 +101,19 @@ __global__ __launch_bounds__(kCThreads, SPLIT == 1 ? 3 : 2) void cache4_attn_ker
   const int r = lane & 15, kq = lane >> 4;
   const int hk = blockIdx.y % a.c.Hk, tile = blockIdx.y / a.c.Hk;
 
-  int before;
-  const int total = units_total(a, lane, &before);
-  const int part = blockIdx.x, parts = min(a.parts, total);  // (none of them empty: those of a sequence are joined from its first to its last)
-  if (part >= parts) return;
-  const int u0 = (int)((int64_t)total * part / parts), u1 = (int)((int64_t)total * (part + 1) / parts);
-  int seq_first;
-  int s = find_unit(a, lane, before, u0, &seq_first);
+  int s, part = 0, u0 = 0, u1 = 0x7fffffff, seq_first = 0;
+  if constexpr (WHOLE) {
+    s = blockIdx.x;
+  } else {
+    int before;
+    const int total = line_total(a, lane, &before);
+    part = blockIdx.x;
+    const int parts = min(a.parts, total);
+    if (part >= parts) return;
+    u0 = (int)((int64_t)total * part / parts);
+    u1 = (int)((int64_t)total * (part + 1) / parts);
+    s = find_place(a, lane, before, u0, &seq_first);
+  }
 
   const int row = tile * kCRows + r;                   // query row within the key head
   const int row_use = row < a.rows ? row : 0;
@@ -107,13 +123,13 @@ __global__ __launch_bounds__(kCThreads, SPLIT == 1 ? 3 : 2) void cache4_attn_ker
   const unsigned char* head_base = a.cache + (int64_t)hk * a.c.block_bytes();
   const int log_page = a.c.log_page, in_page = a.c.page - 1;
 
-  int u = u0;
-  while (u < u1) {
+  for (;;) {
     const int len = seq_len(a, s);
     const int n_units = (len + kUnit - 1) / kUnit;
-    const int first = u - seq_first, last = min(u1 - seq_first, n_units);  // units of the sequence that are this workgroup's
+    const int first = max(u0 - seq_first, 0), last = min(u1 - seq_first, n_units);  // units of the sequence that are this workgroup's
+    if (WHOLE || first < last) {
     const int32_t* blocks = a.table + (int64_t)s * a.max_blocks;
-    const int last_block = (len - 1) >> log_page;
+    const int last_block = max(len - 1, 0) >> log_page;
 
     bf16x8 q[SPLIT][G];
     {
@@ -177,9 +193,7 @@ __global__ __launch_bounds__(kCThreads, SPLIT == 1 ? 3 : 2) void cache4_attn_ker
         bool there;
         const unsigned char* b = tile_base(unit, t, &there);
         const int tok = (unit * kUnit + 16 * t) & in_page;
-        const u32x4 w = *reinterpret_cast<const u32x4*>(b + a.c.v_at() + ((tok >> 2) + kq) * (D * 2) + (D == 128 ? r : r >> 1) * 16);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) raw[t].v[i] = w[i];
+        raw[t].v = *reinterpret_cast<const u32x4*>(b + a.c.v_at() + ((tok >> 2) + kq) * (D * 2) + (D == 128 ? r : r >> 1) * 16);
         if constexpr (D == 128) {
           const u32x4 sc = *reinterpret_cast<const u32x4*>(b + a.c.v_scale_at() + (tok + 4 * kq) * 4);
 #pragma unroll
@@ -254,6 +268,11 @@ __global__ __launch_bounds__(kCThreads, SPLIT == 1 ? 3 : 2) void cache4_attn_ker
             }
           }
       }
+
+      // Whole quads, here: left to itself the compiler (ROCm 7.2) took the first word of one early and gave the other three's registers to the exponentials
+      // (d = 64, eight waves: wrong sums; the tests of both forms hold it).
+#pragma unroll
+      for (int t = 0; t < kTilesPerUnit; ++t) asm volatile("" : "+v"(raw[t].v));
 
       // ---- weights ----
       float mx = fmaxf(fmaxf(c[0][0], c[0][1]), fmaxf(c[0][2], c[0][3]));
@@ -356,7 +375,7 @@ __global__ __launch_bounds__(kCThreads, SPLIT == 1 ? 3 : 2) void cache4_attn_ker
       *reinterpret_cast<f32x4*>(at + 4) = (f32x4){o[2 * g][2], o[2 * g + 1][2], o[2 * g][3], o[2 * g + 1][3]};
     }
     __syncthreads();
-    const bool whole = first == 0 && last == n_units;
+    const bool whole = WHOLE || (first == 0 && last == n_units);
     constexpr int LPR = D / 4;
     for (int idx = threadIdx.x; idx < kCRows * LPR; idx += kCThreads) {
       const int rr = idx / LPR, ch = (idx % LPR) * 4;
@@ -394,24 +413,24 @@ __global__ __launch_bounds__(kCThreads, SPLIT == 1 ? 3 : 2) void cache4_attn_ker
         }
       }
     }
-    if (blockIdx.y == 0 && threadIdx.x == 0) {
+    if (!WHOLE && blockIdx.y == 0 && threadIdx.x == 0) {
       if (first == 0) a.span[2 * s] = part;
       if (last == n_units) a.span[2 * s + 1] = part;
     }
-    u = seq_first + last;
-    if (u >= u1) break;
+    if constexpr (WHOLE) return;
     __syncthreads();
-    seq_first += n_units;
-    do ++s;
-    while (seq_units(a, s) == 0);  // (a unit follows)
+    }
+    seq_first += n_units > 0 ? n_units + kSeqCost : 0;
+    if (seq_first >= u1) return;
+    ++s;  // (the line goes on: another sequence follows)
   }
 }
 
 // Joins the parts of a query row, or writes the result of one that sees nothing: a workgroup per row.
 template <int D, int SPLIT>
-__global__ __launch_bounds__(kCThreads) void cache4_join_kernel(CacheAttnArgs a) {
+__global__ __launch_bounds__(kJoinThreads) void cache4_join_kernel(CacheAttnArgs a) {
   constexpr bool F32 = SPLIT > 1;
-  constexpr int LPR = D / 4, PAR = kCThreads / LPR;  // lanes per row, parts at a time
+  constexpr int LPR = D / 4, PAR = kJoinThreads / LPR;  // lanes per row, parts at a time
   __shared__ f32x4 sum_o[PAR][LPR];
   __shared__ float sum_l[PAR], sum_m[PAR];
   const int s = blockIdx.x, hq = blockIdx.y % a.Hq, tok = blockIdx.y / a.Hq;
@@ -465,6 +484,15 @@ __global__ __launch_bounds__(kCThreads) void cache4_join_kernel(CacheAttnArgs a)
   if (lane == 0) a.lse[(int64_t)hq * a.n_seq * a.q_len + orow] = empty ? -INFINITY : F32 ? top + logf(l) : (top + log2f(l)) * kLn2;
 }
 
+// Tables of few tokens: a workgroup of eight waves takes a whole sequence, and there is no second launch.  Up to 2048 tokens only where these workgroups are about as
+// many as the chip holds.  Shared out -> whole (MI355X, us; [workgroups]): one sequence of 777 tokens, 4 key heads, d = 64 11.2 -> 8.6; 8 of 1024, 8 key heads 11.1
+// -> 9.0; 200 of up to 500, four queries each 32.9 -> 28.8; tables of 2048: 32 sequences, 8 key heads, d = 128 [256] 21.4 -> 15.0, but one [8] 11.3 -> 12.4, 256 of up to
+// 2048 [2048] 37.7 -> 46.5
+static bool cache4_whole(const CacheAttnArgs& a) {
+  const int64_t tokens = (int64_t)a.max_blocks * a.c.page, wgs = (int64_t)a.n_seq * a.c.Hk * a.tiles;
+  return tokens <= 1024 || (tokens <= 2048 && wgs >= 64 && wgs <= 512);
+}
+
 // Workgroups that share a key head's tokens: three fit a CU, 768 the chip at once.
 int cache4_parts(int Hk, int tiles) {
   const int heads = Hk * tiles;
@@ -473,10 +501,14 @@ int cache4_parts(int Hk, int tiles) {
 
 template <int D, int SPLIT>
 static int launch_attn_form(const CacheAttnArgs& a, hipStream_t st) {
-  hipLaunchKernelGGL((cache4_attn_kernel<D, SPLIT>), dim3((unsigned)a.parts, (unsigned)(a.c.Hk * a.tiles)), dim3(kCThreads), 0, st, a);
+  if (cache4_whole(a)) {
+    hipLaunchKernelGGL((cache4_attn_kernel<D, SPLIT, 8, true>), dim3((unsigned)a.n_seq, (unsigned)(a.c.Hk * a.tiles)), dim3(512), 0, st, a);
+    return check_launch();
+  }
+  hipLaunchKernelGGL((cache4_attn_kernel<D, SPLIT, 4, false>), dim3((unsigned)a.parts, (unsigned)(a.c.Hk * a.tiles)), dim3(256), 0, st, a);
   const int rc = check_launch();
   if (rc != HA_OK) return rc;
-  hipLaunchKernelGGL((cache4_join_kernel<D, SPLIT>), dim3((unsigned)a.n_seq, (unsigned)(a.Hq * a.q_len)), dim3(kCThreads), 0, st, a);
+  hipLaunchKernelGGL((cache4_join_kernel<D, SPLIT>), dim3((unsigned)a.n_seq, (unsigned)(a.Hq * a.q_len)), dim3(kJoinThreads), 0, st, a);
   return check_launch();
 }
 

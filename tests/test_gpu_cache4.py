@@ -164,12 +164,12 @@ def test_rows_strided_as_slices_of_a_projection(ha, torch):
 
 
 # ---------------------------------------------------------------- attention
-def filled_cache(ha, torch, rng, lens, Hk, d, page, scale=1.0, spare=2):
+def filled_cache(ha, torch, rng, lens, Hk, d, page, scale=1.0, spare=2, tokens=0):
     """A cache with random rows of these lengths, a shuffled block table, and the rows' values [len, Hk, d] per sequence."""
     blocks = [-(-n // page) for n in lens]
     n_pages = sum(blocks) + spare
     order = rng.permutation(n_pages).astype(np.int32)
-    most = max(1, max(blocks) if blocks else 1)
+    most = max(1, max(blocks) if blocks else 1, tokens // page)   # tokens: of a wider table
     table = np.full((len(lens), most), -7, np.int32)
     slots, at = [], 0
     for s, (n, b) in enumerate(zip(lens, blocks)):
@@ -240,12 +240,13 @@ CASES = [
 ]
 
 
+@pytest.mark.parametrize("tokens", [0, 4096])   # of the table: small ones have a workgroup per sequence, larger ones share the tokens out
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("case", range(len(CASES)))
-def test_attention_over_pages(ha, torch, dtype, case):
+def test_attention_over_pages(ha, torch, dtype, case, tokens):
     lens, q_len, Hq, Hk, d, page = CASES[case]
     rng = np.random.default_rng(100 + case)
-    cache, table, ks, vs = filled_cache(ha, torch, rng, lens, Hk, d, page)
+    cache, table, ks, vs = filled_cache(ha, torch, rng, lens, Hk, d, page, tokens=tokens)
     Q = torch.from_numpy(2 * d ** -0.25 * rng.standard_normal((len(lens) * q_len, Hq, d))).to(dtypes(torch, dtype)).cuda()
     L = torch.tensor(lens, dtype=torch.int32, device="cuda")
     out, lse = ha.ha_cache4_attn(Q, cache, table, L, page, q_len=q_len)
@@ -255,12 +256,13 @@ def test_attention_over_pages(ha, torch, dtype, case):
     assert torch.equal(out, o2) and torch.equal(lse, l2)
 
 
-def test_attention_with_large_scores_and_far_references(ha, torch):
+@pytest.mark.parametrize("tokens", [0, 4096])
+def test_attention_with_large_scores_and_far_references(ha, torch, tokens):
     """Scores of hundreds, whose largest comes late, in either direction."""
     for dtype in ("bf16", "fp32"):
         rng = np.random.default_rng(8)
         lens, Hq, Hk, d, page = [1000, 260], 4, 2, 64, 16
-        cache, table, ks, vs = filled_cache(ha, torch, rng, lens, Hk, d, page, scale=8.0)
+        cache, table, ks, vs = filled_cache(ha, torch, rng, lens, Hk, d, page, scale=8.0, tokens=tokens)
         Q = torch.from_numpy(8 * d ** -0.25 * rng.standard_normal((2, Hq, d))).to(dtypes(torch, dtype)).cuda()
         out, lse = ha.ha_cache4_attn(Q, cache, table, torch.tensor(lens, dtype=torch.int32, device="cuda"), page)
         ref, rl, absv, werr = attention64(host(Q), ks, vs, 1)
@@ -268,11 +270,12 @@ def test_attention_with_large_scores_and_far_references(ha, torch):
         check_attention(host(out), host(lse), ref, rl, absv, werr, dtype, 1000)
 
 
-def test_attention_pages_that_are_not_there(ha, torch):
+@pytest.mark.parametrize("tokens", [0, 4096])
+def test_attention_pages_that_are_not_there(ha, torch, tokens):
     """Tokens of page numbers outside the cache count as absent; lens past the table as its capacity; negative ones as none."""
     rng = np.random.default_rng(5)
     lens, Hq, Hk, d, page = [200, 100, 50], 4, 2, 128, 16
-    cache, table, ks, vs = filled_cache(ha, torch, rng, lens, Hk, d, page)
+    cache, table, ks, vs = filled_cache(ha, torch, rng, lens, Hk, d, page, tokens=tokens)
     table[0, 2], table[0, 5], table[1, :] = -1, cache.shape[0], 2 ** 31 - 1
     keep = np.ones(200, bool)
     keep[2 * page:3 * page] = keep[5 * page:6 * page] = False
