@@ -90,8 +90,8 @@ struct Weights {
 };
 
 // SPLIT: parts of a query number and of a weight: 1 for bf16 queries, 3 for fp32 ones (24 bits); cached values have one.
-// NW waves.  WHOLE: a workgroup per sequence, which it finishes (small tables: no second launch).
-template <int D, int SPLIT, int NW, bool WHOLE>
+// NW waves.  WHOLE: a workgroup per sequence, which it finishes (small tables: no second launch).  ONCE: codes are read past the caches.
+template <int D, int SPLIT, int NW, bool WHOLE, bool ONCE>
 __global__ __launch_bounds__(64 * NW, SPLIT == 1 && NW == 4 ? 3 : 2) void cache4_attn_kernel(CacheAttnArgs a) {
   constexpr int kCWaves = NW, kCThreads = 64 * NW;
   constexpr int G = D / 32;     // groups of channels, products per score
@@ -160,6 +160,14 @@ __global__ __launch_bounds__(64 * NW, SPLIT == 1 && NW == 4 ? 3 : 2) void cache4
     const int all_see = len - a.q_len + 1;        // that every row sees
 
     RawTile<D> raw[kTilesPerUnit];
+    f32x4 o[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) o[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    // reference of the exponentials, moved (and the sums rescaled) where a row's scores exceed it by more than 8; log2 domain for bf16
+    // queries, natural for fp32 ones; l: this lane's share of the row sum
+    float m = -INFINITY, l = 0.f;
+    constexpr float unit_of = F32 ? 2.f : kLog2e;
+    auto fetch = [](const auto* p) { return ONCE ? __builtin_nontemporal_load(p) : *p; };
     int page_of[kTilesPerUnit];
     auto find_pages = [&](int unit) {
 #pragma unroll
@@ -178,12 +186,12 @@ __global__ __launch_bounds__(64 * NW, SPLIT == 1 && NW == 4 ? 3 : 2) void cache4
         const int tok = (unit * kUnit + 16 * t) & in_page;
         const unsigned char* kp = b + (tok + r) * (D / 2) + kq * (D / 8);
         if constexpr (D == 128) {
-          const u32x4 w = *reinterpret_cast<const u32x4*>(kp);
+          const u32x4 w = fetch(reinterpret_cast<const u32x4*>(kp));
 #pragma unroll
           for (int g = 0; g < G; ++g) raw[t].k[g] = w[g];
           raw[t].ks = *reinterpret_cast<const uint32_t*>(b + a.c.k_scale_at() + (tok + r) * 4);
         } else {
-          const u32x2 w = *reinterpret_cast<const u32x2*>(kp);
+          const u32x2 w = fetch(reinterpret_cast<const u32x2*>(kp));
 #pragma unroll
           for (int g = 0; g < G; ++g) raw[t].k[g] = w[g];
           raw[t].ks = *reinterpret_cast<const uint16_t*>(b + a.c.k_scale_at() + (tok + r) * 2);
@@ -196,7 +204,7 @@ __global__ __launch_bounds__(64 * NW, SPLIT == 1 && NW == 4 ? 3 : 2) void cache4
         bool there;
         const unsigned char* b = tile_base(unit, t, &there);
         const int tok = (unit * kUnit + 16 * t) & in_page;
-        raw[t].v = *reinterpret_cast<const u32x4*>(b + a.c.v_at() + ((tok >> 2) + kq) * (D * 2) + (D == 128 ? r : r >> 1) * 16);
+        raw[t].v = fetch(reinterpret_cast<const u32x4*>(b + a.c.v_at() + ((tok >> 2) + kq) * (D * 2) + (D == 128 ? r : r >> 1) * 16));
         if constexpr (D == 128) {
           const u32x4 sc = *reinterpret_cast<const u32x4*>(b + a.c.v_scale_at() + (tok + 4 * kq) * 4);
 #pragma unroll
@@ -208,14 +216,6 @@ __global__ __launch_bounds__(64 * NW, SPLIT == 1 && NW == 4 ? 3 : 2) void cache4
         }
       }
     };
-
-    f32x4 o[MT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) o[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
-    // reference of the exponentials, moved (and the sums rescaled) where a row's scores exceed it by more than 8; log2 domain for bf16
-    // queries, natural for fp32 ones; l: this lane's share of the row sum
-    float m = -INFINITY, l = 0.f;
-    constexpr float unit_of = F32 ? 2.f : kLog2e;
 
     int unit = first + wave;
     if (unit < last) {
@@ -507,13 +507,20 @@ __global__ __launch_bounds__(kJoinThreads) void cache4_join_kernel(CacheAttnArgs
   if (lane == 0) a.lse[(int64_t)hq * a.n_seq * a.q_len + orow] = empty ? -INFINITY : F32 ? top + logf(l) : (top + log2f(l)) * kLn2;
 }
 
-// Tables of few tokens: a workgroup of eight waves takes a whole sequence, and there is no second launch.  Up to 2048 tokens only where these workgroups are about as
-// many as the chip holds.  Shared out -> whole (MI355X, us; [workgroups]): one sequence of 777 tokens, 4 key heads, d = 64 11.2 -> 8.6; 8 of 1024, 8 key heads 11.1
-// -> 9.0; 200 of up to 500, four queries each 32.9 -> 28.8; tables of 2048: 32 sequences, 8 key heads, d = 128 [256] 21.4 -> 15.0, but one [8] 11.3 -> 12.4, 256 of up to
-// 2048 [2048] 37.7 -> 46.5
-static bool cache4_whole(const CacheAttnArgs& a) {
+// Tables of few tokens: a workgroup takes a whole sequence, and there is no second launch; of eight waves (which fill a CU) where there are few, else of four.
+// Up to 2048 tokens from 64 workgroups on.  Shared out -> whole (MI355X, us; [workgroups]): one sequence of 777 tokens, 4 key heads, d = 64 [4] 11.2 -> 8.6; 8 of
+// 1024 [64] 11.1 -> 9.0; tables of 2048: 32 sequences, 8 key heads, d = 128 [256] 21.4 -> 16.0, but one [8] 11.2 -> 12.4; 60 of 2048, d = 64, fp32 [480] 39.8 -> 26.2;
+// 256 of up to 2048 [2048] 34.4 -> 38.8.  Eight waves -> four: 200 of up to 500, four queries each [1600] 28.7 -> 16.1; 32 of 2048 [256] 16.0 -> 18.8
+static int cache4_whole(const CacheAttnArgs& a) {
   const int64_t tokens = (int64_t)a.max_blocks * a.c.page, wgs = (int64_t)a.n_seq * a.c.Hk * a.tiles;
-  return tokens <= 1024 || (tokens <= 2048 && wgs >= 64 && wgs <= 512);
+  if (tokens > 1024 && (tokens > 2048 || wgs < 64 || wgs > 512)) return 0;
+  return wgs > 256 ? 4 : 8;
+}
+
+// Codes that are read once and more of which may come than the last cache holds are read past the caches: 4 sequences of 131072 tokens 114 -> 103 us, 256 of up to
+// 8192 68 -> 64, 64 of 4096, d = 64 74 -> 73; where they would have stayed from one call to the next, 64 of up to 16384 (145 MB) 41.3 -> 42.4.
+static bool cache4_once(const CacheAttnArgs& a) {
+  return a.tiles == 1 && (int64_t)a.n_seq * a.max_blocks * a.c.Hk * a.c.block_bytes() > (256ll << 20);
 }
 
 // Workgroups that share a key head's tokens
@@ -524,11 +531,15 @@ int cache4_parts(int Hk, int tiles) {
 
 template <int D, int SPLIT>
 static int launch_attn_form(const CacheAttnArgs& a, hipStream_t st) {
-  if (cache4_whole(a)) {
-    hipLaunchKernelGGL((cache4_attn_kernel<D, SPLIT, 8, true>), dim3((unsigned)a.n_seq, (unsigned)(a.c.Hk * a.tiles)), dim3(512), 0, st, a);
+  if (const int waves = cache4_whole(a)) {
+    const dim3 grid((unsigned)a.n_seq, (unsigned)(a.c.Hk * a.tiles));
+    if (waves == 8) hipLaunchKernelGGL((cache4_attn_kernel<D, SPLIT, 8, true, false>), grid, dim3(512), 0, st, a);
+    else hipLaunchKernelGGL((cache4_attn_kernel<D, SPLIT, 4, true, false>), grid, dim3(256), 0, st, a);
     return check_launch();
   }
-  hipLaunchKernelGGL((cache4_attn_kernel<D, SPLIT, 4, false>), dim3((unsigned)a.parts, (unsigned)(a.c.Hk * a.tiles)), dim3(256), 0, st, a);
+  const dim3 grid((unsigned)a.parts, (unsigned)(a.c.Hk * a.tiles));
+  if (cache4_once(a)) hipLaunchKernelGGL((cache4_attn_kernel<D, SPLIT, 4, false, true>), grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((cache4_attn_kernel<D, SPLIT, 4, false, false>), grid, dim3(256), 0, st, a);
   const int rc = check_launch();
   if (rc != HA_OK) return rc;
   hipLaunchKernelGGL((cache4_join_kernel<D, SPLIT>), dim3((unsigned)a.n_seq, (unsigned)(a.Hq * a.q_len)), dim3(kJoinThreads), 0, st, a);
