@@ -6,7 +6,10 @@
 // the nearest code, ties to even, and ends at 6: checked on the card against the seven half-way points, at scales from 2^-125 to 2^100.
 // V's words hold channels that lie 32 apart, so their bytes change places among the lanes of a row, by exchanges too.
 //
-// Bound by memory: rows in (16 or 32 bytes a thread, a row of a head at a time), 17/32 byte a value out.
+// Bound by memory: rows in (16 or 32 bytes a thread, a row of a head at a time), 17/32 byte a value out.  16411 rows of 8 heads, d = 128, bf16 (MI355X; a copy
+// moves 4.75 TB/s): into consecutive slots 18.6 us, 4.6 TB/s, from them 13.3 us, 6.4 TB/s; slots in random order, where a row's V takes a quarter of the bytes of
+// two lines, 25.4 and 21.4 us.  (Four heads a thread: 17.6, 14.1; 27.4, 21.4.)  fp32 rows: two pieces of 16 bytes a thread, which only meet in a
+// cache: past the caches the read took 65 us, now 32.
 #include "cache4_common.h"
 
 namespace ha {
@@ -27,16 +30,24 @@ template <bool F32>
 __device__ inline Eight<F32> load_eight(const void* base, int64_t elem) {
   Eight<F32> x;
   const u32x4* p = reinterpret_cast<const u32x4*>(reinterpret_cast<const unsigned char*>(base) + elem * (F32 ? 4 : 2));
-  x.w[0] = __builtin_nontemporal_load(p);
-  if constexpr (F32) x.w[1] = __builtin_nontemporal_load(p + 1);
+  if constexpr (F32) {
+    x.w[0] = p[0];
+    x.w[1] = p[1];
+  } else {
+    x.w[0] = __builtin_nontemporal_load(p);
+  }
   return x;
 }
 
 template <bool F32>
 __device__ inline void store_eight(void* base, int64_t elem, const Eight<F32>& x) {
   u32x4* p = reinterpret_cast<u32x4*>(reinterpret_cast<unsigned char*>(base) + elem * (F32 ? 4 : 2));
-  __builtin_nontemporal_store(x.w[0], p);
-  if constexpr (F32) __builtin_nontemporal_store(x.w[1], p + 1);
+  if constexpr (F32) {
+    p[0] = x.w[0];
+    p[1] = x.w[1];
+  } else {
+    __builtin_nontemporal_store(x.w[0], p);
+  }
 }
 
 // Bits of the largest magnitude as a float's
