@@ -68,6 +68,7 @@ struct PagePlanArgs {
   int32_t* slots;
   int32_t* free_count_out;
   int32_t n_seq, max_blocks, page, log_page, n_pages, rows;
+  int32_t slot_wgs;  // set by the launcher
 };
 int launch_page_plan(const PagePlanArgs& a, hipStream_t st);
 
