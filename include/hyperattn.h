@@ -405,8 +405,8 @@ int hyperattn_forward_alg2(const void* Q, const void* K, const void* V, void* ou
  * at least d and at most 2^22, and so are head strides of what is written at least d.  lse: float [Hq][rows], out_f32: float [rows][Hq][d] contiguous (bf16 tensors; may be NULL).
  * cu_seqlens: device int32 [n_seq + 1], not decreasing, within [0, rows]; values that are not so are clamped where they are read, and
  * no access leaves the tensors.  Rows of no sequence are not read and not written: a batch may be padded at its end.
- * A sequence may be empty.  A key row past its query's sequence counts for nothing, whatever it holds; an Inf or NaN in V reaches, as 0 times
- * itself, also earlier rows of its own sequence that lie in the same tile of 64 rows.
+ * A sequence may be empty.  A key row of another sequence counts for nothing, whatever it holds; causal: an Inf or NaN in a row reaches, as 0 times
+ * itself, also rows of its own sequence that do not see it where both lie in one tile of 128 rows, as in exact_attn_forward and exact_attn_backward.
  * rows <= 2^24, rows * Hq <= 2^27, n_seq * Hq <= 2^22, Hq % Hk == 0, Hq <= 1024; d in {64, 128}.
  * exact_attn_packed_backward: out, lse and out_f32 as exact_attn_packed_forward wrote them; workspace: device, 256-byte aligned, >=
  * exact_attn_packed_backward_workspace_bytes(); nothing in it is kept.  Sums in a fixed order: same inputs, same bits. */
@@ -468,9 +468,11 @@ int ha_cache4_read(const void* cache, const int32_t* slots, void* K, void* V, co
  * verified together).  Q, out: [n_seq * q_len][Hq][d] of dtype, row s * q_len + i the query of token lens[s] - q_len + i, which sees tokens 0 ... lens[s] -
  * q_len + i; strides qo[0], qo[1] (NULL: contiguous).  lse: float [Hq][n_seq * q_len].  Token t of sequence s lies in page block_table[s][t / page]
  * (device int32 [n_seq][max_blocks]).  lens (device int32) are taken within [0, max_blocks * page]; tokens of a page number outside [0, n_pages) count
- * as absent.  A query that sees nothing has out 0 and lse -inf.  What lies in a page behind a sequence's last token counts for nothing.
+ * as absent.  A query that sees nothing has out 0 and lse -inf.  What lies in a page behind a sequence's last token, or in a token behind the
+ * query's own, counts for nothing, NaN included.
  * Products as in exact_attn_forward: bf16 queries on the matrix cores; fp32 queries split in three, to fp32 accuracy of the cached values.
- * 1 <= q_len <= 64, n_seq <= 2^16, n_seq * q_len * Hq <= 2^22, Hq * q_len <= 2^15, Hq % Hk == 0, n_seq * max_blocks <= 2^30, max_blocks * page < 2^31.
+ * 1 <= q_len <= 64, n_seq <= 2^16, n_seq * q_len * Hq <= 2^22, Hq * q_len <= 2^15, Hq % Hk == 0, n_seq * max_blocks <= 2^30, max_blocks * page < 2^31, n_seq *
+ * max_blocks * page <= 2^36.
  * workspace: device, 256-byte aligned, >= ha_cache4_attn_workspace_bytes(); nothing in it is kept.  Two calls may overlap only with
  * different workspaces.  Same inputs, same bits. */
 typedef struct {

@@ -91,7 +91,8 @@ struct Weights {
 
 // SPLIT: parts of a query number and of a weight: 1 for bf16 queries, 3 for fp32 ones (24 bits); cached values have one.
 // NW waves.  WHOLE: a workgroup per sequence, which it finishes (small tables: no second launch).  ONCE: codes are read past the caches.
-template <int D, int SPLIT, int NW, bool WHOLE, bool ONCE>
+// MULTI: several queries a sequence, which see its last tokens in part.
+template <int D, int SPLIT, int NW, bool WHOLE, bool ONCE, bool MULTI>
 __global__ __launch_bounds__(64 * NW, SPLIT == 1 && NW == 4 ? 3 : 2) void cache4_attn_kernel(CacheAttnArgs a) {
   constexpr int kCWaves = NW, kCThreads = 64 * NW;
   constexpr int G = D / 32;     // groups of channels, products per score
@@ -166,6 +167,7 @@ __global__ __launch_bounds__(64 * NW, SPLIT == 1 && NW == 4 ? 3 : 2) void cache4
     // reference of the exponentials, moved (and the sums rescaled) where a row's scores exceed it by more than 8; log2 domain for bf16
     // queries, natural for fp32 ones; l: this lane's share of the row sum
     float m = -INFINITY, l = 0.f;
+    bool some_nan = false;  // (wave-uniform) a group taken out above
     constexpr float unit_of = F32 ? 2.f : kLog2e;
     auto fetch = [](const auto* p) { return ONCE ? __builtin_nontemporal_load(p) : *p; };
     int page_of[kTilesPerUnit];
@@ -258,6 +260,7 @@ __global__ __launch_bounds__(64 * NW, SPLIT == 1 && NW == 4 ? 3 : 2) void cache4
 #pragma unroll
       for (int t = 0; t < kTilesPerUnit; ++t) special = special || !there[t];
       if (special) {
+        uint32_t nan = 0;
 #pragma unroll
         for (int t = 0; t < kTilesPerUnit; ++t)
 #pragma unroll
@@ -268,8 +271,15 @@ __global__ __launch_bounds__(64 * NW, SPLIT == 1 && NW == 4 ? 3 : 2) void cache4
               raw[t].v[i] = 0;
               if (D == 128) raw[t].vs[i % (D / 32)] = 0;
               else raw[t].vs[i / 2] &= i & 1 ? 0x0000ffffu : 0xffff0000u;
+            } else if (MULTI && tok >= all_see) {  // some rows see it: groups that are NaN are taken out here, for the rows that do not
+              uint32_t& w = raw[t].vs[D == 128 ? i % (D / 32) : i / 2];
+              const uint32_t bytes = D == 128 ? 0x01010101u : i & 1 ? 0x01010000u : 0x00000101u;
+              const uint32_t full = (((w & 0x7f7f7f7fu) + 0x01010101u) & w) >> 7 & bytes;  // 1 in every byte that is 255
+              w &= ~(full * 255u);
+              nan |= full;
             }
           }
+        if (MULTI && __any(nan != 0)) some_nan = true;
       }
 
       // Whole quads, here: left to itself the compiler (ROCm 7.2) took the first word of one early and gave the other three's registers to the exponentials
@@ -367,6 +377,16 @@ __global__ __launch_bounds__(64 * NW, SPLIT == 1 && NW == 4 ? 3 : 2) void cache4
     // ---- the waves' sums through LDS.  Lane (r, kq), register i of o[2 g + e]: query row r, channel 32 g + 8 kq + 2 i + e ----
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
+    if (MULTI && some_nan) {  // rare: the tokens again, for the rows that see them
+      for (int tok = max(all_see, 0); tok < len; ++tok) {
+        const int p = blocks[tok >> log_page];
+        if ((unsigned)p >= (unsigned)a.c.n_pages || tok >= limit) continue;
+        const unsigned char* scales = head_base + (int64_t)p * page_bytes + a.c.v_scale_at() + (tok & in_page) * G;
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+          if (scales[i / 2] == 255) o[i] = (f32x4){NAN, NAN, NAN, NAN};
+      }
+    }
     if (kq == 0) {
       merge_m[wave][r] = m;
       merge_l[wave][r] = l;
@@ -529,26 +549,31 @@ int cache4_parts(int Hk, int tiles) {
   return heads >= kMostParts ? 1 : kMostParts / heads;
 }
 
-template <int D, int SPLIT>
+template <int D, int SPLIT, bool MULTI>
 static int launch_attn_form(const CacheAttnArgs& a, hipStream_t st) {
   if (const int waves = cache4_whole(a)) {
     const dim3 grid((unsigned)a.n_seq, (unsigned)(a.c.Hk * a.tiles));
-    if (waves == 8) hipLaunchKernelGGL((cache4_attn_kernel<D, SPLIT, 8, true, false>), grid, dim3(512), 0, st, a);
-    else hipLaunchKernelGGL((cache4_attn_kernel<D, SPLIT, 4, true, false>), grid, dim3(256), 0, st, a);
+    if (waves == 8) hipLaunchKernelGGL((cache4_attn_kernel<D, SPLIT, 8, true, false, MULTI>), grid, dim3(512), 0, st, a);
+    else hipLaunchKernelGGL((cache4_attn_kernel<D, SPLIT, 4, true, false, MULTI>), grid, dim3(256), 0, st, a);
     return check_launch();
   }
   const dim3 grid((unsigned)a.parts, (unsigned)(a.c.Hk * a.tiles));
-  if (cache4_once(a)) hipLaunchKernelGGL((cache4_attn_kernel<D, SPLIT, 4, false, true>), grid, dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((cache4_attn_kernel<D, SPLIT, 4, false, false>), grid, dim3(256), 0, st, a);
+  if (cache4_once(a)) hipLaunchKernelGGL((cache4_attn_kernel<D, SPLIT, 4, false, true, MULTI>), grid, dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((cache4_attn_kernel<D, SPLIT, 4, false, false, MULTI>), grid, dim3(256), 0, st, a);
   const int rc = check_launch();
   if (rc != HA_OK) return rc;
   hipLaunchKernelGGL((cache4_join_kernel<D, SPLIT>), dim3((unsigned)a.n_seq, (unsigned)(a.Hq * a.q_len)), dim3(kJoinThreads), 0, st, a);
   return check_launch();
 }
 
+template <int D, int SPLIT>
+static int launch_attn_q(const CacheAttnArgs& a, hipStream_t st) {
+  return a.q_len > 1 ? launch_attn_form<D, SPLIT, true>(a, st) : launch_attn_form<D, SPLIT, false>(a, st);
+}
+
 int launch_cache4_attn(const CacheAttnArgs& a, int dtype, hipStream_t st) {
-  if (a.c.d == 128) return dtype == HA_BF16 ? launch_attn_form<128, 1>(a, st) : launch_attn_form<128, 3>(a, st);
-  return dtype == HA_BF16 ? launch_attn_form<64, 1>(a, st) : launch_attn_form<64, 3>(a, st);
+  if (a.c.d == 128) return dtype == HA_BF16 ? launch_attn_q<128, 1>(a, st) : launch_attn_q<128, 3>(a, st);
+  return dtype == HA_BF16 ? launch_attn_q<64, 1>(a, st) : launch_attn_q<64, 3>(a, st);
 }
 
 }  // namespace ha

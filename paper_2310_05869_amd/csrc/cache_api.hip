@@ -52,6 +52,7 @@ static int attn_geometry(const ha_cache4* shape, const ha_cache4_query* q, Cache
   if (q->Hq < 1 || q->Hq % shape->Hk != 0 || (int64_t)q->Hq * q->q_len > (1 << 15)) return HA_ERR_SHAPE;
   if ((int64_t)q->n_seq * q->q_len * q->Hq > (1 << 22)) return HA_ERR_SHAPE;
   if ((int64_t)q->n_seq * q->max_blocks > (1ll << 30) || (int64_t)q->max_blocks * shape->page > 0x7fffffffll - 256) return HA_ERR_SHAPE;
+  if ((int64_t)q->n_seq * q->max_blocks * shape->page > (1ll << 36)) return HA_ERR_SHAPE;  // (units of 64 tokens are counted in 32 bits)
   a->n_seq = q->n_seq;
   a->q_len = q->q_len;
   a->Hq = q->Hq;

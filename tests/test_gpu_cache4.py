@@ -291,6 +291,32 @@ def test_attention_pages_that_are_not_there(ha, torch, tokens):
     assert torch.equal(a[1], b[1])
 
 
+@pytest.mark.parametrize("tokens", [0, 4096])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_a_nan_token_counts_for_the_queries_that_see_it(ha, torch, dtype, tokens):
+    """Five queries a sequence, the third of their tokens with a NaN in channels 32 ... 63 of V: NaN there from that query on, nothing elsewhere."""
+    for d in (64, 128):
+        rng = np.random.default_rng(9)
+        lens, Hq, Hk, page, q_len = [77, 130], 4, 2, 16, 5
+        cache, table, ks, vs = filled_cache(ha, torch, rng, lens, Hk, d, page, tokens=tokens)
+        Q = torch.from_numpy(rng.standard_normal((2 * q_len, Hq, d))).to(dtypes(torch, dtype)).cuda()
+        L = torch.tensor(lens, dtype=torch.int32, device="cuda")
+        want, wl = ha.ha_cache4_attn(Q, cache, table, L, page, q_len=q_len)
+        for s, n in enumerate(lens):
+            pos = n - 3
+            slot = torch.tensor([int(table[s, pos // page]) * page + pos % page], dtype=torch.int32, device="cuda")
+            k, v = ha.ha_cache4_read(cache, slot, page, dtype=torch.float32)
+            v[:, 1, 40] = float("nan")   # the second key head
+            ha.ha_cache4_write(k, v, slot, cache, page)
+        out, lse = ha.ha_cache4_attn(Q, cache, table, L, page, q_len=q_len)
+        hit = torch.zeros_like(out, dtype=torch.bool).view(2, q_len, Hq, d)
+        hit[:, 2:, Hq // Hk:, 32:64] = True
+        hit = hit.view(out.shape)
+        assert torch.isnan(out[hit]).all() and torch.equal(lse, wl)
+        # (k went through the cache twice: its values stay; other channels of V too)
+        assert torch.equal(out[~hit], want[~hit])
+
+
 def test_attention_strides_streams_and_a_workspace_kept(ha, torch):
     rng = np.random.default_rng(6)
     lens, Hq, Hk, d, page, q_len = [300, 40], 4, 2, 64, 16, 2
