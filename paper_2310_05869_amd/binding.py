@@ -721,8 +721,8 @@ def alg2_workspace_views(workspace, shape: HaShape, params: HaParams):
 # ---------------------------------------------------------------- packed sequences
 # Rows [rows, heads, d] may be slices of a larger tensor: their strides go along.  These calls run on the current device: tensors or a stream of another one
 # are refused here.  A tensor that fits costs four comparisons, and the sizes of a call go to the library as packed bytes: host time of a decoding
-# step's calls, whose kernels take 3 to 9 us (MI355X; structures of ctypes, devices compared as objects -> this): two calls for rows 17.4 -> 13.0 us, a plan
-# 10.7 -> 7.6, attention over pages 13.9 -> 9.7, over packed prompts 11.7 -> 9.3.
+# step's calls, whose kernels take 3 to 9 us (MI355X; structures of ctypes, devices compared as objects -> this): two calls for rows 17.4 -> 14.9 us, a plan
+# 10.7 -> 8.1, attention over pages 13.9 -> 12.0, over packed prompts 11.7 -> 8.9.
 _PACKED = struct.Struct("7i")
 _PACKED_STRIDES = struct.Struct("16q")
 _STRIDES2 = struct.Struct("4q")

@@ -37,7 +37,7 @@ constexpr int kCRows = 16;       // query rows of a workgroup
 __device__ inline int seq_len(const CacheAttnArgs& a, int s) { return min(max(a.lens[s], 0), a.max_blocks << a.c.log_page); }
 __device__ inline int seq_units(const CacheAttnArgs& a, int s) { return (seq_len(a, s) + kUnit - 1) / kUnit; }
 // What a sequence takes of the line: its units and what its start and its end cost a workgroup, in units.  (0 / 2 / 4 / 8: 64 sequences of up to 16384 tokens,
-// three queries each, 54 / 51 / 45 / 42 us; 256 of up to 8192 94 / 76 / 69 / 68; lengths alike +-0.)
+// three queries each, 54 / 51 / 45 / 44 us; 256 of up to 8192 94 / 76 / 69 / 68; lengths alike +-0.)
 constexpr int kSeqCost = 8;
 __device__ inline int seq_cost(const CacheAttnArgs& a, int s) {
   const int n = seq_units(a, s);
@@ -167,7 +167,7 @@ __global__ __launch_bounds__(64 * NW, SPLIT == 1 && NW == 4 ? 3 : 2) void cache4
     // reference of the exponentials, moved (and the sums rescaled) where a row's scores exceed it by more than 8; log2 domain for bf16
     // queries, natural for fp32 ones; l: this lane's share of the row sum
     float m = -INFINITY, l = 0.f;
-    bool some_nan = false;  // (wave-uniform) a group taken out above
+    bool some_nan = false;  // (wave-uniform) a group was taken out
     constexpr float unit_of = F32 ? 2.f : kLog2e;
     auto fetch = [](const auto* p) { return ONCE ? __builtin_nontemporal_load(p) : *p; };
     int page_of[kTilesPerUnit];
@@ -271,11 +271,12 @@ __global__ __launch_bounds__(64 * NW, SPLIT == 1 && NW == 4 ? 3 : 2) void cache4
               raw[t].v[i] = 0;
               if (D == 128) raw[t].vs[i % (D / 32)] = 0;
               else raw[t].vs[i / 2] &= i & 1 ? 0x0000ffffu : 0xffff0000u;
-            } else if (MULTI && tok >= all_see) {  // some rows see it: groups that are NaN are taken out here, for the rows that do not
+            }
+            if constexpr (MULTI) {  // groups that are NaN, of tokens that some rows see alone, are taken out here, for the rows that do not
               uint32_t& w = raw[t].vs[D == 128 ? i % (D / 32) : i / 2];
               const uint32_t bytes = D == 128 ? 0x01010101u : i & 1 ? 0x01010000u : 0x00000101u;
-              const uint32_t full = (((w & 0x7f7f7f7fu) + 0x01010101u) & w) >> 7 & bytes;  // 1 in every byte that is 255
-              w &= ~(full * 255u);
+              const uint32_t full = (((w & 0x7f7f7f7fu) + 0x01010101u) & w) >> 7 & (tok >= all_see ? bytes : 0u);  // 1 in every byte that is 255
+              w &= ~((full << 8) - full);
               nan |= full;
             }
           }
@@ -538,7 +539,7 @@ static int cache4_whole(const CacheAttnArgs& a) {
 }
 
 // Codes that are read once and more of which may come than the last cache holds are read past the caches: 4 sequences of 131072 tokens 114 -> 103 us, 256 of up to
-// 8192 68 -> 64, 64 of 4096, d = 64 74 -> 73; where they would have stayed from one call to the next, 64 of up to 16384 (145 MB) 41.3 -> 42.4.
+// 8192 68 -> 64, 64 of 4096, d = 64 74 -> 73; where they would have stayed from one call to the next, 64 of up to 16384 (145 MB) 43.2 -> 44.3.
 static bool cache4_once(const CacheAttnArgs& a) {
   return a.tiles == 1 && (int64_t)a.n_seq * a.max_blocks * a.c.Hk * a.c.block_bytes() > (256ll << 20);
 }
