@@ -28,6 +28,8 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kJoinThreads = 256;
+constexpr unsigned kJoinsAtOnce = 2048;  // workgroups of the joining launch that the chip holds at once
+constexpr int kFewParts = 16;
 constexpr int kMostParts = 768;  // workgroups of four waves that the chip holds at once, three per CU
 constexpr int kUnit = 64;        // tokens of a wave's step
 constexpr int kTilesPerUnit = 4; // of 16 tokens
@@ -450,36 +452,41 @@ __global__ __launch_bounds__(64 * NW, SPLIT == 1 && NW == 4 ? 3 : 2) void cache4
   }
 }
 
-// Joins the parts of a query row, or writes the result of one that sees nothing: a workgroup per row, whose threads, in groups of D / 4, take the parts in turn,
-// eight at a time while there are, so that their numbers and rows are read without waiting for one another (one sequence of 131072 tokens, one key head, whose rows have
-// hundreds of parts, one at a time -> eight, the whole call: 44 -> 17 us).  Weights formed first, by all threads, and then the rows: 16 us, but 64 sequences of few
-// parts, 6144 rows, 10.0 us for this launch against 7.6.
+// Joins the parts of the query rows, or writes the result of one that sees nothing.  A group of D / 4 threads holds a row's sums and takes parts eight at a time
+// while there are, so that their numbers and rows are read without waiting for one another (one sequence of 131072 tokens, one key head, whose rows have hundreds of
+// parts, one at a time -> eight, the whole call: 44 -> 17 us).  A row has a workgroup to itself, whose groups take its parts in turn; in launches of more rows than
+// workgroups run at once, a row of few parts has one group alone, and the workgroups too many end at once (the whole call: 64 sequences of up to 16384 tokens, three queries
+// each, 6144 rows, 44.2 -> 42.0 us; 32 of up to 4096, eight each, 8192 rows, 29.5 -> 26.3; but 60 of up to 8000, 960 rows, 24.6 -> 25.5).
 template <int D, int SPLIT>
 __global__ __launch_bounds__(kJoinThreads) void cache4_join_kernel(CacheAttnArgs a) {
   constexpr bool F32 = SPLIT > 1;
   constexpr int LPR = D / 4, PAR = kJoinThreads / LPR, AHEAD = 8;
   __shared__ f32x4 sum_o[PAR][LPR];
   __shared__ float sum_l[PAR], sum_m[PAR];
-  const int s = blockIdx.x, hq = blockIdx.y % a.Hq, tok = blockIdx.y / a.Hq;
+  const int s = blockIdx.x, lane = threadIdx.x % LPR, mine = threadIdx.x / LPR, ch = lane * 4;
   const int len = seq_len(a, s);
   const int p0 = a.span[2 * s], p1 = a.span[2 * s + 1];  // (asked for with the length; of an empty sequence they are what was there)
   const int parts = len > 0 ? p1 - p0 + 1 : 0;
   if (parts == 1) return;  // finished where its tokens were read
+  const bool few = parts <= kFewParts && gridDim.x * gridDim.y > kJoinsAtOnce;
+  const int rows = a.Hq * a.q_len, y = few ? (int)blockIdx.y * PAR + mine : (int)blockIdx.y;
+  if (y >= rows) return;   // (few: no barrier follows; many: all threads alike)
+  const int hq = y % a.Hq, tok = y / a.Hq;
   const int hk = hq / a.group, row = tok * a.group + hq % a.group, tile = row / kCRows, rr = row % kCRows;
   const int64_t orow = (int64_t)s * a.q_len + tok;
-  const int lane = threadIdx.x % LPR, mine = threadIdx.x / LPR, ch = lane * 4;
   const int64_t slot0 = ((int64_t)(tile * a.c.Hk + hk) * (a.parts + a.n_seq) + s + p0) * kCRows + rr;
   auto exp_of = [](float x) { return F32 ? expf(x) : __builtin_amdgcn_exp2f(x); };
   float m = -INFINITY, l = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  int p = mine;
+  const int step = few ? 1 : PAR;
+  int p = few ? 0 : mine;
   auto take = [&](auto count) {
     constexpr int N = decltype(count)::value;
     float pm[N], pl[N];
     f32x4 v[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int64_t slot = slot0 + (int64_t)(p + i * PAR) * kCRows;
+      const int64_t slot = slot0 + (int64_t)(p + i * step) * kCRows;
       pm[i] = a.part_ml[2 * slot];
       pl[i] = a.part_ml[2 * slot + 1];
       v[i] = *reinterpret_cast<const f32x4*>(a.part_o + slot * D + ch);
@@ -497,10 +504,23 @@ __global__ __launch_bounds__(kJoinThreads) void cache4_join_kernel(CacheAttnArgs
       l += w * pl[i];
     }
     m = top;
-    p += N * PAR;
+    p += N * step;
   };
-  while (p + (AHEAD - 1) * PAR < parts) take(std::integral_constant<int, AHEAD>{});
-  while (p < parts) take(std::integral_constant<int, 1>{});
+  while (p + (AHEAD - 1) * step < parts) take(std::integral_constant<int, AHEAD>{});
+  while (p + step < parts) take(std::integral_constant<int, 2>{});
+  if (p < parts) take(std::integral_constant<int, 1>{});
+  auto finish = [&] {
+    const bool empty = l == 0.f;
+    acc *= empty ? 0.f : 1.f / l;
+    const int64_t at = orow * a.o.row + (int64_t)hq * a.o.head + ch;
+    if constexpr (F32) *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.out) + at) = acc;
+    else *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(a.out) + at) = (u32x2){pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3])};
+    if (lane == 0) a.lse[(int64_t)hq * a.n_seq * a.q_len + orow] = empty ? -INFINITY : F32 ? m + logf(l) : (m + log2f(l)) * kLn2;
+  };
+  if (few) {
+    finish();
+    return;
+  }
   sum_o[mine][lane] = acc;
   if (lane == 0) {
     sum_m[mine] = m;
@@ -508,10 +528,9 @@ __global__ __launch_bounds__(kJoinThreads) void cache4_join_kernel(CacheAttnArgs
   }
   __syncthreads();
   if (mine != 0) return;
-  float top = m;
 #pragma unroll
-  for (int i = 1; i < PAR; ++i) top = fmaxf(top, sum_m[i]);
-  const float ref = top == -INFINITY ? 0.f : top;
+  for (int i = 1; i < PAR; ++i) m = fmaxf(m, sum_m[i]);
+  const float ref = m == -INFINITY ? 0.f : m;
   acc = (f32x4){0.f, 0.f, 0.f, 0.f};
   l = 0.f;
 #pragma unroll
@@ -520,12 +539,7 @@ __global__ __launch_bounds__(kJoinThreads) void cache4_join_kernel(CacheAttnArgs
     acc += w * sum_o[i][lane];
     l += w * sum_l[i];
   }
-  const bool empty = l == 0.f;
-  acc *= empty ? 0.f : 1.f / l;
-  const int64_t at = orow * a.o.row + (int64_t)hq * a.o.head + ch;
-  if constexpr (F32) *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.out) + at) = acc;
-  else *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(a.out) + at) = (u32x2){pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3])};
-  if (lane == 0) a.lse[(int64_t)hq * a.n_seq * a.q_len + orow] = empty ? -INFINITY : F32 ? top + logf(l) : (top + log2f(l)) * kLn2;
+  finish();
 }
 
 // Tables of few tokens: a workgroup takes a whole sequence, and there is no second launch; of eight waves (which fill a CU) where there are few, else of four.
