@@ -402,7 +402,8 @@ int hyperattn_forward_alg2(const void* Q, const void* K, const void* V, void* ou
  *
  * Tensors are [rows][heads][d] with the strides given (elements; the d values of a row are consecutive), so that slices of one
  * projection's output are taken as they lie; strides == NULL: contiguous.  Strides are multiples of 16 bytes; row strides are
- * at least d and at most 2^22, and so are head strides of what is written at least d.  lse: float [Hq][rows], out_f32: float [rows][Hq][d] contiguous (bf16 tensors; may be NULL).
+ * at least d and at most 2^22.  In what is written the heads of a row lie within the row stride, or the rows of a head within the head stride, and no output
+ * overlaps another tensor.  lse: float [Hq][rows], out_f32: float [rows][Hq][d] contiguous (bf16 tensors; may be NULL).
  * cu_seqlens: device int32 [n_seq + 1], not decreasing, within [0, rows]; values that are not so are clamped where they are read, and
  * no access leaves the tensors.  Rows of no sequence are not read and not written: a batch may be padded at its end.
  * A sequence may be empty.  A key row of another sequence counts for nothing, whatever it holds; causal: an Inf or NaN in a row reaches, as 0 times
@@ -453,7 +454,7 @@ size_t exact_attn_packed_backward_workspace_bytes(const ha_packed* shape);
  * ha_cache4_write: row i of K and V ([rows][Hk][d] of dtype, strides as above: kv[0] of K, kv[1] of V; NULL: contiguous) to slot slots[i]; rows
  * whose slot lies outside the cache are left out.  Slots given must differ; where two rows name one slot it holds a mixture of both, and no
  * other slot is touched.  ha_cache4_read: the rows of these slots back (exact in both types; rows of slots outside the cache: zeros),
- * for a prefix whose pages are used again. */
+ * for a prefix whose pages are used again.  rows <= 2^26, rows * Hk <= 2^26. */
 typedef struct {
   int32_t n_pages, page, Hk, d;
 } ha_cache4;

@@ -634,7 +634,6 @@ static void fill_alg2_layout(const Geometry& g, const ha_ws_layout& fwd, ha_alg2
   l->total_bytes = off;
 }
 
-
 // Checks of a packed call; fills g and the packed rows of *a but its pointers.
 static int packed_geometry(const ha_packed* sh, const ha_packed_strides* st, bool backward, AttnArgs* a) {
   if (!sh) return HA_ERR_NULL;
@@ -656,7 +655,7 @@ static int packed_geometry(const ha_packed* sh, const ha_packed_strides* st, boo
   p.Hk = sh->Hk;
   p.group = sh->Hq / sh->Hk;
   p.splits = packed_splits(packed_slots<128>(p) * sh->Hk, p.group, sh->dtype);
-  const auto strides = [&](const ha_strides* s, int heads, bool written, RowStrides* out) { return row_strides(s, heads, sh->d, sh->dtype, written, out); };
+  const auto strides = [&](const ha_strides* s, int heads, bool written, RowStrides* out) { return row_strides(s, sh->rows, heads, sh->d, sh->dtype, written, out); };
   int rc = strides(st ? &st->q : nullptr, sh->Hq, false, &p.q);
   if (rc == HA_OK) rc = strides(st ? &st->k : nullptr, sh->Hk, false, &p.k);
   if (rc == HA_OK) rc = strides(st ? &st->v : nullptr, sh->Hk, false, &p.v);
@@ -1102,9 +1101,9 @@ int exact_attn_packed_backward(const void* Q, const void* K, const void* V, cons
   int rc = packed_geometry(shape, strides, true, &a.f);
   if (rc != HA_OK) return rc;
   RowStrides dq, dk, dv;
-  rc = row_strides(strides ? &strides->dq : nullptr, shape->Hq, shape->d, shape->dtype, true, &dq);
-  if (rc == HA_OK) rc = row_strides(strides ? &strides->dk : nullptr, shape->Hk, shape->d, shape->dtype, true, &dk);
-  if (rc == HA_OK) rc = row_strides(strides ? &strides->dv : nullptr, shape->Hk, shape->d, shape->dtype, true, &dv);
+  rc = row_strides(strides ? &strides->dq : nullptr, shape->rows, shape->Hq, shape->d, shape->dtype, true, &dq);
+  if (rc == HA_OK) rc = row_strides(strides ? &strides->dk : nullptr, shape->rows, shape->Hk, shape->d, shape->dtype, true, &dk);
+  if (rc == HA_OK) rc = row_strides(strides ? &strides->dv : nullptr, shape->rows, shape->Hk, shape->d, shape->dtype, true, &dv);
   if (rc != HA_OK) return rc;
   if (out_f32 && shape->dtype != HA_BF16) return HA_ERR_DTYPE;
   if (shape->rows == 0 || shape->n_seq == 0) return HA_OK;

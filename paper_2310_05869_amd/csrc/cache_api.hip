@@ -28,8 +28,8 @@ static int rows_call(const void* K, const void* V, const int32_t* slots, const v
   if (rc != HA_OK) return rc;
   if (dtype != HA_BF16 && dtype != HA_FP32) return HA_ERR_DTYPE;
   if (rows < 0 || rows > (1 << 26) || (int64_t)rows * shape->Hk > (1ll << 26)) return HA_ERR_SHAPE;
-  rc = row_strides(kv, shape->Hk, shape->d, dtype, !write, &a.k);
-  if (rc == HA_OK) rc = row_strides(kv ? kv + 1 : nullptr, shape->Hk, shape->d, dtype, !write, &a.v);
+  rc = row_strides(kv, rows, shape->Hk, shape->d, dtype, !write, &a.k);
+  if (rc == HA_OK) rc = row_strides(kv ? kv + 1 : nullptr, rows, shape->Hk, shape->d, dtype, !write, &a.v);
   if (rc != HA_OK) return rc;
   if (rows == 0 || (write && shape->n_pages == 0)) return HA_OK;
   if (!K || !V || !slots || (!cache && shape->n_pages > 0)) return HA_ERR_NULL;
@@ -109,8 +109,9 @@ int ha_cache4_attn(const void* Q, const void* cache, const int32_t* block_table,
   CacheAttnArgs a{};
   int rc = attn_geometry(shape, query, &a);
   if (rc != HA_OK) return rc;
-  rc = row_strides(qo, a.Hq, a.c.d, query->dtype, false, &a.q);
-  if (rc == HA_OK) rc = row_strides(qo ? qo + 1 : nullptr, a.Hq, a.c.d, query->dtype, true, &a.o);
+  const int64_t rows = (int64_t)a.n_seq * a.q_len;
+  rc = row_strides(qo, rows, a.Hq, a.c.d, query->dtype, false, &a.q);
+  if (rc == HA_OK) rc = row_strides(qo ? qo + 1 : nullptr, rows, a.Hq, a.c.d, query->dtype, true, &a.o);
   if (rc != HA_OK) return rc;
   if (a.n_seq == 0) return HA_OK;
   if (!Q || !lens || !out || !lse || !workspace || (!cache && a.c.n_pages > 0) || (!block_table && a.max_blocks > 0)) return HA_ERR_NULL;

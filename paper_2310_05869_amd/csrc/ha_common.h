@@ -209,14 +209,16 @@ inline bool any_misaligned16(P... ptrs) { return (misaligned(ptrs, 16) || ...); 
 template <typename... P>
 inline bool any_misaligned4(P... ptrs) { return (misaligned(ptrs, 4) || ...); }
 
-// Strides of [rows][heads][d] in elements; null: contiguous.  written: heads may not share elements either.
-inline int row_strides(const ha_strides* given, int heads, int d, int dtype, bool written, RowStrides* out) {
+// Strides of [rows][heads][d] in elements; null: contiguous.  written: no two rows of heads may share elements: either the heads of a row lie within the row
+// stride, or the rows of a head within the head stride.
+inline int row_strides(const ha_strides* given, int64_t rows, int heads, int d, int dtype, bool written, RowStrides* out) {
   *out = RowStrides{(int64_t)heads * d, d};
   if (!given) return HA_OK;
   const int64_t unit = dtype == HA_BF16 ? 8 : 4, most = 1ll << 22;
   if (given->row < d || given->head < 0 || given->row > most || given->head > (1ll << 40)) return HA_ERR_SHAPE;
   if (given->row % unit || given->head % unit) return HA_ERR_ALIGN;
   if (written && heads > 1 && given->head < d) return HA_ERR_SHAPE;
+  if (written && heads > 1 && rows > 1 && given->row < (heads - 1) * given->head + d && given->head < (rows - 1) * given->row + d) return HA_ERR_SHAPE;
   *out = RowStrides{given->row, given->head};
   return HA_OK;
 }

@@ -256,6 +256,18 @@ def test_attention_over_pages(ha, torch, dtype, case, tokens):
     assert torch.equal(out, o2) and torch.equal(lse, l2)
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("fp32", 64)])
+def test_attention_of_many_rows_in_few_and_in_many_parts(ha, torch, dtype, d):
+    """More rows than workgroups run at once: a row of few parts is joined by some threads of a workgroup, one of many by all of them."""
+    lens, q_len, Hq, Hk, page = [9000, 900, 0, 2, 1500, 64, 300, 1, 700, 0, 1100, 90, 65, 500], 5, 32, 8, 64
+    rng = np.random.default_rng(31)
+    cache, table, ks, vs = filled_cache(ha, torch, rng, lens, Hk, d, page)
+    Q = torch.from_numpy(2 * d ** -0.25 * rng.standard_normal((len(lens) * q_len, Hq, d))).to(dtypes(torch, dtype)).cuda()
+    out, lse = ha.ha_cache4_attn(Q, cache, table, torch.tensor(lens, dtype=torch.int32, device="cuda"), page, q_len=q_len)
+    ref, rl, absv, werr = attention64(host(Q), ks, vs, q_len)
+    check_attention(host(out), host(lse), ref, rl, absv, werr, dtype, max(lens))
+
+
 @pytest.mark.parametrize("tokens", [0, 4096])
 def test_attention_with_large_scores_and_far_references(ha, torch, tokens):
     """Scores of hundreds, whose largest comes late, in either direction."""

@@ -56,6 +56,12 @@ def test_packed_pointers_strides_and_workspace(ha):
     for bad, status in (((32, 64), SHAPE), ((-64, 64), SHAPE), ((1 << 23, 64), SHAPE), ((256, -8), SHAPE), ((260, 64), ALIGN), ((256, 4), ALIGN)):
         assert forward(ha, st=strides(q=bad)) == status, bad
     assert forward(ha, st=strides(out=(256, 0))) == SHAPE     # heads that share elements may be read, not written
+    # rows of heads that overlap may not be written: 4 heads over 100 rows, head stride within the row's and across it
+    for bad in ((64, 64), (192, 64), (248, 64), (256, 72), (64, 99 * 64)):
+        assert forward(ha, st=strides(out=bad)) == SHAPE and backward(ha, st=strides(dq=bad), nbytes=0) == SHAPE, bad
+    for good in ((256, 64), (264, 64), (64, 6400), (72, 99 * 72 + 64)):
+        assert backward(ha, st=strides(dq=good), nbytes=0) == WORKSPACE, good
+    assert backward(ha, packed(rows=1), strides(dq=(64, 64)), nbytes=0) == WORKSPACE and backward(ha, packed(Hq=1, Hk=1), strides(dq=(64, 0)), nbytes=0) == WORKSPACE
     assert backward(ha, st=strides(dk=(128, 0))) == SHAPE and backward(ha, st=strides(d_out=(8, 64))) == SHAPE
     assert backward(ha, d_out=None) == NULL and backward(ha, ws=None) == NULL and backward(ha, dq=OK + 8) == ALIGN
     need = ha.exact_attn_packed_backward_workspace_bytes(100, 3, 4, 2, 64)
@@ -89,6 +95,8 @@ def test_cache_bytes_and_rows(ha):
     assert write(OK, OK, OK, OK, cache(), 0, 0, None, None) == 0 and write(OK, OK, OK, None, cache(n_pages=0), 4, 0, None, None) == 0
     assert write(OK, OK, OK, OK, cache(), 4, 0, struct.pack("4q", 128, 64, 32, 64), None) == SHAPE
     assert read(OK, OK, OK, OK, cache(), 4, 0, struct.pack("4q", 128, 0, 128, 64), None) == SHAPE
+    assert read(OK, OK, OK, OK, cache(), 4, 0, struct.pack("4q", 64, 64, 128, 64), None) == SHAPE
+    assert write(OK, OK, OK, OK, cache(), 1 << 26, 0, None, None) == SHAPE and write(OK, OK, OK, OK, cache(), (1 << 26) + 1, 0, None, None) == SHAPE
     assert read(OK, OK, OK, OK, cache(), 4, 0, struct.pack("4q", 132, 64, 128, 64), None) == ALIGN
 
 
@@ -114,6 +122,7 @@ def test_cache_attention_pointers_and_workspace(ha):
     assert attn(*[OK] * 6, cache(), query, None, OK, need - 1, None) == WORKSPACE
     assert attn(*[OK] * 6, cache(), query, None, OK + 64, need, None) == WORKSPACE
     assert attn(*[OK] * 6, cache(), query, struct.pack("4q", 256, 64, 256, 32), OK, need, None) == SHAPE
+    assert attn(*[OK] * 6, cache(), query, struct.pack("4q", 256, 64, 128, 64), OK, need, None) == SHAPE
 
 
 def test_plan(ha):
