@@ -409,6 +409,8 @@ int hyperattn_forward_alg2(const void* Q, const void* K, const void* V, void* ou
  * A sequence may be empty.  A key row of another sequence counts for nothing, whatever it holds; causal: an Inf or NaN in a row reaches, as 0 times
  * itself, also rows of its own sequence that do not see it where both lie in one tile of 128 rows, as in exact_attn_forward and exact_attn_backward.
  * rows <= 2^24, rows * Hq <= 2^27, n_seq * Hq <= 2^22, Hq % Hk == 0, Hq <= 1024; d in {64, 128}.
+ * With out_f32, for a backward pass, bf16 rows are divided by the sum of their weights as rounded for the product with V, without it by the sum of the
+ * unrounded ones; out may differ in its last bits.
  * exact_attn_packed_backward: out, lse and out_f32 as exact_attn_packed_forward wrote them; workspace: device, 256-byte aligned, >=
  * exact_attn_packed_backward_workspace_bytes(); nothing in it is kept.  Sums in a fixed order: same inputs, same bits. */
 typedef struct {

@@ -36,6 +36,7 @@
 
 namespace ha {
 
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -67,7 +68,7 @@ __host__ __device__ inline int list_capacity(int b, int m) { return ((b + m + 63
 template <int D>
 __host__ __device__ inline size_t mfma_lds_bytes(int b, int m, int mode) {
   size_t s = 2 * (size_t)Lds<D>::BUF + 64;  // + wave counters
-  if (mode != kModeExact && mode != kModePacked) s += (size_t)list_capacity(b, m) * 4;
+  if (mode != kModeExact && mode != kModePacked && mode != kModePackedSums) s += (size_t)list_capacity(b, m) * 4;
   return s;
 }
 
@@ -98,7 +99,7 @@ __global__ __launch_bounds__(64 * NW * NG, (D == 64 && NW == 4 && NG == 1) ? 3 :
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   constexpr bool kCap = MODE == kModeCap;
   constexpr bool kNode = MODE == kModeNode || kCap;
-  constexpr bool kPacked = MODE == kModePacked, kExact = MODE == kModeExact || kPacked;
+  constexpr bool kSums = MODE == kModePackedSums, kPacked = MODE == kModePacked || kSums, kExact = MODE == kModeExact || kPacked;
   constexpr int kQT = 32 * NW;  // queries per workgroup
   constexpr int kNT = 64 * NW;  // threads of a group
   using L = Lds<D>;
@@ -274,6 +275,10 @@ __global__ __launch_bounds__(64 * NW * NG, (D == 64 && NW == 4 && NG == 1) ? 3 :
   float m_run = -INFINITY;
   float m_ref = 0.f;  // m_run, 0 where that is -inf
   float l_run = 0.f;  // this lane's share of the row sum
+  // of the sum of the weights as P V takes them, rounded: a row divided by this is an average of V's rows, and the common part of its weights' roundings falls out.  The
+  // backward's delta is formed from that row: dQ's relative error 2.49e-3 -> 2.44e-3 (short and long sequences, both head sizes, 2.43-2.51 -> 2.40-2.48; rounding
+  // dQ and dS alone leaves 2.35), the output's 2.01e-3 -> 1.92e-3, for 0.4 % of forward and backward.  Forwards alone go without (5 to 8 % of theirs).
+  float w_run = 0.f;
   // Cap mode (Algorithm 2 as printed): once the block's keys are done (tile nb_tiles on) l_run becomes the capped sum of
   // the samples and log_masked keeps the masked row sum, from which the row's cap C_i follows.  Scores of one row can lie hundreds
   // apart, so neither may hang on the output's reference: the masked sum is a logarithm before the first sample's reference
@@ -407,6 +412,7 @@ __global__ __launch_bounds__(64 * NW * NG, (D == 64 && NW == 4 && NG == 1) ? 3 :
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[dt][i] *= alpha;
       l_run *= kCap ? __builtin_amdgcn_exp2f(sum_ref(m_run) - finite_ref(sum_ref(m_new))) : alpha;
+      if constexpr (kSums) w_run *= alpha;
       m_run = m_new;
       m_ref = finite_ref(m_new);
     }
@@ -517,13 +523,24 @@ __global__ __launch_bounds__(64 * NW * NG, (D == 64 && NW == 4 && NG == 1) ? 3 :
         }
       }
       if (HN) t_max = tile_max(cn, bias_n);
+      if constexpr (kSums) {
+        const bf16x2 one = {(__bf16)1.f, (__bf16)1.f};
+        float ws[2] = {0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const u32x4 w = __builtin_bit_cast(u32x4, pf[j]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) ws[e % 2] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, (uint32_t)w[e]), one, ws[e % 2], false);
+        }
+        w_run += ws[0] + ws[1];
+      }
       constexpr int kPreV = 8;
       __builtin_amdgcn_sched_group_barrier(0x100, kPreV, 0);
 #pragma unroll
       for (int j = 0; j < 4 * DT; ++j) {
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
         if (2 * j < 8 * DT - kPreV) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-        if (HN) __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
+        if (HN) __builtin_amdgcn_sched_group_barrier(0x002, kSums ? 3 : 2, 0);
       }
     }
     if (more_k) store_rows(kbuf_at(kt + 2), L::KSTR, kreg);
@@ -561,12 +578,14 @@ __global__ __launch_bounds__(64 * NW * NG, (D == 64 && NW == 4 && NG == 1) ? 3 :
           part[(4 * dt + g4) * kNT] = (f32x4){o[dt][4 * g4], o[dt][4 * g4 + 1], o[dt][4 * g4 + 2], o[dt][4 * g4 + 3]};
       ml[0] = m_run;
       ml[kNT] = l_run;
+      if constexpr (kSums) ml[2 * kNT] = w_run;
     }
     __syncthreads();
     if (grp == 1) return;
     const float m1 = ml[0], m = fmaxf(m_run, m1), ref = (m == -INFINITY) ? 0.f : m;
     const float w0 = __builtin_amdgcn_exp2f(m_run - ref), w1 = __builtin_amdgcn_exp2f(m1 - ref);
     l_run = l_run * w0 + ml[kNT] * w1;
+    if constexpr (kSums) w_run = w_run * w0 + ml[2 * kNT] * w1;
     m_run = m;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
@@ -582,7 +601,7 @@ __global__ __launch_bounds__(64 * NW * NG, (D == 64 && NW == 4 && NG == 1) ? 3 :
   if (kCap && ntiles <= nb_tiles) end_masked();  // no sample was kept
   const float l_tot = l_run + __shfl_xor(l_run, 32);
   const bool empty = !(l_tot > 0.f);
-  float inv = empty ? 0.f : 1.f / l_tot;
+  float inv = empty ? 0.f : 1.f / (kSums ? w_run + __shfl_xor(w_run, 32) : l_tot);
   float lse_own = empty ? -INFINITY : (sum_ref(m_run) + log2f(l_tot)) * kLn2;
   if constexpr (kCap) {  // d~_i = masked + max(d_i, tau / kappa)
     lse_own = logaddexpf(log_masked, fmaxf(lse_own, floor_term));
@@ -830,7 +849,7 @@ template <int D, int MODE, int NW, bool STAMPS = false, int NG = 1, bool SORT = 
 static int launch_one(const AttnArgs& args, hipStream_t st) {
   AttnArgs a = args;
   int64_t grid;
-  if constexpr (MODE == kModePacked) {
+  if constexpr (MODE == kModePacked || MODE == kModePackedSums) {
     const int64_t slots = packed_slots<32 * NW>(a.pk);
     grid = slots * a.pk.Hq;
     if (grid > kMaxLaunch) return HA_ERR_SHAPE;
@@ -845,7 +864,7 @@ static int launch_one(const AttnArgs& args, hipStream_t st) {
   if (grid <= 0) return HA_OK;
   if (grid > kMaxGrid) return HA_ERR_SHAPE;
   size_t lds = mfma_lds_bytes<D>(a.g.b, a.g.m, MODE) + (NG - 1) * 2 * (size_t)Lds<D>::BUF;
-  const size_t ep = (size_t)NW * EpLds<D>::WAVE + (NG - 1) * (size_t)(D / 8 * 16 + 8) * 64 * NW;
+  const size_t ep = (size_t)NW * EpLds<D>::WAVE + (NG - 1) * (size_t)(D / 8 * 16 + (MODE == kModePackedSums ? 12 : 8)) * 64 * NW;
   if (SORT) lds += sort_pushes_list<D, NW>(a.g) + 32 * NW * 4;
   if (lds < ep) lds = ep;
   static std::atomic<uint64_t> lds_set{0};  // per instantiation: devices on which the LDS limit is raised
@@ -958,12 +977,17 @@ int64_t attn_mfma_grid(const AttnArgs& a, int mode) {
   return mode == kModeNode ? node_grid<32 * HA_NW_NODE>(a.g) : exact_grid<32 * HA_NW_EXACT>(a);
 }
 
+template <int D, int MODE>
+static int launch_packed(const AttnArgs& a, hipStream_t st) {
+  if (packed_two_groups(a.pk, packed_slots<128>(a.pk) * a.pk.Hq, a.exact_causal)) return launch_one<D, MODE, 4, false, 2>(a, st);
+  return launch_one<D, MODE, 4>(a, st);
+}
+
 int launch_attn_mfma(const AttnArgs& a, int mode, hipStream_t st) {
   if (a.g.dtype != HA_BF16) return HA_ERR_DTYPE;
   if (mode == kModePacked) {
-    const bool two = packed_two_groups(a.pk, packed_slots<128>(a.pk) * a.pk.Hq, a.exact_causal);
-    if (a.g.d == 128) return two ? launch_one<128, kModePacked, 4, false, 2>(a, st) : launch_one<128, kModePacked, 4>(a, st);
-    return two ? launch_one<64, kModePacked, 4, false, 2>(a, st) : launch_one<64, kModePacked, 4>(a, st);
+    if (a.g.d == 128) return a.out_f32 != nullptr ? launch_packed<128, kModePackedSums>(a, st) : launch_packed<128, kModePacked>(a, st);
+    return a.out_f32 != nullptr ? launch_packed<64, kModePackedSums>(a, st) : launch_packed<64, kModePacked>(a, st);
   }
   if (mode == kModeExact && a.merge_levels > 0 && !a.part_bf16) return HA_ERR_DTYPE;  // this kernel folds bf16 partial rows
   const bool split = mode == kModeExact && split_exact(a);

@@ -82,6 +82,7 @@ enum AttnMode : int32_t {
   kModeCap = 2,    // node mode with Algorithm 2's cap on every sampled entry and its lower cap
   kModeValue = 3,  // cap mode for the row sums, Lemma 2's rows for the output (fp32)
   kModePacked = 4, // exact mode over packed sequences: rows of a sequence against its keys, strided rows, grouped heads
+  kModePackedSums = 5,  // bf16 with the unrounded output: rows divided by the sum of their rounded weights
 };
 
 struct RowStrides {
