@@ -438,8 +438,9 @@ __global__ __launch_bounds__(64 * NW * NG, (D == 64 && NW == 4 && NG == 1) ? 3 :
     // slice of exponentials per slot), and gives it back for the P V block, whose slots the neighbour's
     // vector work fills: measured -3 % on the causal base case, -2 % on the node launch (any of the
     // neighbouring placements of the two instructions measured the same; priority during P V alone: no gain;
-    // the d = 64 node launch, where vector issue binds, loses 2 % with it and goes without).
-    constexpr bool kPrio = D == 128 || kExact;
+    // the d = 64 node launch, where vector issue binds, loses 2 % with it and goes without; so do packed sequences at d = 64: 16 of up to 2048, 16 heads,
+    // 38.1 -> 36.9 us without, 12 of up to 4096 78 -> 73, one of 16384, 32 heads, 1178 -> 1183; at d = 128 16 of up to 4096 144-147 -> 149, one of 16384 2024 -> 2083).
+    constexpr bool kPrio = D == 128 || MODE == kModeExact;
     bf16x8 pf[4];
     if constexpr (kPrio) __builtin_amdgcn_s_setprio(1);
     if constexpr (kRequestInBlock && HN) {

@@ -111,7 +111,7 @@ inline int64_t bwd_sample_rows(const Geometry& g) {
 // pass: q0 = first KEY row, [k0, k1) = its queries).
 struct BwdWork {
   TileWork w;
-  int seq_start, heads, tiles_per_head;  // packed passes: the sequence's first row; dK / dV: query heads from w.bh on, and T tiles of each
+  int seq_start, heads;         // packed passes: the sequence's first row; dK / dV: query heads from w.bh on
   int chunk_start, chunk_len;   // sampled-key pass: run of sorted query positions
   int samp0;                    // first sample
   int64_t samp_row0;            // row of sample 0 of this (head, node, chunk) in the pass's output
