@@ -721,8 +721,8 @@ def alg2_workspace_views(workspace, shape: HaShape, params: HaParams):
 # ---------------------------------------------------------------- packed sequences
 # Rows [rows, heads, d] may be slices of a larger tensor: their strides go along.  These calls run on the current device: tensors or a stream of another one
 # are refused here.  A tensor that fits costs four comparisons, and the sizes of a call go to the library as packed bytes: host time of a decoding
-# step's calls, whose kernels take 3 to 9 us (MI355X; structures of ctypes, devices compared as objects -> this): two calls for rows 17.4 -> 14.9 us, a plan
-# 10.7 -> 8.1, attention over pages 13.9 -> 12.0, over packed prompts 11.7 -> 8.9.
+# step's calls, whose kernels take 3 to 9 us (MI355X; structures of ctypes, devices compared as objects -> this): two calls for rows 17.4 -> 12.9 us, a plan
+# 10.7 -> 7.6, attention over pages 13.9 -> 8.1, over packed prompts 11.7 -> 8.8, where their kernel binds.
 _PACKED = struct.Struct("7i")
 _PACKED_STRIDES = struct.Struct("16q")
 _STRIDES2 = struct.Struct("4q")
@@ -730,20 +730,41 @@ _CACHE4 = struct.Struct("4i")
 _FIVE = struct.Struct("5i")  # ha_cache4_query, ha_page_plan_shape
 
 
+def _raw_stream(dev):
+    """Handle of the current stream.  (From the second call on torch's own function.)"""
+    global _raw_stream
+    _raw_stream = getattr(_torch()._C, "_cuda_getCurrentRawStream", None) or (lambda d: _torch().cuda.current_stream(d).cuda_stream)
+    return _raw_stream(dev)
+
+
 def _here(t, name, stream):
     """(device, stream handle) of a call on the current device, where t has to be."""
     torch = _torch()
-    dev, here = t.get_device(), torch.cuda.current_device()
+    dev = t.get_device()
+    if dev < 0:
+        raise ValueError(f"{name} must be a device tensor")
+    here = torch._C._cuda_getDevice()   # (a device tensor is there: the runtime is up)
     if dev != here:
-        if dev < 0:
-            raise ValueError(f"{name} must be a device tensor")
         raise ValueError(f"{name} is on cuda:{dev}, the current device is cuda:{here}")
     if stream is None:
-        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        return dev, torch.cuda.current_stream().cuda_stream if raw is None else raw(dev)
+        return dev, _raw_stream(dev)
     if stream.device.index != here:
         raise ValueError(f"the stream is on {stream.device}, the current device is cuda:{here}")
     return dev, stream.cuda_stream
+
+
+_codes = {}  # ha_dtype by dtype
+
+
+def _code(dtype) -> int:
+    code = _codes.get(dtype)
+    if code is None:
+        torch = _torch()
+        _codes.update({torch.bfloat16: HA_BF16, torch.float32: HA_FP32})
+        code = _codes.get(dtype)
+        if code is None:
+            raise TypeError(f"unsupported tensor dtype {dtype}")
+    return code
 
 
 def _misfit(t, name, shape, dtype, dev):
@@ -761,6 +782,13 @@ def _whole(t, name, shape, dtype, dev):
     if t.shape == shape and t.dtype is dtype and t.get_device() == dev and t.is_contiguous():
         return t.data_ptr()
     return _misfit(t, name, shape, dtype, dev)
+
+
+def _bytes(t, name, dev):
+    """Address of a contiguous byte tensor of any shape."""
+    if t.get_device() == dev and t.is_contiguous() and t.dtype is _torch().uint8:
+        return t.data_ptr()
+    return _misfit(t, name, t.shape, _torch().uint8, dev)
 
 
 def _rows(t, name, shape, dtype, dev):
@@ -789,7 +817,7 @@ def _packed_call(Q, K, cu_seqlens, causal):
         raise ValueError(f"cu_seqlens has shape {tuple(cu_seqlens.shape)}, expected [n_seq + 1]")
     rows, Hq, d = Q.shape
     Hk = K.shape[1]
-    return rows, Hq, Hk, d, _PACKED.pack(cu_seqlens.shape[0] - 1, rows, Hq, Hk, d, _dtype_code(Q), 1 if causal else 0)
+    return rows, Hq, Hk, d, _PACKED.pack(cu_seqlens.shape[0] - 1, rows, Hq, Hk, d, _code(Q.dtype), 1 if causal else 0)
 
 
 def exact_attn_packed_forward(Q, K, V, cu_seqlens, causal=False, out=None, lse=None, stream=None, out_f32=None):
@@ -816,7 +844,7 @@ def exact_attn_packed_forward(Q, K, V, cu_seqlens, causal=False, out=None, lse=N
 
 
 def exact_attn_packed_backward_workspace_bytes(rows, n_seq, Hq, Hk, d, dtype=None) -> int:
-    code = HA_BF16 if dtype is None else _dtype_code(_torch().empty((), dtype=dtype))
+    code = HA_BF16 if dtype is None else _code(dtype)
     return int(lib().exact_attn_packed_backward_workspace_bytes(_PACKED.pack(n_seq, rows, Hq, Hk, d, code, 0)))
 
 
@@ -842,7 +870,7 @@ def exact_attn_packed_backward(Q, K, V, cu_seqlens, out, lse, d_out, causal=Fals
     _check(lib().exact_attn_packed_backward(Q.data_ptr(), K.data_ptr(), V.data_ptr(), _whole(cu_seqlens, "cu_seqlens", cu_seqlens.shape, torch.int32, dev),
                                             out.data_ptr(), None if out_f32 is None else _whole(out_f32, "out_f32", full, f32, dev),
                                             _whole(lse, "lse", (Hq, rows), f32, dev), d_out.data_ptr(), dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), shape,
-                                            strides, _whole(workspace, "workspace", workspace.shape, torch.uint8, dev), workspace.numel(), handle),
+                                            strides, _bytes(workspace, "workspace", dev), workspace.numel(), handle),
            "exact_attn_packed_backward")
     return dQ, dK, dV
 
@@ -883,7 +911,7 @@ def ha_cache4_write(K, V, slots, cache, page, stream=None):
     dev, handle = _here(cache, "cache", stream)
     kv = _STRIDES2.pack(*_rows(K, "K", full, dt, dev), *_rows(V, "V", full, dt, dev))
     _check(lib().ha_cache4_write(K.data_ptr(), V.data_ptr(), _whole(slots, "slots", (rows,), torch.int32, dev),
-                                 _whole(cache, "cache", cache.shape, torch.uint8, dev), _CACHE4.pack(*sizes), rows, _dtype_code(K), kv, handle),
+                                 _bytes(cache, "cache", dev), _CACHE4.pack(*sizes), rows, _code(dt), kv, handle),
            "ha_cache4_write")
 
 
@@ -905,13 +933,13 @@ def ha_cache4_read(cache, slots, page, dtype=None, K=None, V=None, stream=None):
     if V is None:
         V = _empty(stream, full, dtype, cache)
     kv = _STRIDES2.pack(*_rows(K, "K", full, dtype, dev), *_rows(V, "V", full, dtype, dev))
-    _check(lib().ha_cache4_read(_whole(cache, "cache", cache.shape, torch.uint8, dev), _whole(slots, "slots", (rows,), torch.int32, dev), K.data_ptr(),
-                                V.data_ptr(), _CACHE4.pack(*sizes), rows, _dtype_code(K), kv, handle), "ha_cache4_read")
+    _check(lib().ha_cache4_read(_bytes(cache, "cache", dev), _whole(slots, "slots", (rows,), torch.int32, dev), K.data_ptr(),
+                                V.data_ptr(), _CACHE4.pack(*sizes), rows, _code(dtype), kv, handle), "ha_cache4_read")
     return K, V
 
 
 def ha_cache4_attn_workspace_bytes(cache, page, n_seq, q_len, Hq, max_blocks, dtype=None) -> int:
-    code = HA_BF16 if dtype is None else _dtype_code(_torch().empty((), dtype=dtype))
+    code = HA_BF16 if dtype is None else _code(dtype)
     return int(lib().ha_cache4_attn_workspace_bytes(_CACHE4.pack(*_cache4(cache, page)), _FIVE.pack(n_seq, q_len, Hq, code, max_blocks)))
 
 
@@ -928,7 +956,7 @@ def ha_cache4_attn(Q, cache, block_table, lens, page, q_len=1, out=None, lse=Non
         raise ValueError(f"Q has {rows} rows, the block table {tuple(block_table.shape)}, q_len is {q_len}")
     n_seq, max_blocks = block_table.shape
     dt, i32 = Q.dtype, torch.int32
-    query = _FIVE.pack(n_seq, q_len, Hq, _dtype_code(Q), max_blocks)
+    query = _FIVE.pack(n_seq, q_len, Hq, _code(Q.dtype), max_blocks)
     dev, handle = _here(cache, "cache", stream)
     if out is None:
         out = _empty(stream, full, dt, Q)
@@ -937,10 +965,10 @@ def ha_cache4_attn(Q, cache, block_table, lens, page, q_len=1, out=None, lse=Non
     qo = _STRIDES2.pack(*_rows(Q, "Q", full, dt, dev), *_rows(out, "out", full, dt, dev))
     if workspace is None:
         workspace = _empty(stream, (int(lib().ha_cache4_attn_workspace_bytes(sizes, query)),), torch.uint8, Q)
-    _check(lib().ha_cache4_attn(Q.data_ptr(), _whole(cache, "cache", cache.shape, torch.uint8, dev),
+    _check(lib().ha_cache4_attn(Q.data_ptr(), _bytes(cache, "cache", dev),
                                 _whole(block_table, "block_table", block_table.shape, i32, dev), _whole(lens, "lens", (n_seq,), i32, dev), out.data_ptr(),
                                 _whole(lse, "lse", (Hq, rows), torch.float32, dev), sizes, query, qo,
-                                _whole(workspace, "workspace", workspace.shape, torch.uint8, dev), workspace.numel(), handle), "ha_cache4_attn")
+                                _bytes(workspace, "workspace", dev), workspace.numel(), handle), "ha_cache4_attn")
     return out, lse
 
 

@@ -39,7 +39,7 @@ constexpr int kCRows = 16;       // query rows of a workgroup
 __device__ inline int seq_len(const CacheAttnArgs& a, int s) { return min(max(a.lens[s], 0), a.max_blocks << a.c.log_page); }
 __device__ inline int seq_units(const CacheAttnArgs& a, int s) { return (seq_len(a, s) + kUnit - 1) / kUnit; }
 // What a sequence takes of the line: its units and what its start and its end cost a workgroup, in units.  (0 / 2 / 4 / 8: 64 sequences of up to 16384 tokens,
-// three queries each, 54 / 51 / 45 / 44 us; 256 of up to 8192 94 / 76 / 69 / 68; lengths alike +-0.)
+// three queries each, 54 / 51 / 45 / 42 us, 12 and 16 44 and 45; 256 of up to 8192 94 / 76 / 69 / 68, since then 62 and with 12 or 16 69; lengths alike +-0.)
 constexpr int kSeqCost = 8;
 __device__ inline int seq_cost(const CacheAttnArgs& a, int s) {
   const int n = seq_units(a, s);
