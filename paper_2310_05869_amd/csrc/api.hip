@@ -654,7 +654,7 @@ static int packed_geometry(const ha_packed* sh, const ha_packed_strides* st, boo
   p.Hq = sh->Hq;
   p.Hk = sh->Hk;
   p.group = sh->Hq / sh->Hk;
-  p.splits = packed_splits(packed_slots<128>(p) * sh->Hk, p.group, sh->dtype);
+  p.splits = packed_splits(packed_slots<128>(p) * sh->Hk, p.group, sh->dtype, p.rows / (p.n_seq > 0 ? p.n_seq : 1));
   const auto strides = [&](const ha_strides* s, int heads, bool written, RowStrides* out) { return row_strides(s, sh->rows, heads, sh->d, sh->dtype, written, out); };
   int rc = strides(st ? &st->q : nullptr, sh->Hq, false, &p.q);
   if (rc == HA_OK) rc = strides(st ? &st->k : nullptr, sh->Hk, false, &p.k);

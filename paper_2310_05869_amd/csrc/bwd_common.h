@@ -281,8 +281,10 @@ inline int64_t bwd_grid(const BwdArgs& a, int mode) {
 // of 128 rows; each has fp32 rows of its own, which a launch of their own adds up.  The fp32 passes have four times as many workgroups where they are few.
 // Forward and backward (MI355X, us), at least 256 / 512 / 1024 workgroups: bf16: 16 and 4 heads, d = 64: 12 of up to 4096 538 / 370 / 310, 20 of up to 8192, d = 128 -
 // / 4046 / 4014; 16 and 2, 2 of 6000 967 / 771 / 736; 32 and 8, d = 128, 4 of 1024 268 / 249 / 258; fp32: 16 and 8, 8 of 500 177 / 206 / 206; 16 and 4, d = 128, 3 of up
-// to 2500 1320 / 1368 / 1365
-inline int packed_splits(int64_t workgroups, int group, int dtype) {
+// to 2500 1320 / 1368 / 1365.  Sequences of a few rows are done before a second launch would be: forward and backward, shared -> not: 5 of 30, 4 and 2 heads, d = 64 25.5 ->
+// 22.2, 5 of 9 25.6 -> 22.3, fp32 27.6 -> 25.0; 40 of up to 60 (average 15), 8 and 2 heads 26.0 -> 25.9; 5 of 60, 16 and 2, d = 128 31.6 -> 42.0
+inline int packed_splits(int64_t workgroups, int group, int dtype, int64_t avg) {
+  if (avg * (group - 1) < 64) return 1;
   int splits = 1;
   for (int k = 1; k <= group; ++k)
     if (group % k == 0) {
