@@ -1126,19 +1126,25 @@ int exact_attn_packed_backward(const void* Q, const void* K, const void* V, cons
   a.O32 = out_f32;
   a.fin1 = dQ;
   p.fin1 = dq;
-  rc = launch_attn_bwd(a, kBwdDqPacked, st);
-  if (rc != HA_OK) return rc;
-  a.fin1 = dK;
-  a.fin2 = dV;
-  p.fin1 = dk;
-  p.fin2 = dv;
+  BwdArgs b = a;  // dK / dV
+  b.fin1 = dK;
+  b.fin2 = dV;
+  b.f.pk.fin1 = dk;
+  b.f.pk.fin2 = dv;
   if (p.splits > 1) {
-    a.out1 = (float*)(w + sp.part1);
-    a.out2 = (float*)(w + sp.part2);
+    b.out1 = (float*)(w + sp.part1);
+    b.out2 = (float*)(w + sp.part2);
   }
-  rc = launch_attn_bwd(a, kBwdDkvPacked, st);
+  if (packed_together(p, shape->dtype, shape->d, shape->causal != 0)) {
+    a.delta_out = nullptr;
+    rc = launch_packed_delta(a, (float*)w, st);
+    if (rc == HA_OK) rc = use_mfma(a.f.g) ? launch_attn_bwd_packed_mfma(a, b, st) : launch_attn_bwd_packed_f32(a, b, st);
+  } else {
+    rc = launch_attn_bwd(a, kBwdDqPacked, st);
+    if (rc == HA_OK) rc = launch_attn_bwd(b, kBwdDkvPacked, st);
+  }
   if (rc != HA_OK || p.splits == 1) return rc;
-  return launch_packed_sum(p, a.out1, a.out2, dK, dV, shape->d, shape->dtype, st);
+  return launch_packed_sum(b.f.pk, b.out1, b.out2, dK, dV, shape->d, shape->dtype, st);
 }
 
 size_t exact_attn_packed_backward_workspace_bytes(const ha_packed* shape) {

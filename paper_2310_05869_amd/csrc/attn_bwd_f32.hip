@@ -605,6 +605,30 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_bwd_f32_shared_kern
   }
 }
 
+template <int D, int RG, int KW>
+__global__ __launch_bounds__(64 * RG * KW, D == 64 ? 2 : 1) void attn_bwd_f32_packed_kernel(BwdPacked m) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  const PackedTurn t = packed_turn((int)blockIdx.x);
+  if (t.dq) {
+    if (t.wg < m.dq_wgs) bwd_f32_pass<D, kBwdDqPacked, RG, KW, false>(m.dq, t.wg, m.dq_wgs, smem);
+  } else if (t.wg < m.dkv_wgs) {
+    bwd_f32_pass<D, kBwdDkvPacked, RG, KW, false>(m.dkv, t.wg, m.dkv_wgs, smem);
+  }
+}
+
+template <int D, int RG, int KW>
+static int launch_bwd_f32_packed_form(const BwdArgs& dq, const BwdArgs& dkv, hipStream_t st) {
+  BwdPacked m;
+  const int64_t grid = set_bwd_packed<32 * RG>(dq, dkv, &m);
+  if (grid > kMaxLaunch) return HA_ERR_SHAPE;
+  m.dq.f.exact_lpt = m.dkv.f.exact_lpt = KW == 8;
+  const size_t lds = F32BwdLds<D, RG, KW>::bytes(m.dq.f.g, kBwdDqPacked), lds2 = F32BwdLds<D, RG, KW>::bytes(m.dkv.f.g, kBwdDkvPacked);
+  static std::atomic<uint64_t> lds_set{0};  // per instantiation: devices on which the LDS limit is raised
+  if (allow_full_lds(reinterpret_cast<const void*>(&attn_bwd_f32_packed_kernel<D, RG, KW>), lds_set) != HA_OK) return HA_ERR_LAUNCH;
+  hipLaunchKernelGGL((attn_bwd_f32_packed_kernel<D, RG, KW>), dim3((unsigned)grid), dim3(64 * RG * KW), lds > lds2 ? lds : lds2, st, m);
+  return check_launch();
+}
+
 template <int D, int MODE, int RG, int KW, bool FINAL>
 static int launch_bwd_f32_form(const BwdArgs& args, int grid, hipStream_t st) {
   BwdArgs a = args;
@@ -759,17 +783,25 @@ static int launch_bwd_f32_d(const BwdArgs& a, int mode, hipStream_t st) {
 
 // Packed sequences: the same, by the average length and an upper bound of the workgroups.  Forward and backward with dQ / dK and dV of one way, of four (MI355X, us;
 // workgroups of 128 rows at most): d = 64: 12 heads, 6 of up to 3000 (576) dQ 845, 810, dK / dV 845, 692; 16 heads, 8 of 500 (624) 206, 221 and 206, 201; d = 128: 16 and 4
-// heads, 3 of up to 2500 (560) 1277, 1363 and 1322, 1362; eight ways: d = 64, 4 heads, 5 of up to 900 (groups of 32 rows: 172) 95.2 -> 91.3 and 86.6
+// heads, 3 of up to 2500 (560) 1277, 1363 and 1322, 1362
 template <int D, int MODE>
 static int launch_bwd_f32_packed(const BwdArgs& a, hipStream_t st) {
   const PackedRows& p = a.f.pk;
   const int64_t avg = p.rows / (p.n_seq > 0 ? p.n_seq : 1), per = MODE == kBwdDqPacked ? p.Hq : p.Hk * p.splits;
   const int64_t grid = packed_slots<128>(p) * per;
-  if constexpr (D == 64)
-    if (avg >= 128 && packed_slots<32>(p) * per <= (!a.f.exact_causal || avg < 512 ? 256 : avg < 2048 ? 384 : 512)) return launch_bwd_f32_one<D, MODE, 1, 8>(a, st);
   const int64_t enough = a.f.exact_causal ? (D == 128 ? 544 : MODE == kBwdDqPacked ? 600 : 1024) : D == 128 ? 208 : 256;
   const bool fits = 3 * ((avg + 127) / 128 * 128) <= 4 * avg;
   return fits && grid >= enough ? launch_bwd_f32_one<D, MODE, 4, 1>(a, st) : launch_bwd_f32_one<D, MODE, 1, 4>(a, st);
+}
+
+// Together (packed_together) there are few workgroups: of 32 rows, and at d = 64 of eight ways where the longest chain is the launch (passes one behind the other, 4 heads,
+// 5 of up to 900, 172 groups of 32 rows, four -> eight ways: dQ 95.2 -> 91.3, dK / dV -> 86.6 us).
+int launch_attn_bwd_packed_f32(const BwdArgs& dq, const BwdArgs& dkv, hipStream_t st) {
+  if (dq.f.g.d == 128) return launch_bwd_f32_packed_form<128, 1, 4>(dq, dkv, st);
+  const PackedRows& p = dkv.f.pk;
+  const int64_t avg = p.rows / (p.n_seq > 0 ? p.n_seq : 1), per = p.Hk * p.splits;
+  if (avg >= 128 && packed_slots<32>(p) * per <= (!dq.f.exact_causal || avg < 512 ? 256 : avg < 2048 ? 384 : 512)) return launch_bwd_f32_packed_form<64, 1, 8>(dq, dkv, st);
+  return launch_bwd_f32_packed_form<64, 1, 4>(dq, dkv, st);
 }
 
 int launch_attn_bwd_f32(const BwdArgs& a, int mode, hipStream_t st) {

@@ -119,10 +119,9 @@ constexpr int bwd_waves_per_simd(int d, int mode) { return d == 64 && mode == kB
 // FINAL: the node passes of an unmasked problem, which write the final gradients.
 // NG = 2 (exact passes): two groups of four waves take the T tiles in turn, each with tile buffers of its own; their sums are
 // added through LDS.
-// FOUR: held to the registers of four waves per SIMD (bwd_four_workgroups).
-template <int D, int MODE, bool FINAL, int NG, bool FOUR>
-__global__ __launch_bounds__(kBNT * NG, FOUR ? 4 : bwd_waves_per_simd(D, MODE)) void attn_bwd_kernel(BwdArgs a) {
-  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+// wg: the workgroup's number among the pass's wgs.
+template <int D, int MODE, bool FINAL, int NG>
+__device__ __forceinline__ void bwd_pass(const BwdArgs& a, const int wg, const int wgs, unsigned char* smem) {
   using L = BwdLds<D>;
   constexpr bool kPacked = MODE == kBwdDqPacked || MODE == kBwdDkvPacked;
   constexpr bool kDqExact = MODE == kBwdDqExact || MODE == kBwdDqPacked, kDkvExact = MODE == kBwdDkvExact || MODE == kBwdDkvPacked;
@@ -150,7 +149,7 @@ __global__ __launch_bounds__(kBNT * NG, FOUR ? 4 : bwd_waves_per_simd(D, MODE)) 
   int32_t* list = scratch + 16;
 
   // ---- which part of the problem this workgroup owns ----
-  const BwdWork b = decode_bwd_work<kRT, MODE>(a, kExact ? (int)blockIdx.x : logical_block(blockIdx.x, gridDim.x), (int)gridDim.x);
+  const BwdWork b = decode_bwd_work<kRT, MODE>(a, kExact ? wg : logical_block(wg, wgs), wgs);
   const TileWork& w = b.w;
 
   if (kPacked && w.rows_valid <= 0) return;
@@ -732,6 +731,25 @@ __global__ __launch_bounds__(kBNT * NG, FOUR ? 4 : bwd_waves_per_simd(D, MODE)) 
   }
 }
 
+// FOUR: held to the registers of four waves per SIMD (bwd_four_workgroups).
+template <int D, int MODE, bool FINAL, int NG, bool FOUR>
+__global__ __launch_bounds__(kBNT * NG, FOUR ? 4 : bwd_waves_per_simd(D, MODE)) void attn_bwd_kernel(BwdArgs a) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  bwd_pass<D, MODE, FINAL, NG>(a, (int)blockIdx.x, (int)gridDim.x, smem);
+}
+
+// dQ and dK / dV of packed sequences side by side, delta being there: eight workgroups of one pass, one per XCD, and eight of the other in turn, each pass's longest first.
+template <int D, int NG>
+__global__ __launch_bounds__(kBNT * NG, 2) void attn_bwd_packed_kernel(BwdPacked m) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  const PackedTurn t = packed_turn((int)blockIdx.x);
+  if (t.dq) {
+    if (t.wg < m.dq_wgs) bwd_pass<D, kBwdDqPacked, false, NG>(m.dq, t.wg, m.dq_wgs, smem);
+  } else if (t.wg < m.dkv_wgs) {
+    bwd_pass<D, kBwdDkvPacked, false, NG>(m.dkv, t.wg, m.dkv_wgs, smem);
+  }
+}
+
 template <int D, int MODE, bool FINAL, int NG, bool FOUR = false>
 static int launch_bwd_form(const BwdArgs& args, int grid, hipStream_t st) {
   BwdArgs a = args;
@@ -780,7 +798,7 @@ static bool bwd_four_workgroups(int grid) { return grid > 768; }
 template <int D, int MODE>
 static int launch_bwd_one(const BwdArgs& a, int grid, hipStream_t st) {
   if (grid <= 0) return HA_OK;
-  if constexpr (MODE == kBwdDqPacked || MODE == kBwdDkvPacked)
+  if constexpr (D == 128 && (MODE == kBwdDqPacked || MODE == kBwdDkvPacked))  // (d = 64: such passes go together)
     if (packed_two_groups(a.f.pk, grid, a.f.exact_causal)) return launch_bwd_form<D, MODE, false, 2>(a, grid, st);
   if constexpr (MODE == kBwdDqExact || MODE == kBwdDkvExact)
     if (split_bwd_exact(a, grid)) return launch_bwd_form<D, MODE, false, 2>(a, grid, st);
@@ -803,6 +821,25 @@ static int launch_bwd_d(const BwdArgs& a, int mode, int grid, hipStream_t st) {
     case kBwdDkvPacked: return launch_bwd_one<D, kBwdDkvPacked>(a, grid, st);
     default: return HA_ERR_SHAPE;
   }
+}
+
+template <int D, int NG>
+static int launch_bwd_packed_form(const BwdPacked& m, int64_t grid, hipStream_t st) {
+  const size_t lds = bwd_lds_bytes<D, NG>(m.dq, kBwdDqPacked), lds2 = bwd_lds_bytes<D, NG>(m.dkv, kBwdDkvPacked);
+  static std::atomic<uint64_t> lds_set{0};  // per instantiation: devices on which the LDS limit is raised
+  if (allow_full_lds(reinterpret_cast<const void*>(&attn_bwd_packed_kernel<D, NG>), lds_set) != HA_OK) return HA_ERR_LAUNCH;
+  hipLaunchKernelGGL((attn_bwd_packed_kernel<D, NG>), dim3((unsigned)grid), dim3(kBNT * NG), lds > lds2 ? lds : lds2, st, m);
+  return check_launch();
+}
+
+int launch_attn_bwd_packed_mfma(const BwdArgs& dq, const BwdArgs& dkv, hipStream_t st) {
+  BwdPacked m;
+  const int64_t grid = set_bwd_packed<kRT>(dq, dkv, &m);
+  if (grid > kMaxLaunch) return HA_ERR_SHAPE;
+  const bool two = packed_two_groups(m.dkv.f.pk, m.dkv_wgs, m.dkv.f.exact_causal);
+  m.dq.f.exact_lpt = m.dkv.f.exact_lpt = two;
+  if (m.dq.f.g.d == 128) return two ? launch_bwd_packed_form<128, 2>(m, grid, st) : launch_bwd_packed_form<128, 1>(m, grid, st);
+  return two ? launch_bwd_packed_form<64, 2>(m, grid, st) : launch_bwd_packed_form<64, 1>(m, grid, st);
 }
 
 int launch_attn_bwd_mfma(const BwdArgs& args, int mode, hipStream_t st) {

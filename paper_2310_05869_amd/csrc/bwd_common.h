@@ -295,6 +295,45 @@ inline int packed_splits(int64_t workgroups, int group, int dtype, int64_t avg) 
 }
 int launch_packed_sum(const PackedRows& p, const float* part1, const float* part2, void* out1, void* out2, int d, int dtype, hipStream_t st);
 
+// dQ and dK / dV of packed sequences in one launch, behind a small one for delta, which the dQ pass otherwise forms on its way: where the passes leave the chip
+// half empty, by the workgroups of dQ (128 rows, at most) and the average length.  Forward and backward, one behind the other -> together (MI355X, us; [workgroups, average]):
+//   bf16, d = 64: 10 sequences of 120, 12 heads [228, 119] 25.8 -> 23.0, 16 of up to 400, 12 and 2 heads 47.7 -> 38.2, 60 of up to 250 [712, 63] 37.6 -> 34.2, 12 of up to 4096 [1120, 625] 303 ->
+//     290, one of 6000 [768] 421 -> 403, 10 of up to 2048 unmasked 138 -> 131; 16 of 900 [2048, 899] 234 -> 250; 5 of 9 and of 60 [20, 56] 20.4 -> 22.3, 23.1 -> 25.9
+//   d = 128: 2 of 2000 [264, 1999] 154 -> 129, 8 of 900 [768, 899] 199 -> 191, 30 of up to 500 [992, 138] 120 -> 116; 30 of up to 1000 [1440, 259] 232 -> 238, 16 of up to 4096 [1092, 604]
+//     438 -> 439; one of 4000 [512] 348 -> 365; unmasked, 6 of up to 2000 [456, 684] 275 -> 260, of up to 4000 [828, 1351] 866 -> 892
+//   fp32: d = 64: 5 of up to 900 [60, 265] 80.7 -> 66.1, 8 of up to 200 [100] 42.7 -> 35.2, 12 of up to 700 [224, 172] 87 -> 89, 8 of 900 [512, 899] 279 -> 375; d = 128: 8 of up to 900 [200, 281] 213 ->
+//     206, 4 of 900 [256] 342 -> 348
+inline bool packed_together(const PackedRows& p, int dtype, int d, bool causal) {
+  const int64_t workgroups = packed_slots<128>(p) * p.Hq, avg = p.rows / (p.n_seq > 0 ? p.n_seq : 1);
+  if (dtype != HA_BF16) return workgroups <= 160;
+  if (d == 64) return workgroups <= 1280 && (workgroups >= 64 || avg >= 64);
+  return workgroups <= 1024 && avg < (causal ? 2048 : 1024);
+}
+struct BwdPacked {
+  BwdArgs dq, dkv;
+  int32_t dq_wgs, dkv_wgs;
+};
+struct PackedTurn {
+  bool dq;
+  int wg;
+};
+__device__ inline PackedTurn packed_turn(int wg) { return PackedTurn{(wg & 8) != 0, (wg >> 4) * 8 + (wg & 7)}; }
+template <int QT>
+inline int64_t set_bwd_packed(const BwdArgs& dq, const BwdArgs& dkv, BwdPacked* m) {  // the launch's workgroups
+  m->dq = dq;
+  m->dkv = dkv;
+  const int64_t slots = packed_slots<QT>(dq.f.pk), a = slots * dq.f.pk.Hq, b = slots * dkv.f.pk.Hk * dkv.f.pk.splits, most = a > b ? a : b;
+  if (most > kMaxLaunch) return most;
+  m->dq.f.pk.slots = m->dkv.f.pk.slots = (int32_t)slots;
+  m->dq_wgs = (int32_t)a;
+  m->dkv_wgs = (int32_t)b;
+  set_packed_divs(m->dq.f, dq.f.pk.group);
+  set_packed_divs(m->dkv.f, dkv.f.pk.splits);
+  return (most + 7) / 8 * 16;
+}
+int launch_attn_bwd_packed_mfma(const BwdArgs& dq, const BwdArgs& dkv, hipStream_t st);
+int launch_attn_bwd_packed_f32(const BwdArgs& dq, const BwdArgs& dkv, hipStream_t st);
+int launch_packed_delta(const BwdArgs& a, float* delta, hipStream_t st);
 int launch_attn_bwd_mfma(const BwdArgs& a, int mode, hipStream_t st);  // bf16 tensors
 int launch_attn_bwd_f32(const BwdArgs& a, int mode, hipStream_t st);   // fp32 tensors
 // Passes of an fp32 causal problem that do not wait for each other, in one launch: the base case's dK / dV and dQ with the

@@ -270,6 +270,63 @@ int launch_bwd_sample_reduce(const BwdArgs& a, float* samp_k, float* samp_v, hip
   return check_launch();
 }
 
+// delta of packed sequences' rows, [Hq][rows], for the passes that do not form it themselves.
+template <int D, bool F32>
+__global__ __launch_bounds__(256) void packed_delta_kernel(PackedRows p, const void* O, const float* O32, const void* G, float* delta) {
+  constexpr int LPR = D / 8;  // lanes per row of a head, eight values each
+  const int first = min(max(p.cu[0], 0), p.rows), end = min(max(p.cu[p.n_seq], first), p.rows);
+  const int64_t unit = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const uint32_t rh = (uint32_t)(unit / LPR);
+  const int ch = (int)(unit % LPR) * 8, head = (int)(rh / (uint32_t)p.rows), row = (int)(rh - (uint32_t)head * (uint32_t)p.rows);
+  const bool live = head < p.Hq && row >= first && row < end;
+  float s = 0.f;
+  if (live) {
+    const int64_t at_g = row * p.d_o.row + head * p.d_o.head + ch, at_o = row * p.o.row + head * p.o.head + ch;
+    f32x4 o[2], g[2];
+    if constexpr (F32) {
+      const f32x4* op = reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(O) + at_o);
+      const f32x4* gp = reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(G) + at_g);
+      o[0] = op[0], o[1] = op[1], g[0] = gp[0], g[1] = gp[1];
+    } else {
+      auto wide = [](u32x4 x, f32x4 (&y)[2]) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          y[e / 2][2 * (e % 2)] = __uint_as_float(x[e] << 16);
+          y[e / 2][2 * (e % 2) + 1] = __uint_as_float(x[e] & 0xFFFF0000u);
+        }
+      };
+      wide(*reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(G) + at_g), g);
+      if (O32 != nullptr) {
+        const f32x4* op = reinterpret_cast<const f32x4*>(O32 + ((int64_t)row * p.Hq + head) * D + ch);
+        o[0] = op[0], o[1] = op[1];
+      } else {
+        wide(*reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(O) + at_o), o);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s = __builtin_fmaf(o[e / 4][e % 4], g[e / 4][e % 4], s);
+  }
+#pragma unroll
+  for (int off = LPR / 2; off >= 1; off >>= 1) s += __shfl_xor(s, off);
+  if (live && ch == 0) delta[(int64_t)head * p.rows + row] = s;
+}
+
+int launch_packed_delta(const BwdArgs& a, float* delta, hipStream_t st) {
+  const PackedRows& p = a.f.pk;
+  const int d = a.f.g.d;
+  const int64_t wgs = ((int64_t)p.rows * p.Hq * (d / 8) + 255) / 256;
+  if (wgs > kMaxLaunch) return HA_ERR_SHAPE;
+  const dim3 grid((unsigned)wgs);
+  if (a.f.g.dtype == HA_BF16) {
+    if (d == 128) hipLaunchKernelGGL((packed_delta_kernel<128, false>), grid, dim3(256), 0, st, p, a.O, a.O32, a.dO, delta);
+    else hipLaunchKernelGGL((packed_delta_kernel<64, false>), grid, dim3(256), 0, st, p, a.O, a.O32, a.dO, delta);
+  } else {
+    if (d == 128) hipLaunchKernelGGL((packed_delta_kernel<128, true>), grid, dim3(256), 0, st, p, a.O, a.O32, a.dO, delta);
+    else hipLaunchKernelGGL((packed_delta_kernel<64, true>), grid, dim3(256), 0, st, p, a.O, a.O32, a.dO, delta);
+  }
+  return check_launch();
+}
+
 // Packed dK / dV of key heads whose query heads were shared among workgroups: the parts of a row added up in order, into the tensors' dtype.  Rows of no sequence
 // have no parts and are left alone.
 template <int D, bool F32>

@@ -115,6 +115,10 @@ CASES = [
     ([1500], 8, 8, 64, 5),           # heads in eights: a head's tiles on one XCD
     ([300] * 9 + [0] * 70 + [17], 8, 1, 64, 0),   # more sequences than lanes
     ([2100, 40], 4, 2, 128, 0),
+    # the gradients' passes one behind the other: long rows at d = 128, and many workgroups of either type
+    ([2300], 4, 2, 128, 0),
+    ([400] * 6 + [90], 16, 4, 128, 2),
+    ([300] * 12, 32, 8, 128, 0),
 ]
 
 
