@@ -50,7 +50,13 @@ __device__ inline int seq_cost(const CacheAttnArgs& a, int s) {
 __device__ inline int line_total(const CacheAttnArgs& a, int lane, int* before) {
   const int each = (a.n_seq + 63) / 64, s0 = min(a.n_seq, lane * each), s1 = min(a.n_seq, s0 + each);
   int sum = 0;
-  for (int s = s0; s < s1; ++s) sum += seq_cost(a, s);
+  for (int s = s0; s < s1; s += 4) {  // (four lengths asked for at a time: 1000 sequences of up to 4096 52.2 -> 51.2 us)
+    int cost[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) cost[i] = seq_cost(a, min(s + i, s1 - 1));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum += s + i < s1 ? cost[i] : 0;
+  }
   int inc = sum;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
