@@ -301,11 +301,12 @@ int launch_packed_sum(const PackedRows& p, const float* part1, const float* part
 //     290, one of 6000 [768] 421 -> 403, 10 of up to 2048 unmasked 138 -> 131; 16 of 900 [2048, 899] 234 -> 250; 5 of 9 and of 60 [20, 56] 20.4 -> 22.3, 23.1 -> 25.9
 //   d = 128: 2 of 2000 [264, 1999] 154 -> 129, 8 of 900 [768, 899] 199 -> 191, 30 of up to 500 [992, 138] 120 -> 116; 30 of up to 1000 [1440, 259] 232 -> 238, 16 of up to 4096 [1092, 604]
 //     438 -> 439; one of 4000 [512] 348 -> 365; unmasked, 6 of up to 2000 [456, 684] 275 -> 260, of up to 4000 [828, 1351] 866 -> 892
-//   fp32: d = 64: 5 of up to 900 [60, 265] 80.7 -> 66.1, 8 of up to 200 [100] 42.7 -> 35.2, 12 of up to 700 [224, 172] 87 -> 89, 8 of 900 [512, 899] 279 -> 375; d = 128: 8 of up to 900 [200, 281] 213 ->
+//   fp32: d = 64: 5 of up to 900 [60, 265] 80.7 -> 66.1, 8 of up to 200 [100] 42.7 -> 35.2, 12 of up to 700 [224, 172] 87 -> 89, 8 of 900 [512, 899] 279 -> 375, 20 of 30 [192] 27.4 -> 22.5, 40 of 64
+//     [472] 47.1 -> 47.3; d = 128: 20 of 64 [232] 79.6 -> 65.2, 8 of up to 900 [200, 281] 213 ->
 //     206, 4 of 900 [256] 342 -> 348
 inline bool packed_together(const PackedRows& p, int dtype, int d, bool causal) {
   const int64_t workgroups = packed_slots<128>(p) * p.Hq, avg = p.rows / (p.n_seq > 0 ? p.n_seq : 1);
-  if (dtype != HA_BF16) return workgroups <= 160;
+  if (dtype != HA_BF16) return workgroups <= (avg <= 64 ? 256 : 160);
   if (d == 64) return workgroups <= 1280 && (workgroups >= 64 || avg >= 64);
   return workgroups <= 1024 && avg < (causal ? 2048 : 1024);
 }
