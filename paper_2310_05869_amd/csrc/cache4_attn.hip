@@ -559,7 +559,7 @@ static int cache4_whole(const CacheAttnArgs& a) {
 }
 
 // Codes that are read once and more of which may come than the last cache holds are read past the caches: 4 sequences of 131072 tokens 114 -> 103 us, 256 of up to
-// 8192 68 -> 64, 64 of 4096, d = 64 74 -> 73; where they would have stayed from one call to the next, 64 of up to 16384 (145 MB) 43.2 -> 44.3.
+// 8192 68 -> 64, 64 of 4096, d = 64 74 -> 73; where they would have stayed from one call to the next, 64 of up to 16384 (145 MB) 39.8 -> 42.0.
 static bool cache4_once(const CacheAttnArgs& a) {
   return a.tiles == 1 && (int64_t)a.n_seq * a.max_blocks * a.c.Hk * a.c.block_bytes() > (256ll << 20);
 }
