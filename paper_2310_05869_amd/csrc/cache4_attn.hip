@@ -24,6 +24,7 @@ namespace ha {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
@@ -34,6 +35,8 @@ constexpr int kMostParts = 768;  // workgroups of four waves that the chip holds
 constexpr int kUnit = 64;        // tokens of a wave's step
 constexpr int kTilesPerUnit = 4; // of 16 tokens
 constexpr int kCRows = 16;       // query rows of a workgroup
+// V's scales from here on are taken by the rows that see the token alone: 4 times 2^126 and 2 times 2^127 are infinite, 255 is NaN, and 0 times either is NaN.
+constexpr uint32_t kFarScale = 253, kFarSteps = 256 - kFarScale;
 
 // Units of all sequences before s (exclusive), found by one wave: lane l sums a run of sequences.
 __device__ inline int seq_len(const CacheAttnArgs& a, int s) { return min(max(a.lens[s], 0), a.max_blocks << a.c.log_page); }
@@ -175,7 +178,7 @@ __global__ __launch_bounds__(64 * NW, SPLIT == 1 && NW == 4 ? 3 : 2) void cache4
     // reference of the exponentials, moved (and the sums rescaled) where a row's scores exceed it by more than 8; log2 domain for bf16
     // queries, natural for fp32 ones; l: this lane's share of the row sum
     float m = -INFINITY, l = 0.f;
-    bool some_nan = false;  // (wave-uniform) a group was taken out
+    bool some_taken = false;  // (wave-uniform) a group was taken out
     constexpr float unit_of = F32 ? 2.f : kLog2e;
     auto fetch = [](const auto* p) { return ONCE ? __builtin_nontemporal_load(p) : *p; };
     int page_of[kTilesPerUnit];
@@ -268,7 +271,7 @@ __global__ __launch_bounds__(64 * NW, SPLIT == 1 && NW == 4 ? 3 : 2) void cache4
 #pragma unroll
       for (int t = 0; t < kTilesPerUnit; ++t) special = special || !there[t];
       if (special) {
-        uint32_t nan = 0;
+        uint32_t taken = 0;
 #pragma unroll
         for (int t = 0; t < kTilesPerUnit; ++t)
 #pragma unroll
@@ -280,15 +283,15 @@ __global__ __launch_bounds__(64 * NW, SPLIT == 1 && NW == 4 ? 3 : 2) void cache4
               if (D == 128) raw[t].vs[i % (D / 32)] = 0;
               else raw[t].vs[i / 2] &= i & 1 ? 0x0000ffffu : 0xffff0000u;
             }
-            if constexpr (MULTI) {  // groups that are NaN, of tokens that some rows see alone, are taken out here, for the rows that do not
+            if constexpr (MULTI) {  // groups that are NaN or may lie past the largest number, of tokens that some rows see alone, are taken out here
               uint32_t& w = raw[t].vs[D == 128 ? i % (D / 32) : i / 2];
               const uint32_t bytes = D == 128 ? 0x01010101u : i & 1 ? 0x01010000u : 0x00000101u;
-              const uint32_t full = (((w & 0x7f7f7f7fu) + 0x01010101u) & w) >> 7 & (tok >= all_see ? bytes : 0u);  // 1 in every byte that is 255
-              w &= ~((full << 8) - full);
-              nan |= full;
+              const uint32_t far = (((w & 0x7f7f7f7fu) + kFarSteps * 0x01010101u) & w) >> 7 & (tok >= all_see ? bytes : 0u);  // 1 in every byte from kFarScale on
+              w &= ~((far << 8) - far);
+              taken |= far;
             }
           }
-        if (MULTI && __any(nan != 0)) some_nan = true;
+        if (MULTI && __any(taken != 0)) some_taken = true;
       }
 
       // Whole quads, here: left to itself the compiler (ROCm 7.2) took the first word of one early and gave the other three's registers to the exponentials
@@ -386,15 +389,63 @@ __global__ __launch_bounds__(64 * NW, SPLIT == 1 && NW == 4 ? 3 : 2) void cache4
     // ---- the waves' sums through LDS.  Lane (r, kq), register i of o[2 g + e]: query row r, channel 32 g + 8 kq + 2 i + e ----
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
-    if (MULTI && some_nan) {  // rare: the tokens again, for the rows that see them
-      for (int tok = max(all_see, 0); tok < len; ++tok) {
-        const int p = blocks[tok >> log_page];
-        if ((unsigned)p >= (unsigned)a.c.n_pages || tok >= limit) continue;
-        const unsigned char* scales = head_base + (int64_t)p * page_bytes + a.c.v_scale_at() + (tok & in_page) * G;
+    if (MULTI && some_taken) {  // rare: these groups of the wave's own tokens, for the rows that see them
+      // (all that this needs beside m and o is formed again, the query read again: kept, it would take registers from the loop)
+      int thread = threadIdx.x;
+      asm volatile("" : "+v"(thread));
+      const int quad = (thread & 63) >> 4, own_row = tile * kCRows + (thread & 15), own = own_row < a.rows ? own_row : 0, own_tok = own / a.group;
+      const int64_t q_at = ((int64_t)s * a.q_len + own_tok) * a.q.row + (int64_t)(hk * a.group + own % a.group) * a.q.head + 8 * quad;
+      for (int u = first + wave; u < last; u += kCWaves)
+        for (int tok = max(u * kUnit, max(all_see, 0)); tok < min(u * kUnit + kUnit, len); ++tok) {
+          const int page = blocks[tok >> log_page], at = tok & in_page;
+          if ((unsigned)page >= (unsigned)a.c.n_pages) continue;
+          const unsigned char* b = head_base + (int64_t)page * page_bytes;
+          const unsigned char* k_scales = b + a.c.k_scale_at() + at * G;
+          const unsigned char* v_scales = b + a.c.v_scale_at() + at * G;
+          bool any = false;
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
-          if (scales[i / 2] == 255) o[i] = (f32x4){NAN, NAN, NAN, NAN};
-      }
+          for (int g = 0; g < G; ++g) any = any || v_scales[g] >= kFarScale;
+          if (!any) continue;
+          auto two = [](uint32_t w, uint32_t byte, auto sel) {
+            return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, __uint_as_float(byte << 23), decltype(sel)::value);
+          };
+          float score = 0.f;
+          auto add = [&](int c, f32x2 k) {
+            f32x2 x;
+            if constexpr (F32) {
+              x = *reinterpret_cast<const f32x2*>(reinterpret_cast<const float*>(a.Q) + q_at + c);
+            } else {
+              const uint32_t w = *reinterpret_cast<const uint32_t*>(reinterpret_cast<const uint16_t*>(a.Q) + q_at + c);
+              x = (f32x2){__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)};
+            }
+            score = __builtin_fmaf(x[1], k[1], __builtin_fmaf(x[0], k[0], score));
+          };
+#pragma unroll 1
+          for (int g = 0; g < G; ++g) {
+            const uint32_t w = *reinterpret_cast<const uint32_t*>(b + at * (D / 2) + quad * (D / 8) + 4 * g), byte = k_scales[g];
+            add(32 * g, two(w, byte, std::integral_constant<int, 0>{}));
+            add(32 * g + 2, two(w, byte, std::integral_constant<int, 1>{}));
+            add(32 * g + 4, two(w, byte, std::integral_constant<int, 2>{}));
+            add(32 * g + 6, two(w, byte, std::integral_constant<int, 3>{}));
+          }
+          score += __shfl_xor(score, 16);
+          score += __shfl_xor(score, 32);
+          const float ref = m == -INFINITY ? 0.f : m;
+          const float weight = F32 ? expf(score - ref) : (float)(__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(score, kLog2e, -ref));
+          const unsigned char* v_row = b + a.c.v_at() + (at >> 2) * (D * 2) + (at & 3) * 4;
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            if (v_scales[g] < kFarScale || tok >= all_see + own_tok) continue;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {  // channels 32 g + 8 quad + 2 i and the next
+              const int pair = 4 * quad + i, word = D == 128 ? pair : pair / 2, byte = D == 128 ? g : 2 * g + i % 2;
+              const uint32_t w = *reinterpret_cast<const uint32_t*>(v_row + word * 16) >> (8 * byte);
+              const f32x2 v = two(w, v_scales[g], std::integral_constant<int, 0>{});
+              o[2 * g][i] = __builtin_fmaf(weight, v[0], o[2 * g][i]);
+              o[2 * g + 1][i] = __builtin_fmaf(weight, v[1], o[2 * g + 1][i]);
+            }
+          }
+        }
     }
     if (kq == 0) {
       merge_m[wave][r] = m;
