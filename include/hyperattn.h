@@ -489,6 +489,11 @@ int ha_cache4_attn(const void* Q, const void* cache, const int32_t* block_table,
                    size_t workspace_bytes, void* stream);
 size_t ha_cache4_attn_workspace_bytes(const ha_cache4* shape, const ha_cache4_query* query); /* 0 if not valid */
 
+/* Host only.  Which form of its launch ha_cache4_attn takes for these sizes (tests, measurements): *whole_waves is 8 or 4 where a workgroup of so many waves
+ * takes a whole sequence, 0 where the tokens are shared out and a second launch joins their parts; *past_caches 1 if the latter reads codes past the caches.  The rules
+ * know the table's room, not the lengths: only tables of at most 2048 tokens have the first, so max_blocks is best kept near the step's longest sequence. */
+int ha_cache4_attn_form(const ha_cache4* shape, const ha_cache4_query* query, int32_t* whole_waves, int32_t* past_caches);
+
 /* Block tables and slots, on the GPU from the sequences' lengths: one launch before a step's rows are written.
  *   lens[s]   tokens that sequence s holds, in pages block_table[s][0 ... ceil(lens / page) - 1]
  *   add[s]    >= 0: rows that the step appends to it; < 0: it has ended, its pages are free again

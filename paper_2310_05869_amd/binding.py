@@ -105,6 +105,7 @@ _SIGNATURES = {
     "ha_cache4_read": (c_int, [c_void_p] * 4 + [c_void_p, c_int32, c_int32, c_void_p, c_void_p]),
     "ha_cache4_attn": (c_int, [c_void_p] * 6 + [c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
     "ha_cache4_attn_workspace_bytes": (c_size_t, [c_void_p, c_void_p]),
+    "ha_cache4_attn_form": (c_int, [c_void_p, c_void_p, POINTER(c_int32), POINTER(c_int32)]),
     "ha_page_plan": (c_int, [c_void_p] * 9 + [c_void_p, c_void_p]),
     "ha_measure_mfma_rate": (c_int, [c_void_p, c_size_t, c_int32, POINTER(c_float), c_void_p]),
     "ha_measure_hbm_rate": (c_int, [c_void_p, c_size_t, POINTER(c_float), POINTER(c_float), c_void_p]),
@@ -941,6 +942,15 @@ def ha_cache4_read(cache, slots, page, dtype=None, K=None, V=None, stream=None):
 def ha_cache4_attn_workspace_bytes(cache, page, n_seq, q_len, Hq, max_blocks, dtype=None) -> int:
     code = HA_BF16 if dtype is None else _code(dtype)
     return int(lib().ha_cache4_attn_workspace_bytes(_CACHE4.pack(*_cache4(cache, page)), _FIVE.pack(n_seq, q_len, Hq, code, max_blocks)))
+
+
+def ha_cache4_attn_form(n_pages, page, Hk, d, n_seq, q_len, Hq, max_blocks, dtype=None):
+    """(waves of a workgroup that takes a whole sequence, or 0; whether codes are read past the caches) of a call of these sizes."""
+    code = HA_BF16 if dtype is None else _code(dtype)
+    waves, past = c_int32(0), c_int32(0)
+    _check(lib().ha_cache4_attn_form(_CACHE4.pack(n_pages, page, Hk, d), _FIVE.pack(n_seq, q_len, Hq, code, max_blocks), ctypes.byref(waves), ctypes.byref(past)),
+           "ha_cache4_attn_form")
+    return int(waves.value), bool(past.value)
 
 
 def ha_cache4_attn(Q, cache, block_table, lens, page, q_len=1, out=None, lse=None, workspace=None, stream=None):

@@ -603,15 +603,18 @@ __global__ __launch_bounds__(kJoinThreads) void cache4_join_kernel(CacheAttnArgs
 // Up to 2048 tokens from 64 workgroups on.  Shared out -> whole (MI355X, us; [workgroups]): one sequence of 777 tokens, 4 key heads, d = 64 [4] 11.2 -> 8.6; 8 of
 // 1024 [64] 11.1 -> 9.0; tables of 2048: 32 sequences, 8 key heads, d = 128 [256] 21.4 -> 16.0, but one [8] 11.2 -> 12.4; 60 of 2048, d = 64, fp32 [480] 39.8 -> 26.2;
 // 256 of up to 2048 [2048] 34.4 -> 38.8.  Eight waves -> four: 200 of up to 500, four queries each [1600] 28.7 -> 16.1; 32 of 2048 [256] 16.0 -> 18.8
-static int cache4_whole(const CacheAttnArgs& a) {
+int cache4_whole(const CacheAttnArgs& a) {
   const int64_t tokens = (int64_t)a.max_blocks * a.c.page, wgs = (int64_t)a.n_seq * a.c.Hk * a.tiles;
   if (tokens > 1024 && (tokens > 2048 || wgs < 64 || wgs > 512)) return 0;
   return wgs > 256 ? 4 : 8;
 }
 
-// Codes that are read once and more of which may come than the last cache holds are read past the caches: 4 sequences of 131072 tokens 114 -> 103 us, 256 of up to
-// 8192 68 -> 64, 64 of 4096, d = 64 74 -> 73; where they would have stayed from one call to the next, 64 of up to 16384 (145 MB) 39.8 -> 42.0.
-static bool cache4_once(const CacheAttnArgs& a) {
+// Codes that are read once are read past the caches where the table has room for more of them than the last cache holds.  Between two calls over the same pages a program's
+// other layers read theirs, so codes come from memory; without the detour through the caches they come sooner, however many of the table's entries are used (tables
+// of 131072 tokens, states of 79 to 307 MB in turn: 64 sequences of up to 2000 29.5 -> 26.9 us, 16 of up to 16384 38.9 -> 35.2, 64 of up to 8000 62.2 +-0.6; of up to 32768: 256 of
+// up to 1000 49.0 -> 45.3; 64 of up to 16384, three queries each 44.6 -> 42.2; 4 of 131072 114 -> 103).  The price is paid where one call's codes, up to 160 MB, are still
+// there for the next: the same, same state: 26.7 -> 28.0, 34.3 -> 37.2, 41.4 -> 45.3, 39.8 -> 42.0; a small program, whose table has no room for more, goes without.
+bool cache4_once(const CacheAttnArgs& a) {
   return a.tiles == 1 && (int64_t)a.n_seq * a.max_blocks * a.c.Hk * a.c.block_bytes() > (256ll << 20);
 }
 

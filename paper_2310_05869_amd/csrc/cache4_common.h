@@ -56,6 +56,8 @@ struct CacheAttnArgs {
 };
 int launch_cache4_attn(const CacheAttnArgs& a, int dtype, hipStream_t st);
 int cache4_parts(int Hk, int tiles);
+int cache4_whole(const CacheAttnArgs& a);   // waves of a workgroup that takes a whole sequence, 0: tokens are shared out
+bool cache4_once(const CacheAttnArgs& a);   // of shared-out tokens: codes are read past the caches
 
 struct PagePlanArgs {
   const int32_t* lens;

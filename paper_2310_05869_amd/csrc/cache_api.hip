@@ -103,6 +103,17 @@ size_t ha_cache4_attn_workspace_bytes(const ha_cache4* shape, const ha_cache4_qu
   return attn_geometry(shape, query, &a) == HA_OK ? attn_space(a).total : 0;
 }
 
+int ha_cache4_attn_form(const ha_cache4* shape, const ha_cache4_query* query, int32_t* whole_waves, int32_t* past_caches) {
+  if (!whole_waves || !past_caches) return HA_ERR_NULL;
+  CacheAttnArgs a{};
+  const int rc = attn_geometry(shape, query, &a);
+  if (rc != HA_OK) return rc;
+  if (a.c.n_pages == 0) a.max_blocks = 0;
+  *whole_waves = cache4_whole(a);
+  *past_caches = *whole_waves == 0 && cache4_once(a);
+  return HA_OK;
+}
+
 int ha_cache4_attn(const void* Q, const void* cache, const int32_t* block_table, const int32_t* lens, void* out, float* lse,
                    const ha_cache4* shape, const ha_cache4_query* query, const ha_strides* qo, void* workspace, size_t workspace_bytes,
                    void* stream) {
