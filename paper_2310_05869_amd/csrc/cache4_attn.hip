@@ -294,11 +294,6 @@ __global__ __launch_bounds__(64 * NW, SPLIT == 1 && NW == 4 ? 3 : 2) void cache4
         if (MULTI && __any(taken != 0)) some_taken = true;
       }
 
-      // Whole quads, here: left to itself the compiler (ROCm 7.2) took the first word of one early and gave the other three's registers to the exponentials
-      // (d = 64, eight waves: wrong sums; the tests of both forms hold it).
-#pragma unroll
-      for (int t = 0; t < kTilesPerUnit; ++t) asm volatile("" : "+v"(raw[t].v));
-
       // ---- weights ----
       float mx = fmaxf(fmaxf(c[0][0], c[0][1]), fmaxf(c[0][2], c[0][3]));
 #pragma unroll

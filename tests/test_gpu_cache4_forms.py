@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 from ha_testutil import have_gpu
-from test_gpu_cache4 import STEPS, attention64, dtypes, filled_cache, ha, host, torch  # noqa: F401  (ha and torch: fixtures)
+from test_gpu_cache4 import STEPS, attention64, check_attention, dtypes, filled_cache, ha, host, torch  # noqa: F401  (ha and torch: fixtures)
 
 pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not have_gpu(), reason="needs a GPU")]
 
@@ -76,3 +76,51 @@ def test_the_largest_scales_count_for_the_queries_that_see_them(ha, torch, d, dt
     tol = (absv * (half + werr[..., None] + 2.0 ** -24 * max(lens)) + half * np.abs(ref)).reshape(got.shape)
     err = np.abs(np.where(infinite, 0, got - ref.reshape(got.shape)))
     assert (err[~infinite] <= tol[~infinite]).all(), np.max(err[~infinite] / tol[~infinite])
+
+
+# name: (waves of a workgroup that takes a whole sequence, codes past the caches), lens, key heads, page, tokens of the table at least
+RAGGED = [0, 1, 300, 64, 65, 129, 0, 1000, 17, 2, 511]
+FORMS = {
+    "whole, eight waves": ((8, False), RAGGED, 2, 16, 0),
+    "whole, four waves": ((4, False), RAGGED * 12, 2, 16, 0),
+    "shared": ((0, False), [0, 5000, 1, 777, 130, 6], 2, 64, 6000),
+    "shared, past the caches": ((0, True), [0, 5000, 1, 777, 130, 6], 8, 256, 0),
+}
+
+
+def a_call(ha, torch, form, d, dtype, q_len, group=3):
+    want, lens, Hk, page, tokens = FORMS[form]
+    if want[1]:   # a table with room for more than 256 MiB, nearly all of it unused
+        tokens = ((256 << 20) // (Hk * page * (d + d // 16) * len(lens)) + 1) * page
+    rng = np.random.default_rng(40 + d + q_len)
+    cache, table, ks, vs = filled_cache(ha, torch, rng, lens, Hk, d, page, tokens=tokens)
+    Hq, dt = group * Hk, dtypes(torch, dtype)
+    assert ha.ha_cache4_attn_form(cache.shape[0], page, Hk, d, len(lens), q_len, Hq, table.shape[1], dt) == want   # by the rule of the dispatch itself
+    Q = torch.from_numpy(2 * d ** -0.25 * rng.standard_normal((len(lens) * q_len, Hq, d))).to(dt).cuda()
+    return cache, table, ks, vs, Q, torch.tensor(lens, dtype=torch.int32, device="cuda"), page, lens
+
+
+@pytest.mark.parametrize("q_len", [1, 4])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("form", FORMS)
+def test_every_form(ha, torch, form, d, dtype, q_len):
+    cache, table, ks, vs, Q, L, page, lens = a_call(ha, torch, form, d, dtype, q_len)
+    out, lse = ha.ha_cache4_attn(Q, cache, table, L, page, q_len=q_len)
+    ref, rl, absv, werr = attention64(host(Q), ks, vs, q_len)
+    check_attention(host(out), host(lse), ref, rl, absv, werr, dtype, max(lens))
+    again = ha.ha_cache4_attn(Q, cache, table, L, page, q_len=q_len)
+    assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+    if q_len == 1:
+        return
+    # NaN in channels 32 ... 63 of the last tokens' V: for the last query of every sequence, and it alone
+    of = [s for s, n in enumerate(lens) if n > 0]
+    slots = torch.tensor([int(table[s, (lens[s] - 1) // page]) * page + (lens[s] - 1) % page for s in of], dtype=torch.int32, device="cuda")
+    k, v = ha.ha_cache4_read(cache, slots, page, dtype=torch.float32)
+    v[:, :, 40] = float("nan")
+    ha.ha_cache4_write(k, v, slots, cache, page)
+    got, got_lse = ha.ha_cache4_attn(Q, cache, table, L, page, q_len=q_len)
+    hit = torch.zeros((len(lens), q_len, out.shape[1], d), dtype=torch.bool, device="cuda")
+    hit[of, q_len - 1, :, 32:64] = True
+    hit = hit.view(out.shape)
+    assert torch.isnan(got[hit]).all() and torch.equal(got[~hit], out[~hit]) and torch.equal(got_lse, lse)
