@@ -172,6 +172,9 @@ __host__ __device__ inline int64_t exact_grid(const AttnArgs& a) {
 //     likewise, by the sequences' lengths.
 //   more: tiles in order of the sequences; s has the numbers from floor(cu[s] / QT) + s on.  It has at most floor(cu[s + 1] / QT) - floor(cu[s] / QT) + 1
 //     tiles, so the ranges do not meet, and the sequence of a number is found by bisection of cu, 64 probes at a time.
+//     Long sequences behind many others then start late, which costs gradients, while the forward's workgroups find their tiles sooner (MI355X, us, 256 sequences
+//     -> one more, empty: forward; forward and backward: 254 of up to 400 before two of 4000, 16 and 4 heads, d = 128 357 -> 346; 1506 -> 1756; 255 of 40 before one
+//     of 8000 321 -> 304; 1786 -> 1907; lengths up to 600, 12 and 4, d = 64 147 -> 134; 584 -> 574; fp32, up to 300, 8 and 4, d = 64 141 -> 130; 630 -> 627).
 // At most n_seq numbers have no tile; their workgroups end at once.
 template <int QT>
 inline int64_t packed_slots(const PackedRows& p) { return (int64_t)p.rows / QT + p.n_seq; }
