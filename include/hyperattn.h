@@ -404,8 +404,9 @@ int hyperattn_forward_alg2(const void* Q, const void* K, const void* V, void* ou
  * projection's output are taken as they lie; strides == NULL: contiguous.  Strides are multiples of 16 bytes; row strides are
  * at least d and at most 2^22.  In what is written the heads of a row lie within the row stride, or the rows of a head within the head stride, and no output
  * overlaps another tensor.  lse: float [Hq][rows], out_f32: float [rows][Hq][d] contiguous (bf16 tensors; may be NULL).
- * cu_seqlens: device int32 [n_seq + 1], not decreasing, within [0, rows]; values that are not so are clamped where they are read, and
- * no access leaves the tensors.  Rows of no sequence are not read and not written: a batch may be padded at its end.
+ * cu_seqlens: device int32 [n_seq + 1], not decreasing, within [0, rows]; values outside [0, rows] are clamped where they are read.  Whatever
+ * they are no access leaves the tensors and the workspace, but where they decrease the outputs' rows may hold anything, what lay in the workspace
+ * among it.  Rows of no sequence are not read and not written: a batch may be padded at its end.
  * A sequence may be empty.  A key row of another sequence counts for nothing, whatever it holds; causal: an Inf or NaN in a row reaches, as 0 times
  * itself, also rows of its own sequence that do not see it where both lie in one tile of 128 rows, as in exact_attn_forward and exact_attn_backward.
  * rows <= 2^24, rows * Hq <= 2^27, n_seq * Hq <= 2^22, Hq % Hk == 0, Hq <= 1024; d in {64, 128}.
@@ -455,8 +456,8 @@ size_t exact_attn_packed_backward_workspace_bytes(const ha_packed* shape);
  *
  * ha_cache4_write: row i of K and V ([rows][Hk][d] of dtype, strides as above: kv[0] of K, kv[1] of V; NULL: contiguous) to slot slots[i]; rows
  * whose slot lies outside the cache are left out.  Slots given must differ; where two rows name one slot it holds a mixture of both, and no
- * other slot is touched.  ha_cache4_read: the rows of these slots back (exact in both types; rows of slots outside the cache: zeros),
- * for a prefix whose pages are used again.  rows <= 2^26, rows * Hk <= 2^26. */
+ * other slot is touched.  ha_cache4_read: the rows of these slots back, as the cache holds them (exact in both types; rows of slots
+ * outside the cache: zeros).  rows <= 2^26, rows * Hk <= 2^26. */
 typedef struct {
   int32_t n_pages, page, Hk, d;
 } ha_cache4;
@@ -473,7 +474,8 @@ int ha_cache4_read(const void* cache, const int32_t* slots, void* K, void* V, co
  * (device int32 [n_seq][max_blocks]).  lens (device int32) are taken within [0, max_blocks * page]; tokens of a page number outside [0, n_pages) count
  * as absent.  A query that sees nothing has out 0 and lse -inf.  What lies in a page behind a sequence's last token, or in a token behind the
  * query's own, counts for nothing, NaN included.
- * Products as in exact_attn_forward: bf16 queries on the matrix cores; fp32 queries split in three, to fp32 accuracy of the cached values.
+ * Products as in exact_attn_forward: bf16 queries on the matrix cores; fp32 queries split in three, to fp32 accuracy of the cached values.  Weighted sums
+ * are formed before they are divided, by weights of at most 2^8: results are finite where the largest |V| times the tokens lies below 2^120.
  * 1 <= q_len <= 64, n_seq <= 2^16, n_seq * q_len * Hq <= 2^22, Hq * q_len <= 2^15, Hq % Hk == 0, n_seq * max_blocks <= 2^30, max_blocks * page < 2^31, n_seq *
  * max_blocks * page <= 2^36.
  * workspace: device, 256-byte aligned, >= ha_cache4_attn_workspace_bytes(); nothing in it is kept.  Two calls may overlap only with

@@ -124,3 +124,19 @@ def test_every_form(ha, torch, form, d, dtype, q_len):
     hit[of, q_len - 1, :, 32:64] = True
     hit = hit.view(out.shape)
     assert torch.isnan(got[hit]).all() and torch.equal(got[~hit], out[~hit]) and torch.equal(got_lse, lse)
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_large_values_stay_finite(ha, torch, form):
+    """The largest |V| times the tokens just below 2^120, in both types (a scale changes no result but by itself: compared after it is taken out again)."""
+    for dtype in ("bf16", "fp32"):
+        cache, table, ks, vs, Q, L, page, lens = a_call(ha, torch, form, 64, dtype, 1)
+        G, at = 2, page * 66   # V's scale bytes lie last in a block
+        top = max(np.abs(v).max() for v in vs if len(v))
+        up = 119 - int(np.ceil(np.log2(top * max(lens))))
+        scales = cache[:, :, at:]
+        assert scales.shape[2] == page * G
+        scales[scales != 255] += up
+        out, lse = ha.ha_cache4_attn(Q, cache, table, L, page)
+        ref, rl, absv, werr = attention64(host(Q), ks, vs, 1)
+        check_attention(host(out) * 2.0 ** -up, host(lse), ref, rl, absv, werr, dtype, max(lens))
