@@ -738,13 +738,19 @@ def _raw_stream(dev):
     return _raw_stream(dev)
 
 
+def _current_device():
+    """Number of the current device.  (From the second call on torch's own function, as above.)"""
+    global _current_device
+    _current_device = getattr(_torch()._C, "_cuda_getDevice", None) or _torch().cuda.current_device
+    return _current_device()
+
+
 def _here(t, name, stream):
     """(device, stream handle) of a call on the current device, where t has to be."""
-    torch = _torch()
     dev = t.get_device()
     if dev < 0:
         raise ValueError(f"{name} must be a device tensor")
-    here = torch._C._cuda_getDevice()   # (a device tensor is there: the runtime is up)
+    here = _current_device()   # (a device tensor is there: the runtime is up)
     if dev != here:
         raise ValueError(f"{name} is on cuda:{dev}, the current device is cuda:{here}")
     if stream is None:
