@@ -103,6 +103,7 @@ struct Weights {
 // SPLIT: parts of a query number and of a weight: 1 for bf16 queries, 3 for fp32 ones (24 bits); cached values have one.
 // NW waves.  WHOLE: a workgroup per sequence, which it finishes (small tables: no second launch).  ONCE: codes are read past the caches.
 // MULTI: several queries a sequence, which see its last tokens in part.
+// bf16, four waves, d = 128, tokens shared out: held to the 168 registers of three workgroups a CU, which costs 2 spilled ones, MULTI 4 (12 and 20 bytes of scratch).
 template <int D, int SPLIT, int NW, bool WHOLE, bool ONCE, bool MULTI>
 __global__ __launch_bounds__(64 * NW, SPLIT == 1 && NW == 4 ? 3 : 2) void cache4_attn_kernel(CacheAttnArgs a) {
   constexpr int kCWaves = NW, kCThreads = 64 * NW;
