@@ -84,7 +84,7 @@ FORMS = {
     "whole, eight waves": ((8, False), RAGGED, 2, 16, 0),
     "whole, four waves": ((4, False), RAGGED * 12, 2, 16, 0),
     "shared": ((0, False), [0, 5000, 1, 777, 130, 6], 2, 64, 6000),
-    "shared, past the caches": ((0, True), [0, 5000, 1, 777, 130, 6], 8, 256, 0),
+    "shared, past the caches": ((0, True), [0, 5000, 1, 777, 130, 6], 4, 256, 0),
 }
 
 
