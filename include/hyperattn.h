@@ -496,6 +496,26 @@ size_t ha_cache4_attn_workspace_bytes(const ha_cache4* shape, const ha_cache4_qu
  * know the table's room, not the lengths: only tables of at most 2048 tokens have the first, so max_blocks is best kept near the step's longest sequence. */
 int ha_cache4_attn_form(const ha_cache4* shape, const ha_cache4_query* query, int32_t* whole_waves, int32_t* past_caches);
 
+/* Attention of chunks of new tokens over the cache: any number of them for every sequence (a piece of a prompt, a turn behind a cached prefix, one token of a decoding
+ * step, none), in one batch of rows.  Sequence s brings rows [cu_seqlens[s], cu_seqlens[s + 1]) of Q and out ([rows][Hq][d], strides qo[0], qo[1]; NULL: contiguous),
+ * the queries of the last n_s = cu_seqlens[s + 1] - cu_seqlens[s] of the lens[s] tokens that the cache holds of it, their own among them: row i of the n_s sees
+ * tokens 0 ... lens[s] - n_s + i.  lse: float [Hq][rows].  cu_seqlens: device int32 [n_seq + 1], as exact_attn_packed_forward takes them and
+ * ha_page_plan writes them: values outside [0, rows] are clamped, rows of no sequence are not read and not written, and where they decrease the rows may hold
+ * anything, but no access leaves the tensors and the workspace.
+ * Everything else as in ha_cache4_attn: products, lens and pages, what counts for nothing, the range of results.
+ * rows <= 2^22, rows * Hq <= 2^26, n_seq <= 2^16, n_seq * Hq <= 2^22, Hq % Hk == 0, Hq <= 1024, n_seq * max_blocks <= 2^30, max_blocks * page < 2^31 - 256.
+ * workspace: device, 256-byte aligned, >= ha_cache4_attn_chunk_workspace_bytes() (at most 65 MiB; 0: none is needed, and it may be NULL); nothing in it is kept.  Same inputs, same bits. */
+typedef struct {
+  int32_t n_seq, rows, Hq;
+  int32_t dtype; /* ha_dtype of Q and out */
+  int32_t max_blocks;
+} ha_cache4_chunk;
+
+int ha_cache4_attn_chunk(const void* Q, const void* cache, const int32_t* cu_seqlens, const int32_t* block_table, const int32_t* lens, void* out,
+                         float* lse, const ha_cache4* shape, const ha_cache4_chunk* chunk, const ha_strides* qo, void* workspace,
+                         size_t workspace_bytes, void* stream);
+size_t ha_cache4_attn_chunk_workspace_bytes(const ha_cache4* shape, const ha_cache4_chunk* chunk); /* 0 too if not valid */
+
 /* Block tables and slots, on the GPU from the sequences' lengths: one launch before a step's rows are written.
  *   lens[s]   tokens that sequence s holds, in pages block_table[s][0 ... ceil(lens / page) - 1]
  *   add[s]    >= 0: rows that the step appends to it; < 0: it has ended, its pages are free again

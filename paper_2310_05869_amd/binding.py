@@ -106,6 +106,8 @@ _SIGNATURES = {
     "ha_cache4_attn": (c_int, [c_void_p] * 6 + [c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
     "ha_cache4_attn_workspace_bytes": (c_size_t, [c_void_p, c_void_p]),
     "ha_cache4_attn_form": (c_int, [c_void_p, c_void_p, POINTER(c_int32), POINTER(c_int32)]),
+    "ha_cache4_attn_chunk": (c_int, [c_void_p] * 7 + [c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "ha_cache4_attn_chunk_workspace_bytes": (c_size_t, [c_void_p, c_void_p]),
     "ha_page_plan": (c_int, [c_void_p] * 9 + [c_void_p, c_void_p]),
     "ha_measure_mfma_rate": (c_int, [c_void_p, c_size_t, c_int32, POINTER(c_float), c_void_p]),
     "ha_measure_hbm_rate": (c_int, [c_void_p, c_size_t, POINTER(c_float), POINTER(c_float), c_void_p]),
@@ -728,7 +730,7 @@ _PACKED = struct.Struct("7i")
 _PACKED_STRIDES = struct.Struct("16q")
 _STRIDES2 = struct.Struct("4q")
 _CACHE4 = struct.Struct("4i")
-_FIVE = struct.Struct("5i")  # ha_cache4_query, ha_page_plan_shape
+_FIVE = struct.Struct("5i")  # ha_cache4_query, ha_cache4_chunk, ha_page_plan_shape
 
 
 def _raw_stream(dev):
@@ -985,6 +987,46 @@ def ha_cache4_attn(Q, cache, block_table, lens, page, q_len=1, out=None, lse=Non
                                 _whole(block_table, "block_table", block_table.shape, i32, dev), _whole(lens, "lens", (n_seq,), i32, dev), out.data_ptr(),
                                 _whole(lse, "lse", (Hq, rows), torch.float32, dev), sizes, query, qo,
                                 _bytes(workspace, "workspace", dev), workspace.numel(), handle), "ha_cache4_attn")
+    return out, lse
+
+
+def _chunk_call(Q, cache, cu_seqlens, block_table, page):
+    """(shape of Q, the cache's sizes, the call's) of new tokens' queries over a cache."""
+    if Q.dim() != 3:
+        raise ValueError(f"Q has shape {tuple(Q.shape)}, expected [rows, Hq, d]")
+    rows, Hq, d = full = tuple(Q.shape)
+    sizes = _CACHE4.pack(*_cache4(cache, page, d))
+    if block_table.dim() != 2 or cu_seqlens.dim() != 1 or cu_seqlens.shape[0] != block_table.shape[0] + 1:
+        raise ValueError(f"block_table has shape {tuple(block_table.shape)}, cu_seqlens {tuple(cu_seqlens.shape)}, expected [n_seq, max_blocks] and [n_seq + 1]")
+    n_seq, max_blocks = block_table.shape
+    return full, sizes, _FIVE.pack(n_seq, rows, Hq, _code(Q.dtype), max_blocks)
+
+
+def ha_cache4_attn_chunk_workspace_bytes(cache, page, n_seq, rows, Hq, max_blocks, dtype=None) -> int:
+    code = HA_BF16 if dtype is None else _code(dtype)
+    return int(lib().ha_cache4_attn_chunk_workspace_bytes(_CACHE4.pack(*_cache4(cache, page)), _FIVE.pack(n_seq, rows, Hq, code, max_blocks)))
+
+
+def ha_cache4_attn_chunk(Q, cache, cu_seqlens, block_table, lens, page, out=None, lse=None, workspace=None, stream=None):
+    """out, lse: attention of every sequence's new tokens over its pages.  Q [rows, Hq, d] (bf16 or fp32; strided as it lies): rows cu_seqlens[s] to
+    cu_seqlens[s + 1] (int32 [n_seq + 1]) are the last of the lens[s] tokens (int32 [n_seq]) that the cache holds of sequence s, any number of them; block_table
+    int32 [n_seq, max_blocks].  lse: float32 [Hq, rows].  Rows of no sequence are left as they were."""
+    torch = _torch()
+    full, sizes, chunk = _chunk_call(Q, cache, cu_seqlens, block_table, page)
+    rows, Hq, _ = full
+    dt, i32 = Q.dtype, torch.int32
+    dev, handle = _here(cache, "cache", stream)
+    if out is None:
+        out = _empty(stream, full, dt, Q)
+    if lse is None:
+        lse = _empty(stream, (Hq, rows), torch.float32, Q)
+    qo = _STRIDES2.pack(*_rows(Q, "Q", full, dt, dev), *_rows(out, "out", full, dt, dev))
+    if workspace is None:
+        workspace = _empty(stream, (int(lib().ha_cache4_attn_chunk_workspace_bytes(sizes, chunk)),), torch.uint8, Q)
+    _check(lib().ha_cache4_attn_chunk(Q.data_ptr(), _bytes(cache, "cache", dev), _whole(cu_seqlens, "cu_seqlens", cu_seqlens.shape, i32, dev),
+                                      _whole(block_table, "block_table", block_table.shape, i32, dev), _whole(lens, "lens", (block_table.shape[0],), i32, dev),
+                                      out.data_ptr(), _whole(lse, "lse", (Hq, rows), torch.float32, dev), sizes, chunk, qo,
+                                      _bytes(workspace, "workspace", dev), workspace.numel(), handle), "ha_cache4_attn_chunk")
     return out, lse
 
 

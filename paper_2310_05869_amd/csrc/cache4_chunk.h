@@ -1,0 +1,75 @@
+// Chunks of new tokens over the paged 4-bit cache: how work is found from lengths that only the device knows.  Shared by attention (cache4_chunk.hip) and by
+// the sums of attention weights (cache4_weights.hip).
+//
+// Sequence s brings n_s new tokens, rows cu[s] ... cu[s + 1] - 1 of Q, the last of the lens[s] that the cache holds of it.  The query heads of a key head
+// read the same keys, so a tile of query rows holds all of them for some tokens: row r is token r / sub_group of the tile, head r % sub_group.  A key head with
+// more query heads than a tile has rows counts as several ("heads" below: key heads times these runs).
+#pragma once
+
+#include "attn_common.h"
+#include "cache4_common.h"
+
+namespace ha {
+
+struct ChunkSeq {
+  int start, n;   // rows
+  int len, held;  // tokens in the cache, those before the new ones (negative: more rows than tokens; the first rows see nothing)
+};
+
+__device__ inline ChunkSeq chunk_seq(const CacheChunkArgs& a, int s) {
+  ChunkSeq q;
+  q.start = min(max(a.cu[s], 0), a.rows);
+  q.n = max(min(max(a.cu[s + 1], 0), a.rows) - q.start, 0);
+  q.len = min(max(a.lens[s], 0), a.max_blocks << a.c.log_page);
+  q.held = q.len - q.n;
+  return q;
+}
+
+__device__ inline ChunkSeq uniform_seq(ChunkSeq q) {
+  q.start = __builtin_amdgcn_readfirstlane(q.start);
+  q.n = __builtin_amdgcn_readfirstlane(q.n);
+  q.len = __builtin_amdgcn_readfirstlane(q.len);
+  q.held = __builtin_amdgcn_readfirstlane(q.held);
+  return q;
+}
+
+__device__ inline int64_t uniform64(int64_t x) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x), hi = __builtin_amdgcn_readfirstlane((uint32_t)(x >> 32));
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
+// All sequences' work as one line: sequence s takes cost(s) >= 0 of it.  A lane sums a run of sequences; the sum is the same for all lanes, *before: what
+// precedes the lane's run.
+template <class Cost>
+__device__ inline int64_t chunk_line(int n_seq, int lane, int64_t* before, Cost&& cost) {
+  const int each = (n_seq + 63) / 64, s0 = min(n_seq, lane * each), s1 = min(n_seq, s0 + each);
+  int64_t sum = 0;
+  for (int s = s0; s < s1; ++s) sum += cost(s);
+  int64_t inc = sum;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t up = __shfl_up((long long)inc, o);
+    if (lane >= o) inc += up;
+  }
+  *before = inc - sum;
+  return uniform64(__shfl((long long)inc, 63));
+}
+
+// The sequence at place u of the line (0 <= u < its length), and where it begins
+template <class Cost>
+__device__ inline int chunk_place(int n_seq, int64_t before, int64_t u, int64_t* first, Cost&& cost) {
+  const int each = (n_seq + 63) / 64;
+  const unsigned long long le = __ballot(before <= u);  // (runs without work begin where the next one does)
+  const int run = 63 - __builtin_clzll(le);
+  int64_t at = uniform64(__shfl((long long)before, run));
+  int s = min(run * each, n_seq - 1);
+  for (; s < n_seq - 1; ++s) {
+    const int64_t n = uniform64(cost(s));
+    if (u < at + n) break;
+    at += n;
+  }
+  *first = at;
+  return __builtin_amdgcn_readfirstlane(s);
+}
+
+}  // namespace ha

@@ -1,0 +1,590 @@
+// Attention of chunks of new tokens over their sequences' pages of the 4-bit cache (ha_cache4_attn_chunk).
+//
+// One pass over the keys with a running reference and sum of the softmax, as in attn_mfma.hip: a wave keeps 32 query rows, S^T = K Q^T by
+// v_mfma_f32_32x32x16_bf16 over 64 tokens a step, the weights are the B operand of O^T += V^T P^T.  What differs is where tiles come from: the query
+// heads of a key head and some tokens of theirs share a workgroup (128 rows), which turns the codes of a step into bf16 once, in registers, and lays them
+// into LDS for its four waves.  Cached values are exact in bf16, so products are those of bf16 tensors.
+//   * A wave takes the K codes, V codes and scales of 16 tokens, which lie in one page: a uniform base.  v_cvt_scalef32_pk_bf16_fp4 makes two values of a
+//     byte, scale included; a lane's words become whole pieces of 16 bytes of LDS rows, because channels may lie in any order that the other
+//     operand shares: K's rows hold the page's words in their order, Q is loaded alike; V's rows hold a word's eight channels together, and
+//     the output's channels are put in order when it is written.
+//   * Split: the tiles of all sequences and heads are one line, a tile's length in it the tokens that its last row sees (and what its start and end
+//     cost), cut into equal runs, a workgroup each: whatever the lengths are, all have the same to do.  Sums of tiles that a cut divides go to the
+//     workspace and are joined by a second launch.
+#include <type_traits>
+
+#include "cache4_chunk.h"
+
+namespace ha {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef s16x4 __attribute__((address_space(3))) * lds_s16x4_ptr;
+
+constexpr int kStep = 64;           // tokens of a step
+constexpr int kTileCost = 128;      // what a tile's start and end cost, in tokens
+constexpr int kLeastRun = 512;      // tokens of the line that a workgroup takes, at least
+constexpr int kMostParts = 512;     // workgroups that the chip holds at once, two per CU
+constexpr int kJoinThreads = 256;
+constexpr uint32_t kFarScale = 253; // V's scales from here on give values that may lie past the largest number, or NaN: taken by the rows that see the token alone
+
+template <int D>
+struct ChunkLds {
+  static constexpr int KSTR = (D + 8) * 2;   // bytes per K row (+16: conflict-free 16-byte row reads)
+  static constexpr int VSTR = (D + 32) * 2;  // bytes per V row (+64: conflict-free transposing reads)
+  static constexpr int K_BYTES = kStep * KSTR;
+  static constexpr int BUF = K_BYTES + kStep * VSTR;
+  static constexpr int ROW = D * 4 + 16;           // a row of the output on its way out
+  static constexpr int WAVE = 32 * ROW + 32 * 8;
+  static constexpr int bytes(int nw) { return (2 * BUF > nw * WAVE ? 2 * BUF : nw * WAVE) + 16; }
+};
+
+// What a wave holds of 16 tokens: K words and scales of a token, V words and scales of four (d = 64: two) tokens
+template <int D>
+struct RawK {
+  std::conditional_t<D == 128, u32x4, u32x2> w;
+  uint32_t sc;
+};
+template <int D>
+struct RawV {
+  std::conditional_t<D == 128, u32x4, u32x2> w;
+  std::conditional_t<D == 128, u32x4, uint32_t> sc;
+};
+
+__device__ inline float scale_of(uint32_t bytes, int i) { return __uint_as_float(i < 3 ? bytes << (23 - 8 * i) : bytes >> 1); }  // (the exponent alone counts)
+
+template <int SEL>
+__device__ inline uint32_t two_values(uint32_t w, float sc) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc, SEL));
+}
+
+// SPLIT: parts of a query number and of a weight: 1 for bf16 queries, 3 for fp32 ones (24 bits); cached values have one.  WHOLE: a workgroup per tile.
+template <int D, int SPLIT, int NW, bool WHOLE>
+__global__ __launch_bounds__(64 * NW, 2) void cache4_chunk_kernel(CacheChunkArgs a) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  using L = ChunkLds<D>;
+  constexpr int QT = 32 * NW, KS = D / 16, DT = D / 32, G = D / kCacheGroup;
+  constexpr bool F32 = SPLIT > 1;
+  int* far_flag = reinterpret_cast<int*>(smem + L::bytes(NW) - 16);
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lq = lane & 31, h = lane >> 5;
+  const int part16 = wave & 3;  // the 16 tokens of a step that the wave lays into LDS
+
+  // ---- place ----
+  const int tt = a.tile_tokens, heads = a.c.Hk * a.subs;
+  auto tiles_of = [&](const ChunkSeq& q) { return (q.n + tt - 1) / tt; };
+  auto upto = [&](const ChunkSeq& q, int64_t t) { return t * (max(q.held, 0) + kTileCost) + tt * (t * (t + 1) / 2); };  // line before tile t of a head
+  auto cost = [&](int s) -> int64_t {
+    const ChunkSeq q = chunk_seq(a, s);
+    const int T = tiles_of(q);
+    return heads * (WHOLE ? (int64_t)T : upto(q, T));
+  };
+  int64_t before;
+  const int64_t total = chunk_line(a.n_seq, lane, &before, cost);
+  int parts = 1, part = 0;
+  int64_t u0 = blockIdx.x, u1 = 0;
+  auto part_begin = [&](int p) { return total / parts * p + total % parts * p / parts; };
+  if constexpr (WHOLE) {
+    if (u0 >= total) return;
+  } else {
+    parts = (int)min((int64_t)a.parts, max(total / kLeastRun, (int64_t)1));
+    if (parts > 8) parts &= ~7;
+    part = blockIdx.x;
+    if (part < parts && (parts & 7) == 0) part = (part & 7) * (parts >> 3) + (part >> 3);  // a run of the line per XCD: neighbours share keys
+    if (threadIdx.x == 0) a.joins[4 * part] = -1;
+    if (part >= parts || total == 0) return;
+    u0 = part_begin(part);
+    u1 = part_begin(part + 1);
+  }
+  int64_t tile_first;
+  int s = chunk_place(a.n_seq, before, u0, &tile_first, cost);
+  ChunkSeq q = uniform_seq(chunk_seq(a, s));
+  int T = tiles_of(q), hh, t;
+  {
+    const int64_t head_cost = WHOLE ? (int64_t)T : upto(q, T), rem = u0 - tile_first;
+    hh = (int)(rem / head_cost);
+    const int64_t in_head = rem - hh * head_cost;
+    if constexpr (WHOLE) {
+      t = T - 1 - (int)in_head;
+    } else {
+      int lo = 0, hi = T;  // upto(lo) <= in_head < upto(hi)
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (upto(q, mid) <= in_head) lo = mid;
+        else hi = mid;
+      }
+      t = lo;
+      tile_first += hh * head_cost + upto(q, t);
+    }
+    hh = __builtin_amdgcn_readfirstlane(hh);
+    t = __builtin_amdgcn_readfirstlane(t);
+    tile_first = uniform64(tile_first);
+  }
+
+  const int64_t page_bytes = (int64_t)a.c.Hk * a.c.block_bytes();
+  const int log_page = a.c.log_page, in_page = a.c.page - 1;
+
+  for (;;) {
+    const int seen = min(max(q.held + min((t + 1) * tt, q.n), 0), q.len);  // tokens that the tile's last row sees
+    const int all_see = q.held + t * tt + 1;                               // that all rows see
+    const int nsteps = (seen + kStep - 1) / kStep;
+    const int64_t length = max(q.held, 0) + (int64_t)(t + 1) * tt + kTileCost;
+    auto step_at = [&](int64_t x) { return x <= 0 ? 0 : (int)min((x + kStep - 1) / kStep, (int64_t)nsteps); };
+    const int first = WHOLE ? 0 : step_at(u0 - tile_first), last = WHOLE ? nsteps : step_at(min(u1 - tile_first, length));
+    if (first < last || (nsteps == 0 && (WHOLE || tile_first >= u0))) {
+      const int kv = hh / a.subs, head0 = kv * a.group + (hh - kv * a.subs) * a.sub_group;
+      const int head_end = (kv + 1) * a.group;
+      const unsigned char* head_base = a.cache + (int64_t)kv * a.c.block_bytes();
+      const int32_t* blocks = a.table + (int64_t)s * a.max_blocks;
+      const int last_block = max(q.len - 1, 0) >> log_page;
+
+      // ---- the lane's query row ----
+      const int r = wave * 32 + lq, r_tok = r / a.sub_group, r_head = head0 + (r - r_tok * a.sub_group);
+      const bool valid = r_tok < tt && t * tt + r_tok < q.n && r_head < head_end;
+      const int tok = t * tt + (valid ? r_tok : 0), head = valid ? r_head : head0;  // (a lane without a row repeats the tile's first)
+      const int limit = q.held + tok + 1;  // tokens that it sees
+      bf16x8 qreg[SPLIT][KS];
+      {
+        const int64_t at = (int64_t)(q.start + tok) * a.q.row + (int64_t)head * a.q.head;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          const int j = 2 * ks + h, c = 32 * (j % G) + 8 * (j / G);  // piece j of a K row: word j of the token
+          if constexpr (!F32) {
+            qreg[0][ks] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(a.Q) + at + c));
+          } else {
+            const f32x4* p = reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(a.Q) + at + c);
+            const f32x4 x0 = p[0], x1 = p[1];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              float x = 0.5f * (i < 4 ? x0[i % 4] : x1[i % 4]);  // (at half: rounding the first part up leaves the largest finite)
+#pragma unroll
+              for (int z = 0; z < SPLIT; ++z) {
+                qreg[z][ks][i] = (__bf16)x;
+                x -= (float)qreg[z][ks][i];
+              }
+            }
+          }
+        }
+      }
+
+      // ---- codes into LDS ----
+      auto find_page = [&](int step, int sub) { return blocks[min((step * kStep + 16 * sub) >> log_page, last_block)]; };
+      auto there = [&](int page) { return (unsigned)page < (unsigned)a.c.n_pages; };
+      auto base_of = [&](int page) {
+        const int p = __builtin_amdgcn_readfirstlane(page);
+        return head_base + (int64_t)(there(p) ? p : 0) * page_bytes;
+      };
+      auto load_k = [&](int step, int page, RawK<D>& k) {
+        const unsigned char* b = base_of(page);
+        const int at = ((step * kStep + 16 * part16) & in_page) + (lane >> 2);
+        k.w = *reinterpret_cast<const decltype(k.w)*>(b + at * (D / 2) + (lane & 3) * (D / 8));
+        if constexpr (D == 128) k.sc = *reinterpret_cast<const uint32_t*>(b + a.c.k_scale_at() + at * 4);
+        else k.sc = *reinterpret_cast<const uint16_t*>(b + a.c.k_scale_at() + at * 2);
+      };
+      // V: a lane has a word (of D / 8) of four tokens (d = 64: of two)
+      const int v_word = D == 128 ? lane & 15 : lane & 7;
+      const int v_tok = D == 128 ? 4 * (lane >> 4) : 4 * ((lane >> 3) & 3) + 2 * (lane >> 5);  // the first of them
+      auto load_v = [&](int step, int page, RawV<D>& v) {
+        const unsigned char* b = base_of(page);
+        const int at = (step * kStep + 16 * part16) & in_page;
+        v.w = *reinterpret_cast<const decltype(v.w)*>(b + a.c.v_at() + ((at + v_tok) >> 2) * (D * 2) + v_word * 16 + (v_tok & 3) * 4);
+        v.sc = *reinterpret_cast<const decltype(v.sc)*>(b + a.c.v_scale_at() + (at + v_tok) * G);
+      };
+      auto store_k = [&](unsigned char* buf, const RawK<D>& k) {
+        unsigned char* to = buf + (16 * part16 + (lane >> 2)) * L::KSTR + (lane & 3) * (16 * G);
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          const float sc = scale_of(k.sc, g);
+          *reinterpret_cast<u32x4*>(to + 16 * g) = (u32x4){two_values<0>(k.w[g], sc), two_values<1>(k.w[g], sc), two_values<2>(k.w[g], sc), two_values<3>(k.w[g], sc)};
+        }
+      };
+      constexpr int VT = D == 128 ? 4 : 2;  // tokens of a lane
+      auto store_v = [&](unsigned char* buf, int step, int page, RawV<D>& v) {
+        const int tok0 = step * kStep + 16 * part16 + v_tok;
+        if (F32 || step * kStep + kStep > all_see || !there(__builtin_amdgcn_readfirstlane(page))) {
+          const bool here = there(page);
+          uint32_t taken = 0;
+#pragma unroll
+          for (int i = 0; i < VT; ++i) {
+            uint32_t sc = D == 128 ? ((const uint32_t*)&v.sc)[i] : (((const uint32_t*)&v.sc)[0] >> (16 * i)) & 0xffffu;
+            if (!here || tok0 + i >= seen) {  // whatever lies there: weight 0 times a NaN would be NaN
+              v.w[i] = 0;
+              sc = 0;
+            } else if (F32 || tok0 + i >= all_see) {
+              // groups that are NaN or may lie past the largest number, of tokens that some rows see alone, are taken out here (fp32 queries: of all
+              // tokens; an infinity times the parts of a weight, some of them 0 or negative, would be NaN)
+              const uint32_t far = ((sc & 0x7f7f7f7fu) + (256 - kFarScale) * 0x01010101u) & sc & 0x80808080u;  // the top bit of every byte from kFarScale on
+              sc &= ~((far << 1) - (far >> 7));
+              taken |= far;
+            }
+            if constexpr (D == 128) v.sc[i] = sc;
+            else v.sc = i == 0 ? (v.sc & 0xffff0000u) | sc : (v.sc & 0xffffu) | sc << 16;
+          }
+          if (taken) *far_flag = 1;
+        }
+        unsigned char* to = buf + L::K_BYTES + (16 * part16 + v_tok) * L::VSTR + v_word * 16;
+#pragma unroll
+        for (int i = 0; i < VT; ++i) {
+          u32x4 x;
+          if constexpr (D == 128) {
+            x = (u32x4){two_values<0>(v.w[i], scale_of(v.sc[i], 0)), two_values<1>(v.w[i], scale_of(v.sc[i], 1)),
+                        two_values<2>(v.w[i], scale_of(v.sc[i], 2)), two_values<3>(v.w[i], scale_of(v.sc[i], 3))};
+          } else {
+            const float s0 = scale_of(v.sc, 2 * i), s1 = scale_of(v.sc, 2 * i + 1);
+            x = (u32x4){two_values<0>(v.w[i], s0), two_values<1>(v.w[i], s0), two_values<2>(v.w[i], s1), two_values<3>(v.w[i], s1)};
+          }
+          *reinterpret_cast<u32x4*>(to + i * L::VSTR) = x;
+        }
+      };
+      auto buf_at = [&](int step) { return smem + ((step - first) & 1) * L::BUF; };
+      auto absent = [&](int step) {  // which quarters of a step lie in pages that are not there
+        uint32_t bits = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) bits |= (uint32_t)!there(find_page(step, i)) << i;
+        return (uint32_t)__builtin_amdgcn_readfirstlane(bits);
+      };
+
+      // ---- state ----
+      f32x16 o[DT];
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
+      // reference of the exponentials, moved (and the sums rescaled) where a row's scores exceed it by more than 8; log2 domain for bf16
+      // queries, natural for fp32 ones; l: this lane's share of the row sum
+      float m = -INFINITY, l = 0.f;
+      constexpr float unit_of = F32 ? 2.f : kLog2e;
+      const int vtr_off = ((lane & 15) >> 2) * L::VSTR + ((lane & 3) * 4 + ((lane >> 4) & 1) * 16) * 2 + (4 * h) * L::VSTR;
+
+      // scores of 32 tokens: sub 0 or 1 of the step
+      auto scores = [&](int step, int sub) {
+        f32x16 c;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) c[i] = 0.f;
+        const unsigned char* kp = buf_at(step) + (32 * sub + lq) * L::KSTR + 16 * h;
+#pragma unroll
+        for (int j = 0; j < KS; ++j) {
+          const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kp + 32 * j);
+#pragma unroll
+          for (int z = SPLIT - 1; z >= 0; --z) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qreg[z][j], c, 0, 0, 0);
+        }
+        return c;
+      };
+      auto mask = [&](f32x16& c, int step, int sub, uint32_t gone) {
+        const int base = step * kStep + 32 * sub;
+        if (base + 32 <= all_see && gone == 0) return;
+        const int lim = limit - base - 4 * h;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int off = 8 * (i / 4) + i % 4;
+          if (off >= lim || (gone >> (2 * sub + i / 8) & 1)) c[i] = -INFINITY;
+        }
+      };
+      auto add_values = [&](int step, int j, bf16x8 (&w)[SPLIT]) {  // 16 tokens
+        const unsigned char* vb = buf_at(step) + L::K_BYTES + vtr_off + (16 * j) * L::VSTR;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          const unsigned char* vp = vb + (32 * dt) * 2;
+          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(vp));
+          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(vp + 8 * L::VSTR));
+          const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+          for (int z = SPLIT - 1; z >= 0; --z) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, both), w[z], o[dt], 0, 0, 0);
+        }
+      };
+
+      __syncthreads();  // (the tile before has left LDS)
+      if (threadIdx.x == 0) *far_flag = 0;
+      __syncthreads();
+      if (first < last) {
+        RawK<D> k;
+        RawV<D> v;
+        const int p0 = find_page(first, part16);
+        load_k(first, p0, k);
+        load_v(first, p0, v);
+        store_k(buf_at(first), k);
+        store_v(buf_at(first), first, p0, v);
+        __syncthreads();
+        for (int step = first; step < last; ++step) {
+          const bool more = step + 1 < last;
+          int page = 0;
+          if (more) {
+            page = find_page(step + 1, part16);
+            load_k(step + 1, page, k);
+            load_v(step + 1, page, v);
+          }
+          const uint32_t gone = absent(step);
+#pragma unroll
+          for (int sub = 0; sub < 2; ++sub) {
+            f32x16 c = scores(step, sub);
+            mask(c, step, sub, gone);
+            float mx = c[0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) mx = fmaxf(mx, c[i]);
+            mx *= unit_of;
+            if (__any(mx > m + (F32 ? 5.5f : 8.f))) {
+              mx = fmaxf(mx, __shfl_xor(mx, 32));
+              const float m_new = fmaxf(m, mx), ref = m_new == -INFINITY ? 0.f : m_new;
+              const float alpha = F32 ? expf(m - ref) : __builtin_amdgcn_exp2f(m - ref);
+#pragma unroll
+              for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[dt][i] *= alpha;
+              l *= alpha;
+              m = m_new;
+            }
+            const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+            for (int jj = 0; jj < 2; ++jj) {
+              u32x4 w[SPLIT];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                float x0 = __builtin_fmaf(c[8 * jj + 2 * e], unit_of, -ref), x1 = __builtin_fmaf(c[8 * jj + 2 * e + 1], unit_of, -ref);
+                if constexpr (F32) {
+                  x0 = exp_split(x0);
+                  x1 = exp_split(x1);
+                } else {
+                  x0 = __builtin_amdgcn_exp2f(x0);
+                  x1 = __builtin_amdgcn_exp2f(x1);
+                }
+                l += x0 + x1;
+#pragma unroll
+                for (int z = 0; z < SPLIT; ++z) {
+                  w[z][e] = pack_bf16x2(x0, x1);
+                  if (z + 1 < SPLIT) {
+                    x0 -= __uint_as_float(w[z][e] << 16);
+                    x1 -= __uint_as_float(w[z][e] & 0xffff0000u);
+                  }
+                }
+              }
+              bf16x8 pf[SPLIT];
+#pragma unroll
+              for (int z = 0; z < SPLIT; ++z) pf[z] = __builtin_bit_cast(bf16x8, w[z]);
+              add_values(step, 2 * sub + jj, pf);
+            }
+          }
+          if (more) {
+            store_k(buf_at(step + 1), k);
+            store_v(buf_at(step + 1), step + 1, page, v);
+          }
+          __syncthreads();
+        }
+      }
+
+      // ---- groups that were taken out, for the rows that see them (rare) ----
+      if (*far_flag) {
+        for (int x = F32 ? first * kStep : max(first * kStep, max(all_see, 0)); x < min(last * kStep, seen); ++x) {
+          const int page = find_page(x / kStep, (x & (kStep - 1)) >> 4), at = x & in_page;
+          if (!there(page)) continue;
+          const unsigned char* b = base_of(page);
+          const unsigned char* k_scales = b + a.c.k_scale_at() + at * G;
+          const unsigned char* v_scales = b + a.c.v_scale_at() + at * G;
+          bool any = false;
+#pragma unroll
+          for (int g = 0; g < G; ++g) any = any || v_scales[g] >= kFarScale;
+          if (!any) continue;
+          float score = 0.f;
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) {
+            const int j = 2 * ks + h;
+            const uint32_t w = *reinterpret_cast<const uint32_t*>(b + at * (D / 2) + 4 * j);
+            const float sc = __uint_as_float((uint32_t)k_scales[j % G] << 23);
+            const f32x2 k01 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, sc, 0), k23 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, sc, 1);
+            const f32x2 k45 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, sc, 2), k67 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, sc, 3);
+            const float kk[8] = {k01[0], k01[1], k23[0], k23[1], k45[0], k45[1], k67[0], k67[1]};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              float x = 0.f;
+#pragma unroll
+              for (int z = SPLIT - 1; z >= 0; --z) x += (float)qreg[z][ks][i];
+              score = __builtin_fmaf(F32 ? 2.f * x : x, kk[i], score);
+            }
+          }
+          score += __shfl_xor(score, 32);
+          const float ref = m == -INFINITY ? 0.f : m;
+          const float weight = F32 ? expf(score - ref) : (float)(__bf16)__builtin_amdgcn_exp2f(__builtin_fmaf(score, kLog2e, -ref));
+          if (x < limit) {
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+              for (int i = 0; i < 16; i += 2) {  // word 4 dt + i / 4, byte 2 h + i % 4 / 2
+                const int byte = 2 * h + i % 4 / 2, g = D == 128 ? byte : byte / 2;
+                if (v_scales[g] < kFarScale) continue;
+                const uint32_t w = *reinterpret_cast<const uint32_t*>(b + a.c.v_at() + (at >> 2) * (D * 2) + (4 * dt + i / 4) * 16 + (at & 3) * 4) >> (8 * byte);
+                const f32x2 v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, __uint_as_float((uint32_t)v_scales[g] << 23), 0);
+                o[dt][i] = __builtin_fmaf(weight, v[0], o[dt][i]);
+                o[dt][i + 1] = __builtin_fmaf(weight, v[1], o[dt][i + 1]);
+              }
+          }
+        }
+      }
+
+      // ---- out: rows through LDS, channels in their order ----
+      __syncthreads();  // (far_flag has been read, tiles too)
+      const bool whole = WHOLE || (first == 0 && last == nsteps);
+      l += __shfl_xor(l, 32);
+      const bool empty = l == 0.f;
+      if (whole) {
+        const float inv = empty ? 0.f : 1.f / l;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[dt][i] *= inv;
+      }
+      unsigned char* ep = smem + wave * L::WAVE;
+      int64_t* ep_rows = reinterpret_cast<int64_t*>(ep + 32 * L::ROW);
+      const int64_t slot = WHOLE ? 0 : 2 * (int64_t)part + (tile_first >= u0);
+      if (h == 0) {
+        ep_rows[lq] = !valid ? -1 : whole ? (int64_t)(q.start + tok) * a.o.row + (int64_t)head * a.o.head : (slot * QT + r) * D;
+        if (valid) {
+          if (whole) {
+            a.lse[(int64_t)head * a.rows + q.start + tok] = empty ? -INFINITY : F32 ? m + logf(l) : (m + log2f(l)) * kLn2;
+          } else {
+            a.part_ml[2 * (slot * QT + r)] = m;
+            a.part_ml[2 * (slot * QT + r) + 1] = l;
+          }
+        }
+      }
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int g4 = 0; g4 < 4; ++g4) {
+          const int word = 4 * dt + g4;
+          unsigned char* to = ep + lq * L::ROW;
+          if constexpr (D == 128) {
+            *reinterpret_cast<f32x2*>(to + (64 * h + 2 * word) * 4) = (f32x2){o[dt][4 * g4], o[dt][4 * g4 + 1]};
+            *reinterpret_cast<f32x2*>(to + (64 * h + 32 + 2 * word) * 4) = (f32x2){o[dt][4 * g4 + 2], o[dt][4 * g4 + 3]};
+          } else {
+            *reinterpret_cast<f32x4*>(to + (32 * h + 4 * word) * 4) = (f32x4){o[dt][4 * g4], o[dt][4 * g4 + 1], o[dt][4 * g4 + 2], o[dt][4 * g4 + 3]};
+          }
+        }
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      constexpr int CH = D / 8;  // pieces of eight channels
+#pragma unroll
+      for (int it = 0; it < 32 * CH / 64; ++it) {
+        const int idx = lane + 64 * it, row = idx / CH, ch = idx % CH * 8;
+        const int64_t at = ep_rows[row];
+        const f32x4 x0 = *reinterpret_cast<const f32x4*>(ep + row * L::ROW + ch * 4), x1 = *reinterpret_cast<const f32x4*>(ep + row * L::ROW + ch * 4 + 16);
+        if (at < 0) continue;
+        if (!whole || F32) {
+          f32x4* to = reinterpret_cast<f32x4*>((whole ? reinterpret_cast<float*>(a.out) : a.part_o) + at + ch);
+          to[0] = x0;
+          to[1] = x1;
+        } else {
+          *reinterpret_cast<u32x4*>(reinterpret_cast<uint16_t*>(a.out) + at + ch) =
+              (u32x4){pack_bf16x2(x0[0], x0[1]), pack_bf16x2(x0[2], x0[3]), pack_bf16x2(x1[0], x1[1]), pack_bf16x2(x1[2], x1[3])};
+        }
+      }
+      if (!WHOLE && !whole && last == nsteps && threadIdx.x == 0) {  // others began the tile: the second launch joins it
+        int p = (int)min(tile_first / (total / parts), (int64_t)part - 1);
+        while (part_begin(p) > tile_first) --p;
+        while (part_begin(p + 1) <= tile_first) ++p;
+        a.joins[4 * part + 1] = hh;
+        a.joins[4 * part + 2] = t;
+        a.joins[4 * part + 3] = p;
+        a.joins[4 * part] = s;
+      }
+    }
+    if constexpr (WHOLE) return;
+    tile_first += length;
+    if (tile_first >= u1) return;
+    if (++t == T) {
+      t = 0;
+      if (++hh == heads) {
+        hh = 0;
+        do {
+          if (++s >= a.n_seq) return;
+          q = uniform_seq(chunk_seq(a, s));
+          T = tiles_of(q);
+        } while (T == 0);
+      }
+    }
+  }
+}
+
+// Joins the sums of tiles that a cut divides: workgroup p those of the tile that run p ended, D / 4 threads a row.
+template <int D, int SPLIT, int NW>
+__global__ __launch_bounds__(kJoinThreads) void cache4_chunk_join_kernel(CacheChunkArgs a) {
+  constexpr bool F32 = SPLIT > 1;
+  constexpr int LPR = D / 4, ROWS = kJoinThreads / LPR, QT = 32 * NW;
+  const int p1 = blockIdx.x, s = a.joins[4 * p1];
+  if (s < 0) return;
+  const int hh = a.joins[4 * p1 + 1], t = a.joins[4 * p1 + 2], p0 = a.joins[4 * p1 + 3];
+  const ChunkSeq q = chunk_seq(a, s);
+  const int kv = hh / a.subs, head0 = kv * a.group + (hh - kv * a.subs) * a.sub_group;
+  const int r = blockIdx.y * ROWS + threadIdx.x / LPR, ch = threadIdx.x % LPR * 4;
+  const int r_tok = r / a.sub_group, head = head0 + (r - r_tok * a.sub_group), tok = t * a.tile_tokens + r_tok;
+  if (r_tok >= a.tile_tokens || tok >= q.n || head >= (kv + 1) * a.group) return;
+  auto exp_of = [](float x) { return F32 ? expf(x) : __builtin_amdgcn_exp2f(x); };
+  float m = -INFINITY, l = 0.f;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  for (int p = p0; p <= p1; ++p) {
+    const int64_t row = (2 * (int64_t)p + (p == p0)) * QT + r;
+    const float pm = a.part_ml[2 * row], pl = a.part_ml[2 * row + 1];
+    const f32x4 v = *reinterpret_cast<const f32x4*>(a.part_o + row * D + ch);
+    const float top = fmaxf(m, pm), ref = top == -INFINITY ? 0.f : top, w0 = exp_of(m - ref), w1 = exp_of(pm - ref);
+    acc = w0 * acc + w1 * v;
+    l = w0 * l + w1 * pl;
+    m = top;
+  }
+  const bool empty = l == 0.f;
+  acc *= empty ? 0.f : 1.f / l;
+  const int64_t at = (int64_t)(q.start + tok) * a.o.row + (int64_t)head * a.o.head + ch;
+  if constexpr (F32) *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.out) + at) = acc;
+  else *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(a.out) + at) = (u32x2){pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3])};
+  if (ch == 0) a.lse[(int64_t)head * a.rows + q.start + tok] = empty ? -INFINITY : F32 ? m + logf(l) : (m + log2f(l)) * kLn2;
+}
+
+// Tables of few tokens: a workgroup per tile, and no second launch.
+void cache4_chunk_split(CacheChunkArgs* a) {
+  a->subs = (a->group + kChunkRows - 1) / kChunkRows;
+  a->sub_group = (a->group + a->subs - 1) / a->subs;
+  a->tile_tokens = kChunkRows / a->sub_group;
+  const int64_t tokens = (int64_t)a->max_blocks << a->c.log_page, heads = (int64_t)a->c.Hk * a->subs;
+  const int64_t tiles = ((int64_t)a->rows / a->tile_tokens + a->n_seq) * heads;
+  if (tokens <= 1024 && tiles <= kMaxLaunch) {
+    a->parts = 0;
+    return;
+  }
+  const int64_t runs = tiles * (tokens + kTileCost) / kLeastRun;
+  a->parts = (int32_t)(runs < 1 ? 1 : runs > kMostParts ? kMostParts : runs);
+}
+
+template <int D, int SPLIT, int NW>
+static int launch_chunk_one(const CacheChunkArgs& a, hipStream_t st) {
+  constexpr size_t lds = ChunkLds<D>::bytes(NW);
+  static std::atomic<uint64_t> set_whole{0}, set_parts{0};
+  if (a.parts == 0) {
+    const auto kernel = &cache4_chunk_kernel<D, SPLIT, NW, true>;
+    const int rc = allow_full_lds(reinterpret_cast<const void*>(kernel), set_whole);
+    if (rc != HA_OK) return rc;
+    const int64_t grid = ((int64_t)a.rows / a.tile_tokens + a.n_seq) * a.c.Hk * a.subs;  // tiles that there can be
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * NW), lds, st, a);
+    return check_launch();
+  }
+  const auto kernel = &cache4_chunk_kernel<D, SPLIT, NW, false>;
+  int rc = allow_full_lds(reinterpret_cast<const void*>(kernel), set_parts);
+  if (rc != HA_OK) return rc;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)a.parts), dim3(64 * NW), lds, st, a);
+  rc = check_launch();
+  if (rc != HA_OK) return rc;
+  constexpr int per = kJoinThreads / (D / 4);
+  hipLaunchKernelGGL((cache4_chunk_join_kernel<D, SPLIT, NW>), dim3((unsigned)a.parts, 32 * NW / per), dim3(kJoinThreads), 0, st, a);
+  return check_launch();
+}
+
+int launch_cache4_chunk(const CacheChunkArgs& a, int dtype, hipStream_t st) {
+  if (a.c.d == 128) return dtype == HA_BF16 ? launch_chunk_one<128, 1, 4>(a, st) : launch_chunk_one<128, 3, 4>(a, st);
+  return dtype == HA_BF16 ? launch_chunk_one<64, 1, 4>(a, st) : launch_chunk_one<64, 3, 4>(a, st);
+}
+
+}  // namespace ha

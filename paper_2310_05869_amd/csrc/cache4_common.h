@@ -59,6 +59,33 @@ int cache4_parts(int Hk, int tiles);
 int cache4_whole(const CacheAttnArgs& a);   // waves of a workgroup that takes a whole sequence, 0: tokens are shared out
 bool cache4_once(const CacheAttnArgs& a);   // of shared-out tokens: codes are read past the caches
 
+// Chunks of new tokens over the cache (cache4_chunk.h)
+struct CacheChunkArgs {
+  const void* Q;
+  const unsigned char* cache;
+  const int32_t* cu;
+  const int32_t* table;
+  const int32_t* lens;
+  void* out;
+  float* lse;                // attention writes it, the sums of weights read it
+  float* weights;            // sums of weights: [n_pages][Hk][page]
+  CacheGeometry c;
+  RowStrides q, o;
+  int32_t n_seq, rows, Hq, max_blocks;
+  int32_t group;             // query heads per key head
+  int32_t subs, sub_group;   // a key head's query heads in `subs` runs of sub_group, each of which fits a tile
+  int32_t tile_tokens;       // new tokens of a tile: tile_tokens * sub_group rows
+  int32_t fresh;             // sums of weights: earlier ones do not count
+  int32_t parts;             // workgroups that share all work; 0: a workgroup per tile
+  // workspace: per workgroup, the tile that it ends of those that others began (four integers), and two tiles of sums with their references and row sums
+  int32_t* joins;
+  float* part_o;
+  float* part_ml;
+};
+int launch_cache4_chunk(const CacheChunkArgs& a, int dtype, hipStream_t st);
+void cache4_chunk_split(CacheChunkArgs* a);  // sets subs, sub_group, tile_tokens and parts
+constexpr int kChunkRows = 128;              // query rows of a tile
+
 struct PagePlanArgs {
   const int32_t* lens;
   const int32_t* add;

@@ -77,6 +77,38 @@ static AttnSpace attn_space(const CacheAttnArgs& a) {
   return s;
 }
 
+// Fills all of *a but the pointers and strides.
+static int chunk_geometry(const ha_cache4* shape, const ha_cache4_chunk* q, CacheChunkArgs* a) {
+  const int rc = cache_geometry(shape, &a->c);
+  if (rc != HA_OK) return rc;
+  if (!q) return HA_ERR_NULL;
+  if (q->dtype != HA_BF16 && q->dtype != HA_FP32) return HA_ERR_DTYPE;
+  if (q->n_seq < 0 || q->n_seq > (1 << 16) || q->rows < 0 || q->rows > (1 << 22) || q->max_blocks < 0) return HA_ERR_SHAPE;
+  if (q->Hq < 1 || q->Hq > 1024 || q->Hq % shape->Hk != 0) return HA_ERR_SHAPE;
+  if ((int64_t)q->rows * q->Hq > (1 << 26) || (int64_t)q->n_seq * q->Hq > (1 << 22)) return HA_ERR_SHAPE;
+  if ((int64_t)q->n_seq * q->max_blocks > (1ll << 30) || (int64_t)q->max_blocks * shape->page > 0x7fffffffll - 256) return HA_ERR_SHAPE;
+  a->n_seq = q->n_seq;
+  a->rows = q->rows;
+  a->Hq = q->Hq;
+  a->max_blocks = q->max_blocks;
+  a->group = q->Hq / shape->Hk;
+  return HA_OK;
+}
+
+struct ChunkSpace {
+  size_t part_o, part_ml, total;
+};
+static ChunkSpace chunk_space(CacheChunkArgs a) {
+  cache4_chunk_split(&a);
+  auto align = [](size_t x) { return (x + 255) & ~(size_t)255; };
+  const size_t rows = 2 * (size_t)a.parts * kChunkRows;
+  ChunkSpace s;
+  s.part_o = align((size_t)a.parts * 16);
+  s.part_ml = s.part_o + align(rows * a.c.d * 4);
+  s.total = s.part_ml + align(rows * 8);
+  return s;
+}
+
 }  // namespace ha
 
 using namespace ha;
@@ -141,6 +173,42 @@ int ha_cache4_attn(const void* Q, const void* cache, const int32_t* block_table,
   a.part_o = reinterpret_cast<float*>(w + sp.part_o);
   a.part_ml = reinterpret_cast<float*>(w + sp.part_ml);
   return launch_cache4_attn(a, query->dtype, (hipStream_t)stream);
+}
+
+size_t ha_cache4_attn_chunk_workspace_bytes(const ha_cache4* shape, const ha_cache4_chunk* chunk) {
+  CacheChunkArgs a{};
+  return chunk_geometry(shape, chunk, &a) == HA_OK ? chunk_space(a).total : 0;
+}
+
+int ha_cache4_attn_chunk(const void* Q, const void* cache, const int32_t* cu_seqlens, const int32_t* block_table, const int32_t* lens, void* out,
+                         float* lse, const ha_cache4* shape, const ha_cache4_chunk* chunk, const ha_strides* qo, void* workspace,
+                         size_t workspace_bytes, void* stream) {
+  CacheChunkArgs a{};
+  int rc = chunk_geometry(shape, chunk, &a);
+  if (rc != HA_OK) return rc;
+  rc = row_strides(qo, a.rows, a.Hq, a.c.d, chunk->dtype, false, &a.q);
+  if (rc == HA_OK) rc = row_strides(qo ? qo + 1 : nullptr, a.rows, a.Hq, a.c.d, chunk->dtype, true, &a.o);
+  if (rc != HA_OK) return rc;
+  if (a.n_seq == 0 || a.rows == 0) return HA_OK;
+  const ChunkSpace sp = chunk_space(a);
+  if (!Q || !cu_seqlens || !lens || !out || !lse || (sp.total > 0 && !workspace) || (!cache && a.c.n_pages > 0) || (!block_table && a.max_blocks > 0))
+    return HA_ERR_NULL;
+  if (any_misaligned16(Q, cache, out) || any_misaligned4(cu_seqlens, block_table, lens, lse)) return HA_ERR_ALIGN;
+  if (workspace_bytes < sp.total || ((uintptr_t)workspace & 255) != 0) return HA_ERR_WORKSPACE;
+  if (a.c.n_pages == 0) a.max_blocks = 0;  // (no page is there: every sequence counts as empty)
+  a.Q = Q;
+  a.cache = reinterpret_cast<const unsigned char*>(cache);
+  a.cu = cu_seqlens;
+  a.table = block_table;
+  a.lens = lens;
+  a.out = out;
+  a.lse = lse;
+  unsigned char* w = reinterpret_cast<unsigned char*>(workspace);
+  a.joins = reinterpret_cast<int32_t*>(w);
+  a.part_o = reinterpret_cast<float*>(w + sp.part_o);
+  a.part_ml = reinterpret_cast<float*>(w + sp.part_ml);
+  cache4_chunk_split(&a);
+  return launch_cache4_chunk(a, chunk->dtype, (hipStream_t)stream);
 }
 
 int ha_page_plan(const int32_t* lens, const int32_t* add, int32_t* block_table, int32_t* free_pages, const int32_t* free_count,

@@ -1,0 +1,68 @@
+"""Refusals of the calls over chunks of new tokens that need no GPU.  (The addresses here are never dereferenced.)"""
+import struct
+
+import pytest
+
+from test_host_packed_cache import ALIGN, DTYPE, NULL, OK, SHAPE, WORKSPACE, cache, ha  # noqa: F401  (ha: fixture)
+
+
+def chunk(n_seq=2, rows=10, Hq=4, dtype=0, max_blocks=100):
+    return struct.pack("5i", n_seq, rows, Hq, dtype, max_blocks)
+
+
+def attn(ha, p=None, c=None, q=None, st=None, ws=OK, nbytes=1 << 40):
+    return ha.lib().ha_cache4_attn_chunk(*(p or [OK] * 7), c or cache(), q or chunk(), st, ws, nbytes, None)
+
+
+BAD = [(dict(n_seq=-1), SHAPE), (dict(n_seq=(1 << 16) + 1), SHAPE), (dict(rows=-1), SHAPE), (dict(rows=(1 << 22) + 1), SHAPE), (dict(Hq=0), SHAPE), (dict(Hq=3), SHAPE),
+       (dict(Hq=2048), SHAPE), (dict(rows=1 << 22, Hq=32), SHAPE), (dict(n_seq=1 << 16, Hq=128), SHAPE), (dict(max_blocks=-1), SHAPE), (dict(max_blocks=0x7FFFFFFF), SHAPE),
+       (dict(n_seq=1 << 16, max_blocks=1 << 15), SHAPE), (dict(dtype=2), DTYPE)]
+
+
+@pytest.mark.parametrize("over,status", BAD)
+def test_sizes(ha, over, status):
+    assert attn(ha, q=chunk(**over)) == status
+    assert ha.lib().ha_cache4_attn_chunk_workspace_bytes(cache(), chunk(**over)) == 0
+
+
+def test_nothing_to_do(ha):
+    assert attn(ha, q=chunk(n_seq=0)) == 0 and attn(ha, q=chunk(rows=0)) == 0
+
+
+def test_pointers_strides_and_workspace(ha):
+    need = ha.lib().ha_cache4_attn_chunk_workspace_bytes(cache(), chunk())
+    assert 0 < need <= 65 << 20
+    for i in range(7):
+        p = [OK] * 7
+        p[i] = None
+        assert attn(ha, p) == NULL, i
+        p[i] = OK + 2
+        assert attn(ha, p) == ALIGN, i
+    assert attn(ha, c=struct.pack("4i", 8, 16, 2, 96)) == SHAPE and attn(ha, ws=None) == NULL
+    assert attn(ha, nbytes=need - 1) == WORKSPACE and attn(ha, ws=OK + 128, nbytes=need) == WORKSPACE
+    for bad, status in (((32, 64), SHAPE), ((1 << 23, 64), SHAPE), ((256, -8), SHAPE), ((260, 64), ALIGN), ((256, 4), ALIGN)):
+        assert attn(ha, st=struct.pack("4q", *bad, 256, 64)) == status, bad
+    for bad in ((256, 0), (256, 32), (128, 64), (64, 9 * 64)):   # rows of heads that overlap may be read, not written
+        assert attn(ha, st=struct.pack("4q", 256, 64, *bad), nbytes=0) == SHAPE, bad
+        assert attn(ha, st=struct.pack("4q", 256, 0, 256, 64), nbytes=0) == WORKSPACE
+    # tables of few tokens need none; the most that any call needs
+    assert ha.lib().ha_cache4_attn_chunk_workspace_bytes(cache(), chunk(max_blocks=4)) == 0
+    assert ha.lib().ha_cache4_attn_chunk_workspace_bytes(cache(d=128, page=256), chunk(n_seq=1000, rows=1 << 20, Hq=64, max_blocks=10000)) <= 65 << 20
+
+
+def test_binding_refuses_what_a_kernel_cannot_take(ha):
+    """On tensors of the CPU every call raises before it reaches the library."""
+    import torch
+    i32 = torch.int32
+    Q, cu, lens = torch.zeros(6, 4, 64, dtype=torch.bfloat16), torch.zeros(3, dtype=i32), torch.zeros(2, dtype=i32)
+    pages, table = torch.zeros(4, 2, 16 * 68, dtype=torch.uint8), torch.zeros(2, 5, dtype=i32)
+    with pytest.raises(ValueError, match="Q has shape"):
+        ha.ha_cache4_attn_chunk(Q[0], pages, cu, table, lens, 16)
+    with pytest.raises(ValueError, match="cache has shape"):
+        ha.ha_cache4_attn_chunk(Q, pages, cu, table, lens, 32)
+    with pytest.raises(ValueError, match="n_seq"):
+        ha.ha_cache4_attn_chunk(Q, pages, cu[:2], table, lens, 16)
+    with pytest.raises(TypeError):
+        ha.ha_cache4_attn_chunk(Q.half(), pages, cu, table, lens, 16)
+    with pytest.raises(ValueError, match="device tensor"):
+        ha.ha_cache4_attn_chunk(Q, pages, cu, table, lens, 16)
