@@ -516,6 +516,21 @@ int ha_cache4_attn_chunk(const void* Q, const void* cache, const int32_t* cu_seq
                          size_t workspace_bytes, void* stream);
 size_t ha_cache4_attn_chunk_workspace_bytes(const ha_cache4* shape, const ha_cache4_chunk* chunk); /* 0 too if not valid */
 
+/* What attention weight the cache's tokens got from new queries: for token t of sequence s and key head h the sum, over the rows i of the sequence that see it and the query
+ * heads x of h, of exp(<Q[i][x], K[t][h]> - lse[x][i]), by what ha_cache4_attn_chunk (or, with one row a sequence, ha_cache4_attn) gave as lse for the same Q, cu_seqlens,
+ * block_table and lens.  Rows of part of the new tokens are taken too, as long as they are the last ones.
+ *   weights: float [n_pages][Hk][page], 4-byte aligned: token t's lies at weights[block_table[s][t / page]][h][t % page], as its rows do in the cache, and goes where
+ *   these go.  Tokens that the rows bring (the last cu_seqlens[s + 1] - cu_seqlens[s] of lens[s]) start from 0; for the others the sum is added to what is there,
+ *   or, with fresh != 0, also starts from 0.  Nothing else is touched: not what lies behind a sequence, nor pages that no sequence holds.
+ *   A page belongs to one sequence and lies once in its row of block_table: where two places name one page it holds the sum of some of them.
+ * Sums are fp32 in a fixed order (same inputs, same bits); a row whose lse is -inf gives nothing, one that is NaN makes what it sees NaN, and so does a NaN in K its token.
+ * fp32 queries as in ha_cache4_attn.  Sizes as in ha_cache4_attn_chunk.  workspace: device, 256-byte aligned, >= ha_cache4_weights_workspace_bytes() (at most 2 MiB;
+ * 0: none is needed, and it may be NULL); nothing in it is kept. */
+int ha_cache4_weights(const void* Q, const void* cache, const int32_t* cu_seqlens, const int32_t* block_table, const int32_t* lens, const float* lse,
+                      float* weights, const ha_cache4* shape, const ha_cache4_chunk* chunk, int32_t fresh, const ha_strides* q, void* workspace,
+                      size_t workspace_bytes, void* stream);
+size_t ha_cache4_weights_workspace_bytes(const ha_cache4* shape, const ha_cache4_chunk* chunk); /* 0 too if not valid */
+
 /* Block tables and slots, on the GPU from the sequences' lengths: one launch before a step's rows are written.
  *   lens[s]   tokens that sequence s holds, in pages block_table[s][0 ... ceil(lens / page) - 1]
  *   add[s]    >= 0: rows that the step appends to it; < 0: it has ended, its pages are free again

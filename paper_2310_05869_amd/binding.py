@@ -108,6 +108,8 @@ _SIGNATURES = {
     "ha_cache4_attn_form": (c_int, [c_void_p, c_void_p, POINTER(c_int32), POINTER(c_int32)]),
     "ha_cache4_attn_chunk": (c_int, [c_void_p] * 7 + [c_void_p, c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
     "ha_cache4_attn_chunk_workspace_bytes": (c_size_t, [c_void_p, c_void_p]),
+    "ha_cache4_weights": (c_int, [c_void_p] * 7 + [c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "ha_cache4_weights_workspace_bytes": (c_size_t, [c_void_p, c_void_p]),
     "ha_page_plan": (c_int, [c_void_p] * 9 + [c_void_p, c_void_p]),
     "ha_measure_mfma_rate": (c_int, [c_void_p, c_size_t, c_int32, POINTER(c_float), c_void_p]),
     "ha_measure_hbm_rate": (c_int, [c_void_p, c_size_t, POINTER(c_float), POINTER(c_float), c_void_p]),
@@ -730,6 +732,7 @@ _PACKED = struct.Struct("7i")
 _PACKED_STRIDES = struct.Struct("16q")
 _STRIDES2 = struct.Struct("4q")
 _CACHE4 = struct.Struct("4i")
+_STRIDES1 = struct.Struct("2q")
 _FIVE = struct.Struct("5i")  # ha_cache4_query, ha_cache4_chunk, ha_page_plan_shape
 
 
@@ -1028,6 +1031,35 @@ def ha_cache4_attn_chunk(Q, cache, cu_seqlens, block_table, lens, page, out=None
                                       out.data_ptr(), _whole(lse, "lse", (Hq, rows), torch.float32, dev), sizes, chunk, qo,
                                       _bytes(workspace, "workspace", dev), workspace.numel(), handle), "ha_cache4_attn_chunk")
     return out, lse
+
+
+def alloc_cache4_weights(n_pages, page, Hk, device="cuda"):
+    """The weights that go with a cache of these sizes, float32 [n_pages, Hk, page], zeros."""
+    return _torch().zeros((n_pages, Hk, page), dtype=_torch().float32, device=device)
+
+
+def ha_cache4_weights_workspace_bytes(cache, page, n_seq, rows, Hq, max_blocks, dtype=None) -> int:
+    code = HA_BF16 if dtype is None else _code(dtype)
+    return int(lib().ha_cache4_weights_workspace_bytes(_CACHE4.pack(*_cache4(cache, page)), _FIVE.pack(n_seq, rows, Hq, code, max_blocks)))
+
+
+def ha_cache4_weights(Q, cache, cu_seqlens, block_table, lens, lse, weights, page, fresh=False, workspace=None, stream=None):
+    """weights (float32 [n_pages, Hk, page], changed in place): the attention weight that every token of the sequences got from their new queries is added to what
+    lies at its place; tokens that the rows bring start from 0, with `fresh` all do.  Q, cu_seqlens, block_table, lens as ha_cache4_attn_chunk took them, lse as it
+    gave it (float32 [Hq, rows])."""
+    torch = _torch()
+    full, sizes, chunk = _chunk_call(Q, cache, cu_seqlens, block_table, page)
+    rows, Hq, _ = full
+    i32, f32 = torch.int32, torch.float32
+    dev, handle = _here(cache, "cache", stream)
+    if workspace is None:
+        workspace = _empty(stream, (int(lib().ha_cache4_weights_workspace_bytes(sizes, chunk)),), torch.uint8, Q)
+    _check(lib().ha_cache4_weights(Q.data_ptr(), _bytes(cache, "cache", dev), _whole(cu_seqlens, "cu_seqlens", cu_seqlens.shape, i32, dev),
+                                   _whole(block_table, "block_table", block_table.shape, i32, dev), _whole(lens, "lens", (block_table.shape[0],), i32, dev),
+                                   _whole(lse, "lse", (Hq, rows), f32, dev), _whole(weights, "weights", (cache.shape[0], cache.shape[1], page), f32, dev), sizes, chunk,
+                                   1 if fresh else 0, _STRIDES1.pack(*_rows(Q, "Q", full, Q.dtype, dev)), _bytes(workspace, "workspace", dev), workspace.numel(), handle),
+           "ha_cache4_weights")
+    return weights
 
 
 def ha_page_plan(lens, add, block_table, free_pages, free_count, page, rows=None, lens_out=None, cu_seqlens=None, slots=None, free_count_out=None,

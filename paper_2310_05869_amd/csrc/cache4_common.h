@@ -77,6 +77,8 @@ struct CacheChunkArgs {
   int32_t tile_tokens;       // new tokens of a tile: tile_tokens * sub_group rows
   int32_t fresh;             // sums of weights: earlier ones do not count
   int32_t parts;             // workgroups that share all work; 0: a workgroup per tile
+  int32_t cut, least_run;    // sums of weights: whether tiles are shared among workgroups, and what each of these takes at least
+  FastDiv div_group;
   // workspace: per workgroup, the tile that it ends of those that others began (four integers), and two tiles of sums with their references and row sums
   int32_t* joins;
   float* part_o;
@@ -85,6 +87,10 @@ struct CacheChunkArgs {
 int launch_cache4_chunk(const CacheChunkArgs& a, int dtype, hipStream_t st);
 void cache4_chunk_split(CacheChunkArgs* a);  // sets subs, sub_group, tile_tokens and parts
 constexpr int kChunkRows = 128;              // query rows of a tile
+int launch_cache4_weights(const CacheChunkArgs& a, int dtype, hipStream_t st);
+void cache4_weights_split(CacheChunkArgs* a);  // sets div_group, cut, least_run and parts
+constexpr int kWeightsParts = 512;             // workgroups that the chip holds at once, two per CU
+constexpr int kWeightsTokens = 256;            // of a tile
 
 struct PagePlanArgs {
   const int32_t* lens;

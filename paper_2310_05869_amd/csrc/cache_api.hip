@@ -211,6 +211,48 @@ int ha_cache4_attn_chunk(const void* Q, const void* cache, const int32_t* cu_seq
   return launch_cache4_chunk(a, chunk->dtype, (hipStream_t)stream);
 }
 
+static size_t weights_space(const CacheChunkArgs& a, size_t* sums) {
+  auto align = [](size_t x) { return (x + 255) & ~(size_t)255; };
+  *sums = a.cut ? align((size_t)a.parts * 16) : 0;
+  return a.cut ? *sums + align(2 * (size_t)a.parts * kWeightsTokens * 4) : 0;
+}
+
+size_t ha_cache4_weights_workspace_bytes(const ha_cache4* shape, const ha_cache4_chunk* chunk) {
+  CacheChunkArgs a{};
+  if (chunk_geometry(shape, chunk, &a) != HA_OK) return 0;
+  cache4_weights_split(&a);
+  size_t sums;
+  return weights_space(a, &sums);
+}
+
+int ha_cache4_weights(const void* Q, const void* cache, const int32_t* cu_seqlens, const int32_t* block_table, const int32_t* lens, const float* lse,
+                      float* weights, const ha_cache4* shape, const ha_cache4_chunk* chunk, int32_t fresh, const ha_strides* q, void* workspace,
+                      size_t workspace_bytes, void* stream) {
+  CacheChunkArgs a{};
+  int rc = chunk_geometry(shape, chunk, &a);
+  if (rc != HA_OK) return rc;
+  rc = row_strides(q, a.rows, a.Hq, a.c.d, chunk->dtype, false, &a.q);
+  if (rc != HA_OK) return rc;
+  if (a.n_seq == 0 || a.c.n_pages == 0 || a.max_blocks == 0 || (a.rows == 0 && !fresh)) return HA_OK;
+  cache4_weights_split(&a);
+  size_t sums;
+  const size_t total = weights_space(a, &sums);
+  if ((a.rows > 0 && (!Q || !lse)) || !cache || !cu_seqlens || !block_table || !lens || !weights || (total > 0 && !workspace)) return HA_ERR_NULL;
+  if (any_misaligned16(Q, cache) || any_misaligned4(cu_seqlens, block_table, lens, lse, weights)) return HA_ERR_ALIGN;
+  if (workspace_bytes < total || ((uintptr_t)workspace & 255) != 0) return HA_ERR_WORKSPACE;
+  a.Q = Q;
+  a.cache = reinterpret_cast<const unsigned char*>(cache);
+  a.cu = cu_seqlens;
+  a.table = block_table;
+  a.lens = lens;
+  a.lse = const_cast<float*>(lse);
+  a.weights = weights;
+  a.fresh = fresh != 0;
+  a.joins = reinterpret_cast<int32_t*>(workspace);
+  a.part_o = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(workspace) + sums);
+  return launch_cache4_weights(a, chunk->dtype, (hipStream_t)stream);
+}
+
 int ha_page_plan(const int32_t* lens, const int32_t* add, int32_t* block_table, int32_t* free_pages, const int32_t* free_count,
                  int32_t* lens_out, int32_t* cu_seqlens, int32_t* slots, int32_t* free_count_out, const ha_page_plan_shape* sh,
                  void* stream) {

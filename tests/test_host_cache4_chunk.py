@@ -14,6 +14,10 @@ def attn(ha, p=None, c=None, q=None, st=None, ws=OK, nbytes=1 << 40):
     return ha.lib().ha_cache4_attn_chunk(*(p or [OK] * 7), c or cache(), q or chunk(), st, ws, nbytes, None)
 
 
+def weights(ha, p=None, c=None, q=None, st=None, ws=OK, nbytes=1 << 40, fresh=0):
+    return ha.lib().ha_cache4_weights(*(p or [OK] * 7), c or cache(), q or chunk(), fresh, st, ws, nbytes, None)
+
+
 BAD = [(dict(n_seq=-1), SHAPE), (dict(n_seq=(1 << 16) + 1), SHAPE), (dict(rows=-1), SHAPE), (dict(rows=(1 << 22) + 1), SHAPE), (dict(Hq=0), SHAPE), (dict(Hq=3), SHAPE),
        (dict(Hq=2048), SHAPE), (dict(rows=1 << 22, Hq=32), SHAPE), (dict(n_seq=1 << 16, Hq=128), SHAPE), (dict(max_blocks=-1), SHAPE), (dict(max_blocks=0x7FFFFFFF), SHAPE),
        (dict(n_seq=1 << 16, max_blocks=1 << 15), SHAPE), (dict(dtype=2), DTYPE)]
@@ -23,10 +27,14 @@ BAD = [(dict(n_seq=-1), SHAPE), (dict(n_seq=(1 << 16) + 1), SHAPE), (dict(rows=-
 def test_sizes(ha, over, status):
     assert attn(ha, q=chunk(**over)) == status
     assert ha.lib().ha_cache4_attn_chunk_workspace_bytes(cache(), chunk(**over)) == 0
+    assert weights(ha, q=chunk(**over)) == status
+    assert ha.lib().ha_cache4_weights_workspace_bytes(cache(), chunk(**over)) == 0
 
 
 def test_nothing_to_do(ha):
     assert attn(ha, q=chunk(n_seq=0)) == 0 and attn(ha, q=chunk(rows=0)) == 0
+    for nothing in (dict(q=chunk(n_seq=0)), dict(q=chunk(rows=0)), dict(q=chunk(max_blocks=0)), dict(c=cache(n_pages=0))):
+        assert weights(ha, **nothing) == 0
 
 
 def test_pointers_strides_and_workspace(ha):
@@ -50,6 +58,23 @@ def test_pointers_strides_and_workspace(ha):
     assert ha.lib().ha_cache4_attn_chunk_workspace_bytes(cache(d=128, page=256), chunk(n_seq=1000, rows=1 << 20, Hq=64, max_blocks=10000)) <= 66 << 20
 
 
+def test_pointers_strides_and_workspace_of_weights(ha):
+    many = chunk(rows=1000)
+    need = ha.lib().ha_cache4_weights_workspace_bytes(cache(), many)
+    assert 0 < need <= 2 << 20 and ha.lib().ha_cache4_weights_workspace_bytes(cache(), chunk(rows=2)) == 0
+    for i in range(7):
+        p = [OK] * 7
+        p[i] = None
+        assert weights(ha, p, q=many) == NULL, i
+        p[i] = OK + 2
+        assert weights(ha, p, q=many) == ALIGN, i
+    assert weights(ha, c=struct.pack("4i", 8, 16, 2, 96)) == SHAPE and weights(ha, q=many, ws=None) == NULL
+    assert weights(ha, q=many, nbytes=need - 1) == WORKSPACE and weights(ha, q=many, ws=OK + 128, nbytes=need) == WORKSPACE
+    for bad, status in (((32, 64), SHAPE), ((1 << 23, 64), SHAPE), ((256, -8), SHAPE), ((260, 64), ALIGN), ((256, 4), ALIGN)):
+        assert weights(ha, q=many, st=struct.pack("2q", *bad)) == status, bad
+    assert weights(ha, q=many, st=struct.pack("2q", 64, 0), nbytes=0) == WORKSPACE   # heads that share elements may be read
+
+
 def test_binding_refuses_what_a_kernel_cannot_take(ha):
     """On tensors of the CPU every call raises before it reaches the library."""
     import torch
@@ -66,3 +91,35 @@ def test_binding_refuses_what_a_kernel_cannot_take(ha):
         ha.ha_cache4_attn_chunk(Q.half(), pages, cu, table, lens, 16)
     with pytest.raises(ValueError, match="device tensor"):
         ha.ha_cache4_attn_chunk(Q, pages, cu, table, lens, 16)
+    lse, w = torch.zeros(4, 6), ha.alloc_cache4_weights(4, 16, 2, device="cpu")
+    assert w.shape == (4, 2, 16) and (w == 0).all()
+    with pytest.raises(ValueError, match="n_seq"):
+        ha.ha_cache4_weights(Q, pages, cu[:2], table, lens, lse, w, 16)
+    with pytest.raises(ValueError, match="device tensor"):
+        ha.ha_cache4_weights(Q, pages, cu, table, lens, lse, w, 16)
+
+
+@pytest.mark.gpu
+def test_binding_refuses_tensors_that_do_not_fit(ha):
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    i32 = torch.int32
+    Q, cu, lens = torch.zeros(6, 4, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(3, dtype=i32, device="cuda"), torch.zeros(2, dtype=i32, device="cuda")
+    pages, table = torch.zeros(4, 2, 16 * 68, dtype=torch.uint8, device="cuda"), torch.zeros(2, 5, dtype=i32, device="cuda")
+    lse, w = torch.zeros(4, 6, device="cuda"), ha.alloc_cache4_weights(4, 16, 2)
+    for call, what in ((lambda: ha.ha_cache4_attn_chunk(Q, pages, cu, table, lens[:1], 16), "lens has shape"),
+                       (lambda: ha.ha_cache4_attn_chunk(Q, pages, cu, table, lens, 16, lse=lse.T), "lse has shape"),
+                       (lambda: ha.ha_cache4_attn_chunk(Q.cpu(), pages, cu, table, lens, 16), "Q is on"),
+                       (lambda: ha.ha_cache4_attn_chunk(Q, pages, cu, table.T.contiguous().T, lens, 16), "contiguous"),
+                       (lambda: ha.ha_cache4_weights(Q, pages, cu, table, lens, lse, w[:3], 16), "weights has shape"),
+                       (lambda: ha.ha_cache4_weights(Q, pages, cu, table, lens, lse[:3], w, 16), "lse has shape"),
+                       (lambda: ha.ha_cache4_weights(Q, pages, cu, table, lens, lse, w.cpu(), 16), "weights is on")):
+        with pytest.raises(ValueError, match=what):
+            call()
+    with pytest.raises(TypeError):
+        ha.ha_cache4_weights(Q, pages, cu, table, lens, lse, w.double(), 16)
+    with pytest.raises(TypeError):
+        ha.ha_cache4_attn_chunk(Q, pages, cu.long(), table, lens, 16)
+    with pytest.raises(ha.HyperAttnError):
+        ha.ha_cache4_attn_chunk(Q, pages, cu, torch.zeros(2, 500, dtype=i32, device="cuda"), lens, 16, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
