@@ -519,7 +519,7 @@ size_t ha_cache4_attn_chunk_workspace_bytes(const ha_cache4* shape, const ha_cac
 /* What attention weight the cache's tokens got from new queries: for token t of sequence s and key head h the sum, over the rows i of the sequence that see it and the query
  * heads x of h, of exp(<Q[i][x], K[t][h]> - lse[x][i]), by what ha_cache4_attn_chunk (or, with one row a sequence, ha_cache4_attn) gave as lse for the same Q, cu_seqlens,
  * block_table and lens.  Rows of part of the new tokens are taken too, as long as they are the last ones.
- *   weights: float [n_pages][Hk][page], 4-byte aligned: token t's lies at weights[block_table[s][t / page]][h][t % page], as its rows do in the cache, and goes where
+ *   weights: float [n_pages][Hk][page], 16-byte aligned: token t's lies at weights[block_table[s][t / page]][h][t % page], as its rows do in the cache, and goes where
  *   these go.  Tokens that the rows bring (the last cu_seqlens[s + 1] - cu_seqlens[s] of lens[s]) start from 0; for the others the sum is added to what is there,
  *   or, with fresh != 0, also starts from 0.  Nothing else is touched: not what lies behind a sequence, nor pages that no sequence holds.
  *   A page belongs to one sequence and lies once in its row of block_table: where two places name one page it holds the sum of some of them.
@@ -530,6 +530,30 @@ int ha_cache4_weights(const void* Q, const void* cache, const int32_t* cu_seqlen
                       float* weights, const ha_cache4* shape, const ha_cache4_chunk* chunk, int32_t fresh, const ha_strides* q, void* workspace,
                       size_t workspace_bytes, void* stream);
 size_t ha_cache4_weights_workspace_bytes(const ha_cache4* shape, const ha_cache4_chunk* chunk); /* 0 too if not valid */
+
+/* Eviction: sequence s, of n = lens[s] tokens, is cut to k = keep[s] (device int32 [n_seq]; negative, or at least n: it stays as it is).  Its last r = min(recent, k) tokens stay,
+ * and of the n - r others, for every key head by itself, the k - r of largest weights[page][h][token] (as ha_cache4_weights lays them out), of equal ones the first; NaN,
+ * and what lies in a page that is not there, counts less than any number.  Afterwards the sequence has places 0 ... k - 1 of its pages:
+ *   places 0 ... k - r - 1: kept tokens that lie there stay; the other kept ones, in order, fill the places between, in order
+ *   places k - r ... k - 1: the last r tokens, in order
+ * (attention does not ask for the order of tokens that all its rows see; a token's place is another one for every key head).  Rows of K and V move as they lie, and
+ * their weights go with them, read from weights and written to weights_out, which may be the same array (entries of rows that stay are not written).  What the places hold that
+ * come free is not defined.
+ *   lens_out[s]   k, or the length where the sequence stays as it is
+ *   free_pages    the pages that its tokens no longer need, block_table[s][ceil(k / page) ... ceil(n / page) - 1], are put on top of the stack, sequences in order
+ *   free_count_out  as ha_page_plan has them (at most n_pages)
+ * block_table is not changed: lens_out tells which entries count.  A page belongs to one sequence and lies once in its row; rows from or to pages that are
+ * not there are left out.  lens are taken within [0, max_blocks * page].  lens_out may be neither lens nor keep, free_count_out not free_count.
+ * n_seq <= 8192, n_seq * Hk <= 2^20, n_seq * max_blocks <= 2^30, max_blocks * page <= 2^30.  weights, weights_out: 16-byte aligned.
+ * workspace: device, 256-byte aligned, >= ha_cache4_evict_workspace_bytes(): four bytes for every token and key head that the table has room for; nothing in it is kept. */
+typedef struct {
+  int32_t n_seq, max_blocks, recent;
+} ha_cache4_eviction;
+
+int ha_cache4_evict(void* cache, const float* weights, float* weights_out, const int32_t* block_table, const int32_t* lens, const int32_t* keep,
+                    int32_t* free_pages, const int32_t* free_count, int32_t* lens_out, int32_t* free_count_out, const ha_cache4* shape,
+                    const ha_cache4_eviction* evict, void* workspace, size_t workspace_bytes, void* stream);
+size_t ha_cache4_evict_workspace_bytes(const ha_cache4* shape, const ha_cache4_eviction* evict); /* 0 too if not valid */
 
 /* Block tables and slots, on the GPU from the sequences' lengths: one launch before a step's rows are written.
  *   lens[s]   tokens that sequence s holds, in pages block_table[s][0 ... ceil(lens / page) - 1]

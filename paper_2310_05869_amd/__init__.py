@@ -9,7 +9,7 @@ from .binding import (  # noqa: F401
     ha_merge_unpermute, ha_sampled_attn, ha_seg_sort, ha_workspace_bytes, ha_workspace_layout, hyperattn_backward, hyperattn_backward_timed, hyperattn_forward, hyperattn_forward_alg2, hyperattn_forward_static, hyperattn_forward_timed, ha_static_scratch_bytes, ha_forward_workgroups, ha_call_routes, ha_fp32_ways, hyperattn_forward_stamped, STAMP_NAMES, STAMP_WORDS, stamp_place,
     exact_attn_packed_backward, exact_attn_packed_backward_workspace_bytes, exact_attn_packed_forward,
     alloc_cache4, ha_cache4_attn, ha_cache4_attn_chunk, ha_cache4_attn_chunk_workspace_bytes, ha_cache4_attn_form, ha_cache4_attn_workspace_bytes, ha_cache4_bytes, ha_cache4_read, ha_cache4_write,
-    alloc_cache4_weights, ha_cache4_weights, ha_cache4_weights_workspace_bytes,
+    alloc_cache4_weights, ha_cache4_evict, ha_cache4_evict_workspace_bytes, ha_cache4_weights, ha_cache4_weights_workspace_bytes,
     ha_page_plan,
     lib, make_params, make_shape, strerror, workspace_views,
 )

@@ -110,6 +110,8 @@ _SIGNATURES = {
     "ha_cache4_attn_chunk_workspace_bytes": (c_size_t, [c_void_p, c_void_p]),
     "ha_cache4_weights": (c_int, [c_void_p] * 7 + [c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_size_t, c_void_p]),
     "ha_cache4_weights_workspace_bytes": (c_size_t, [c_void_p, c_void_p]),
+    "ha_cache4_evict": (c_int, [c_void_p] * 10 + [c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
+    "ha_cache4_evict_workspace_bytes": (c_size_t, [c_void_p, c_void_p]),
     "ha_page_plan": (c_int, [c_void_p] * 9 + [c_void_p, c_void_p]),
     "ha_measure_mfma_rate": (c_int, [c_void_p, c_size_t, c_int32, POINTER(c_float), c_void_p]),
     "ha_measure_hbm_rate": (c_int, [c_void_p, c_size_t, POINTER(c_float), POINTER(c_float), c_void_p]),
@@ -733,6 +735,7 @@ _PACKED_STRIDES = struct.Struct("16q")
 _STRIDES2 = struct.Struct("4q")
 _CACHE4 = struct.Struct("4i")
 _STRIDES1 = struct.Struct("2q")
+_THREE = struct.Struct("3i")  # ha_cache4_eviction
 _FIVE = struct.Struct("5i")  # ha_cache4_query, ha_cache4_chunk, ha_page_plan_shape
 
 
@@ -1060,6 +1063,39 @@ def ha_cache4_weights(Q, cache, cu_seqlens, block_table, lens, lse, weights, pag
                                    1 if fresh else 0, _STRIDES1.pack(*_rows(Q, "Q", full, Q.dtype, dev)), _bytes(workspace, "workspace", dev), workspace.numel(), handle),
            "ha_cache4_weights")
     return weights
+
+
+def ha_cache4_evict_workspace_bytes(cache, page, n_seq, max_blocks) -> int:
+    return int(lib().ha_cache4_evict_workspace_bytes(_CACHE4.pack(*_cache4(cache, page)), _THREE.pack(n_seq, max_blocks, 0)))
+
+
+def ha_cache4_evict(cache, weights, block_table, lens, keep, free_pages, free_count, page, recent=0, weights_out=None, lens_out=None, free_count_out=None,
+                    workspace=None, stream=None):
+    """(lens_out, free_count_out): sequences of more than keep[s] tokens (int32 [n_seq]; < 0: all stay) keep the last `recent` of them and, for every key head, those of
+    largest weight (float32 [n_pages, Hk, page], as ha_cache4_weights has them) among the others.  Rows of the cache move to the sequence's first keep[s] places, their
+    weights with them (into weights_out; None: weights itself); pages that it no longer needs are put on free_pages (int32 [n_pages], changed in place; free_count
+    int32 [1]).  block_table int32 [n_seq, max_blocks] and lens int32 [n_seq] stay as they are."""
+    i32, f32 = _torch().int32, _torch().float32
+    sizes = _cache4(cache, page)
+    if block_table.dim() != 2:
+        raise ValueError(f"block_table has shape {tuple(block_table.shape)}, expected [n_seq, max_blocks]")
+    n_seq, max_blocks = block_table.shape
+    dev, handle = _here(cache, "cache", stream)
+    if lens_out is None:
+        lens_out = _empty(stream, (n_seq,), i32, lens)
+    if free_count_out is None:
+        free_count_out = _empty(stream, (1,), i32, lens)
+    size, evict, of_weights = _CACHE4.pack(*sizes), _THREE.pack(n_seq, max_blocks, recent), (sizes[0], sizes[2], page)
+    if workspace is None:
+        workspace = _empty(stream, (int(lib().ha_cache4_evict_workspace_bytes(size, evict)),), _torch().uint8, cache)
+    at = _whole(weights, "weights", of_weights, f32, dev)
+    _check(lib().ha_cache4_evict(_bytes(cache, "cache", dev), at, at if weights_out is None else _whole(weights_out, "weights_out", of_weights, f32, dev),
+                                 _whole(block_table, "block_table", (n_seq, max_blocks), i32, dev), _whole(lens, "lens", (n_seq,), i32, dev),
+                                 _whole(keep, "keep", (n_seq,), i32, dev), _whole(free_pages, "free_pages", (sizes[0],), i32, dev),
+                                 _whole(free_count, "free_count", (1,), i32, dev), _whole(lens_out, "lens_out", (n_seq,), i32, dev),
+                                 _whole(free_count_out, "free_count_out", (1,), i32, dev), size, evict, _bytes(workspace, "workspace", dev), workspace.numel(), handle),
+           "ha_cache4_evict")
+    return lens_out, free_count_out
 
 
 def ha_page_plan(lens, add, block_table, free_pages, free_count, page, rows=None, lens_out=None, cu_seqlens=None, slots=None, free_count_out=None,

@@ -20,7 +20,7 @@ LIB = os.path.join(HERE, "libhyperattn.so")
 
 SOURCES = ["api.hip", "lsh_hash.hip", "lsh_hash_mfma.hip", "seg_sort.hip", "stage_kernels.hip", "attn_mfma.hip", "attn_f32.hip",
            "calib.hip", "attn_bwd_mfma.hip", "attn_bwd_f32.hip", "bwd_kernels.hip", "alg2_kernels.hip", "alg2_mfma.hip",
-           "page_plan.hip", "cache4_rows.hip", "cache4_attn.hip", "cache4_chunk.hip", "cache4_weights.hip", "cache_api.hip"]
+           "page_plan.hip", "cache4_rows.hip", "cache4_attn.hip", "cache4_chunk.hip", "cache4_weights.hip", "cache4_evict.hip", "cache_api.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

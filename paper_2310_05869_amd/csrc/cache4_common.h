@@ -92,6 +92,26 @@ void cache4_weights_split(CacheChunkArgs* a);  // sets div_group, cut, least_run
 constexpr int kWeightsParts = 512;             // workgroups that the chip holds at once, two per CU
 constexpr int kWeightsTokens = 256;            // of a tile
 
+struct CacheEvictArgs {
+  unsigned char* cache;
+  const float* weights;
+  float* weights_out;
+  const int32_t* table;
+  const int32_t* lens;
+  const int32_t* keep;
+  int32_t* free_pages;
+  const int32_t* free_count;
+  int32_t* lens_out;
+  int32_t* free_count_out;
+  CacheGeometry c;
+  int32_t n_seq, max_blocks, recent;
+  // workspace: per sequence and key head, how many rows change places, and from which slot to which
+  int32_t* counts;
+  int2* moves;
+  int64_t moves_most;   // of a sequence and key head
+};
+int launch_cache4_evict(const CacheEvictArgs& a, hipStream_t st);
+
 struct PagePlanArgs {
   const int32_t* lens;
   const int32_t* add;

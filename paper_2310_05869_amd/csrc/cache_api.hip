@@ -238,7 +238,7 @@ int ha_cache4_weights(const void* Q, const void* cache, const int32_t* cu_seqlen
   size_t sums;
   const size_t total = weights_space(a, &sums);
   if ((a.rows > 0 && (!Q || !lse)) || !cache || !cu_seqlens || !block_table || !lens || !weights || (total > 0 && !workspace)) return HA_ERR_NULL;
-  if (any_misaligned16(Q, cache) || any_misaligned4(cu_seqlens, block_table, lens, lse, weights)) return HA_ERR_ALIGN;
+  if (any_misaligned16(Q, cache, weights) || any_misaligned4(cu_seqlens, block_table, lens, lse)) return HA_ERR_ALIGN;
   if (workspace_bytes < total || ((uintptr_t)workspace & 255) != 0) return HA_ERR_WORKSPACE;
   a.Q = Q;
   a.cache = reinterpret_cast<const unsigned char*>(cache);
@@ -251,6 +251,64 @@ int ha_cache4_weights(const void* Q, const void* cache, const int32_t* cu_seqlen
   a.joins = reinterpret_cast<int32_t*>(workspace);
   a.part_o = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(workspace) + sums);
   return launch_cache4_weights(a, chunk->dtype, (hipStream_t)stream);
+}
+
+// Fills all of *a but the pointers.
+static int evict_geometry(const ha_cache4* shape, const ha_cache4_eviction* e, CacheEvictArgs* a) {
+  const int rc = cache_geometry(shape, &a->c);
+  if (rc != HA_OK) return rc;
+  if (!e) return HA_ERR_NULL;
+  if (e->n_seq < 0 || e->n_seq > 8192 || e->max_blocks < 0 || e->recent < 0) return HA_ERR_SHAPE;
+  if ((int64_t)e->n_seq * shape->Hk > (1 << 20) || (int64_t)e->n_seq * e->max_blocks > (1ll << 30)) return HA_ERR_SHAPE;
+  if ((int64_t)e->max_blocks * shape->page > (1ll << 30)) return HA_ERR_SHAPE;
+  a->n_seq = e->n_seq;
+  a->max_blocks = e->max_blocks;
+  a->recent = e->recent;
+  a->moves_most = (int64_t)e->max_blocks * shape->page / 2;  // the places that come free are as many as the tokens that fill them, and neither count twice
+  return HA_OK;
+}
+
+static size_t evict_space(const CacheEvictArgs& a, size_t* moves) {
+  auto align = [](size_t x) { return (x + 255) & ~(size_t)255; };
+  const size_t heads = (size_t)a.n_seq * a.c.Hk;
+  *moves = align(heads * 4);
+  return heads == 0 ? 0 : *moves + align(heads * (size_t)a.moves_most * 8);
+}
+
+size_t ha_cache4_evict_workspace_bytes(const ha_cache4* shape, const ha_cache4_eviction* evict) {
+  CacheEvictArgs a{};
+  size_t moves;
+  return evict_geometry(shape, evict, &a) == HA_OK ? evict_space(a, &moves) : 0;
+}
+
+int ha_cache4_evict(void* cache, const float* weights, float* weights_out, const int32_t* block_table, const int32_t* lens, const int32_t* keep,
+                    int32_t* free_pages, const int32_t* free_count, int32_t* lens_out, int32_t* free_count_out, const ha_cache4* shape,
+                    const ha_cache4_eviction* evict, void* workspace, size_t workspace_bytes, void* stream) {
+  CacheEvictArgs a{};
+  const int rc = evict_geometry(shape, evict, &a);
+  if (rc != HA_OK) return rc;
+  size_t moves;
+  const size_t total = evict_space(a, &moves);
+  if (!free_count || !free_count_out || (total > 0 && !workspace)) return HA_ERR_NULL;
+  if (a.c.n_pages > 0 && (!cache || !weights || !weights_out || !free_pages)) return HA_ERR_NULL;
+  if (a.n_seq > 0 && (!lens || !keep || !lens_out || (a.max_blocks > 0 && !block_table))) return HA_ERR_NULL;
+  if (any_misaligned16(cache, weights, weights_out)) return HA_ERR_ALIGN;
+  if (any_misaligned4(block_table, lens, keep, free_pages) || any_misaligned4(free_count, lens_out, free_count_out)) return HA_ERR_ALIGN;
+  if (free_count == free_count_out || (a.n_seq > 0 && (lens == lens_out || keep == lens_out))) return HA_ERR_SHAPE;  // (read by workgroups that others write ahead of)
+  if (workspace_bytes < total || ((uintptr_t)workspace & 255) != 0) return HA_ERR_WORKSPACE;
+  a.cache = reinterpret_cast<unsigned char*>(cache);
+  a.weights = weights;
+  a.weights_out = weights_out;
+  a.table = block_table;
+  a.lens = lens;
+  a.keep = keep;
+  a.free_pages = free_pages;
+  a.free_count = free_count;
+  a.lens_out = lens_out;
+  a.free_count_out = free_count_out;
+  a.counts = reinterpret_cast<int32_t*>(workspace);
+  a.moves = reinterpret_cast<int2*>(reinterpret_cast<unsigned char*>(workspace) + moves);
+  return launch_cache4_evict(a, (hipStream_t)stream);
 }
 
 int ha_page_plan(const int32_t* lens, const int32_t* add, int32_t* block_table, int32_t* free_pages, const int32_t* free_count,

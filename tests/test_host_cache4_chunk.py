@@ -123,3 +123,58 @@ def test_binding_refuses_tensors_that_do_not_fit(ha):
         ha.ha_cache4_attn_chunk(Q, pages, cu.long(), table, lens, 16)
     with pytest.raises(ha.HyperAttnError):
         ha.ha_cache4_attn_chunk(Q, pages, cu, torch.zeros(2, 500, dtype=i32, device="cuda"), lens, 16, workspace=torch.empty(16, dtype=torch.uint8, device="cuda"))
+
+
+def evict(ha, p=None, c=None, e=(2, 100, 4), ws=OK, nbytes=1 << 40):
+    return ha.lib().ha_cache4_evict(*(p or [OK + 64 * i for i in range(10)]), c or cache(), struct.pack("3i", *e), ws, nbytes, None)
+
+
+def test_eviction(ha):
+    for e in ((-1, 4, 0), (8193, 4, 0), (2, -1, 0), (2, 4, -1), (2, (1 << 26) + 1, 0), (8192, 1 << 18, 0)):
+        assert evict(ha, e=e) == SHAPE, e
+        assert ha.lib().ha_cache4_evict_workspace_bytes(cache(), struct.pack("3i", *e)) == 0
+    assert evict(ha, c=cache(Hk=1024), e=(1025, 4, 0)) == SHAPE and evict(ha, c=cache(page=24)) == SHAPE
+    assert ha.lib().ha_cache4_evict(*[OK + 64 * i for i in range(10)], cache(), None, OK, 1 << 40, None) == NULL
+    need = ha.lib().ha_cache4_evict_workspace_bytes(cache(), struct.pack("3i", 2, 100, 4))
+    assert 2 * 2 * 1600 * 4 <= need <= 2 * 2 * 1600 * 4 + 512
+    for i in range(10):
+        p = [OK + 64 * j for j in range(10)]
+        p[i] = None
+        assert evict(ha, p) == NULL, i
+        p[i] = OK + 2
+        assert evict(ha, p) == ALIGN, i
+    for i, j in ((8, 4), (8, 5), (9, 7)):   # lens_out over lens or keep, free_count_out over free_count
+        p = [OK + 64 * x for x in range(10)]
+        p[i] = p[j]
+        assert evict(ha, p) == SHAPE, (i, j)
+    assert evict(ha, ws=None) == NULL and evict(ha, nbytes=need - 1) == WORKSPACE and evict(ha, ws=OK + 128, nbytes=need) == WORKSPACE
+
+
+def test_binding_of_eviction(ha):
+    import torch
+    i32 = torch.int32
+    pages, w, table = torch.zeros(4, 2, 16 * 68, dtype=torch.uint8), torch.zeros(4, 2, 16), torch.zeros(2, 5, dtype=i32)
+    two, free, one = torch.zeros(2, dtype=i32), torch.zeros(4, dtype=i32), torch.zeros(1, dtype=i32)
+    with pytest.raises(ValueError, match="block_table has shape"):
+        ha.ha_cache4_evict(pages, w, table[0], two, two, free, one, 16)
+    with pytest.raises(ValueError, match="cache has shape"):
+        ha.ha_cache4_evict(pages, w, table, two, two, free, one, 32)
+    with pytest.raises(ValueError, match="device tensor"):
+        ha.ha_cache4_evict(pages, w, table, two, two, free, one, 16)
+
+
+@pytest.mark.gpu
+def test_binding_of_eviction_refuses_tensors_that_do_not_fit(ha):
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    zeros = lambda *shape, dtype=torch.int32: torch.zeros(shape, dtype=dtype, device="cuda")  # noqa: E731
+    pages, w, table, two, free, one = zeros(4, 2, 16 * 68, dtype=torch.uint8), ha.alloc_cache4_weights(4, 16, 2), zeros(2, 5), zeros(2), zeros(4), zeros(1)
+    for call, what in ((lambda: ha.ha_cache4_evict(pages, w[:2], table, two, two, free, one, 16), "weights has shape"),
+                       (lambda: ha.ha_cache4_evict(pages, w, table, two, two[:1], free, one, 16), "keep has shape"),
+                       (lambda: ha.ha_cache4_evict(pages, w, table, two, two, free[:3], one, 16), "free_pages has shape"),
+                       (lambda: ha.ha_cache4_evict(pages, w, table, two, two, free, one, 16, weights_out=w.cpu()), "weights_out is on")):
+        with pytest.raises(ValueError, match=what):
+            call()
+    with pytest.raises(ha.HyperAttnError):
+        ha.ha_cache4_evict(pages, w, table, two, two, free, one, 16, recent=-1)
