@@ -34,29 +34,38 @@ constexpr int kFewParts = 16;
 constexpr int kMostParts = 768;  // workgroups of four waves that the chip holds at once, three per CU
 constexpr int kUnit = 64;        // tokens of a wave's step
 constexpr int kTilesPerUnit = 4; // of 16 tokens
-constexpr int kCRows = 16;       // query rows of a workgroup
+constexpr int kCRows = kNarrowRows;  // query rows of a workgroup
 // V's scales from here on are taken by the rows that see the token alone: 4 times 2^126 and 2 times 2^127 are infinite, 255 is NaN, and 0 times either is NaN.
 constexpr uint32_t kFarScale = 253, kFarSteps = 256 - kFarScale;
 
 // Units of all sequences before s (exclusive), found by one wave: lane l sums a run of sequences.
 __device__ inline int seq_len(const CacheAttnArgs& a, int s) { return min(max(a.lens[s], 0), a.max_blocks << a.c.log_page); }
 __device__ inline int seq_units(const CacheAttnArgs& a, int s) { return (seq_len(a, s) + kUnit - 1) / kUnit; }
+// RAGGED: a sequence's queries are its rows cu[s] ... cu[s + 1] - 1, and sequences of more than a tile of rows are others' work
+__device__ inline int ragged_start(const CacheAttnArgs& a, int s) { return min(max(a.cu[s], 0), a.rows_all); }
+__device__ inline int ragged_queries(const CacheAttnArgs& a, int s) {  // 0: none, or too many
+  const int n = max(ragged_start(a, s + 1) - ragged_start(a, s), 0);
+  return (int64_t)n * a.group <= kCRows ? n : 0;
+}
 // What a sequence takes of the line: its units and what its start and its end cost a workgroup, in units.  (0 / 2 / 4 / 8: 64 sequences of up to 16384 tokens,
 // three queries each, 54 / 51 / 45 / 42 us, 12 and 16 44 and 45; 256 of up to 8192 94 / 76 / 69 / 68, since then 62 and with 12 or 16 69; lengths alike +-0.)
 constexpr int kSeqCost = 8;
+template <bool RAGGED>
 __device__ inline int seq_cost(const CacheAttnArgs& a, int s) {
   const int n = seq_units(a, s);
+  if (RAGGED && ragged_queries(a, s) == 0) return 0;
   return n > 0 ? n + kSeqCost : 0;
 }
 
 // The line's length, and *before: what precedes the lane's run of sequences.  Wave-uniform results.
+template <bool RAGGED>
 __device__ inline int line_total(const CacheAttnArgs& a, int lane, int* before) {
   const int each = (a.n_seq + 63) / 64, s0 = min(a.n_seq, lane * each), s1 = min(a.n_seq, s0 + each);
   int sum = 0;
   for (int s = s0; s < s1; s += 4) {  // (four lengths asked for at a time: 1000 sequences of up to 4096 52.2 -> 51.2 us)
     int cost[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) cost[i] = seq_cost(a, min(s + i, s1 - 1));
+    for (int i = 0; i < 4; ++i) cost[i] = seq_cost<RAGGED>(a, min(s + i, s1 - 1));
 #pragma unroll
     for (int i = 0; i < 4; ++i) sum += s + i < s1 ? cost[i] : 0;
   }
@@ -70,6 +79,7 @@ __device__ inline int line_total(const CacheAttnArgs& a, int lane, int* before) 
   return __builtin_amdgcn_readfirstlane(__shfl(inc, 63));
 }
 // The sequence at place u of the line (u < total), and where it begins
+template <bool RAGGED>
 __device__ inline int find_place(const CacheAttnArgs& a, int lane, int before, int u, int* seq_first) {
   const int each = (a.n_seq + 63) / 64;
   // the last lane whose run starts at or before u (runs without units start where the next one does)
@@ -78,7 +88,7 @@ __device__ inline int find_place(const CacheAttnArgs& a, int lane, int before, i
   int at = __builtin_amdgcn_readfirstlane(__shfl(before, run));
   int s = run * each;
   for (; s < a.n_seq - 1; ++s) {
-    const int n = seq_cost(a, s);
+    const int n = seq_cost<RAGGED>(a, s);
     if (u < at + n) break;
     at += n;
   }
@@ -104,7 +114,7 @@ struct Weights {
 // NW waves.  WHOLE: a workgroup per sequence, which it finishes (small tables: no second launch).  ONCE: codes are read past the caches.
 // MULTI: several queries a sequence, which see its last tokens in part.
 // bf16, four waves, d = 128, tokens shared out: held to the 168 registers of three workgroups a CU, which costs 2 spilled ones, MULTI 4 (12 and 20 bytes of scratch).
-template <int D, int SPLIT, int NW, bool WHOLE, bool ONCE, bool MULTI>
+template <int D, int SPLIT, int NW, bool WHOLE, bool ONCE, bool MULTI, bool RAGGED = false>
 __global__ __launch_bounds__(64 * NW, SPLIT == 1 && NW == 4 ? 3 : 2) void cache4_attn_kernel(CacheAttnArgs a) {
   constexpr int kCWaves = NW, kCThreads = 64 * NW;
   constexpr int G = D / 32;     // groups of channels, products per score
@@ -122,18 +132,19 @@ __global__ __launch_bounds__(64 * NW, SPLIT == 1 && NW == 4 ? 3 : 2) void cache4
     s = blockIdx.x;
   } else {
     int before;
-    const int total = line_total(a, lane, &before);
+    const int total = line_total<RAGGED>(a, lane, &before);
     part = blockIdx.x;
     const int parts = min(a.parts, (total + NW - 1) / NW);  // (a unit for every wave)
     if (part >= parts) return;
     u0 = (int)((int64_t)total * part / parts);
     u1 = (int)((int64_t)total * (part + 1) / parts);
-    s = find_place(a, lane, before, u0, &seq_first);
+    s = find_place<RAGGED>(a, lane, before, u0, &seq_first);
   }
 
+  // (RAGGED: a sequence's own numbers, below)
   const int row = tile * kCRows + r;                   // query row within the key head
   const int row_use = row < a.rows ? row : 0;
-  const int q_tok = row_use / a.group, q_head = hk * a.group + row_use % a.group;
+  int q_tok = row_use / a.group, q_head = hk * a.group + row_use % a.group;
 
   const int64_t page_bytes = (int64_t)a.c.Hk * a.c.block_bytes();
   const unsigned char* head_base = a.cache + (int64_t)hk * a.c.block_bytes();
@@ -141,15 +152,24 @@ __global__ __launch_bounds__(64 * NW, SPLIT == 1 && NW == 4 ? 3 : 2) void cache4
 
   for (;;) {
     const int len = seq_len(a, s);
-    const int n_units = (len + kUnit - 1) / kUnit;
+    const int n_queries = RAGGED ? __builtin_amdgcn_readfirstlane(ragged_queries(a, s)) : a.q_len;
+    const int n_rows = RAGGED ? n_queries * a.group : a.rows;
+    const int64_t row_first = RAGGED ? __builtin_amdgcn_readfirstlane(ragged_start(a, s)) : (int64_t)s * a.q_len;
+    const int64_t all_rows = RAGGED ? (int64_t)a.rows_all : (int64_t)a.n_seq * a.q_len;
+    if constexpr (RAGGED) {
+      const int use = row < n_rows ? row : 0;
+      q_tok = use / a.group;
+      q_head = hk * a.group + use % a.group;
+    }
+    const int n_units = RAGGED && n_queries == 0 ? 0 : (len + kUnit - 1) / kUnit;
     const int first = max(u0 - seq_first, 0), last = min(u1 - seq_first, n_units);  // units of the sequence that are this workgroup's
-    if (WHOLE || first < last) {
+    if ((WHOLE && !(RAGGED && n_queries == 0)) || first < last) {
     const int32_t* blocks = a.table + (int64_t)s * a.max_blocks;
     const int last_block = max(len - 1, 0) >> log_page;
 
     bf16x8 q[SPLIT][G];
     {
-      const int64_t at = ((int64_t)s * a.q_len + q_tok) * a.q.row + (int64_t)q_head * a.q.head + 8 * kq;
+      const int64_t at = (row_first + q_tok) * a.q.row + (int64_t)q_head * a.q.head + 8 * kq;
 #pragma unroll
       for (int g = 0; g < G; ++g) {
         if constexpr (!F32) {
@@ -169,8 +189,8 @@ __global__ __launch_bounds__(64 * NW, SPLIT == 1 && NW == 4 ? 3 : 2) void cache4
         }
       }
     }
-    const int limit = len - a.q_len + 1 + q_tok;  // tokens that the lane's row sees
-    const int all_see = len - a.q_len + 1;        // that every row sees
+    const int limit = len - n_queries + 1 + q_tok;  // tokens that the lane's row sees
+    const int all_see = len - n_queries + 1;        // that every row sees
 
     RawTile<D> raw[kTilesPerUnit];
     f32x4 o[MT];
@@ -389,8 +409,8 @@ __global__ __launch_bounds__(64 * NW, SPLIT == 1 && NW == 4 ? 3 : 2) void cache4
       // (all that this needs beside m and o is formed again, the query read again: kept, it would take registers from the loop)
       int thread = threadIdx.x;
       asm volatile("" : "+v"(thread));
-      const int quad = (thread & 63) >> 4, own_row = tile * kCRows + (thread & 15), own = own_row < a.rows ? own_row : 0, own_tok = own / a.group;
-      const int64_t q_at = ((int64_t)s * a.q_len + own_tok) * a.q.row + (int64_t)(hk * a.group + own % a.group) * a.q.head + 8 * quad;
+      const int quad = (thread & 63) >> 4, own_row = tile * kCRows + (thread & 15), own = own_row < n_rows ? own_row : 0, own_tok = own / a.group;
+      const int64_t q_at = (row_first + own_tok) * a.q.row + (int64_t)(hk * a.group + own % a.group) * a.q.head + 8 * quad;
       for (int u = first + wave; u < last; u += kCWaves)
         for (int tok = max(u * kUnit, max(all_see, 0)); tok < min(u * kUnit + kUnit, len); ++tok) {
           const int page = blocks[tok >> log_page], at = tok & in_page;
@@ -459,7 +479,7 @@ __global__ __launch_bounds__(64 * NW, SPLIT == 1 && NW == 4 ? 3 : 2) void cache4
     for (int idx = threadIdx.x; idx < kCRows * LPR; idx += kCThreads) {
       const int rr = idx / LPR, ch = (idx % LPR) * 4;
       const int rw = tile * kCRows + rr;
-      if (rw >= a.rows) break;
+      if (rw >= n_rows) break;
       float top = merge_m[0][rr];
 #pragma unroll
       for (int w = 1; w < kCWaves; ++w) top = fmaxf(top, merge_m[w][rr]);
@@ -476,15 +496,16 @@ __global__ __launch_bounds__(64 * NW, SPLIT == 1 && NW == 4 ? 3 : 2) void cache4
         const bool empty = sum == 0.f;
         const float inv = empty ? 0.f : 1.f / sum;
         acc *= inv;
-        const int64_t orow = (int64_t)s * a.q_len + rw / a.group;
+        const int64_t orow = row_first + rw / a.group;
         const int head = hk * a.group + rw % a.group;
         const int64_t at = orow * a.o.row + (int64_t)head * a.o.head + ch;
         if constexpr (F32) *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.out) + at) = acc;
         else *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(a.out) + at) = (u32x2){pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3])};
         if (ch == 0)
-          a.lse[(int64_t)head * a.n_seq * a.q_len + orow] = empty ? -INFINITY : F32 ? top + logf(sum) : (top + log2f(sum)) * kLn2;
+          a.lse[(int64_t)head * all_rows + orow] = empty ? -INFINITY : F32 ? top + logf(sum) : (top + log2f(sum)) * kLn2;
       } else {
-        const int64_t slot = ((int64_t)blockIdx.y * (a.parts + a.n_seq) + part + s) * kCRows + rr;
+        // (RAGGED: of a run two sequences at most are others' work too, the one that it begins with and the one that it ends with)
+        const int64_t slot = (RAGGED ? ((int64_t)blockIdx.y * a.parts + part) * 2 + (first == 0) : (int64_t)blockIdx.y * (a.parts + a.n_seq) + part + s) * kCRows + rr;
         *reinterpret_cast<f32x4*>(a.part_o + slot * D + ch) = acc;
         if (ch == 0) {
           a.part_ml[2 * slot] = top;
@@ -499,6 +520,7 @@ __global__ __launch_bounds__(64 * NW, SPLIT == 1 && NW == 4 ? 3 : 2) void cache4
     if constexpr (WHOLE) return;
     __syncthreads();
     }
+    if constexpr (WHOLE) return;
     seq_first += n_units > 0 ? n_units + kSeqCost : 0;
     if (seq_first >= u1) return;
     ++s;  // (the line goes on: another sequence follows)
@@ -510,7 +532,8 @@ __global__ __launch_bounds__(64 * NW, SPLIT == 1 && NW == 4 ? 3 : 2) void cache4
 // parts, one at a time -> eight, the whole call: 44 -> 17 us).  A row has a workgroup to itself, whose groups take its parts in turn; in launches of more rows than
 // workgroups run at once, a row of few parts has one group alone, and the workgroups too many end at once (the whole call: 64 sequences of up to 16384 tokens, three queries
 // each, 6144 rows, 44.2 -> 42.0 us; 32 of up to 4096, eight each, 8192 rows, 29.5 -> 26.3; but 60 of up to 8000, 960 rows, 24.6 -> 25.5).
-template <int D, int SPLIT>
+// RAGGED: row y of a sequence is row y % 16 of key head y / 16.
+template <int D, int SPLIT, bool RAGGED = false>
 __global__ __launch_bounds__(kJoinThreads) void cache4_join_kernel(CacheAttnArgs a) {
   constexpr bool F32 = SPLIT > 1;
   constexpr int LPR = D / 4, PAR = kJoinThreads / LPR, AHEAD = 8;
@@ -521,13 +544,25 @@ __global__ __launch_bounds__(kJoinThreads) void cache4_join_kernel(CacheAttnArgs
   const int p0 = a.span[2 * s], p1 = a.span[2 * s + 1];  // (asked for with the length; of an empty sequence they are what was there)
   const int parts = len > 0 ? p1 - p0 + 1 : 0;
   if (parts == 1) return;  // finished where its tokens were read
-  const bool few = parts <= kFewParts && gridDim.x * gridDim.y > kJoinsAtOnce;
-  const int rows = a.Hq * a.q_len, y = few ? (int)blockIdx.y * PAR + mine : (int)blockIdx.y;
+  const bool few = RAGGED && a.join_few ? true : parts <= kFewParts && gridDim.x * gridDim.y > kJoinsAtOnce;
+  const int rows = RAGGED ? a.c.Hk * kCRows : a.Hq * a.q_len, y = few ? (int)blockIdx.y * PAR + mine : (int)blockIdx.y;
   if (y >= rows) return;   // (few: no barrier follows; many: all threads alike)
-  const int hq = y % a.Hq, tok = y / a.Hq;
-  const int hk = hq / a.group, row = tok * a.group + hq % a.group, tile = row / kCRows, rr = row % kCRows;
-  const int64_t orow = (int64_t)s * a.q_len + tok;
-  const int64_t slot0 = ((int64_t)(tile * a.c.Hk + hk) * (a.parts + a.n_seq) + s + p0) * kCRows + rr;
+  int hq, tok, hk, row;
+  if constexpr (RAGGED) {
+    hk = y / kCRows;
+    row = y % kCRows;
+    if (row >= ragged_queries(a, s) * a.group) return;
+    tok = row / a.group;
+    hq = hk * a.group + row % a.group;
+  } else {
+    hq = y % a.Hq;
+    tok = y / a.Hq;
+    hk = hq / a.group;
+    row = tok * a.group + hq % a.group;
+  }
+  const int tile = row / kCRows, rr = row % kCRows;
+  const int64_t orow = (RAGGED ? (int64_t)ragged_start(a, s) : (int64_t)s * a.q_len) + tok, all_rows = RAGGED ? (int64_t)a.rows_all : (int64_t)a.n_seq * a.q_len;
+  const int64_t slot0 = (RAGGED ? ((int64_t)hk * a.parts + p0) * 2 : (int64_t)(tile * a.c.Hk + hk) * (a.parts + a.n_seq) + s + p0) * kCRows + rr;
   auto exp_of = [](float x) { return F32 ? expf(x) : __builtin_amdgcn_exp2f(x); };
   float m = -INFINITY, l = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
@@ -539,7 +574,8 @@ __global__ __launch_bounds__(kJoinThreads) void cache4_join_kernel(CacheAttnArgs
     f32x4 v[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int64_t slot = slot0 + (int64_t)(p + i * step) * kCRows;
+      const int q = p + i * step;
+      const int64_t slot = slot0 + (int64_t)(RAGGED ? 2 * q + (q == 0) : q) * kCRows;
       pm[i] = a.part_ml[2 * slot];
       pl[i] = a.part_ml[2 * slot + 1];
       v[i] = *reinterpret_cast<const f32x4*>(a.part_o + slot * D + ch);
@@ -568,7 +604,7 @@ __global__ __launch_bounds__(kJoinThreads) void cache4_join_kernel(CacheAttnArgs
     const int64_t at = orow * a.o.row + (int64_t)hq * a.o.head + ch;
     if constexpr (F32) *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.out) + at) = acc;
     else *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(a.out) + at) = (u32x2){pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3])};
-    if (lane == 0) a.lse[(int64_t)hq * a.n_seq * a.q_len + orow] = empty ? -INFINITY : F32 ? m + logf(l) : (m + log2f(l)) * kLn2;
+    if (lane == 0) a.lse[(int64_t)hq * all_rows + orow] = empty ? -INFINITY : F32 ? m + logf(l) : (m + log2f(l)) * kLn2;
   };
   if (few) {
     finish();
@@ -640,6 +676,35 @@ static int launch_attn_form(const CacheAttnArgs& a, hipStream_t st) {
 template <int D, int SPLIT>
 static int launch_attn_q(const CacheAttnArgs& a, hipStream_t st) {
   return a.q_len > 1 ? launch_attn_form<D, SPLIT, true>(a, st) : launch_attn_form<D, SPLIT, false>(a, st);
+}
+
+// Sequences of few rows among chunks (cache4_chunk.hip): tokens shared out, or a workgroup per sequence and key head.
+template <int D, int SPLIT>
+static int launch_ragged_one(const CacheAttnArgs& a, bool whole, hipStream_t st) {
+  if (whole) {
+    hipLaunchKernelGGL((cache4_attn_kernel<D, SPLIT, 4, true, false, true, true>), dim3((unsigned)a.n_seq, (unsigned)a.c.Hk), dim3(256), 0, st, a);
+    return check_launch();
+  }
+  const dim3 grid((unsigned)a.parts, (unsigned)a.c.Hk);
+  hipLaunchKernelGGL((cache4_attn_kernel<D, SPLIT, 4, false, false, true, true>), grid, dim3(256), 0, st, a);
+  return check_launch();
+}
+template <int D, int SPLIT>
+static int join_ragged_one(const CacheAttnArgs& args, hipStream_t st) {
+  CacheAttnArgs a = args;
+  constexpr int PAR = kJoinThreads / (D / 4);
+  const int64_t rows = (int64_t)a.c.Hk * kCRows;
+  a.join_few = a.n_seq * rows > (1 << 20);  // (a launch counts its threads in 32 bits)
+  hipLaunchKernelGGL((cache4_join_kernel<D, SPLIT, true>), dim3((unsigned)a.n_seq, (unsigned)(a.join_few ? (rows + PAR - 1) / PAR : rows)), dim3(kJoinThreads), 0, st, a);
+  return check_launch();
+}
+int launch_cache4_ragged(const CacheAttnArgs& a, bool whole, int dtype, hipStream_t st) {
+  if (a.c.d == 128) return dtype == HA_BF16 ? launch_ragged_one<128, 1>(a, whole, st) : launch_ragged_one<128, 3>(a, whole, st);
+  return dtype == HA_BF16 ? launch_ragged_one<64, 1>(a, whole, st) : launch_ragged_one<64, 3>(a, whole, st);
+}
+int join_cache4_ragged(const CacheAttnArgs& a, int dtype, hipStream_t st) {
+  if (a.c.d == 128) return dtype == HA_BF16 ? join_ragged_one<128, 1>(a, st) : join_ragged_one<128, 3>(a, st);
+  return dtype == HA_BF16 ? join_ragged_one<64, 1>(a, st) : join_ragged_one<64, 3>(a, st);
 }
 
 int launch_cache4_attn(const CacheAttnArgs& a, int dtype, hipStream_t st) {

@@ -79,7 +79,7 @@ __global__ __launch_bounds__(64 * NW, 2) void cache4_chunk_kernel(CacheChunkArgs
 
   // ---- place ----
   const int tt = a.tile_tokens, heads = a.c.Hk * a.subs;
-  auto tiles_of = [&](const ChunkSeq& q) { return (q.n + tt - 1) / tt; };
+  auto tiles_of = [&](const ChunkSeq& q) { return (int64_t)q.n * a.group <= a.narrow ? 0 : (q.n + tt - 1) / tt; };
   auto upto = [&](const ChunkSeq& q, int64_t t) { return t * (max(q.held, 0) + kTileCost) + tt * (t * (t + 1) / 2); };  // line before tile t of a head
   auto cost = [&](int s) -> int64_t {
     const ChunkSeq q = chunk_seq(a, s);
@@ -544,11 +544,14 @@ __global__ __launch_bounds__(kJoinThreads) void cache4_chunk_join_kernel(CacheCh
   if (ch == 0) a.lse[(int64_t)head * a.rows + q.start + tok] = empty ? -INFINITY : F32 ? m + logf(l) : (m + log2f(l)) * kLn2;
 }
 
-// Tables of few tokens: a workgroup per tile, and no second launch.
-void cache4_chunk_split(CacheChunkArgs* a) {
+// Tables of few tokens: a workgroup per tile, and no second launch.  Sequences whose rows of a key head fit 16 go to launches of their own, in which the waves of a
+// workgroup take different tokens (cache4_attn.hip), where there can be several.
+void cache4_chunk_split(CacheChunkArgs* a, CacheAttnArgs* narrow) {
   a->subs = (a->group + kChunkRows - 1) / kChunkRows;
   a->sub_group = (a->group + a->subs - 1) / a->subs;
   a->tile_tokens = kChunkRows / a->sub_group;
+  a->narrow = a->group <= kNarrowRows && a->n_seq >= 4 ? kNarrowRows : 0;
+  narrow->parts = a->narrow ? cache4_parts(a->c.Hk, 1) : 0;
   const int64_t tokens = (int64_t)a->max_blocks << a->c.log_page, heads = (int64_t)a->c.Hk * a->subs;
   const int64_t tiles = ((int64_t)a->rows / a->tile_tokens + a->n_seq) * heads;
   if (tokens <= 1024 && tiles <= kMaxLaunch) {
@@ -582,9 +585,18 @@ static int launch_chunk_one(const CacheChunkArgs& a, hipStream_t st) {
   return check_launch();
 }
 
-int launch_cache4_chunk(const CacheChunkArgs& a, int dtype, hipStream_t st) {
+static int launch_chunk_wide(const CacheChunkArgs& a, int dtype, hipStream_t st) {
   if (a.c.d == 128) return dtype == HA_BF16 ? launch_chunk_one<128, 1, 4>(a, st) : launch_chunk_one<128, 3, 4>(a, st);
   return dtype == HA_BF16 ? launch_chunk_one<64, 1, 4>(a, st) : launch_chunk_one<64, 3, 4>(a, st);
+}
+
+int launch_cache4_chunk(const CacheChunkArgs& a, const CacheAttnArgs& narrow, int dtype, hipStream_t st) {
+  int rc = HA_OK;
+  const bool whole = a.parts == 0;
+  if (a.narrow) rc = launch_cache4_ragged(narrow, whole, dtype, st);
+  if (rc == HA_OK) rc = launch_chunk_wide(a, dtype, st);
+  if (rc == HA_OK && a.narrow && !whole) rc = join_cache4_ragged(narrow, dtype, st);
+  return rc;
 }
 
 }  // namespace ha

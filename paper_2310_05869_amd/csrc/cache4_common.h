@@ -53,7 +53,13 @@ struct CacheAttnArgs {
   int32_t* span;               // [n_seq][2]
   float* part_o;
   float* part_ml;
+  // sequences of few rows among chunks of any number (cache4_chunk.hip): rows of Q, those of a sequence, and whether the joining launch has no workgroup per row
+  const int32_t* cu;
+  int32_t rows_all, join_few;
 };
+constexpr int kNarrowRows = 16;  // query rows of a key head that a wave keeps beside codes in registers
+int launch_cache4_ragged(const CacheAttnArgs& a, bool whole, int dtype, hipStream_t st);
+int join_cache4_ragged(const CacheAttnArgs& a, int dtype, hipStream_t st);
 int launch_cache4_attn(const CacheAttnArgs& a, int dtype, hipStream_t st);
 int cache4_parts(int Hk, int tiles);
 int cache4_whole(const CacheAttnArgs& a);   // waves of a workgroup that takes a whole sequence, 0: tokens are shared out
@@ -75,6 +81,7 @@ struct CacheChunkArgs {
   int32_t group;             // query heads per key head
   int32_t subs, sub_group;   // a key head's query heads in `subs` runs of sub_group, each of which fits a tile
   int32_t tile_tokens;       // new tokens of a tile: tile_tokens * sub_group rows
+  int32_t narrow;            // attention: sequences of up to so many rows of a key head are left to launches of their own; 0: none
   int32_t fresh;             // sums of weights: earlier ones do not count
   int32_t parts;             // workgroups that share all work; 0: a workgroup per tile
   int32_t cut, least_run;    // sums of weights: whether tiles are shared among workgroups, and what each of these takes at least
@@ -84,8 +91,8 @@ struct CacheChunkArgs {
   float* part_o;
   float* part_ml;
 };
-int launch_cache4_chunk(const CacheChunkArgs& a, int dtype, hipStream_t st);
-void cache4_chunk_split(CacheChunkArgs* a);  // sets subs, sub_group, tile_tokens and parts
+int launch_cache4_chunk(const CacheChunkArgs& a, const CacheAttnArgs& narrow, int dtype, hipStream_t st);
+void cache4_chunk_split(CacheChunkArgs* a, CacheAttnArgs* narrow);  // sets subs, sub_group, tile_tokens, narrow and parts; parts of the narrow ones
 constexpr int kChunkRows = 128;              // query rows of a tile
 int launch_cache4_weights(const CacheChunkArgs& a, int dtype, hipStream_t st);
 void cache4_weights_split(CacheChunkArgs* a);  // sets div_group, cut, least_run and parts

@@ -87,6 +87,7 @@ static int chunk_geometry(const ha_cache4* shape, const ha_cache4_chunk* q, Cach
   if (q->Hq < 1 || q->Hq > 1024 || q->Hq % shape->Hk != 0) return HA_ERR_SHAPE;
   if ((int64_t)q->rows * q->Hq > (1 << 26) || (int64_t)q->n_seq * q->Hq > (1 << 22)) return HA_ERR_SHAPE;
   if ((int64_t)q->n_seq * q->max_blocks > (1ll << 30) || (int64_t)q->max_blocks * shape->page > 0x7fffffffll - 256) return HA_ERR_SHAPE;
+  if ((int64_t)q->n_seq * q->max_blocks * shape->page > (1ll << 36)) return HA_ERR_SHAPE;  // (units of 64 tokens are counted in 32 bits)
   a->n_seq = q->n_seq;
   a->rows = q->rows;
   a->Hq = q->Hq;
@@ -95,18 +96,27 @@ static int chunk_geometry(const ha_cache4* shape, const ha_cache4_chunk* q, Cach
   return HA_OK;
 }
 
-struct ChunkSpace {
-  size_t part_o, part_ml, total;
-};
-static ChunkSpace chunk_space(CacheChunkArgs a) {
-  cache4_chunk_split(&a);
-  auto align = [](size_t x) { return (x + 255) & ~(size_t)255; };
-  const size_t rows = 2 * (size_t)a.parts * kChunkRows;
-  ChunkSpace s;
-  s.part_o = align((size_t)a.parts * 16);
-  s.part_ml = s.part_o + align(rows * a.c.d * 4);
-  s.total = s.part_ml + align(rows * 8);
-  return s;
+// Sets how the work is split, and both kinds' places in the workspace.
+static size_t chunk_space(CacheChunkArgs* a, CacheAttnArgs* n, void* workspace) {
+  cache4_chunk_split(a, n);
+  unsigned char* const base = reinterpret_cast<unsigned char*>(workspace);
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    unsigned char* p = base + at;
+    at += (bytes + 255) & ~(size_t)255;
+    return p;
+  };
+  const size_t rows = 2 * (size_t)a->parts * kChunkRows;
+  a->joins = reinterpret_cast<int32_t*>(take((size_t)a->parts * 16));
+  a->part_o = reinterpret_cast<float*>(take(rows * a->c.d * 4));
+  a->part_ml = reinterpret_cast<float*>(take(rows * 8));
+  if (a->narrow && a->parts > 0) {
+    const size_t slots = (size_t)a->c.Hk * n->parts * 2 * kNarrowRows;
+    n->span = reinterpret_cast<int32_t*>(take((size_t)a->n_seq * 8));
+    n->part_o = reinterpret_cast<float*>(take(slots * a->c.d * 4));
+    n->part_ml = reinterpret_cast<float*>(take(slots * 8));
+  }
+  return at;
 }
 
 }  // namespace ha
@@ -177,24 +187,26 @@ int ha_cache4_attn(const void* Q, const void* cache, const int32_t* block_table,
 
 size_t ha_cache4_attn_chunk_workspace_bytes(const ha_cache4* shape, const ha_cache4_chunk* chunk) {
   CacheChunkArgs a{};
-  return chunk_geometry(shape, chunk, &a) == HA_OK ? chunk_space(a).total : 0;
+  CacheAttnArgs narrow{};
+  return chunk_geometry(shape, chunk, &a) == HA_OK ? chunk_space(&a, &narrow, nullptr) : 0;
 }
 
 int ha_cache4_attn_chunk(const void* Q, const void* cache, const int32_t* cu_seqlens, const int32_t* block_table, const int32_t* lens, void* out,
                          float* lse, const ha_cache4* shape, const ha_cache4_chunk* chunk, const ha_strides* qo, void* workspace,
                          size_t workspace_bytes, void* stream) {
   CacheChunkArgs a{};
+  CacheAttnArgs n{};
   int rc = chunk_geometry(shape, chunk, &a);
   if (rc != HA_OK) return rc;
   rc = row_strides(qo, a.rows, a.Hq, a.c.d, chunk->dtype, false, &a.q);
   if (rc == HA_OK) rc = row_strides(qo ? qo + 1 : nullptr, a.rows, a.Hq, a.c.d, chunk->dtype, true, &a.o);
   if (rc != HA_OK) return rc;
   if (a.n_seq == 0 || a.rows == 0) return HA_OK;
-  const ChunkSpace sp = chunk_space(a);
-  if (!Q || !cu_seqlens || !lens || !out || !lse || (sp.total > 0 && !workspace) || (!cache && a.c.n_pages > 0) || (!block_table && a.max_blocks > 0))
+  const size_t space = chunk_space(&a, &n, workspace);
+  if (!Q || !cu_seqlens || !lens || !out || !lse || (space > 0 && !workspace) || (!cache && a.c.n_pages > 0) || (!block_table && a.max_blocks > 0))
     return HA_ERR_NULL;
   if (any_misaligned16(Q, cache, out) || any_misaligned4(cu_seqlens, block_table, lens, lse)) return HA_ERR_ALIGN;
-  if (workspace_bytes < sp.total || ((uintptr_t)workspace & 255) != 0) return HA_ERR_WORKSPACE;
+  if (workspace_bytes < space || ((uintptr_t)workspace & 255) != 0) return HA_ERR_WORKSPACE;
   if (a.c.n_pages == 0) a.max_blocks = 0;  // (no page is there: every sequence counts as empty)
   a.Q = Q;
   a.cache = reinterpret_cast<const unsigned char*>(cache);
@@ -203,12 +215,24 @@ int ha_cache4_attn_chunk(const void* Q, const void* cache, const int32_t* cu_seq
   a.lens = lens;
   a.out = out;
   a.lse = lse;
-  unsigned char* w = reinterpret_cast<unsigned char*>(workspace);
-  a.joins = reinterpret_cast<int32_t*>(w);
-  a.part_o = reinterpret_cast<float*>(w + sp.part_o);
-  a.part_ml = reinterpret_cast<float*>(w + sp.part_ml);
-  cache4_chunk_split(&a);
-  return launch_cache4_chunk(a, chunk->dtype, (hipStream_t)stream);
+  n.Q = Q;
+  n.cache = a.cache;
+  n.table = block_table;
+  n.lens = lens;
+  n.out = out;
+  n.lse = lse;
+  n.c = a.c;
+  n.q = a.q;
+  n.o = a.o;
+  n.n_seq = a.n_seq;
+  n.Hq = a.Hq;
+  n.max_blocks = a.max_blocks;
+  n.group = a.group;
+  n.rows = kNarrowRows;
+  n.tiles = 1;
+  n.cu = cu_seqlens;
+  n.rows_all = a.rows;
+  return launch_cache4_chunk(a, n, chunk->dtype, (hipStream_t)stream);
 }
 
 static size_t weights_space(const CacheChunkArgs& a, size_t* sums) {
