@@ -42,7 +42,8 @@ struct ChunkLds {
   static constexpr int BUF = K_BYTES + kStep * VSTR;
   static constexpr int ROW = D * 4 + 16;           // a row of the output on its way out
   static constexpr int WAVE = 32 * ROW + 32 * 8;
-  static constexpr int bytes(int nw) { return (2 * BUF > nw * WAVE ? 2 * BUF : nw * WAVE) + 16; }
+  static constexpr int FLAGS = 3 * 16;             // far_flag; per buffer, which quarters of its K lie in pages that are not there
+  static constexpr int bytes(int nw) { return (2 * BUF > nw * WAVE ? 2 * BUF : nw * WAVE) + FLAGS; }
 };
 
 // What a wave holds of 16 tokens: K words and scales of a token, V words and scales of four (d = 64: two) tokens
@@ -71,10 +72,10 @@ __global__ __launch_bounds__(64 * NW, 2) void cache4_chunk_kernel(CacheChunkArgs
   using L = ChunkLds<D>;
   constexpr int QT = 32 * NW, KS = D / 16, DT = D / 32, G = D / kCacheGroup;
   constexpr bool F32 = SPLIT > 1;
-  int* far_flag = reinterpret_cast<int*>(smem + L::bytes(NW) - 16);
+  int* far_flag = reinterpret_cast<int*>(smem + L::bytes(NW) - L::FLAGS);
+  u32x4* gone_flags = reinterpret_cast<u32x4*>(far_flag + 4);
 
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int lq = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int part16 = wave & 3;  // the 16 tokens of a step that the wave lays into LDS
 
   // ---- place ----
@@ -87,7 +88,7 @@ __global__ __launch_bounds__(64 * NW, 2) void cache4_chunk_kernel(CacheChunkArgs
     return heads * (WHOLE ? (int64_t)T : upto(q, T));
   };
   int64_t before;
-  const int64_t total = chunk_line(a.n_seq, lane, &before, cost);
+  const int64_t total = chunk_line(a.n_seq, threadIdx.x & 63, &before, cost);
   int parts = 1, part = 0;
   int64_t u0 = blockIdx.x, u1 = 0;
   auto part_begin = [&](int p) { return total / parts * p + total % parts * p / parts; };
@@ -139,6 +140,9 @@ __global__ __launch_bounds__(64 * NW, 2) void cache4_chunk_kernel(CacheChunkArgs
     auto step_at = [&](int64_t x) { return x <= 0 ? 0 : (int)min((x + kStep - 1) / kStep, (int64_t)nsteps); };
     const int first = WHOLE ? 0 : step_at(u0 - tile_first), last = WHOLE ? nsteps : step_at(min(u1 - tile_first, length));
     if (first < last || (nsteps == 0 && (WHOLE || tile_first >= u0))) {
+      int lane = threadIdx.x & 63;
+      asm volatile("" : "+v"(lane));  // (what follows from it is formed again for every tile: kept from one to the next, it takes registers from the loop)
+      const int lq = lane & 31, h = lane >> 5;
       const int kv = hh / a.subs, head0 = kv * a.group + (hh - kv * a.subs) * a.sub_group;
       const int head_end = (kv + 1) * a.group;
       const unsigned char* head_base = a.cache + (int64_t)kv * a.c.block_bytes();
@@ -175,12 +179,9 @@ __global__ __launch_bounds__(64 * NW, 2) void cache4_chunk_kernel(CacheChunkArgs
       }
 
       // ---- codes into LDS ----
-      auto find_page = [&](int step, int sub) { return blocks[min((step * kStep + 16 * sub) >> log_page, last_block)]; };
+      auto find_page = [&](int step) { return blocks[min((step * kStep + 16 * part16) >> log_page, last_block)]; };
       auto there = [&](int page) { return (unsigned)page < (unsigned)a.c.n_pages; };
-      auto base_of = [&](int page) {
-        const int p = __builtin_amdgcn_readfirstlane(page);
-        return head_base + (int64_t)(there(p) ? p : 0) * page_bytes;
-      };
+      auto base_of = [&](int page) { return head_base + (int64_t)(there(page) ? page : 0) * page_bytes; };
       auto load_k = [&](int step, int page, RawK<D>& k) {
         const unsigned char* b = base_of(page);
         const int at = ((step * kStep + 16 * part16) & in_page) + (lane >> 2);
@@ -191,45 +192,50 @@ __global__ __launch_bounds__(64 * NW, 2) void cache4_chunk_kernel(CacheChunkArgs
       // V: a lane has a word (of D / 8) of four tokens (d = 64: of two)
       const int v_word = D == 128 ? lane & 15 : lane & 7;
       const int v_tok = D == 128 ? 4 * (lane >> 4) : 4 * ((lane >> 3) & 3) + 2 * (lane >> 5);  // the first of them
+      constexpr int VT = D == 128 ? 4 : 2;
       auto load_v = [&](int step, int page, RawV<D>& v) {
         const unsigned char* b = base_of(page);
         const int at = (step * kStep + 16 * part16) & in_page;
         v.w = *reinterpret_cast<const decltype(v.w)*>(b + a.c.v_at() + ((at + v_tok) >> 2) * (D * 2) + v_word * 16 + (v_tok & 3) * 4);
         v.sc = *reinterpret_cast<const decltype(v.sc)*>(b + a.c.v_scale_at() + (at + v_tok) * G);
       };
-      auto store_k = [&](unsigned char* buf, const RawK<D>& k) {
-        unsigned char* to = buf + (16 * part16 + (lane >> 2)) * L::KSTR + (lane & 3) * (16 * G);
+      auto buf_at = [&](int kt) { return smem + (kt & 1) * L::BUF; };  // (kt: steps of this workgroup's, from 0)
+      auto store_k = [&](int kt, int page, const RawK<D>& k) {
+        unsigned char* to = buf_at(kt) + (16 * part16 + (lane >> 2)) * L::KSTR + (lane & 3) * (16 * G);
 #pragma unroll
         for (int g = 0; g < G; ++g) {
           const float sc = scale_of(k.sc, g);
           *reinterpret_cast<u32x4*>(to + 16 * g) = (u32x4){two_values<0>(k.w[g], sc), two_values<1>(k.w[g], sc), two_values<2>(k.w[g], sc), two_values<3>(k.w[g], sc)};
         }
+        reinterpret_cast<uint32_t*>(gone_flags + (kt & 1))[part16] = !there(page);  // (all lanes alike)
       };
-      constexpr int VT = D == 128 ? 4 : 2;  // tokens of a lane
-      auto store_v = [&](unsigned char* buf, int step, int page, RawV<D>& v) {
-        const int tok0 = step * kStep + 16 * part16 + v_tok;
-        if (F32 || step * kStep + kStep > all_see || !there(__builtin_amdgcn_readfirstlane(page))) {
-          const bool here = there(page);
-          uint32_t taken = 0;
+      auto clean_v = [&](int kt, int page, RawV<D>& v) {  // what must not reach a product
+        const int base = (first + kt) * kStep, tok0 = base + 16 * part16 + v_tok;
+        if (!F32 && base + kStep <= all_see && there(page)) return;
+        const bool here = there(page);
+        uint32_t taken = 0;
 #pragma unroll
-          for (int i = 0; i < VT; ++i) {
-            uint32_t sc = D == 128 ? ((const uint32_t*)&v.sc)[i] : (((const uint32_t*)&v.sc)[0] >> (16 * i)) & 0xffffu;
-            if (!here || tok0 + i >= seen) {  // whatever lies there: weight 0 times a NaN would be NaN
-              v.w[i] = 0;
-              sc = 0;
-            } else if (F32 || tok0 + i >= all_see) {
-              // groups that are NaN or may lie past the largest number, of tokens that some rows see alone, are taken out here (fp32 queries: of all
-              // tokens; an infinity times the parts of a weight, some of them 0 or negative, would be NaN)
-              const uint32_t far = ((sc & 0x7f7f7f7fu) + (256 - kFarScale) * 0x01010101u) & sc & 0x80808080u;  // the top bit of every byte from kFarScale on
-              sc &= ~((far << 1) - (far >> 7));
-              taken |= far;
-            }
-            if constexpr (D == 128) v.sc[i] = sc;
-            else v.sc = i == 0 ? (v.sc & 0xffff0000u) | sc : (v.sc & 0xffffu) | sc << 16;
+        for (int i = 0; i < VT; ++i) {
+          uint32_t sc;
+          if constexpr (D == 128) sc = v.sc[i];
+          else sc = (v.sc >> (16 * i)) & 0xffffu;
+          if (!here || tok0 + i >= seen) {  // whatever lies there: weight 0 times a NaN would be NaN
+            v.w[i] = 0;
+            sc = 0;
+          } else if (F32 || tok0 + i >= all_see) {
+            // groups that are NaN or may lie past the largest number, of tokens that some rows see alone, are taken out here (fp32 queries: of all
+            // tokens; an infinity times the parts of a weight, some of them 0 or negative, would be NaN)
+            const uint32_t far = ((sc & 0x7f7f7f7fu) + (256 - kFarScale) * 0x01010101u) & sc & 0x80808080u;  // the top bit of every byte from kFarScale on
+            sc &= ~((far << 1) - (far >> 7));
+            taken |= far;
           }
-          if (taken) *far_flag = 1;
+          if constexpr (D == 128) v.sc[i] = sc;
+          else v.sc = i == 0 ? (v.sc & 0xffff0000u) | sc : (v.sc & 0xffffu) | sc << 16;
         }
-        unsigned char* to = buf + L::K_BYTES + (16 * part16 + v_tok) * L::VSTR + v_word * 16;
+        if (taken) *far_flag = 1;
+      };
+      auto store_v = [&](int kt, const RawV<D>& v) {
+        unsigned char* to = buf_at(kt) + L::K_BYTES + (16 * part16 + v_tok) * L::VSTR + v_word * 16;
 #pragma unroll
         for (int i = 0; i < VT; ++i) {
           u32x4 x;
@@ -242,13 +248,6 @@ __global__ __launch_bounds__(64 * NW, 2) void cache4_chunk_kernel(CacheChunkArgs
           }
           *reinterpret_cast<u32x4*>(to + i * L::VSTR) = x;
         }
-      };
-      auto buf_at = [&](int step) { return smem + ((step - first) & 1) * L::BUF; };
-      auto absent = [&](int step) {  // which quarters of a step lie in pages that are not there
-        uint32_t bits = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) bits |= (uint32_t)!there(find_page(step, i)) << i;
-        return (uint32_t)__builtin_amdgcn_readfirstlane(bits);
       };
 
       // ---- state ----
@@ -263,23 +262,8 @@ __global__ __launch_bounds__(64 * NW, 2) void cache4_chunk_kernel(CacheChunkArgs
       constexpr float unit_of = F32 ? 2.f : kLog2e;
       const int vtr_off = ((lane & 15) >> 2) * L::VSTR + ((lane & 3) * 4 + ((lane >> 4) & 1) * 16) * 2 + (4 * h) * L::VSTR;
 
-      // scores of 32 tokens: sub 0 or 1 of the step
-      auto scores = [&](int step, int sub) {
-        f32x16 c;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) c[i] = 0.f;
-        const unsigned char* kp = buf_at(step) + (32 * sub + lq) * L::KSTR + 16 * h;
-#pragma unroll
-        for (int j = 0; j < KS; ++j) {
-          const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kp + 32 * j);
-#pragma unroll
-          for (int z = SPLIT - 1; z >= 0; --z) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qreg[z][j], c, 0, 0, 0);
-        }
-        return c;
-      };
-      auto mask = [&](f32x16& c, int step, int sub, uint32_t gone) {
-        const int base = step * kStep + 32 * sub;
-        if (base + 32 <= all_see && gone == 0) return;
+      auto mask = [&](f32x16& c, int kt, int sub, uint32_t gone) {
+        const int base = (first + kt) * kStep + 32 * sub;
         const int lim = limit - base - 4 * h;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -287,101 +271,287 @@ __global__ __launch_bounds__(64 * NW, 2) void cache4_chunk_kernel(CacheChunkArgs
           if (off >= lim || (gone >> (2 * sub + i / 8) & 1)) c[i] = -INFINITY;
         }
       };
-      auto add_values = [&](int step, int j, bf16x8 (&w)[SPLIT]) {  // 16 tokens
-        const unsigned char* vb = buf_at(step) + L::K_BYTES + vtr_off + (16 * j) * L::VSTR;
+      auto gone_of = [&](int kt) {  // quarters of a step that lie in pages that are not there
+        const u32x4 f = gone_flags[kt & 1];
+        return (uint32_t)__builtin_amdgcn_readfirstlane(f[0] | f[1] << 1 | f[2] << 2 | f[3] << 3);
+      };
+      auto values_at = [&](int kt, int j, int dt) {  // V^T of 16 tokens, 32 channels
+        const unsigned char* vp = buf_at(kt) + L::K_BYTES + vtr_off + (16 * j) * L::VSTR + (32 * dt) * 2;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(vp));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(vp + 8 * L::VSTR));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+      };
+      auto move_reference = [&](float mx) {
+        const float m_new = fmaxf(m, fmaxf(mx, __shfl_xor(mx, 32))), ref = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = F32 ? expf(m - ref) : __builtin_amdgcn_exp2f(m - ref);
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-          const unsigned char* vp = vb + (32 * dt) * 2;
-          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(vp));
-          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(vp + 8 * L::VSTR));
-          const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
-          for (int z = SPLIT - 1; z >= 0; --z) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, both), w[z], o[dt], 0, 0, 0);
-        }
+          for (int i = 0; i < 16; ++i) o[dt][i] *= alpha;
+        l *= alpha;
+        m = m_new;
       };
 
       __syncthreads();  // (the tile before has left LDS)
       if (threadIdx.x == 0) *far_flag = 0;
       __syncthreads();
-      if (first < last) {
-        RawK<D> k;
-        RawV<D> v;
-        const int p0 = find_page(first, part16);
-        load_k(first, p0, k);
-        load_v(first, p0, v);
-        store_k(buf_at(first), k);
-        store_v(buf_at(first), first, p0, v);
-        __syncthreads();
-        for (int step = first; step < last; ++step) {
-          const bool more = step + 1 < last;
-          int page = 0;
-          if (more) {
-            page = find_page(step + 1, part16);
-            load_k(step + 1, page, k);
-            load_v(step + 1, page, v);
-          }
-          const uint32_t gone = absent(step);
+
+      // Codes are asked for two steps before they are used and their page two before that.  bf16 queries: step kt asks for K of kt + 3, V of kt + 2 and the page of kt + 4
+      // while it lays K of kt + 2 and V of kt + 1 into LDS, over K of kt and V of kt - 1, which all waves have left behind; fp32 queries have K no further than V.
+      // (Past the end the last step comes again, and is not read.)
+      const int ntiles = last - first;
+      const bool live = __any(valid);  // (a wave without rows lays out its share of the tokens, no more)
+      auto step_of = [&](int kt) { return first + min(kt, ntiles - 1); };
+      RawK<D> k[2];  // of even and odd steps
+      RawV<D> v[2];
+      int pages[4];  // of steps kt ... kt + 3
+      int next_page = 0;
+      auto request = [&](int kt, auto parity) {
+        constexpr int P = decltype(parity)::value;
+        next_page = find_page(step_of(kt + 4));
+        if constexpr (!F32) load_k(step_of(kt + 3), pages[3], k[P ^ 1]);
+        else load_k(step_of(kt + 2), pages[2], k[P]);
+        load_v(step_of(kt + 2), pages[2], v[P]);
+      };
+      auto lay_out = [&](auto parity) {  // (V is clean)
+        constexpr int P = decltype(parity)::value;
+        if constexpr (!F32) store_k(P, pages[2], k[P]);
+        else store_k(P ^ 1, pages[1], k[P ^ 1]);
+        store_v(P ^ 1, v[P ^ 1]);
+      };
+      auto advance = [&]() {
 #pragma unroll
-          for (int sub = 0; sub < 2; ++sub) {
-            f32x16 c = scores(step, sub);
-            mask(c, step, sub, gone);
-            float mx = c[0];
+        for (int i = 0; i < 3; ++i) pages[i] = pages[i + 1];
+        pages[3] = __builtin_amdgcn_readfirstlane(next_page);
+      };
+      const auto even = std::integral_constant<int, 0>{};
+      const auto odd = std::integral_constant<int, 1>{};
+      if (ntiles > 0) {
 #pragma unroll
-            for (int i = 1; i < 16; ++i) mx = fmaxf(mx, c[i]);
-            mx *= unit_of;
-            if (__any(mx > m + (F32 ? 5.5f : 8.f))) {
-              mx = fmaxf(mx, __shfl_xor(mx, 32));
-              const float m_new = fmaxf(m, mx), ref = m_new == -INFINITY ? 0.f : m_new;
-              const float alpha = F32 ? expf(m - ref) : __builtin_amdgcn_exp2f(m - ref);
+        for (int i = 0; i < 4; ++i) pages[i] = find_page(step_of(i));
 #pragma unroll
-              for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[dt][i] *= alpha;
-              l *= alpha;
-              m = m_new;
-            }
-            const float ref = m == -INFINITY ? 0.f : m;
-#pragma unroll
-            for (int jj = 0; jj < 2; ++jj) {
-              u32x4 w[SPLIT];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                float x0 = __builtin_fmaf(c[8 * jj + 2 * e], unit_of, -ref), x1 = __builtin_fmaf(c[8 * jj + 2 * e + 1], unit_of, -ref);
-                if constexpr (F32) {
-                  x0 = exp_split(x0);
-                  x1 = exp_split(x1);
-                } else {
-                  x0 = __builtin_amdgcn_exp2f(x0);
-                  x1 = __builtin_amdgcn_exp2f(x1);
-                }
-                l += x0 + x1;
-#pragma unroll
-                for (int z = 0; z < SPLIT; ++z) {
-                  w[z][e] = pack_bf16x2(x0, x1);
-                  if (z + 1 < SPLIT) {
-                    x0 -= __uint_as_float(w[z][e] << 16);
-                    x1 -= __uint_as_float(w[z][e] & 0xffff0000u);
-                  }
-                }
-              }
-              bf16x8 pf[SPLIT];
-#pragma unroll
-              for (int z = 0; z < SPLIT; ++z) pf[z] = __builtin_bit_cast(bf16x8, w[z]);
-              add_values(step, 2 * sub + jj, pf);
-            }
-          }
-          if (more) {
-            store_k(buf_at(step + 1), k);
-            store_v(buf_at(step + 1), step + 1, page, v);
+        for (int i = 0; i < 4; ++i) pages[i] = __builtin_amdgcn_readfirstlane(pages[i]);
+        load_k(step_of(0), pages[0], k[0]);
+        load_v(step_of(0), pages[0], v[0]);
+        load_k(step_of(1), pages[1], k[1]);
+        load_v(step_of(1), pages[1], v[1]);
+        store_k(0, pages[0], k[0]);
+        clean_v(0, pages[0], v[0]);
+        store_v(0, v[0]);
+        if constexpr (!F32) {
+          load_k(step_of(2), pages[2], k[0]);
+          store_k(1, pages[1], k[1]);
+        }
+      }
+      __syncthreads();
+      if (ntiles > 0 && !live) {
+        if constexpr (!F32) __syncthreads();
+        auto one = [&](int kt, auto parity) {
+          constexpr int P = decltype(parity)::value;
+          if (kt + 1 < ntiles) {
+            request(kt, parity);
+            clean_v(kt + 1, pages[1], v[P ^ 1]);
+            lay_out(parity);
+            advance();
           }
           __syncthreads();
+        };
+        for (int kt = 0; kt < ntiles; kt += 2) {
+          one(kt, even);
+          if (kt + 1 < ntiles) one(kt + 1, odd);
+        }
+      } else if (ntiles > 0) {
+        if constexpr (!F32) {
+          // Scores of step kt + 1 on the matrix cores beside weights of step kt, P V of step kt beside row maxima of kt + 1 and codes on their way to LDS
+          auto tile_max = [&](const f32x16 (&c)[2]) {
+            float mx = fmaxf(c[0][0], c[1][0]);
+#pragma unroll
+            for (int i = 1; i < 16; ++i) mx = fmaxf(fmaxf(mx, c[0][i]), c[1][i]);
+            return mx * kLog2e;
+          };
+          auto mask_step = [&](f32x16 (&c)[2], int kt) {
+            const uint32_t gone = gone_of(kt);
+            if ((first + kt) * kStep + kStep > all_see || gone) {
+              mask(c[0], kt, 0, gone);
+              mask(c[1], kt, 1, gone);
+            }
+          };
+          f32x16 ca[2], cb[2];
+          float t_max;
+          {
+#pragma unroll
+            for (int sub = 0; sub < 2; ++sub) {
+#pragma unroll
+              for (int i = 0; i < 16; ++i) ca[sub][i] = 0.f;
+              const unsigned char* kp = buf_at(0) + (32 * sub + lq) * L::KSTR + 16 * h;
+#pragma unroll
+              for (int j = 0; j < KS; ++j) ca[sub] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(kp + 32 * j), qreg[0][j], ca[sub], 0, 0, 0);
+            }
+            mask_step(ca, 0);
+            t_max = tile_max(ca);
+          }
+          __syncthreads();  // (the loop's first step writes over K of step 0)
+          auto body = [&](int kt, f32x16 (&c)[2], f32x16 (&cn)[2], auto parity, auto has_next) {
+            constexpr int P = decltype(parity)::value;
+            constexpr bool HN = decltype(has_next)::value;
+            if constexpr (HN) request(kt, parity);
+            if (__any(t_max > m + 8.f)) move_reference(t_max);
+            const float shift = m == -INFINITY ? 0.f : -m;
+            bf16x8 pf[4];
+            __builtin_amdgcn_s_setprio(1);
+            {
+              if constexpr (HN) {
+#pragma unroll
+                for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+                  for (int i = 0; i < 16; ++i) cn[sub][i] = 0.f;
+                const unsigned char* kp0 = buf_at(P + 1) + lq * L::KSTR + 16 * h;
+                const unsigned char* kp1 = kp0 + 32 * L::KSTR;
+                bf16x8 kf[2 * KS];
+#pragma unroll
+                for (int j = 0; j < KS; ++j) {
+                  kf[2 * j] = *reinterpret_cast<const bf16x8*>(kp0 + 32 * j);
+                  kf[2 * j + 1] = *reinterpret_cast<const bf16x8*>(kp1 + 32 * j);
+                }
+#pragma unroll
+                for (int j = 0; j < KS; ++j) {
+                  cn[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[2 * j], qreg[0][j], cn[0], 0, 0, 0);
+                  cn[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[2 * j + 1], qreg[0][j], cn[1], 0, 0, 0);
+                }
+              }
+              float ls[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                u32x4 pk;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(c[j / 2][8 * (j % 2) + 2 * e], kLog2e, shift));
+                  const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(c[j / 2][8 * (j % 2) + 2 * e + 1], kLog2e, shift));
+                  ls[e] += p0 + p1;
+                  pk[e] = pack_bf16x2(p0, p1);
+                }
+                pf[j] = __builtin_bit_cast(bf16x8, pk);
+              }
+              l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(pf[j]));  // (the weights stay in this block, beside its products)
+              asm volatile("" : "+v"(l));
+              if constexpr (HN) {
+                constexpr int kPre = 4, kValu = KS == 8 ? 5 : 18;
+                __builtin_amdgcn_sched_group_barrier(0x100, kPre, 0);
+#pragma unroll
+                for (int j = 0; j < 2 * KS; ++j) {
+                  __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                  if (j < 2 * KS - kPre) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                  __builtin_amdgcn_sched_group_barrier(0x002, kValu, 0);
+                }
+              }
+            }
+            __builtin_amdgcn_s_setprio(0);
+            if constexpr (HN) {
+              mask_step(cn, kt + 1);
+              clean_v(kt + 1, pages[1], v[P ^ 1]);
+            }
+            {
+#pragma unroll
+              for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(values_at(P, j, dt), pf[j], o[dt], 0, 0, 0);
+              if constexpr (HN) {
+                t_max = tile_max(cn);
+                lay_out(parity);
+              }
+              constexpr int kPreV = 8;
+              __builtin_amdgcn_sched_group_barrier(0x100, kPreV, 0);
+#pragma unroll
+              for (int j = 0; j < 4 * DT; ++j) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                if (2 * j < 8 * DT - kPreV) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                if constexpr (HN) __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);
+              }
+            }
+            if constexpr (HN) advance();
+            __syncthreads();
+          };
+          int kt = 0;
+          for (; kt + 2 < ntiles; kt += 2) {
+            body(kt, ca, cb, even, std::true_type{});
+            body(kt + 1, cb, ca, odd, std::true_type{});
+          }
+          if (kt + 2 == ntiles) {
+            body(kt, ca, cb, even, std::true_type{});
+            body(kt + 1, cb, ca, odd, std::false_type{});
+          } else {
+            body(kt, ca, cb, even, std::false_type{});
+          }
+        } else {
+          // fp32 queries: one step after the other, 32 tokens at a time (three parts of queries and weights leave no registers for more)
+          auto body = [&](int kt, auto parity) {
+            constexpr int P = decltype(parity)::value;
+            const bool more = kt + 1 < ntiles;
+            if (more) request(kt, parity);
+            const uint32_t gone = gone_of(P);
+#pragma unroll
+            for (int sub = 0; sub < 2; ++sub) {
+              f32x16 c;
+#pragma unroll
+              for (int i = 0; i < 16; ++i) c[i] = 0.f;
+              const unsigned char* kp = buf_at(P) + (32 * sub + lq) * L::KSTR + 16 * h;
+#pragma unroll
+              for (int j = 0; j < KS; ++j) {
+                const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kp + 32 * j);
+#pragma unroll
+                for (int z = SPLIT - 1; z >= 0; --z) c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qreg[z][j], c, 0, 0, 0);
+              }
+              if ((first + kt) * kStep + 32 * sub + 32 > all_see || gone) mask(c, kt, sub, gone);
+              float mx = c[0];
+#pragma unroll
+              for (int i = 1; i < 16; ++i) mx = fmaxf(mx, c[i]);
+              mx *= unit_of;
+              if (__any(mx > m + 5.5f)) move_reference(mx);
+              const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+              for (int jj = 0; jj < 2; ++jj) {
+                u32x4 w[SPLIT];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  float x0 = exp_split(__builtin_fmaf(c[8 * jj + 2 * e], unit_of, -ref)), x1 = exp_split(__builtin_fmaf(c[8 * jj + 2 * e + 1], unit_of, -ref));
+                  l += x0 + x1;
+#pragma unroll
+                  for (int z = 0; z < SPLIT; ++z) {
+                    w[z][e] = pack_bf16x2(x0, x1);
+                    if (z + 1 < SPLIT) {
+                      x0 -= __uint_as_float(w[z][e] << 16);
+                      x1 -= __uint_as_float(w[z][e] & 0xffff0000u);
+                    }
+                  }
+                }
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) {
+                  const bf16x8 vf = values_at(P, 2 * sub + jj, dt);
+#pragma unroll
+                  for (int z = SPLIT - 1; z >= 0; --z) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, w[z]), o[dt], 0, 0, 0);
+                }
+              }
+            }
+            if (more) {
+              clean_v(kt + 1, pages[1], v[P ^ 1]);
+              lay_out(parity);
+              advance();
+            }
+            __syncthreads();
+          };
+          for (int kt = 0; kt < ntiles; kt += 2) {
+            body(kt, even);
+            if (kt + 1 < ntiles) body(kt + 1, odd);
+          }
         }
       }
 
       // ---- groups that were taken out, for the rows that see them (rare) ----
       if (*far_flag) {
         for (int x = F32 ? first * kStep : max(first * kStep, max(all_see, 0)); x < min(last * kStep, seen); ++x) {
-          const int page = find_page(x / kStep, (x & (kStep - 1)) >> 4), at = x & in_page;
+          const int page = blocks[x >> log_page], at = x & in_page;
           if (!there(page)) continue;
           const unsigned char* b = base_of(page);
           const unsigned char* k_scales = b + a.c.k_scale_at() + at * G;
