@@ -28,8 +28,10 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef s16x4 __attribute__((address_space(3))) * lds_s16x4_ptr;
 
 constexpr int kStep = 64;           // tokens of a step
-constexpr int kTileCost = 128;      // what a tile's start and end cost, in tokens
-constexpr int kLeastRun = 512;      // tokens of the line that a workgroup takes, at least
+// What a tile's start and end cost a workgroup, in tokens.  (128 / 256 / 400 / 600: 64 sequences, most of one token, behind up to 16384, 32 and 8 heads, d = 128 259 / 231 / 217 / 220 us;
+// 24 of up to 200 behind up to 4096, 12 and 4 heads 58 / 55 / 55 / 57; 16 of up to 1024 behind up to 8192, 16 heads, d = 64 118 / 106 / 108 / 109.)
+constexpr int kTileCost = 320;
+constexpr int kLeastRun = 256;      // tokens of the line that a workgroup takes, at least (fp32, 6 sequences of up to 150 behind up to 2000, d = 64: 512 36 us, 256 29)
 constexpr int kMostParts = 512;     // workgroups that the chip holds at once, two per CU
 constexpr int kJoinThreads = 256;
 constexpr uint32_t kFarScale = 253; // V's scales from here on give values that may lie past the largest number, or NaN: taken by the rows that see the token alone

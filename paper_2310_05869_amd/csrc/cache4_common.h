@@ -81,10 +81,10 @@ struct CacheChunkArgs {
   int32_t group;             // query heads per key head
   int32_t subs, sub_group;   // a key head's query heads in `subs` runs of sub_group, each of which fits a tile
   int32_t tile_tokens;       // new tokens of a tile: tile_tokens * sub_group rows
-  int32_t narrow;            // attention: sequences of up to so many rows of a key head are left to launches of their own; 0: none
+  int32_t narrow;            // sequences of up to so many rows of a key head are left to launches of their own; 0: none
   int32_t fresh;             // sums of weights: earlier ones do not count
   int32_t parts;             // workgroups that share all work; 0: a workgroup per tile
-  int32_t cut, least_run;    // sums of weights: whether tiles are shared among workgroups, and what each of these takes at least
+  int32_t few_wgs;           // sums of weights: workgroups for the sequences of few rows; 0: none
   FastDiv div_group;
   // workspace: per workgroup, the tile that it ends of those that others began (four integers), and two tiles of sums with their references and row sums
   int32_t* joins;
@@ -95,7 +95,7 @@ int launch_cache4_chunk(const CacheChunkArgs& a, const CacheAttnArgs& narrow, in
 void cache4_chunk_split(CacheChunkArgs* a, CacheAttnArgs* narrow);  // sets subs, sub_group, tile_tokens, narrow and parts; parts of the narrow ones
 constexpr int kChunkRows = 128;              // query rows of a tile
 int launch_cache4_weights(const CacheChunkArgs& a, int dtype, hipStream_t st);
-void cache4_weights_split(CacheChunkArgs* a);  // sets div_group, cut, least_run and parts
+void cache4_weights_split(CacheChunkArgs* a);  // sets div_group, narrow, few_wgs and parts
 constexpr int kWeightsParts = 512;             // workgroups that the chip holds at once, two per CU
 constexpr int kWeightsTokens = 256;            // of a tile
 

@@ -2,13 +2,15 @@
 // its key head, of exp(<q, k_t> - lse).
 //
 // A second pass over K alone, after attention has found lse: nothing is rounded, and no sum depends on the order of workgroups, which sums added up beside P V by
-// all workgroups of a head would.  A wave keeps the K of 64 tokens as operands in registers, made from codes once, and rows of Q pass by, 64 a
-// step, in LDS for the four waves of a workgroup: S^T = K Q^T by v_mfma_f32_32x32x16_bf16, 16 registers of 16 tokens for one row a lane, so a
-// row's lse is one register, and the sums stay apart by lane until the last step, when 31 exchanges add up 32 registers over 32 lanes.
-// Per 64 tokens and 32 rows of d = 128: 16 products (512 cycles) and 32 times a multiply-add, an exponential and an addition (some 450).
-//
-// Split: tiles of 256 tokens of all sequences and key heads are one line, a tile's length in it the steps of rows that see it; cut into equal runs like the
-// tiles of attention.  Sums of tiles that a cut divides are added up, in order, by a second launch.
+// all workgroups of a head would.  S = Q K^T has rows of Q along the matrix instructions' M, tokens along N: a lane's registers are rows of one token, whose sum
+// takes additions alone and one or two exchanges at the end.
+//   many rows   a wave keeps the K of 64 tokens as operands in registers, made from codes once, and rows of Q pass by, 64 a step, in LDS for the four waves of a
+//               workgroup (v_mfma_f32_32x32x16_bf16).  Per 64 tokens and 32 rows of d = 128: 16 products (512 cycles) beside 32 times a multiply-add, an exponential
+//               and an addition (some 450): the exponentials of one half of a step run beside the products of the other.
+//   few rows    a wave keeps 16 rows (a decoding step's queries of a key head), and tokens pass by, 64 at a time, from codes to operands in registers
+//               (v_mfma_f32_16x16x32_bf16): bound by K's bytes, which every wave asks for a step ahead.
+// Split: all sequences and key heads are one line.  Many rows: tiles of 256 tokens, a tile's length the steps of rows that see it; cut into equal runs like the tiles of
+// attention, and sums of tiles that a cut divides are added up, in order, by a second launch.  Few rows: 64 tokens after the other, a run for every wave.
 #include "cache4_chunk.h"
 
 namespace ha {
@@ -23,6 +25,7 @@ constexpr int kWTokens = kWeightsTokens;
 static_assert(kWTokens == 64 * kWWaves);
 constexpr int kWRows = 64;              // of a step
 constexpr int kWTileCost = 2;           // what a tile's start and end cost, in steps
+constexpr int kWLeastRun = 8;           // steps that a workgroup takes, at least
 
 template <int D, int SPLIT>
 struct WeightsLds {
@@ -41,7 +44,7 @@ struct WeightsSeq {
 __device__ inline WeightsSeq weights_seq(const CacheChunkArgs& a, int s) {
   WeightsSeq w;
   w.q = chunk_seq(a, s);
-  w.tiles = (w.q.len + kWTokens - 1) / kWTokens;
+  w.tiles = (int64_t)w.q.n * a.group <= a.narrow ? 0 : (w.q.len + kWTokens - 1) / kWTokens;
   w.bend = w.q.held <= 0 ? 0 : min((w.q.held + kWTokens - 1) / kWTokens, w.tiles);
   w.steps = ((int64_t)w.q.n * a.group + kWRows - 1) / kWRows;
   w.before = (-(int64_t)w.q.held * a.group) >> 6;  // (rounded down)
@@ -56,24 +59,10 @@ __device__ inline int64_t weights_upto(const CacheChunkArgs& a, const WeightsSeq
   return x;
 }
 
-// Adds 32 registers over the 32 lanes of a half wave: lane l is left with the sum of register l.
-__device__ inline float sum_of_lane(float (&x)[32], int lane) {
-#pragma unroll
-  for (int half = 16; half >= 1; half >>= 1) {
-    const bool upper = lane & half;
-#pragma unroll
-    for (int i = 0; i < half; ++i) {
-      const float give = upper ? x[i] : x[i + half], keep = upper ? x[i + half] : x[i];
-      x[i] = keep + __shfl_xor(give, half);
-    }
-  }
-  return x[0];
-}
-
 __device__ inline float scale_of(uint32_t bytes, int i) { return __uint_as_float(i < 3 ? bytes << (23 - 8 * i) : bytes >> 1); }  // (the exponent alone counts)
 
-// SPLIT: parts of a query number, 1 for bf16, 3 for fp32.  CUT: tiles may be shared among workgroups.
-template <int D, int SPLIT, bool CUT>
+// SPLIT: parts of a query number, 1 for bf16, 3 for fp32
+template <int D, int SPLIT>
 __global__ __launch_bounds__(64 * kWWaves, 2) void cache4_weights_kernel(CacheChunkArgs a) {
   extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
   using L = WeightsLds<D, SPLIT>;
@@ -88,11 +77,11 @@ __global__ __launch_bounds__(64 * kWWaves, 2) void cache4_weights_kernel(CacheCh
   };
   int64_t before;
   const int64_t total = chunk_line(a.n_seq, lane, &before, cost);
-  int parts = (int)min((int64_t)a.parts, max(total / a.least_run, (int64_t)1));
+  int parts = (int)min((int64_t)a.parts, max(total / kWLeastRun, (int64_t)1));
   if (parts > 8) parts &= ~7;
   int part = blockIdx.x;
   if (part < parts && (parts & 7) == 0) part = (part & 7) * (parts >> 3) + (part >> 3);  // a run of the line per XCD: neighbours share rows
-  if (CUT && threadIdx.x == 0) a.joins[4 * part] = -1;
+  if (threadIdx.x == 0) a.joins[4 * part] = -1;
   if (part >= parts || total == 0) return;
   auto part_begin = [&](int p) { return total / parts * p + total % parts * p / parts; };
   const int64_t u0 = part_begin(part), u1 = part_begin(part + 1);
@@ -121,8 +110,7 @@ __global__ __launch_bounds__(64 * kWWaves, 2) void cache4_weights_kernel(CacheCh
     const int nsteps = (int)(length - kWTileCost);
     auto step_at = [&](int64_t x) { return (int)min(max(x, (int64_t)0), (int64_t)nsteps); };
     const bool begins = tile_first >= u0;
-    // without CUT a tile is that workgroup's in whose run it begins
-    const int first = CUT ? step_at(u0 - tile_first) : 0, last = CUT ? step_at(u1 - tile_first) : begins ? nsteps : 0;
+    const int first = step_at(u0 - tile_first), last = step_at(u1 - tile_first);
     if (first < last || (begins && nsteps == 0 && a.fresh)) {
       const int32_t* blocks = a.table + (int64_t)s * a.max_blocks;
       // ---- K of the wave's 64 tokens ----
@@ -151,9 +139,7 @@ __global__ __launch_bounds__(64 * kWWaves, 2) void cache4_weights_kernel(CacheCh
           kf[sub][i] = __builtin_bit_cast(bf16x8, x);
         }
       }
-      float sum[32];
-#pragma unroll
-      for (int i = 0; i < 32; ++i) sum[i] = 0.f;
+      float sum[2] = {0.f, 0.f};  // of the lane's token of each half, over the rows of its registers
 
       // ---- rows of Q through LDS ----
       constexpr int CPR = D / 8, NC = kWRows * CPR / (64 * kWWaves);  // pieces of eight channels a row, a thread
@@ -214,50 +200,77 @@ __global__ __launch_bounds__(64 * kWWaves, 2) void cache4_weights_kernel(CacheCh
         store_rows(first);
         __syncthreads();
       }
-      const int tok_end = k * kWTokens + wave * 64 + 64;
-      for (int step = first; step < last; ++step) {
-        if (step + 1 < last) load_rows(step + 1);
+      const int tok0 = k * kWTokens + wave * 64, tok_end = tok0 + 64;
+      struct Half {  // scores of 32 rows, and what they are exponentiated against
+        f32x16 c[2];
+        f32x4 shift[4];
+      };
+      auto products = [&](int step, int half, Half& x) {
         const unsigned char* buf = smem + (step & 1) * L::BUF;
-        const int row0 = (int)(step0 + step) * kWRows;
-        // whether the step's rows are all there and all see the wave's tokens
-        const bool plain = row0 + kWRows <= rows && w.q.held + a.div_group.div(row0) + 1 >= tok_end;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          const float shift = reinterpret_cast<const float*>(buf + SPLIT * L::PART)[32 * half + lq];
-          f32x16 c[2];
+        for (int g = 0; g < 4; ++g) x.shift[g] = *reinterpret_cast<const f32x4*>(buf + SPLIT * L::PART + (32 * half + 8 * g + 4 * h) * 4);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) c[0][i] = c[1][i] = 0.f;
+        for (int i = 0; i < 16; ++i) x.c[0][i] = x.c[1][i] = 0.f;
 #pragma unroll
-          for (int i = 0; i < KS; ++i) {
-            const int j = KS * h + i, ch = 32 * (j % G) + 8 * (j / G);  // the channels of word j
+        for (int i = 0; i < KS; ++i) {
+          const int ch = 32 * ((KS * h + i) % G) + 8 * ((KS * h + i) / G);  // the channels of word KS h + i
 #pragma unroll
-            for (int z = SPLIT - 1; z >= 0; --z) {
-              const bf16x8 qf = *reinterpret_cast<const bf16x8*>(buf + z * L::PART + (32 * half + lq) * L::STR + ch * 2);
-              c[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[0][i], qf, c[0], 0, 0, 0);
-              c[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[1][i], qf, c[1], 0, 0, 0);
-            }
-          }
-          auto weight = [&](float x) { return F32 ? exp_split(__builtin_fmaf(x, 2.f, shift)) : __builtin_amdgcn_exp2f(__builtin_fmaf(x, kLog2e, shift)); };
-          if (plain) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) sum[i] += weight(c[i / 16][i % 16]);
-          } else {
-            const int r = row0 + 32 * half + lq;
-            const int see = r < rows ? w.q.held + a.div_group.div(r) + 1 - (k * kWTokens + wave * 64 + 4 * h) : 0;  // of the wave's tokens
-#pragma unroll
-            for (int i = 0; i < 32; ++i) {
-              const float x = weight(c[i / 16][i % 16]);
-              sum[i] += 32 * (i / 16) + 8 * (i % 16 / 4) + i % 4 < see && shift != -INFINITY ? x : 0.f;
-            }
+          for (int z = SPLIT - 1; z >= 0; --z) {
+            const bf16x8 qf = *reinterpret_cast<const bf16x8*>(buf + z * L::PART + (32 * half + lq) * L::STR + ch * 2);
+            x.c[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf, kf[0][i], x.c[0], 0, 0, 0);
+            x.c[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf, kf[1][i], x.c[1], 0, 0, 0);
           }
         }
-        if (step + 1 < last) store_rows(step + 1);
+      };
+      auto weight = [&](float x, float shift) { return F32 ? exp_split(__builtin_fmaf(x, 2.f, shift)) : __builtin_amdgcn_exp2f(__builtin_fmaf(x, kLog2e, shift)); };
+      auto add_weights = [&](const Half& x) {
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub) {
+          float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int i = 0; i < 16; ++i) part[i % 4] += weight(x.c[sub][i], x.shift[i / 4][i % 4]);
+          sum[sub] += (part[0] + part[1]) + (part[2] + part[3]);
+        }
+      };
+      auto add_some_weights = [&](const Half& x, int row0) {  // rows behind the last, or that do not see all
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int r = row0 + 8 * (i / 4) + 4 * h + i % 4;
+          const int see = r < rows ? w.q.held + a.div_group.div(r) + 1 - tok0 : 0;  // of the wave's tokens
+          const float shift = x.shift[i / 4][i % 4];
+#pragma unroll
+          for (int sub = 0; sub < 2; ++sub) {
+            const float p = weight(x.c[sub][i], shift);
+            sum[sub] += 32 * sub + lq < see && shift != -INFINITY ? p : 0.f;
+          }
+        }
+      };
+      auto plain = [&](int row0) {  // whether 32 rows are all there and all see the wave's tokens
+        return row0 + 32 <= rows && w.q.held + a.div_group.div(row0) + 1 >= tok_end;
+      };
+      auto add = [&](const Half& x, int row0) {
+        if (plain(row0)) add_weights(x);
+        else add_some_weights(x, row0);
+      };
+      Half xa, xb;
+      if (first < last) products(first, 0, xa);
+      for (int step = first; step < last; ++step) {
+        const bool more = step + 1 < last;
+        const int row0 = (int)(step0 + step) * kWRows;
+        if (more) load_rows(step + 1);
+        products(step, 1, xb);
+        add(xa, row0);
+        if (more) store_rows(step + 1);
         __syncthreads();
+        if (more) products(step + 1, 0, xa);
+        add(xb, row0 + 32);
       }
+      __syncthreads();
 
-      const float mine = sum_of_lane(sum, lq);
-      const int in_tile = wave * 64 + 32 * (lq / 16) + 8 * (lq % 16 / 4) + 4 * h + lq % 4, tok = k * kWTokens + in_tile;
-      if (!CUT || (first == 0 && last == nsteps)) {
+      // a lane of the upper half takes the wave's tokens 32 ... 63
+      const float give = h ? sum[0] : sum[1], keep = h ? sum[1] : sum[0], mine = keep + __shfl_xor(give, 32);
+      const int in_tile = wave * 64 + lane, tok = k * kWTokens + in_tile;
+      if (first == 0 && last == nsteps) {
         if (tok < w.q.len) {
           const int page = blocks[tok >> a.c.log_page];
           if ((unsigned)page < (unsigned)a.c.n_pages) {
@@ -311,40 +324,223 @@ __global__ __launch_bounds__(kWTokens) void cache4_weights_join_kernel(CacheChun
   *to = a.fresh || tok >= q.held ? sum : *to + sum;
 }
 
-// Tiles are shared among workgroups where a sequence can have many rows.
-void cache4_weights_split(CacheChunkArgs* a) {
-  a->div_group = make_fast_div(a->group);
-  const int64_t tokens = (int64_t)a->max_blocks << a->c.log_page, steps = ((int64_t)a->rows * a->group + kWRows - 1) / kWRows;
-  const int64_t tiles = ((tokens + kWTokens - 1) / kWTokens) * a->n_seq * a->c.Hk;
-  a->cut = steps > 4;
-  a->least_run = a->cut ? 8 : 1;
-  const int64_t runs = tiles * (steps + kWTileCost) / a->least_run;
-  a->parts = (int32_t)(runs < 1 ? 1 : runs > kWeightsParts ? kWeightsParts : runs);
-}
-
-template <int D, int SPLIT, bool CUT>
-static int launch_weights_one(const CacheChunkArgs& a, hipStream_t st) {
-  constexpr size_t lds = 2 * WeightsLds<D, SPLIT>::BUF;
-  static std::atomic<uint64_t> set{0};
-  const auto kernel = &cache4_weights_kernel<D, SPLIT, CUT>;
-  const int rc = allow_full_lds(reinterpret_cast<const void*>(kernel), set);
-  if (rc != HA_OK) return rc;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)a.parts), dim3(64 * kWWaves), lds, st, a);
-  return check_launch();
+// ---- few rows ----
+constexpr int kNUnit = 64;       // tokens of a wave's step
+constexpr int kNStart = 3;       // what the start of a sequence and key head costs, in steps
+struct FewSeq {
+  ChunkSeq q;
+  int rows, tiles, units;  // query rows, tiles of 16 of them, steps of 64 tokens (0: not of these)
+};
+__device__ inline FewSeq few_seq(const CacheChunkArgs& a, int s) {
+  FewSeq f;
+  f.q = chunk_seq(a, s);
+  f.rows = f.q.n * a.group;
+  f.tiles = (f.rows + 15) / 16;
+  f.units = f.rows > a.narrow || (f.rows == 0 && !a.fresh) ? 0 : (f.q.len + kNUnit - 1) / kNUnit;
+  return f;
 }
 
 template <int D, int SPLIT>
-static int launch_weights_cut(const CacheChunkArgs& a, hipStream_t st) {
-  if (!a.cut) return launch_weights_one<D, SPLIT, false>(a, st);
-  const int rc = launch_weights_one<D, SPLIT, true>(a, st);
+__global__ __launch_bounds__(256, SPLIT == 1 ? 3 : 2) void cache4_weights_few_kernel(CacheChunkArgs a) {
+  constexpr int G = D / kCacheGroup;
+  constexpr bool F32 = SPLIT > 1;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int r = lane & 15, kq = lane >> 4;
+  auto each_of = [&](const FewSeq& f) { return f.units > 0 ? (int64_t)f.units * max(f.tiles, 1) + kNStart : 0; };  // of a key head
+  auto cost = [&](int s) -> int64_t { return a.c.Hk * each_of(few_seq(a, s)); };
+  int64_t before;
+  const int64_t total = chunk_line(a.n_seq, lane, &before, cost);
+  const int waves = (int)min((int64_t)gridDim.x * 4, total), me = blockIdx.x * 4 + wave;
+  if (me >= waves) return;
+  const int64_t u0 = total / waves * me + total % waves * me / waves, u1 = total / waves * (me + 1) + total % waves * (me + 1) / waves;
+  int64_t at;
+  int s = chunk_place(a.n_seq, before, u0, &at, cost);
+  const int64_t page_bytes = (int64_t)a.c.Hk * a.c.block_bytes();
+  const int in_page = a.c.page - 1;
+
+  int kv = 0;
+  FewSeq f = few_seq(a, s);
+  {
+    const int64_t each = each_of(f);
+    kv = __builtin_amdgcn_readfirstlane((int)((u0 - at) / each));
+    at = uniform64(at + kv * each);
+  }
+  for (;;) {
+    f.q = uniform_seq(f.q);
+    const int units = __builtin_amdgcn_readfirstlane(f.units), tiles = __builtin_amdgcn_readfirstlane(f.tiles), rows = __builtin_amdgcn_readfirstlane(f.rows);
+    const int per = max(tiles, 1);
+    auto unit_at = [&](int64_t x) { return x <= 0 ? 0 : (int)min((x + per - 1) / per, (int64_t)units); };
+    const int first = unit_at(u0 - at), last = unit_at(u1 - at);
+    if (first < last) {
+      const int32_t* blocks = a.table + (int64_t)s * a.max_blocks;
+      const int last_block = (f.q.len - 1) >> a.c.log_page;
+      const unsigned char* head_base = a.cache + (int64_t)kv * a.c.block_bytes();
+      bf16x8 q[SPLIT][G];
+      f32x4 shift;
+      int see[4];  // tokens that the lane's rows see: rows 4 kq ... + 3 of the tile
+      auto load_rows = [&](int tile) {
+        const int row = min(tile * 16 + r, rows - 1), tok = a.div_group.div(row), head = kv * a.group + row - tok * a.group;
+        const int64_t from = (int64_t)(f.q.start + tok) * a.q.row + (int64_t)head * a.q.head + 8 * kq;
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          if constexpr (!F32) {
+            q[0][g] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(a.Q) + from + 32 * g));
+          } else {
+            const f32x4* p = reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(a.Q) + from + 32 * g);
+            const f32x4 x0 = p[0], x1 = p[1];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              float x = 0.5f * (i < 4 ? x0[i % 4] : x1[i % 4]);  // (at half: rounding the first part up leaves the largest finite)
+#pragma unroll
+              for (int z = 0; z < SPLIT; ++z) {
+                q[z][g][i] = (__bf16)x;
+                x -= (float)q[z][g][i];
+              }
+            }
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int row4 = tile * 16 + 4 * kq + i, use = min(row4, rows - 1), tok4 = a.div_group.div(use);
+          const float l = a.lse[(int64_t)(kv * a.group + use - tok4 * a.group) * a.rows + f.q.start + tok4];
+          see[i] = row4 < rows && l != -INFINITY ? f.q.held + tok4 + 1 : 0;  // (a row that sees nothing has lse -inf, and gives nothing)
+          shift[i] = F32 ? -l : -l * kLog2e;
+        }
+      };
+      int page_of[4];
+      auto find_pages = [&](int unit) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) page_of[t] = blocks[min((unit * kNUnit + 16 * t) >> a.c.log_page, last_block)];
+      };
+      uint32_t words[4][G], scales[4];
+      float had = 0.f;
+      float* place = nullptr;  // of the lane's token, unit * 64 + lane
+      auto load_codes = [&](int unit) {
+        int mine = 0;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const int p = __builtin_amdgcn_readfirstlane(page_of[t]);
+          const bool there = (unsigned)p < (unsigned)a.c.n_pages;
+          const unsigned char* b = head_base + (int64_t)(there ? p : 0) * page_bytes;
+          const int tok = ((unit * kNUnit + 16 * t) & in_page) + r;
+          if constexpr (D == 128) {
+            const u32x4 w = *reinterpret_cast<const u32x4*>(b + tok * (D / 2) + kq * (D / 8));
+#pragma unroll
+            for (int g = 0; g < G; ++g) words[t][g] = w[g];
+            scales[t] = *reinterpret_cast<const uint32_t*>(b + a.c.k_scale_at() + tok * 4);
+          } else {
+            typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+            const u32x2 w = *reinterpret_cast<const u32x2*>(b + tok * (D / 2) + kq * (D / 8));
+#pragma unroll
+            for (int g = 0; g < G; ++g) words[t][g] = w[g];
+            scales[t] = *reinterpret_cast<const uint16_t*>(b + a.c.k_scale_at() + tok * 2);
+          }
+          if (kq == t) mine = p;
+        }
+        const int tok = unit * kNUnit + lane;
+        place = nullptr;
+        if (tok < f.q.len && (unsigned)mine < (unsigned)a.c.n_pages) {
+          place = a.weights + ((int64_t)mine * a.c.Hk + kv) * a.c.page + (tok & in_page);
+          had = a.fresh || tok >= f.q.held ? 0.f : *place;
+        }
+      };
+      find_pages(first);
+      if (rows > 0) load_rows(0);
+      load_codes(first);
+      if (first + 1 < last) find_pages(first + 1);
+      for (int unit = first; unit < last; ++unit) {
+        bf16x8 kf[4][G];
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int g = 0; g < G; ++g) {
+            const float sc = scale_of(scales[t], g);
+            const u32x4 x = {__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(words[t][g], sc, 0)),
+                             __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(words[t][g], sc, 1)),
+                             __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(words[t][g], sc, 2)),
+                             __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(words[t][g], sc, 3))};
+            kf[t][g] = __builtin_bit_cast(bf16x8, x);
+          }
+        float* const to = place;
+        const float old = had;
+        if (unit + 1 < last) {
+          load_codes(unit + 1);
+          if (unit + 2 < last) find_pages(unit + 2);
+        }
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};  // of token 16 t + r, over the lane's rows
+        for (int tile = 0; tile < tiles; ++tile) {
+          if (tiles > 1) load_rows(tile);
+          f32x4 c[4];
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            c[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+              for (int z = SPLIT - 1; z >= 0; --z) c[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[z][g], kf[t][g], c[t], 0, 0, 0);
+          }
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float p = F32 ? exp_split(__builtin_fmaf(c[t][i], 2.f, shift[i])) : __builtin_amdgcn_exp2f(__builtin_fmaf(c[t][i], kLog2e, shift[i]));
+              sum[t] += unit * kNUnit + 16 * t + r < see[i] ? p : 0.f;
+            }
+        }
+        // over the four lanes of a token; lane (r, kq) is left with token 16 kq + r
+        const bool up = lane & 32, odd = lane & 16;
+        const float g0 = up ? sum[0] : sum[2], g1 = up ? sum[1] : sum[3];
+        const float k0 = (up ? sum[2] : sum[0]) + __shfl_xor(g0, 32), k1 = (up ? sum[3] : sum[1]) + __shfl_xor(g1, 32);
+        const float mine = (odd ? k1 : k0) + __shfl_xor(odd ? k0 : k1, 16);
+        if (to) *to = old + mine;
+      }
+    }
+    at += units > 0 ? (int64_t)units * per + kNStart : 0;
+    if (at >= u1) return;
+    if (++kv == a.c.Hk) {
+      kv = 0;
+      do {
+        if (++s >= a.n_seq) return;
+        f = few_seq(a, s);
+      } while (__builtin_amdgcn_readfirstlane(f.units) == 0);
+    }
+  }
+}
+
+// Few rows a sequence on average, or in all: the second form takes all of them.  Else it takes sequences of up to 64 rows, where there can be several.
+void cache4_weights_split(CacheChunkArgs* a) {
+  a->div_group = make_fast_div(a->group);
+  const int64_t tokens = (int64_t)a->max_blocks << a->c.log_page, rows = (int64_t)a->rows * a->group, steps = (rows + kWRows - 1) / kWRows;
+  const int64_t heads = (int64_t)a->n_seq * a->c.Hk;
+  a->narrow = rows <= 64 || rows <= 32 * (int64_t)a->n_seq ? 0x7fffffff : a->n_seq >= 4 ? 64 : -1;
+  const int64_t units = (tokens + kNUnit - 1) / kNUnit * heads * ((steps + 3) / 4 * 4);
+  a->few_wgs = a->narrow < 0 ? 0 : (int32_t)(units / 4 + 1 > 768 ? 768 : units / 4 + 1);
+  const int64_t runs = (tokens + kWTokens - 1) / kWTokens * heads * (steps + kWTileCost) / kWLeastRun;
+  a->parts = a->narrow == 0x7fffffff ? 0 : (int32_t)(runs < 1 ? 1 : runs > kWeightsParts ? kWeightsParts : runs);
+}
+
+template <int D, int SPLIT>
+static int launch_weights_one(const CacheChunkArgs& a, hipStream_t st) {
+  if (a.few_wgs > 0) {
+    hipLaunchKernelGGL((cache4_weights_few_kernel<D, SPLIT>), dim3((unsigned)a.few_wgs), dim3(256), 0, st, a);
+    const int rc = check_launch();
+    if (rc != HA_OK || a.parts == 0) return rc;
+  }
+  constexpr size_t lds = 2 * WeightsLds<D, SPLIT>::BUF;
+  static std::atomic<uint64_t> set{0};
+  const auto kernel = &cache4_weights_kernel<D, SPLIT>;
+  int rc = allow_full_lds(reinterpret_cast<const void*>(kernel), set);
+  if (rc != HA_OK) return rc;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)a.parts), dim3(64 * kWWaves), lds, st, a);
+  rc = check_launch();
   if (rc != HA_OK) return rc;
   hipLaunchKernelGGL(cache4_weights_join_kernel, dim3((unsigned)a.parts), dim3(kWTokens), 0, st, a);
   return check_launch();
 }
 
 int launch_cache4_weights(const CacheChunkArgs& a, int dtype, hipStream_t st) {
-  if (a.c.d == 128) return dtype == HA_BF16 ? launch_weights_cut<128, 1>(a, st) : launch_weights_cut<128, 3>(a, st);
-  return dtype == HA_BF16 ? launch_weights_cut<64, 1>(a, st) : launch_weights_cut<64, 3>(a, st);
+  if (a.c.d == 128) return dtype == HA_BF16 ? launch_weights_one<128, 1>(a, st) : launch_weights_one<128, 3>(a, st);
+  return dtype == HA_BF16 ? launch_weights_one<64, 1>(a, st) : launch_weights_one<64, 3>(a, st);
 }
 
 }  // namespace ha

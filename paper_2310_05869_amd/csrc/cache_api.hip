@@ -237,8 +237,8 @@ int ha_cache4_attn_chunk(const void* Q, const void* cache, const int32_t* cu_seq
 
 static size_t weights_space(const CacheChunkArgs& a, size_t* sums) {
   auto align = [](size_t x) { return (x + 255) & ~(size_t)255; };
-  *sums = a.cut ? align((size_t)a.parts * 16) : 0;
-  return a.cut ? *sums + align(2 * (size_t)a.parts * kWeightsTokens * 4) : 0;
+  *sums = align((size_t)a.parts * 16);
+  return *sums + align(2 * (size_t)a.parts * kWeightsTokens * 4);
 }
 
 size_t ha_cache4_weights_workspace_bytes(const ha_cache4* shape, const ha_cache4_chunk* chunk) {
