@@ -146,24 +146,56 @@ __global__ __launch_bounds__(64 * kWWaves, 2) void cache4_weights_kernel(CacheCh
       const int rows = w.q.n * a.group;
       u32x4 raw[NC][F32 ? 2 : 1];
       float raw_lse = 0.f;
-      auto load_rows = [&](int step) {
+      // The thread's rows of a step lie 64 behind those of the step before: token and head go on by 64 / group and 64 % group.  (A division for every row and step took a
+      // third of the vector instructions.)
+      const int esz = F32 ? 4 : 2, on_tok = kWRows / a.group, on_head = kWRows - on_tok * a.group;
+      struct Place {
+        const unsigned char* at;
+        int row, head;  // within the sequence and key head, within the group
+      };
+      Place from[NC], from_lse;
+      auto begin = [&](Place& p, int row, const void* base, int64_t per_tok, int64_t per_head) {
+        const int tok = a.div_group.div(row);
+        p.row = row;
+        p.head = row - tok * a.group;
+        p.at = reinterpret_cast<const unsigned char*>(base) + (w.q.start + tok) * per_tok + (kv * a.group + p.head) * per_head;
+      };
+      auto go_on = [&](Place& p, int64_t per_tok, int64_t per_head) {
+        p.row += kWRows;
+        p.at += on_tok * per_tok + on_head * per_head;
+        if (on_head != 0) {
+          p.head += on_head;
+          if (p.head >= a.group) {
+            p.head -= a.group;
+            p.at += per_tok - a.group * per_head;
+          }
+        }
+      };
+      const int64_t q_tok = a.q.row * esz, q_head = a.q.head * esz, l_tok = 4, l_head = 4 * (int64_t)a.rows;
+      auto begin_rows = [&](int step) {
         const int row0 = (int)(step0 + step) * kWRows;
 #pragma unroll
         for (int i = 0; i < NC; ++i) {
-          const int r = row0 + threadIdx.x / CPR + i * (64 * kWWaves / CPR), c = threadIdx.x % CPR * 8;
-          const int use = min(r, rows - 1), tok = a.div_group.div(use), head = kv * a.group + use - tok * a.group;
-          const int64_t at = (int64_t)(w.q.start + tok) * a.q.row + (int64_t)head * a.q.head + c;
-          if constexpr (F32) {
-            const u32x4* p = reinterpret_cast<const u32x4*>(reinterpret_cast<const float*>(a.Q) + at);
+          begin(from[i], row0 + (int)threadIdx.x / CPR + i * (64 * kWWaves / CPR), a.Q, q_tok, q_head);
+          from[i].at += threadIdx.x % CPR * 8 * esz;
+          raw[i][0] = (u32x4){0, 0, 0, 0};
+          raw[i][F32 ? 1 : 0] = (u32x4){0, 0, 0, 0};
+        }
+        begin(from_lse, row0 + (int)threadIdx.x % kWRows, a.lse, l_tok, l_head);
+      };
+      auto load_rows = [&]() {  // (of rows behind the last what was there before: they count for nothing)
+#pragma unroll
+        for (int i = 0; i < NC; ++i) {
+          if (from[i].row < rows) {
+            const u32x4* p = reinterpret_cast<const u32x4*>(from[i].at);
             raw[i][0] = p[0];
-            raw[i][1] = p[1];
-          } else {
-            raw[i][0] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(a.Q) + at);
+            if constexpr (F32) raw[i][1] = p[1];
           }
+          go_on(from[i], q_tok, q_head);
         }
         if (threadIdx.x < kWRows) {
-          const int use = min(row0 + (int)threadIdx.x, rows - 1), tok = a.div_group.div(use), head = kv * a.group + use - tok * a.group;
-          raw_lse = a.lse[(int64_t)head * a.rows + w.q.start + tok];
+          if (from_lse.row < rows) raw_lse = *reinterpret_cast<const float*>(from_lse.at);
+          go_on(from_lse, l_tok, l_head);
         }
       };
       auto store_rows = [&](int step) {
@@ -195,9 +227,11 @@ __global__ __launch_bounds__(64 * kWWaves, 2) void cache4_weights_kernel(CacheCh
       };
 
       if (first < last) {
-        load_rows(first);
+        begin_rows(first);
+        load_rows();
         __syncthreads();  // (the tile before has left LDS)
         store_rows(first);
+        if (first + 1 < last) load_rows();  // (rows are asked for a step before they are stored, two before they are used)
         __syncthreads();
       }
       const int tok0 = k * kWTokens + wave * 64, tok_end = tok0 + 64;
@@ -248,21 +282,67 @@ __global__ __launch_bounds__(64 * kWWaves, 2) void cache4_weights_kernel(CacheCh
       auto plain = [&](int row0) {  // whether 32 rows are all there and all see the wave's tokens
         return row0 + 32 <= rows && w.q.held + a.div_group.div(row0) + 1 >= tok_end;
       };
+      // Weights of one half beside products of the next: a slice of the vector work behind every two products, rows two products ahead.  (The order is held by hand: left to
+      // itself, the compiler puts all products before all exponentials.)
+      auto both = [&](const Half& x, int row0, int step, int half, Half& next) {
+        if (!plain(row0)) {
+          products(step, half, next);
+          add_some_weights(x, row0);
+          return;
+        }
+        const unsigned char* buf = smem + (step & 1) * L::BUF;
+        const unsigned char* at = buf + (32 * half + lq) * L::STR;
+        auto fragment = [&](int i, int z) {
+          return *reinterpret_cast<const bf16x8*>(at + z * L::PART + (32 * ((KS * h + i) % G) + 8 * ((KS * h + i) / G)) * 2);
+        };
+        bf16x8 qf[2][SPLIT];
+#pragma unroll
+        for (int z = 0; z < SPLIT; ++z) qf[0][z] = fragment(0, z);
+#pragma unroll
+        for (int z = 0; z < SPLIT; ++z) qf[1][z] = fragment(1, z);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) next.c[0][i] = next.c[1][i] = 0.f;
+        float part[4] = {0.f, 0.f, 0.f, 0.f};  // even and odd rows of both tokens
+#pragma unroll
+        for (int i = 0; i < KS; ++i) {
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int z = SPLIT - 1; z >= 0; --z) {
+            next.c[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[i % 2][z], kf[0][i], next.c[0], 0, 0, 0);
+            next.c[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(qf[i % 2][z], kf[1][i], next.c[1], 0, 0, 0);
+          }
+          if (i + 2 < KS)
+#pragma unroll
+            for (int z = 0; z < SPLIT; ++z) qf[i % 2][z] = fragment(i + 2, z);
+          if (i >= KS - 4) next.shift[i - KS + 4] = *reinterpret_cast<const f32x4*>(buf + SPLIT * L::PART + (32 * half + 8 * (i - KS + 4) + 4 * h) * 4);
+#pragma unroll
+          for (int e = i * 16 / KS; e < (i + 1) * 16 / KS; ++e) {
+            part[e % 2] += weight(x.c[0][e], x.shift[e / 4][e % 4]);
+            part[2 + e % 2] += weight(x.c[1][e], x.shift[e / 4][e % 4]);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        sum[0] += part[0] + part[1];
+        sum[1] += part[2] + part[3];
+      };
       auto add = [&](const Half& x, int row0) {
         if (plain(row0)) add_weights(x);
         else add_some_weights(x, row0);
       };
-      Half xa, xb;
-      if (first < last) products(first, 0, xa);
-      for (int step = first; step < last; ++step) {
-        const bool more = step + 1 < last;
+      if (first < last) {
+        Half xa, xb;
+        products(first, 0, xa);
+        int step = first;
+        for (; step + 1 < last; ++step) {
+          const int row0 = (int)(step0 + step) * kWRows;
+          both(xa, row0, step, 1, xb);
+          store_rows(step + 1);
+          if (step + 2 < last) load_rows();
+          __syncthreads();
+          both(xb, row0 + 32, step + 1, 0, xa);
+        }
         const int row0 = (int)(step0 + step) * kWRows;
-        if (more) load_rows(step + 1);
-        products(step, 1, xb);
-        add(xa, row0);
-        if (more) store_rows(step + 1);
-        __syncthreads();
-        if (more) products(step + 1, 0, xa);
+        both(xa, row0, step, 1, xb);
         add(xb, row0 + 32);
       }
       __syncthreads();
