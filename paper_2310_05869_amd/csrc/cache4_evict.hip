@@ -3,13 +3,15 @@
 //
 // Of n tokens k stay, r of them the last ones; the other k - r are the largest of n - r.  Kept tokens among the first k - r places stay where they are, the others move
 // into the places that come free there, first to first: in a steady state a step moves as many rows as it lets go, where closing up would move nearly all.
-// Then the last r follow, in order.  Three launches:
-//   select   a workgroup per sequence and key head finds the (k - r)-th largest weight by three histograms of 11, 11 and 10 bits of the weights' bits, made so that they
-//            order as numbers do, then who moves where from prefix sums: with c(p) tokens kept before place p, a free place p is the (p - c(p))-th, a kept token the
-//            (c(p) - c(k - r))-th that moves.  A wave has a run of places of its own, so that only 16 numbers cross the waves.
+// Then the last r follow, in order.
+//   select   a workgroup per sequence and key head finds the (k - r)-th largest weight by histograms of 11, 11 and 10 bits of the weights' bits, made so that they
+//            order as numbers do (as soon as no more than 256 are left to choose from, their ranks are counted instead), then who moves where from prefix sums: with c(p)
+//            tokens kept before place p, a free place p is the (p - c(p))-th, a kept token the (c(p) - c(k - r))-th that moves.  A wave has a run of places of its own,
+//            so that only 16 numbers cross the waves.
 //   move     rows of these lists, D / 8 lanes a row
-//   last     the last r rows, whose places may overlap: read, a barrier, written, some hundred at a time; lengths and free pages
-// Bound by latency: the weights that are chosen from are 4 bytes a token and head beside 136 of its rows.
+//   last     the last r rows, whose places may overlap: read, a barrier, written, some hundred at a time; beside them lengths and free pages
+// One launch, in which the workgroup that chose moves the rows too, where the sequences and key heads fill the chip or are short; three launches else, so that the rows of few heads
+// are moved by all of it.
 #include <type_traits>
 
 #include "cache4_common.h"
@@ -42,17 +44,23 @@ __device__ inline uint32_t order_of(float x) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+// Sum of the lanes up to this one
+__device__ inline uint32_t wave_scan(uint32_t x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);  // row_shr:1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, true);  // row_bcast:15 into rows 1 and 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, true);  // row_bcast:31 into rows 2 and 3
+  return x;
+}
+
 // Sum of the values of the threads before (exclusive) and of all; one barrier before the scratch may be written again is the caller's
 template <int NT>
 __device__ inline uint32_t block_scan(uint32_t x, uint32_t* all, uint32_t* scratch) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint32_t inc = x;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const uint32_t up = __shfl_up(inc, o);
-    if (lane >= o) inc += up;
-  }
-  if (lane == 63) scratch[wave] = inc;
+  const int wave = threadIdx.x >> 6;
+  const uint32_t inc = wave_scan(x);
+  if ((threadIdx.x & 63) == 63) scratch[wave] = inc;
   __syncthreads();
   uint32_t before = 0, total = 0;
 #pragma unroll
@@ -65,18 +73,21 @@ __device__ inline uint32_t block_scan(uint32_t x, uint32_t* all, uint32_t* scrat
   return before + inc - x;
 }
 
+constexpr int kRanked = 256;  // numbers whose ranks are counted
 template <int NT>
 struct SelectLds {
-  uint32_t hist[kBins];
+  uint32_t hist[2][kBins];
+  alignas(16) uint32_t left[kRanked];
+  uint32_t n_left;
   uint32_t scratch[NT / 64];
   uint32_t gt[NT / 64], eq[NT / 64];  // kept for certain, and equal to the limit, of every wave's places
   uint32_t gt_head, eq_head;          // among the first k - r places
-  uint32_t bin, want;
+  uint32_t bin, want, here;
 };
 
-// HELD: the weights are few enough to stay in registers, eight pieces of four a thread
+// Writes the list of rows that change places and returns how many they are.  HELD: the weights are few enough to stay in registers, eight pieces of four a thread
 template <int NT, bool HELD>
-__device__ inline void select_moves(const CacheEvictArgs& a, const EvictSeq& q, int s, int kv, SelectLds<NT>& lds) {
+__device__ inline int select_moves(const CacheEvictArgs& a, const EvictSeq& q, int s, int kv, SelectLds<NT>& lds) {
   constexpr int NW = NT / 64, PIECES = 8;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int from = q.n - q.r, stay = q.k - q.r;  // places that are chosen from, and how many of them
@@ -112,39 +123,47 @@ __device__ inline void select_moves(const CacheEvictArgs& a, const EvictSeq& q, 
   };
 
   uint32_t prefix = 0, want = stay;
+  for (int i = threadIdx.x; i < kBins; i += NT) lds.hist[0][i] = lds.hist[1][i] = 0;
+  if (threadIdx.x == 0) lds.n_left = 0;
+  __syncthreads();
 #pragma unroll
   for (int pass = 0; pass < 3; ++pass) {
     const int bits = pass == 2 ? 10 : 11, shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
-    for (int i = threadIdx.x; i < kBins; i += NT) lds.hist[i] = 0;
-    __syncthreads();
+    uint32_t* const hist = lds.hist[pass & 1];
+    if (pass == 2) {  // (the first pass's table again)
+      for (int i = threadIdx.x; i < kBins; i += NT) hist[i] = 0;
+      __syncthreads();
+    }
     all_keys([&](int, const u32x4& key) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const bool in = key[e] != 0 && (pass == 0 || key[e] >> (shift + bits) == prefix);
         const uint32_t bin = (key[e] >> shift) & ((1u << bits) - 1);
-        // (weights that are all alike, zeros say, would queue for one counter: the first lane's bin is counted for all that have it)
         const unsigned long long some = __ballot(in);
         if (some == 0) continue;
-        const int lead = __builtin_ctzll(some);
-        const uint32_t first = __builtin_amdgcn_readlane(bin, lead);
-        const unsigned long long same = __ballot(in && bin == first);
-        if (lane == lead) atomicAdd(&lds.hist[first], (uint32_t)__popcll(same));
-        else if (in && bin != first) atomicAdd(&lds.hist[bin], 1u);
+        // (weights that are all alike, zeros say, would queue for one counter)
+        const uint32_t one = __builtin_amdgcn_readlane(bin, __builtin_ctzll(some));
+        if (__ballot(in && bin != one) == 0) {
+          if (lane == 0) atomicAdd(&hist[one], (uint32_t)__popcll(some));
+        } else if (in) {
+          atomicAdd(&hist[bin], 1u);
+        }
       }
     });
     __syncthreads();
     constexpr int EACH = kBins / NT;
     uint32_t mine = 0, total;
 #pragma unroll
-    for (int j = 0; j < EACH; ++j) mine += lds.hist[kBins - 1 - (threadIdx.x * EACH + j)];  // from the largest down
+    for (int j = 0; j < EACH; ++j) mine += hist[kBins - 1 - (threadIdx.x * EACH + j)];  // from the largest down
     uint32_t above = block_scan<NT>(mine, &total, lds.scratch);
     if (above < want && want <= above + mine) {
       for (int j = 0; j < EACH; ++j) {
         const int bin = kBins - 1 - (threadIdx.x * EACH + j);
-        const uint32_t here = lds.hist[bin];
+        const uint32_t here = hist[bin];
         if (want <= above + here) {
           lds.bin = bin;
           lds.want = want - above;
+          lds.here = here;
           break;
         }
         above += here;
@@ -153,6 +172,32 @@ __device__ inline void select_moves(const CacheEvictArgs& a, const EvictSeq& q, 
     __syncthreads();
     prefix = prefix << bits | lds.bin;
     want = lds.want;
+    if (pass < 2 && lds.here <= kRanked) {
+      const int m = lds.here;
+      all_keys([&](int, const u32x4& key) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (key[e] != 0 && key[e] >> shift == prefix) lds.left[atomicAdd(&lds.n_left, 1u)] = key[e];
+      });
+      __syncthreads();
+      if ((int)threadIdx.x < m) {
+        const uint32_t my = lds.left[threadIdx.x];
+        uint32_t more = 0, same = 0;
+        for (int i = 0; i < m; ++i) {
+          const uint32_t x = lds.left[i];
+          more += x > my;
+          same += x == my;
+        }
+        if (more < want && want <= more + same) {  // (all that are equal to it write the same)
+          lds.bin = my;
+          lds.here = want - more;
+        }
+      }
+      __syncthreads();
+      prefix = lds.bin;
+      want = lds.here;
+      break;
+    }
   }
 
   // prefix: the last one that is kept; of those equal to it, the first `want`
@@ -190,12 +235,7 @@ __device__ inline void select_moves(const CacheEvictArgs& a, const EvictSeq& q, 
     uint32_t here = 0;  // kept for certain in the upper half, equal in the lower
 #pragma unroll
     for (int e = 0; e < 4; ++e) here += key[e] > prefix ? 0x10000u : key[e] == prefix ? 1u : 0u;
-    uint32_t inc = here;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const uint32_t up = __shfl_up(inc, o);
-      if (lane >= o) inc += up;
-    }
+    const uint32_t inc = wave_scan(here);
     uint32_t g = gt_before + ((inc - here) >> 16), t = eq_before + ((inc - here) & 0xffffu);
     const uint32_t both = __builtin_amdgcn_readlane(inc, 63);
     gt_before += both >> 16;
@@ -213,20 +253,7 @@ __device__ inline void select_moves(const CacheEvictArgs& a, const EvictSeq& q, 
       t += same;
     }
   });
-  if (threadIdx.x == 0) a.counts[s * a.c.Hk + kv] = stay - (int)kept_head;
-}
-
-template <int NT>
-__global__ __launch_bounds__(NT) void cache4_select_kernel(CacheEvictArgs a) {
-  __shared__ SelectLds<NT> lds;
-  const int s = blockIdx.x / a.c.Hk, kv = blockIdx.x - s * a.c.Hk;
-  const EvictSeq q = evict_seq(a, s);
-  if (q.k == q.n || q.k == q.r) {
-    if (threadIdx.x == 0) a.counts[blockIdx.x] = 0;
-    return;
-  }
-  if (q.n - q.r <= NT * 32) select_moves<NT, true>(a, q, s, kv, lds);
-  else select_moves<NT, false>(a, q, s, kv, lds);
+  return stay - (int)kept_head;
 }
 
 // A row's share of a lane: lane j of D / 8 has word j of K and of V; the first three also K's scales, V's and the weight
@@ -260,73 +287,67 @@ __device__ inline void store_piece(const CacheEvictArgs& a, int kv, int slot, in
   else if (j == 2) a.weights_out[head * a.c.page + t] = __uint_as_float(x.more);
 }
 
-template <int D>
-__global__ __launch_bounds__(kMoveThreads) void cache4_move_kernel(CacheEvictArgs a) {
-  constexpr int LPR = D / 8, ROWS = kMoveThreads / LPR, AHEAD = 4;
-  const int count = a.counts[blockIdx.x], kv = blockIdx.x % a.c.Hk, j = threadIdx.x % LPR;
-  const int2* moves = a.moves + (int64_t)blockIdx.x * a.moves_most;
-  for (int i0 = blockIdx.y * ROWS * AHEAD + threadIdx.x / LPR; i0 < count; i0 += gridDim.y * ROWS * AHEAD) {
+// Rows of the list, by workgroup `part` of `parts`
+template <int D, int NT>
+__device__ inline void move_rows(const CacheEvictArgs& a, int head, int count, int part, int parts) {
+  constexpr int LPR = D / 8, ROWS = NT / LPR, AHEAD = 4;
+  const int kv = head % a.c.Hk, j = threadIdx.x % LPR;
+  const int2* moves = a.moves + (int64_t)head * a.moves_most;
+  for (int i0 = part * ROWS * AHEAD + threadIdx.x / LPR; i0 < count; i0 += parts * ROWS * AHEAD) {
     int2 m[AHEAD];
     RowPiece<D> x[AHEAD];
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      const int i = i0 + u * ROWS;
-      m[u] = i < count ? moves[i] : int2{-1, -1};
+    for (int u = 0; u < AHEAD; ++u) m[u] = i0 + u * ROWS < count ? moves[i0 + u * ROWS] : int2{-1, -1};
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
       if (m[u].x >= 0) x[u] = load_piece<D>(a, kv, m[u].x, j);
-    }
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u)
       if (m[u].x >= 0 && m[u].y >= 0) store_piece<D>(a, kv, m[u].y, j, x[u]);
   }
 }
 
-template <int D>
-__global__ __launch_bounds__(kLastThreads) void cache4_last_kernel(CacheEvictArgs a) {
-  constexpr int LPR = D / 8, ROWS = kLastThreads / LPR, AHEAD = 4;
-  extern __shared__ uint32_t upto[];  // pages that sequences before give back
-  __shared__ uint32_t scratch[kLastThreads / 64];
-  if ((int)blockIdx.x < a.n_seq * a.c.Hk) {
-    const int s = blockIdx.x / a.c.Hk, kv = blockIdx.x - s * a.c.Hk, j = threadIdx.x % LPR;
-    const EvictSeq q = evict_seq(a, s);
-    if (q.k == q.n) return;
-    const int32_t* blocks = a.table + (int64_t)s * a.max_blocks;
-    auto slot_of = [&](int p) {
-      const int page = blocks[p >> a.c.log_page];
-      return (unsigned)page < (unsigned)a.c.n_pages ? (page << a.c.log_page) + (p & (a.c.page - 1)) : -1;
-    };
-    // rows that lie apart from their places are shared among workgroups; else one takes them in order: what it writes lies before what is still to be read
-    const bool apart = q.n - q.k >= q.r;
-    if (!apart && blockIdx.y > 0) return;
-    for (int i0 = apart ? blockIdx.y * ROWS * AHEAD : 0; i0 < q.r; i0 += (apart ? gridDim.y : 1) * ROWS * AHEAD) {
-      int to[AHEAD];
-      RowPiece<D> x[AHEAD];
+// The last rows.  Those that lie apart from their places are shared among workgroups; else one takes them in order: what it writes lies before what is still to be read.
+template <int D, int NT>
+__device__ inline void move_last(const CacheEvictArgs& a, const EvictSeq& q, int s, int kv, int part, int parts) {
+  constexpr int LPR = D / 8, ROWS = NT / LPR, AHEAD = 4;
+  const int j = threadIdx.x % LPR;
+  const int32_t* blocks = a.table + (int64_t)s * a.max_blocks;
+  auto slot_of = [&](int p) {
+    const int page = blocks[p >> a.c.log_page];
+    return (unsigned)page < (unsigned)a.c.n_pages ? (page << a.c.log_page) + (p & (a.c.page - 1)) : -1;
+  };
+  const bool apart = q.n - q.k >= q.r;
+  if (!apart && part > 0) return;
+  for (int i0 = apart ? part * ROWS * AHEAD : 0; i0 < q.r; i0 += (apart ? parts : 1) * ROWS * AHEAD) {
+    int at[AHEAD], to[AHEAD];
+    RowPiece<D> x[AHEAD];
 #pragma unroll
-      for (int u = 0; u < AHEAD; ++u) {
-        const int i = i0 + u * ROWS + threadIdx.x / LPR;
-        to[u] = -1;
-        x[u] = RowPiece<D>{0, 0, 0};
-        if (i < q.r) {
-          const int at = slot_of(q.n - q.r + i);
-          if (at >= 0) {
-            to[u] = slot_of(q.k - q.r + i);
-            x[u] = load_piece<D>(a, kv, at, j);
-          }
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < AHEAD; ++u) asm volatile("" : "+v"(x[u].k), "+v"(x[u].v), "+v"(x[u].more));  // (all of them are here before the barrier)
-      __syncthreads();
-#pragma unroll
-      for (int u = 0; u < AHEAD; ++u)
-        if (to[u] >= 0) store_piece<D>(a, kv, to[u], j, x[u]);
+    for (int u = 0; u < AHEAD; ++u) {
+      const int i = i0 + u * ROWS + threadIdx.x / LPR;
+      at[u] = i < q.r ? slot_of(q.n - q.r + i) : -1;
+      to[u] = i < q.r ? slot_of(q.k - q.r + i) : -1;
     }
-    return;
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      x[u] = RowPiece<D>{0, 0, 0};
+      if (at[u] >= 0) x[u] = load_piece<D>(a, kv, at[u], j);
+    }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) asm volatile("" : "+v"(x[u].k), "+v"(x[u].v), "+v"(x[u].more));  // (all of them are here before the barrier)
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (at[u] >= 0 && to[u] >= 0) store_piece<D>(a, kv, to[u], j, x[u]);
   }
-  if (blockIdx.y > 0) return;
-  // ---- lengths, and the pages that come free, on top of the stack in order ----
+}
+
+// Lengths, and the pages that come free, on top of the stack in order.  upto: n_seq words.
+template <int NT>
+__device__ inline void free_pages(const CacheEvictArgs& a, uint32_t* upto, uint32_t* scratch) {
   auto pages_of = [&](int tokens) { return (int)(((int64_t)tokens + a.c.page - 1) >> a.c.log_page); };
   const int count = min(max(*a.free_count, 0), a.c.n_pages);
-  const int each = (a.n_seq + kLastThreads - 1) / kLastThreads, s0 = min(a.n_seq, (int)threadIdx.x * each), s1 = min(a.n_seq, s0 + each);
+  const int each = (a.n_seq + NT - 1) / NT, s0 = min(a.n_seq, (int)threadIdx.x * each), s1 = min(a.n_seq, s0 + each);
   uint32_t mine = 0, all;
   for (int s = s0; s < s1; ++s) {
     const EvictSeq q = evict_seq(a, s);
@@ -334,11 +355,11 @@ __global__ __launch_bounds__(kLastThreads) void cache4_last_kernel(CacheEvictArg
     upto[s] = mine;
     mine += pages_of(q.n) - pages_of(q.k);
   }
-  const uint32_t before = block_scan<kLastThreads>(mine, &all, scratch);
+  const uint32_t before = block_scan<NT>(mine, &all, scratch);
   for (int s = s0; s < s1; ++s) upto[s] += before;
   __syncthreads();
   if (threadIdx.x == 0) *a.free_count_out = (int)min((int64_t)count + all, (int64_t)a.c.n_pages);
-  for (int s = threadIdx.x >> 6; s < a.n_seq; s += kLastThreads / 64) {
+  for (int s = threadIdx.x >> 6; s < a.n_seq; s += NT / 64) {
     const EvictSeq q = evict_seq(a, s);
     const int left = pages_of(q.k), freed = pages_of(q.n) - left;
     for (int i = threadIdx.x & 63; i < freed; i += 64) {
@@ -348,25 +369,67 @@ __global__ __launch_bounds__(kLastThreads) void cache4_last_kernel(CacheEvictArg
   }
 }
 
+// The first workgroup has lengths and pages, each of the others a sequence and key head.  ALL: it moves the rows too.
+template <int D, int NT, bool ALL>
+__global__ __launch_bounds__(NT) void cache4_select_kernel(CacheEvictArgs a) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char evict_lds[];
+  SelectLds<NT>& lds = *reinterpret_cast<SelectLds<NT>*>(evict_lds);
+  if (blockIdx.x == 0) {
+    free_pages<NT>(a, reinterpret_cast<uint32_t*>(evict_lds + sizeof(SelectLds<NT>)), lds.scratch);
+    return;
+  }
+  const int head = blockIdx.x - 1, s = head / a.c.Hk, kv = head - s * a.c.Hk;
+  const EvictSeq q = evict_seq(a, s);
+  int count = 0;
+  if (q.k < q.n && q.r < q.k) count = q.n - q.r <= NT * 32 ? select_moves<NT, true>(a, q, s, kv, lds) : select_moves<NT, false>(a, q, s, kv, lds);
+  if constexpr (ALL) {
+    if (q.k == q.n) return;
+    __syncthreads();  // (the list is written, by all waves)
+    move_rows<D, NT>(a, head, count, 0, 1);
+    __syncthreads();  // (rows have been read that the last ones are written over)
+    move_last<D, NT>(a, q, s, kv, 0, 1);
+  } else {
+    if (threadIdx.x == 0) a.counts[head] = count;
+  }
+}
+
+template <int D>
+__global__ __launch_bounds__(kMoveThreads) void cache4_move_kernel(CacheEvictArgs a) {
+  move_rows<D, kMoveThreads>(a, blockIdx.x, a.counts[blockIdx.x], blockIdx.y, gridDim.y);
+}
+
+template <int D>
+__global__ __launch_bounds__(kLastThreads) void cache4_last_kernel(CacheEvictArgs a) {
+  const int s = blockIdx.x / a.c.Hk, kv = blockIdx.x - s * a.c.Hk;
+  const EvictSeq q = evict_seq(a, s);
+  if (q.k < q.n) move_last<D, kLastThreads>(a, q, s, kv, blockIdx.y, gridDim.y);
+}
+
+template <int D, int NT, bool ALL>
+static int launch_select(const CacheEvictArgs& a, hipStream_t st) {
+  const auto kernel = &cache4_select_kernel<D, NT, ALL>;
+  static std::atomic<uint64_t> set{0};
+  const int rc = allow_full_lds(reinterpret_cast<const void*>(kernel), set);
+  if (rc != HA_OK) return rc;
+  const size_t lds = sizeof(SelectLds<NT>) + (size_t)a.n_seq * 4;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(a.n_seq * a.c.Hk + 1)), dim3(NT), lds, st, a);
+  return check_launch();
+}
+
 template <int D>
 static int launch_evict_d(const CacheEvictArgs& a, hipStream_t st) {
   const int64_t tokens = (int64_t)a.max_blocks << a.c.log_page;
   const int heads = a.n_seq * a.c.Hk;
-  if (heads > 0 && tokens > 0) {
-    if (tokens <= 256 * 32) hipLaunchKernelGGL(cache4_select_kernel<256>, dim3(heads), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(cache4_select_kernel<1024>, dim3(heads), dim3(1024), 0, st, a);
-    int rc = check_launch();
-    if (rc != HA_OK) return rc;
-    constexpr int64_t per = 4 * kMoveThreads / (D / 8);
-    const int64_t most = (a.moves_most + per - 1) / per, fill = 2048 / heads + 1;
-    hipLaunchKernelGGL(cache4_move_kernel<D>, dim3(heads, (unsigned)(most < fill ? most : fill)), dim3(kMoveThreads), 0, st, a);
-    rc = check_launch();
-    if (rc != HA_OK) return rc;
-  }
-  constexpr int64_t per = 4 * kLastThreads / (D / 8);
-  const int64_t most = ((int64_t)a.recent + per - 1) / per + 1, fill = 512 / (heads + 1) + 1;
-  const size_t lds = ((size_t)a.n_seq * 4 + 15) & ~(size_t)15;
-  hipLaunchKernelGGL(cache4_last_kernel<D>, dim3(heads + 1, (unsigned)(most < fill ? most : fill)), dim3(kLastThreads), lds, st, a);
+  if (tokens <= 2048 || heads >= 256) return tokens <= 256 * 32 ? launch_select<D, 256, true>(a, st) : launch_select<D, 1024, true>(a, st);
+  int rc = tokens <= 256 * 32 ? launch_select<D, 256, false>(a, st) : launch_select<D, 1024, false>(a, st);
+  if (rc != HA_OK) return rc;
+  constexpr int64_t per = 4 * kMoveThreads / (D / 8), per_last = 4 * kLastThreads / (D / 8);
+  const int64_t most = (a.moves_most + per - 1) / per, fill = 2048 / heads + 1;
+  hipLaunchKernelGGL(cache4_move_kernel<D>, dim3(heads, (unsigned)(most < fill ? most : fill)), dim3(kMoveThreads), 0, st, a);
+  rc = check_launch();
+  if (rc != HA_OK || a.recent == 0) return rc;
+  const int64_t most_last = ((int64_t)a.recent + per_last - 1) / per_last, fill_last = 512 / heads + 1;
+  hipLaunchKernelGGL(cache4_last_kernel<D>, dim3(heads, (unsigned)(most_last < fill_last ? most_last : fill_last)), dim3(kLastThreads), 0, st, a);
   return check_launch();
 }
 
