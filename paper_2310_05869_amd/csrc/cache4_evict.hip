@@ -23,6 +23,9 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kBins = 2048;
 constexpr int kMoveThreads = 256, kLastThreads = 1024;
+constexpr int kManyHeads = 256;  // sequences and key heads that fill the chip: a workgroup moves its own rows (64 of them, 3800 rows each: 70 us apart, 101 in one)
+constexpr int kAhead = 8;  // rows that a lane has in flight
+constexpr int kSmall = 512;  // threads of a workgroup that chooses from up to 32 times as many places
 
 struct EvictSeq {
   int n, k, r;  // tokens, those that stay, the last ones among these
@@ -74,14 +77,15 @@ __device__ inline uint32_t block_scan(uint32_t x, uint32_t* all, uint32_t* scrat
 }
 
 constexpr int kRanked = 256;  // numbers whose ranks are counted
+constexpr int kCopies = 4;
 template <int NT>
 struct SelectLds {
-  uint32_t hist[2][kBins];
+  uint32_t hist[kCopies][kBins];  // by lane, for the first pass: weights of like size queue for their counters less
   alignas(16) uint32_t left[kRanked];
   uint32_t n_left;
   uint32_t scratch[NT / 64];
   uint32_t gt[NT / 64], eq[NT / 64];  // kept for certain, and equal to the limit, of every wave's places
-  uint32_t gt_head, eq_head;          // among the first k - r places
+  uint32_t gaps;
   uint32_t bin, want, here;
 };
 
@@ -94,47 +98,67 @@ __device__ inline int select_moves(const CacheEvictArgs& a, const EvictSeq& q, i
   const int32_t* blocks = a.table + (int64_t)s * a.max_blocks;
   const int per = (from + NW * 256 - 1) / (NW * 256);  // pieces of 256 places a wave
   const int place0 = wave * per * 256 + lane * 4;
-  auto fetch = [&](int i) {
+  // (Page numbers of all pieces first, then all weights, then what they are made into: with a piece after the other, each waits for two loads by itself.)
+  auto page_at = [&](int i) { return blocks[min(place0 + i * 256, from - 1) >> a.c.log_page]; };
+  auto weights_at = [&](int i, int page) {
+    const int p = min(place0 + i * 256, (from - 1) & ~3);
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    if (a.c.n_pages > 0) x = *reinterpret_cast<const f32x4*>(a.weights + ((int64_t)((unsigned)page < (unsigned)a.c.n_pages ? page : 0) * a.c.Hk + kv) * a.c.page + (p & (a.c.page - 1)));
+    return x;
+  };
+  auto key_of = [&](int i, int page, const f32x4& x) {
     const int p = place0 + i * 256;
-    u32x4 key = {0, 0, 0, 0};
-    if (i < per && p < from) {
-      const int page = blocks[p >> a.c.log_page];
-      const bool there = (unsigned)page < (unsigned)a.c.n_pages;
-      f32x4 x = {0.f, 0.f, 0.f, 0.f};
-      if (there) x = *reinterpret_cast<const f32x4*>(a.weights + ((int64_t)page * a.c.Hk + kv) * a.c.page + (p & (a.c.page - 1)));
+    const bool there = (unsigned)page < (unsigned)a.c.n_pages;
+    u32x4 key;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) key[e] = p + e >= from ? 0u : there ? order_of(x[e]) : 1u;
-    }
+    for (int e = 0; e < 4; ++e) key[e] = i >= per || p + e >= from ? 0u : there ? order_of(x[e]) : 1u;
     return key;
   };
   u32x4 held[HELD ? PIECES : 1];
+  int held_page[HELD ? PIECES : 1];
   if constexpr (HELD) {
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) held[i] = fetch(i);
+    for (int i = 0; i < PIECES; ++i) held_page[i] = page_at(i);
+    f32x4 x[PIECES];
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) x[i] = weights_at(i, held_page[i]);
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) held[i] = key_of(i, held_page[i], x[i]);
   }
-  auto all_keys = [&](auto&& f) {  // f(piece, its keys)
+  auto all_keys = [&](auto&& f) {  // f(piece, its keys, their page)
     if constexpr (HELD) {
 #pragma unroll
       for (int i = 0; i < PIECES; ++i)
-        if (i < per) f(i, held[i]);
+        if (i < per) f(i, held[i], held_page[i]);
     } else {
-      for (int i = 0; i < per; ++i) f(i, fetch(i));
+      for (int i0 = 0; i0 < per; i0 += PIECES) {
+        int page[PIECES];
+        f32x4 x[PIECES];
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) page[i] = page_at(i0 + i);
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) x[i] = weights_at(i0 + i, page[i]);
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i)
+          if (i0 + i < per) f(i0 + i, key_of(i0 + i, page[i], x[i]), page[i]);
+      }
     }
   };
 
   uint32_t prefix = 0, want = stay;
-  for (int i = threadIdx.x; i < kBins; i += NT) lds.hist[0][i] = lds.hist[1][i] = 0;
-  if (threadIdx.x == 0) lds.n_left = 0;
+  for (int i = threadIdx.x; i < kCopies * kBins; i += NT) lds.hist[0][i] = 0;
+  if (threadIdx.x < kRanked) lds.left[threadIdx.x] = 0;
+  if (threadIdx.x == 0) lds.n_left = lds.gaps = 0;
   __syncthreads();
 #pragma unroll
   for (int pass = 0; pass < 3; ++pass) {
     const int bits = pass == 2 ? 10 : 11, shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
-    uint32_t* const hist = lds.hist[pass & 1];
-    if (pass == 2) {  // (the first pass's table again)
+    uint32_t* const hist = pass == 0 ? lds.hist[lane % kCopies] : lds.hist[0];
+    if (pass > 0) {
       for (int i = threadIdx.x; i < kBins; i += NT) hist[i] = 0;
       __syncthreads();
     }
-    all_keys([&](int, const u32x4& key) {
+    all_keys([&](int, const u32x4& key, int) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const bool in = key[e] != 0 && (pass == 0 || key[e] >> (shift + bits) == prefix);
@@ -153,13 +177,20 @@ __device__ inline int select_moves(const CacheEvictArgs& a, const EvictSeq& q, i
     __syncthreads();
     constexpr int EACH = kBins / NT;
     uint32_t mine = 0, total;
+    auto in_bin = [&](int bin) {
+      uint32_t n = lds.hist[0][bin];
+      if (pass == 0)
 #pragma unroll
-    for (int j = 0; j < EACH; ++j) mine += hist[kBins - 1 - (threadIdx.x * EACH + j)];  // from the largest down
+        for (int c = 1; c < kCopies; ++c) n += lds.hist[c][bin];
+      return n;
+    };
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) mine += in_bin(kBins - 1 - (threadIdx.x * EACH + j));  // from the largest down
     uint32_t above = block_scan<NT>(mine, &total, lds.scratch);
     if (above < want && want <= above + mine) {
       for (int j = 0; j < EACH; ++j) {
         const int bin = kBins - 1 - (threadIdx.x * EACH + j);
-        const uint32_t here = hist[bin];
+        const uint32_t here = in_bin(bin);
         if (want <= above + here) {
           lds.bin = bin;
           lds.want = want - above;
@@ -174,7 +205,7 @@ __device__ inline int select_moves(const CacheEvictArgs& a, const EvictSeq& q, i
     want = lds.want;
     if (pass < 2 && lds.here <= kRanked) {
       const int m = lds.here;
-      all_keys([&](int, const u32x4& key) {
+      all_keys([&](int, const u32x4& key, int) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           if (key[e] != 0 && key[e] >> shift == prefix) lds.left[atomicAdd(&lds.n_left, 1u)] = key[e];
@@ -183,10 +214,14 @@ __device__ inline int select_moves(const CacheEvictArgs& a, const EvictSeq& q, i
       if ((int)threadIdx.x < m) {
         const uint32_t my = lds.left[threadIdx.x];
         uint32_t more = 0, same = 0;
-        for (int i = 0; i < m; ++i) {
-          const uint32_t x = lds.left[i];
-          more += x > my;
-          same += x == my;
+#pragma unroll 4
+        for (int i = 0; i < m; i += 4) {  // (zeros behind the last count for nothing)
+          const u32x4 x = *reinterpret_cast<const u32x4*>(&lds.left[i]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            more += x[e] > my;
+            same += x[e] == my;
+          }
         }
         if (more < want && want <= more + same) {  // (all that are equal to it write the same)
           lds.bin = my;
@@ -201,37 +236,29 @@ __device__ inline int select_moves(const CacheEvictArgs& a, const EvictSeq& q, i
   }
 
   // prefix: the last one that is kept; of those equal to it, the first `want`
-  uint32_t gt = 0, eq = 0, gt_head = 0, eq_head = 0;
-  all_keys([&](int i, const u32x4& key) {
+  uint32_t gt = 0, eq = 0;
+  all_keys([&](int, const u32x4& key, int) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const bool head = place0 + i * 256 + e < stay;
-      const unsigned long long g = __ballot(key[e] > prefix), q2 = __ballot(key[e] == prefix), h = __ballot(head);
-      gt += __popcll(g);
-      eq += __popcll(q2);
-      gt_head += __popcll(g & h);
-      eq_head += __popcll(q2 & h);
+      gt += key[e] > prefix;
+      eq += key[e] == prefix;
     }
   });
-  if (threadIdx.x == 0) lds.gt_head = lds.eq_head = 0;
-  if (lane == 0) {
+  gt = wave_scan(gt);
+  eq = wave_scan(eq);
+  if (lane == 63) {
     lds.gt[wave] = gt;
     lds.eq[wave] = eq;
   }
   __syncthreads();
-  if (lane == 0) {
-    atomicAdd(&lds.gt_head, gt_head);
-    atomicAdd(&lds.eq_head, eq_head);
-  }
-  __syncthreads();
-  const uint32_t kept_head = lds.gt_head + min(lds.eq_head, want);  // kept among the first k - r places
   uint32_t gt_before = 0, eq_before = 0;
   for (int w = 0; w < wave; ++w) {
     gt_before += lds.gt[w];
     eq_before += lds.eq[w];
   }
   int2* moves = a.moves + ((int64_t)s * a.c.Hk + kv) * a.moves_most;
-  all_keys([&](int i, const u32x4& key) {
+  uint32_t gaps = 0;
+  all_keys([&](int i, const u32x4& key, int page) {
     uint32_t here = 0;  // kept for certain in the upper half, equal in the lower
 #pragma unroll
     for (int e = 0; e < 4; ++e) here += key[e] > prefix ? 0x10000u : key[e] == prefix ? 1u : 0u;
@@ -241,19 +268,24 @@ __device__ inline int select_moves(const CacheEvictArgs& a, const EvictSeq& q, i
     gt_before += both >> 16;
     eq_before += both & 0xffffu;
     const int p = place0 + i * 256;
-    const int page = p < from ? blocks[p >> a.c.log_page] : -1;
     const int slot = (unsigned)page < (unsigned)a.c.n_pages ? (page << a.c.log_page) + (p & (a.c.page - 1)) : -4;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const bool more = key[e] > prefix, same = key[e] == prefix, kept = more || (same && t < want);
       const uint32_t rank = g + min(t, want);  // kept before
-      if (kept && p + e >= stay) moves[rank - kept_head].x = slot + e;
-      if (!kept && p + e < stay) moves[p + e - rank].y = slot + e;
+      // (how many stay is not known yet, so rows that move are counted from the last one)
+      if (kept && p + e >= stay) moves[stay - 1 - rank].x = slot + e;
+      const bool gap = !kept && p + e < stay;
+      if (gap) moves[p + e - rank].y = slot + e;
+      gaps += gap;
       g += more;
       t += same;
     }
   });
-  return stay - (int)kept_head;
+  gaps = wave_scan(gaps);
+  if (lane == 63) atomicAdd(&lds.gaps, gaps);
+  __syncthreads();
+  return (int)lds.gaps;
 }
 
 // A row's share of a lane: lane j of D / 8 has word j of K and of V; the first three also K's scales, V's and the weight
@@ -287,17 +319,20 @@ __device__ inline void store_piece(const CacheEvictArgs& a, int kv, int slot, in
   else if (j == 2) a.weights_out[head * a.c.page + t] = __uint_as_float(x.more);
 }
 
-// Rows of the list, by workgroup `part` of `parts`
+// Rows of the list, by workgroup `part` of `parts`: places that come free from the first on, rows that move from the last
 template <int D, int NT>
 __device__ inline void move_rows(const CacheEvictArgs& a, int head, int count, int part, int parts) {
-  constexpr int LPR = D / 8, ROWS = NT / LPR, AHEAD = 4;
+  constexpr int LPR = D / 8, ROWS = NT / LPR, AHEAD = kAhead;
   const int kv = head % a.c.Hk, j = threadIdx.x % LPR;
   const int2* moves = a.moves + (int64_t)head * a.moves_most;
   for (int i0 = part * ROWS * AHEAD + threadIdx.x / LPR; i0 < count; i0 += parts * ROWS * AHEAD) {
     int2 m[AHEAD];
     RowPiece<D> x[AHEAD];
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) m[u] = i0 + u * ROWS < count ? moves[i0 + u * ROWS] : int2{-1, -1};
+    for (int u = 0; u < AHEAD; ++u) {
+      const int i = i0 + u * ROWS;
+      m[u] = i < count ? int2{moves[count - 1 - i].x, moves[i].y} : int2{-1, -1};
+    }
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u)
       if (m[u].x >= 0) x[u] = load_piece<D>(a, kv, m[u].x, j);
@@ -310,7 +345,7 @@ __device__ inline void move_rows(const CacheEvictArgs& a, int head, int count, i
 // The last rows.  Those that lie apart from their places are shared among workgroups; else one takes them in order: what it writes lies before what is still to be read.
 template <int D, int NT>
 __device__ inline void move_last(const CacheEvictArgs& a, const EvictSeq& q, int s, int kv, int part, int parts) {
-  constexpr int LPR = D / 8, ROWS = NT / LPR, AHEAD = 4;
+  constexpr int LPR = D / 8, ROWS = NT / LPR, AHEAD = kAhead;
   const int j = threadIdx.x % LPR;
   const int32_t* blocks = a.table + (int64_t)s * a.max_blocks;
   auto slot_of = [&](int p) {
@@ -420,10 +455,10 @@ template <int D>
 static int launch_evict_d(const CacheEvictArgs& a, hipStream_t st) {
   const int64_t tokens = (int64_t)a.max_blocks << a.c.log_page;
   const int heads = a.n_seq * a.c.Hk;
-  if (tokens <= 2048 || heads >= 256) return tokens <= 256 * 32 ? launch_select<D, 256, true>(a, st) : launch_select<D, 1024, true>(a, st);
-  int rc = tokens <= 256 * 32 ? launch_select<D, 256, false>(a, st) : launch_select<D, 1024, false>(a, st);
+  if (tokens <= 2048 || heads >= kManyHeads) return tokens <= kSmall * 32 ? launch_select<D, kSmall, true>(a, st) : launch_select<D, 1024, true>(a, st);
+  int rc = tokens <= kSmall * 32 ? launch_select<D, kSmall, false>(a, st) : launch_select<D, 1024, false>(a, st);
   if (rc != HA_OK) return rc;
-  constexpr int64_t per = 4 * kMoveThreads / (D / 8), per_last = 4 * kLastThreads / (D / 8);
+  constexpr int64_t per = kAhead * kMoveThreads / (D / 8), per_last = kAhead * kLastThreads / (D / 8);
   const int64_t most = (a.moves_most + per - 1) / per, fill = 2048 / heads + 1;
   hipLaunchKernelGGL(cache4_move_kernel<D>, dim3(heads, (unsigned)(most < fill ? most : fill)), dim3(kMoveThreads), 0, st, a);
   rc = check_launch();
