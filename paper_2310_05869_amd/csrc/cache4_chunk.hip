@@ -13,16 +13,12 @@
 //     workspace and are joined by a second launch.
 #include <type_traits>
 
+#include "cache4_attn.h"
 #include "cache4_chunk.h"
 
 namespace ha {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef s16x4 __attribute__((address_space(3))) * lds_s16x4_ptr;
@@ -32,9 +28,7 @@ constexpr int kStep = 64;           // tokens of a step
 // 24 of up to 200 behind up to 4096, 12 and 4 heads 58 / 55 / 55 / 57; 16 of up to 1024 behind up to 8192, 16 heads, d = 64 118 / 106 / 108 / 109.)
 constexpr int kTileCost = 320;
 constexpr int kLeastRun = 256;      // tokens of the line that a workgroup takes, at least (fp32, 6 sequences of up to 150 behind up to 2000, d = 64: 512 36 us, 256 29)
-constexpr int kMostParts = 512;     // workgroups that the chip holds at once, two per CU
-constexpr int kJoinThreads = 256;
-constexpr uint32_t kFarScale = 253; // V's scales from here on give values that may lie past the largest number, or NaN: taken by the rows that see the token alone
+constexpr int kChunkParts = 512;    // workgroups that the chip holds at once, two per CU
 
 template <int D>
 struct ChunkLds {
@@ -68,9 +62,9 @@ __device__ inline uint32_t two_values(uint32_t w, float sc) {
 }
 
 // SPLIT: parts of a query number and of a weight: 1 for bf16 queries, 3 for fp32 ones (24 bits); cached values have one.  WHOLE: a workgroup per tile.
+// x: the workgroup's number.
 template <int D, int SPLIT, int NW, bool WHOLE>
-__global__ __launch_bounds__(64 * NW, 2) void cache4_chunk_kernel(CacheChunkArgs a) {
-  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+__device__ __forceinline__ void cache4_chunk_run(const CacheChunkArgs& a, unsigned char* smem, int x) {
   using L = ChunkLds<D>;
   constexpr int QT = 32 * NW, KS = D / 16, DT = D / 32, G = D / kCacheGroup;
   constexpr bool F32 = SPLIT > 1;
@@ -92,14 +86,14 @@ __global__ __launch_bounds__(64 * NW, 2) void cache4_chunk_kernel(CacheChunkArgs
   int64_t before;
   const int64_t total = chunk_line(a.n_seq, threadIdx.x & 63, &before, cost);
   int parts = 1, part = 0;
-  int64_t u0 = blockIdx.x, u1 = 0;
+  int64_t u0 = x, u1 = 0;
   auto part_begin = [&](int p) { return total / parts * p + total % parts * p / parts; };
   if constexpr (WHOLE) {
     if (u0 >= total) return;
   } else {
     parts = (int)min((int64_t)a.parts, max(total / kLeastRun, (int64_t)1));
     if (parts > 8) parts &= ~7;
-    part = blockIdx.x;
+    part = x;
     if (part < parts && (parts & 7) == 0) part = (part & 7) * (parts >> 3) + (part >> 3);  // a run of the line per XCD: neighbours share keys
     if (threadIdx.x == 0) a.joins[4 * part] = -1;
     if (part >= parts || total == 0) return;
@@ -683,17 +677,43 @@ __global__ __launch_bounds__(64 * NW, 2) void cache4_chunk_kernel(CacheChunkArgs
   }
 }
 
-// Joins the sums of tiles that a cut divides: workgroup p those of the tile that run p ended, D / 4 threads a row.
+// Tiles of many rows and sequences of few in one launch.  WHOLE: the first workgroups have a tile each, the others a sequence and key head.  Else every workgroup has a run of
+// both lines, and of two that share a CU one begins with the one, one with the other: the few rows wait for memory where the many keep the matrix cores busy.
+template <int D, int SPLIT, int NW, bool WHOLE>
+__global__ __launch_bounds__(64 * NW, 2) void cache4_chunk_kernel(CacheChunkArgs a, CacheAttnArgs n) {
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  auto few = [&](int x, int y) {
+    cache4_attn_run<D, SPLIT, NW, WHOLE, false, true, true>(n, *reinterpret_cast<CacheAttnLds<D, NW>*>(smem), x, y);
+  };
+  if constexpr (WHOLE) {
+    const int i = (int)blockIdx.x - a.tiles;
+    if (i < 0) cache4_chunk_run<D, SPLIT, NW, true>(a, smem, blockIdx.x);
+    else few(i / a.c.Hk, i % a.c.Hk);
+    return;
+  }
+  const bool mine = (int)blockIdx.x < n.parts * a.c.Hk, late = (blockIdx.x >> 8) & 1;
+  if (mine && !late) {
+    few(blockIdx.x / a.c.Hk, blockIdx.x % a.c.Hk);
+    __syncthreads();
+  }
+  if ((int)blockIdx.x < a.parts) cache4_chunk_run<D, SPLIT, NW, false>(a, smem, blockIdx.x);
+  if (mine && late) {
+    __syncthreads();
+    few(blockIdx.x / a.c.Hk, blockIdx.x % a.c.Hk);
+  }
+}
+
+// Joins the sums of tiles that a cut divides: workgroups of p those of the tile that run p ended, D / 4 threads a row.
 template <int D, int SPLIT, int NW>
-__global__ __launch_bounds__(kJoinThreads) void cache4_chunk_join_kernel(CacheChunkArgs a) {
+__device__ __forceinline__ void cache4_chunk_join(const CacheChunkArgs& a, int p1, int block) {
   constexpr bool F32 = SPLIT > 1;
   constexpr int LPR = D / 4, ROWS = kJoinThreads / LPR, QT = 32 * NW;
-  const int p1 = blockIdx.x, s = a.joins[4 * p1];
+  const int s = a.joins[4 * p1];
   if (s < 0) return;
   const int hh = a.joins[4 * p1 + 1], t = a.joins[4 * p1 + 2], p0 = a.joins[4 * p1 + 3];
   const ChunkSeq q = chunk_seq(a, s);
   const int kv = hh / a.subs, head0 = kv * a.group + (hh - kv * a.subs) * a.sub_group;
-  const int r = blockIdx.y * ROWS + threadIdx.x / LPR, ch = threadIdx.x % LPR * 4;
+  const int r = block * ROWS + threadIdx.x / LPR, ch = threadIdx.x % LPR * 4;
   const int r_tok = r / a.sub_group, head = head0 + (r - r_tok * a.sub_group), tok = t * a.tile_tokens + r_tok;
   if (r_tok >= a.tile_tokens || tok >= q.n || head >= (kv + 1) * a.group) return;
   auto exp_of = [](float x) { return F32 ? expf(x) : __builtin_amdgcn_exp2f(x); };
@@ -716,59 +736,66 @@ __global__ __launch_bounds__(kJoinThreads) void cache4_chunk_join_kernel(CacheCh
   if (ch == 0) a.lse[(int64_t)head * a.rows + q.start + tok] = empty ? -INFINITY : F32 ? m + logf(l) : (m + log2f(l)) * kLn2;
 }
 
-// Tables of few tokens: a workgroup per tile, and no second launch.  Sequences whose rows of a key head fit 16 go to launches of their own, in which the waves of a
-// workgroup take different tokens (cache4_attn.hip), where there can be several.
+// Tables of few tokens: a workgroup per tile, and no second launch.  Sequences whose rows of a key head fit 16 are read with the waves of a workgroup on different tokens
+// (cache4_attn.h), where there can be several.
 void cache4_chunk_split(CacheChunkArgs* a, CacheAttnArgs* narrow) {
   a->subs = (a->group + kChunkRows - 1) / kChunkRows;
   a->sub_group = (a->group + a->subs - 1) / a->subs;
   a->tile_tokens = kChunkRows / a->sub_group;
   a->narrow = a->group <= kNarrowRows && a->n_seq >= 4 ? kNarrowRows : 0;
-  narrow->parts = a->narrow ? cache4_parts(a->c.Hk, 1) : 0;
+  narrow->parts = a->narrow ? (a->c.Hk < kChunkParts ? kChunkParts / a->c.Hk : 1) : 0;
   const int64_t tokens = (int64_t)a->max_blocks << a->c.log_page, heads = (int64_t)a->c.Hk * a->subs;
   const int64_t tiles = ((int64_t)a->rows / a->tile_tokens + a->n_seq) * heads;
-  if (tokens <= 1024 && tiles <= kMaxLaunch) {
+  if (tokens <= 1024 && tiles + heads * a->n_seq <= kMaxLaunch) {
+    a->tiles = (int32_t)tiles;
     a->parts = 0;
     return;
   }
   const int64_t runs = tiles * (tokens + kTileCost) / kLeastRun;
-  a->parts = (int32_t)(runs < 1 ? 1 : runs > kMostParts ? kMostParts : runs);
+  a->parts = (int32_t)(runs < 1 ? 1 : runs > kChunkParts ? kChunkParts : runs);
+}
+
+// Both kinds' joins
+template <int D, int SPLIT, int NW>
+__global__ __launch_bounds__(kJoinThreads) void cache4_chunk_join_kernel(CacheChunkArgs a, CacheAttnArgs n, int wide, int each) {
+  __shared__ CacheJoinLds<D, SPLIT> lds;
+  constexpr int PER = 32 * NW / (kJoinThreads / (D / 4));  // workgroups of a tile
+  const int i = (int)blockIdx.x - wide;
+  if (i < 0) cache4_chunk_join<D, SPLIT, NW>(a, blockIdx.x / PER, blockIdx.x % PER);
+  else cache4_join_run<D, SPLIT, true>(n, lds, i / each, i % each, (int64_t)n.n_seq * each);
 }
 
 template <int D, int SPLIT, int NW>
-static int launch_chunk_one(const CacheChunkArgs& a, hipStream_t st) {
-  constexpr size_t lds = ChunkLds<D>::bytes(NW);
+static int launch_chunk_one(const CacheChunkArgs& args, const CacheAttnArgs& few, hipStream_t st) {
+  constexpr size_t chunk_lds = ChunkLds<D>::bytes(NW), few_lds = sizeof(CacheAttnLds<D, NW>), lds = chunk_lds > few_lds ? chunk_lds : few_lds;
   static std::atomic<uint64_t> set_whole{0}, set_parts{0};
+  CacheChunkArgs a = args;
+  CacheAttnArgs n = few;
   if (a.parts == 0) {
     const auto kernel = &cache4_chunk_kernel<D, SPLIT, NW, true>;
     const int rc = allow_full_lds(reinterpret_cast<const void*>(kernel), set_whole);
     if (rc != HA_OK) return rc;
-    const int64_t grid = ((int64_t)a.rows / a.tile_tokens + a.n_seq) * a.c.Hk * a.subs;  // tiles that there can be
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * NW), lds, st, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(a.tiles + (a.narrow ? a.n_seq * a.c.Hk : 0))), dim3(64 * NW), lds, st, a, n);
     return check_launch();
   }
   const auto kernel = &cache4_chunk_kernel<D, SPLIT, NW, false>;
   int rc = allow_full_lds(reinterpret_cast<const void*>(kernel), set_parts);
   if (rc != HA_OK) return rc;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)a.parts), dim3(64 * NW), lds, st, a);
+  const int few_runs = n.parts * a.c.Hk, grid = few_runs > a.parts ? few_runs : a.parts;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * NW), lds, st, a, n);
   rc = check_launch();
   if (rc != HA_OK) return rc;
-  constexpr int per = kJoinThreads / (D / 4);
-  hipLaunchKernelGGL((cache4_chunk_join_kernel<D, SPLIT, NW>), dim3((unsigned)a.parts, 32 * NW / per), dim3(kJoinThreads), 0, st, a);
+  constexpr int PAR = kJoinThreads / (D / 4);
+  const int64_t rows = (int64_t)a.c.Hk * kNarrowRows;
+  n.join_few = a.n_seq * rows > (1 << 20);  // (a launch counts its threads in 32 bits)
+  const int wide = a.parts * (32 * NW / PAR), each = (int)(n.join_few ? (rows + PAR - 1) / PAR : rows);
+  hipLaunchKernelGGL((cache4_chunk_join_kernel<D, SPLIT, NW>), dim3((unsigned)(wide + (a.narrow ? a.n_seq * each : 0))), dim3(kJoinThreads), 0, st, a, n, wide, each);
   return check_launch();
 }
 
-static int launch_chunk_wide(const CacheChunkArgs& a, int dtype, hipStream_t st) {
-  if (a.c.d == 128) return dtype == HA_BF16 ? launch_chunk_one<128, 1, 4>(a, st) : launch_chunk_one<128, 3, 4>(a, st);
-  return dtype == HA_BF16 ? launch_chunk_one<64, 1, 4>(a, st) : launch_chunk_one<64, 3, 4>(a, st);
-}
-
-int launch_cache4_chunk(const CacheChunkArgs& a, const CacheAttnArgs& narrow, int dtype, hipStream_t st) {
-  int rc = HA_OK;
-  const bool whole = a.parts == 0;
-  if (a.narrow) rc = launch_cache4_ragged(narrow, whole, dtype, st);
-  if (rc == HA_OK) rc = launch_chunk_wide(a, dtype, st);
-  if (rc == HA_OK && a.narrow && !whole) rc = join_cache4_ragged(narrow, dtype, st);
-  return rc;
+int launch_cache4_chunk(const CacheChunkArgs& a, const CacheAttnArgs& n, int dtype, hipStream_t st) {
+  if (a.c.d == 128) return dtype == HA_BF16 ? launch_chunk_one<128, 1, 4>(a, n, st) : launch_chunk_one<128, 3, 4>(a, n, st);
+  return dtype == HA_BF16 ? launch_chunk_one<64, 1, 4>(a, n, st) : launch_chunk_one<64, 3, 4>(a, n, st);
 }
 
 }  // namespace ha

@@ -58,8 +58,6 @@ struct CacheAttnArgs {
   int32_t rows_all, join_few;
 };
 constexpr int kNarrowRows = 16;  // query rows of a key head that a wave keeps beside codes in registers
-int launch_cache4_ragged(const CacheAttnArgs& a, bool whole, int dtype, hipStream_t st);
-int join_cache4_ragged(const CacheAttnArgs& a, int dtype, hipStream_t st);
 int launch_cache4_attn(const CacheAttnArgs& a, int dtype, hipStream_t st);
 int cache4_parts(int Hk, int tiles);
 int cache4_whole(const CacheAttnArgs& a);   // waves of a workgroup that takes a whole sequence, 0: tokens are shared out
@@ -81,9 +79,10 @@ struct CacheChunkArgs {
   int32_t group;             // query heads per key head
   int32_t subs, sub_group;   // a key head's query heads in `subs` runs of sub_group, each of which fits a tile
   int32_t tile_tokens;       // new tokens of a tile: tile_tokens * sub_group rows
-  int32_t narrow;            // sequences of up to so many rows of a key head are left to launches of their own; 0: none
+  int32_t narrow;            // sequences of up to so many rows of a key head are read in another form, for few rows; 0 (sums of weights: -1): none
   int32_t fresh;             // sums of weights: earlier ones do not count
   int32_t parts;             // workgroups that share all work; 0: a workgroup per tile
+  int32_t tiles;             // a workgroup per tile: tiles that there can be
   int32_t few_wgs;           // sums of weights: workgroups for the sequences of few rows; 0: none
   FastDiv div_group;
   // workspace: per workgroup, the tile that it ends of those that others began (four integers), and two tiles of sums with their references and row sums
