@@ -34,7 +34,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kJoinThreads = 256;
 constexpr unsigned kJoinsAtOnce = 2048;  // workgroups of the joining launch that the chip holds at once
-constexpr int kFewParts = 16;
+constexpr int kFewParts = 16, kFewRaggedParts = 64;
 constexpr int kMostParts = 768;  // workgroups of four waves that the chip holds at once, three per CU
 constexpr int kUnit = 64;        // tokens of a wave's step
 constexpr int kTilesPerUnit = 4; // of 16 tokens
@@ -543,11 +543,10 @@ __device__ __forceinline__ void cache4_attn_run(const CacheAttnArgs& a, CacheAtt
 // parts, one at a time -> eight, the whole call: 44 -> 17 us).  A row has a workgroup to itself, whose groups take its parts in turn; in launches of more rows than
 // workgroups run at once, a row of few parts has one group alone, and the workgroups too many end at once (the whole call: 64 sequences of up to 16384 tokens, three queries
 // each, 6144 rows, 44.2 -> 42.0 us; 32 of up to 4096, eight each, 8192 rows, 29.5 -> 26.3; but 60 of up to 8000, 960 rows, 24.6 -> 25.5).
-// RAGGED: row y of a sequence is row y % 16 of key head y / 16.
 // block, blocks: the workgroup's number among those of sequence s, workgroups of the launch in all.
 template <int D, int SPLIT>
 struct CacheJoinLds {
-  static constexpr int LPR = D / 4, PAR = kJoinThreads / LPR;
+  static constexpr int LPR = D / 4, PAR = kJoinThreads / LPR;  // threads of a row, rows at a time
   f32x4 o[PAR][LPR];
   float l[PAR], m[PAR];
 };
@@ -563,17 +562,20 @@ __device__ __forceinline__ void cache4_join_run(const CacheAttnArgs& a, CacheJoi
   const int p0 = a.span[2 * s], p1 = a.span[2 * s + 1];  // (asked for with the length; of an empty sequence they are what was there)
   const int parts = len > 0 ? p1 - p0 + 1 : 0;
   if (parts == 1) return;  // finished where its tokens were read
-  const bool few = RAGGED && a.join_few ? true : parts <= kFewParts && blocks > kJoinsAtOnce;
-  const int rows = RAGGED ? a.c.Hk * kCRows : a.Hq * a.q_len, y = few ? block * PAR + mine : block;
-  if (y >= rows) return;   // (few: no barrier follows; many: all threads alike)
+  const bool few = parts <= (RAGGED ? kFewRaggedParts : kFewParts) && (RAGGED || blocks > kJoinsAtOnce);
   int hq, tok, hk, row;
+  // RAGGED: PAR of a key head's 16 rows, a group of threads each; one after the other, with all threads, where there are many parts
+  for (int i = 0; i < (RAGGED && !few ? PAR : 1); ++i) {
   if constexpr (RAGGED) {
-    hk = y / kCRows;
-    row = y % kCRows;
+    constexpr int per = kCRows / PAR;
+    hk = block / per;
+    row = block % per * PAR + (few ? mine : i);
     if (row >= ragged_queries(a, s) * a.group) return;
     tok = row / a.group;
     hq = hk * a.group + row % a.group;
   } else {
+    const int y = few ? block * PAR + mine : block;
+    if (y >= a.Hq * a.q_len) return;   // (few: no barrier follows; many: all threads alike)
     hq = y % a.Hq;
     tok = y / a.Hq;
     hk = hq / a.group;
@@ -629,13 +631,17 @@ __device__ __forceinline__ void cache4_join_run(const CacheAttnArgs& a, CacheJoi
     finish();
     return;
   }
+  if (RAGGED && i > 0) __syncthreads();  // (the row before has been added up)
   sum_o[mine][lane] = acc;
   if (lane == 0) {
     sum_m[mine] = m;
     sum_l[mine] = l;
   }
   __syncthreads();
-  if (mine != 0) return;
+  if (mine != 0) {
+    if constexpr (RAGGED) continue;
+    return;
+  }
 #pragma unroll
   for (int i = 1; i < PAR; ++i) m = fmaxf(m, sum_m[i]);
   const float ref = m == -INFINITY ? 0.f : m;
@@ -648,6 +654,7 @@ __device__ __forceinline__ void cache4_join_run(const CacheAttnArgs& a, CacheJoi
     l += w * sum_l[i];
   }
   finish();
+  }
 }
 
 }  // namespace ha

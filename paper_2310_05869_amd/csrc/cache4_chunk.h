@@ -38,6 +38,25 @@ __device__ inline int64_t uniform64(int64_t x) {
   return (int64_t)((uint64_t)hi << 32 | lo);
 }
 
+// Where run p of `parts` begins on a line.  (Rounded down from a product in double, by every workgroup alike; a division of 64 bits takes a microsecond.)
+__device__ inline int64_t run_begin(int64_t total, int parts, int p) { return p >= parts ? total : (int64_t)((double)total * ((double)p / (double)parts)); }
+
+// x / y, rounded down, for x of less than 2^62 and quotients of less than 2^31
+__device__ inline int whole_part(int64_t x, int64_t y) {
+  int64_t n = (int64_t)((double)x / (double)y);
+  while (n * y > x) --n;
+  while ((n + 1) * y <= x) ++n;
+  return (int)n;
+}
+
+// The run of `parts` that place x lies in
+__device__ inline int run_of(int64_t total, int parts, int64_t x) {
+  int p = min((int)((double)x / (double)total * parts), parts - 1);
+  while (p > 0 && run_begin(total, parts, p) > x) --p;
+  while (run_begin(total, parts, p + 1) <= x) ++p;
+  return p;
+}
+
 // All sequences' work as one line: sequence s takes cost(s) >= 0 of it.  A lane sums a run of sequences; the sum is the same for all lanes, *before: what
 // precedes the lane's run.
 template <class Cost>

@@ -76,7 +76,7 @@ __device__ __forceinline__ void cache4_chunk_run(const CacheChunkArgs& a, unsign
 
   // ---- place ----
   const int tt = a.tile_tokens, heads = a.c.Hk * a.subs;
-  auto tiles_of = [&](const ChunkSeq& q) { return (int64_t)q.n * a.group <= a.narrow ? 0 : (q.n + tt - 1) / tt; };
+  auto tiles_of = [&](const ChunkSeq& q) { return (int64_t)q.n * a.group <= a.narrow ? 0 : a.div_tokens.div(q.n + tt - 1); };
   auto upto = [&](const ChunkSeq& q, int64_t t) { return t * (max(q.held, 0) + kTileCost) + tt * (t * (t + 1) / 2); };  // line before tile t of a head
   auto cost = [&](int s) -> int64_t {
     const ChunkSeq q = chunk_seq(a, s);
@@ -87,7 +87,6 @@ __device__ __forceinline__ void cache4_chunk_run(const CacheChunkArgs& a, unsign
   const int64_t total = chunk_line(a.n_seq, threadIdx.x & 63, &before, cost);
   int parts = 1, part = 0;
   int64_t u0 = x, u1 = 0;
-  auto part_begin = [&](int p) { return total / parts * p + total % parts * p / parts; };
   if constexpr (WHOLE) {
     if (u0 >= total) return;
   } else {
@@ -95,10 +94,10 @@ __device__ __forceinline__ void cache4_chunk_run(const CacheChunkArgs& a, unsign
     if (parts > 8) parts &= ~7;
     part = x;
     if (part < parts && (parts & 7) == 0) part = (part & 7) * (parts >> 3) + (part >> 3);  // a run of the line per XCD: neighbours share keys
-    if (threadIdx.x == 0) a.joins[4 * part] = -1;
+    if (threadIdx.x == 0) a.joins[8 * part] = -1;
     if (part >= parts || total == 0) return;
-    u0 = part_begin(part);
-    u1 = part_begin(part + 1);
+    u0 = run_begin(total, parts, part);
+    u1 = run_begin(total, parts, part + 1);
   }
   int64_t tile_first;
   int s = chunk_place(a.n_seq, before, u0, &tile_first, cost);
@@ -106,8 +105,8 @@ __device__ __forceinline__ void cache4_chunk_run(const CacheChunkArgs& a, unsign
   int T = tiles_of(q), hh, t;
   {
     const int64_t head_cost = WHOLE ? (int64_t)T : upto(q, T), rem = u0 - tile_first;
-    hh = (int)(rem / head_cost);
-    const int64_t in_head = rem - hh * head_cost;
+    hh = whole_part(rem, head_cost);
+    const int64_t in_head = rem - (int64_t)hh * head_cost;
     if constexpr (WHOLE) {
       t = T - 1 - (int)in_head;
     } else {
@@ -146,7 +145,7 @@ __device__ __forceinline__ void cache4_chunk_run(const CacheChunkArgs& a, unsign
       const int last_block = max(q.len - 1, 0) >> log_page;
 
       // ---- the lane's query row ----
-      const int r = wave * 32 + lq, r_tok = r / a.sub_group, r_head = head0 + (r - r_tok * a.sub_group);
+      const int r = wave * 32 + lq, r_tok = a.div_heads.div(r), r_head = head0 + (r - r_tok * a.sub_group);
       const bool valid = r_tok < tt && t * tt + r_tok < q.n && r_head < head_end;
       const int tok = t * tt + (valid ? r_tok : 0), head = valid ? r_head : head0;  // (a lane without a row repeats the tile's first)
       const int limit = q.held + tok + 1;  // tokens that it sees
@@ -650,14 +649,14 @@ __device__ __forceinline__ void cache4_chunk_run(const CacheChunkArgs& a, unsign
               (u32x4){pack_bf16x2(x0[0], x0[1]), pack_bf16x2(x0[2], x0[3]), pack_bf16x2(x1[0], x1[1]), pack_bf16x2(x1[2], x1[3])};
         }
       }
-      if (!WHOLE && !whole && last == nsteps && threadIdx.x == 0) {  // others began the tile: the second launch joins it
-        int p = (int)min(tile_first / (total / parts), (int64_t)part - 1);
-        while (part_begin(p) > tile_first) --p;
-        while (part_begin(p + 1) <= tile_first) ++p;
-        a.joins[4 * part + 1] = hh;
-        a.joins[4 * part + 2] = t;
-        a.joins[4 * part + 3] = p;
-        a.joins[4 * part] = s;
+      if (!WHOLE && first > 0 && threadIdx.x == 0) {  // others began the tile: the second launch joins it
+        int32_t* j = a.joins + 8 * part;
+        j[1] = head0;
+        j[2] = q.start + t * tt;
+        j[3] = min(q.n - t * tt, tt);
+        j[4] = head_end - head0;
+        j[5] = run_of(total, parts, tile_first + (int64_t)(nsteps - 1) * kStep);  // that has the last step
+        j[0] = run_of(total, parts, tile_first);
       }
     }
     if constexpr (WHOLE) return;
@@ -703,37 +702,83 @@ __global__ __launch_bounds__(64 * NW, 2) void cache4_chunk_kernel(CacheChunkArgs
   }
 }
 
-// Joins the sums of tiles that a cut divides: workgroups of p those of the tile that run p ended, D / 4 threads a row.
+// Joins the sums of tiles that a cut divides, D / 4 threads a row.  Of the runs p0 ... p1 that share a tile those behind the first have kJoinWgs workgroups each for its
+// rows: a tile of few runs has several rows a thread, in turn, a tile of many (few rows behind a long sequence) a row of some threads, and pieces in flight.
+constexpr int kJoinWgs = 4;
 template <int D, int SPLIT, int NW>
-__device__ __forceinline__ void cache4_chunk_join(const CacheChunkArgs& a, int p1, int block) {
+__device__ __forceinline__ void cache4_chunk_join(const CacheChunkArgs& a, int p, int block) {
   constexpr bool F32 = SPLIT > 1;
-  constexpr int LPR = D / 4, ROWS = kJoinThreads / LPR, QT = 32 * NW;
-  const int s = a.joins[4 * p1];
-  if (s < 0) return;
-  const int hh = a.joins[4 * p1 + 1], t = a.joins[4 * p1 + 2], p0 = a.joins[4 * p1 + 3];
-  const ChunkSeq q = chunk_seq(a, s);
-  const int kv = hh / a.subs, head0 = kv * a.group + (hh - kv * a.subs) * a.sub_group;
-  const int r = block * ROWS + threadIdx.x / LPR, ch = threadIdx.x % LPR * 4;
-  const int r_tok = r / a.sub_group, head = head0 + (r - r_tok * a.sub_group), tok = t * a.tile_tokens + r_tok;
-  if (r_tok >= a.tile_tokens || tok >= q.n || head >= (kv + 1) * a.group) return;
+  constexpr int LPR = D / 4, ROWS = kJoinThreads / LPR, QT = 32 * NW, GROUPS = QT / ROWS;
+  const int32_t* j = a.joins + 8 * p;
+  const int p0 = j[0], head0 = j[1], row0 = j[2], tokens = j[3], heads = min(j[4], a.sub_group), p1 = j[5];
+  if (p0 < 0) return;
+  const int ch = threadIdx.x % LPR * 4;
   auto exp_of = [](float x) { return F32 ? expf(x) : __builtin_amdgcn_exp2f(x); };
-  float m = -INFINITY, l = 0.f;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  for (int p = p0; p <= p1; ++p) {
-    const int64_t row = (2 * (int64_t)p + (p == p0)) * QT + r;
-    const float pm = a.part_ml[2 * row], pl = a.part_ml[2 * row + 1];
-    const f32x4 v = *reinterpret_cast<const f32x4*>(a.part_o + row * D + ch);
-    const float top = fmaxf(m, pm), ref = top == -INFINITY ? 0.f : top, w0 = exp_of(m - ref), w1 = exp_of(pm - ref);
-    acc = w0 * acc + w1 * v;
-    l = w0 * l + w1 * pl;
-    m = top;
+  auto join = [&](auto rows_tag, auto ahead_tag, int first_group, int step) {  // rows of groups first_group, first_group + step, ...
+    constexpr int U = decltype(rows_tag)::value, Z = decltype(ahead_tag)::value;
+    float m[U], l[U];
+    f32x4 acc[U];
+    int r[U], tok[U], head[U];
+    bool live[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      r[u] = (first_group + u * step) * ROWS + threadIdx.x / LPR;
+      tok[u] = a.div_heads.div(r[u]);
+      head[u] = r[u] - tok[u] * a.sub_group;
+      live[u] = tok[u] < tokens && head[u] < heads;
+      m[u] = -INFINITY;
+      l[u] = 0.f;
+      acc[u] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    }
+    for (int q = p0; q <= p1; q += Z) {
+      float pm[Z][U], pl[Z][U];
+      f32x4 v[Z][U];
+#pragma unroll
+      for (int z = 0; z < Z; ++z)
+#pragma unroll
+        for (int u = 0; u < U; ++u) {  // (past the last the last again, which counts once)
+          const int qq = min(q + z, p1);
+          const int64_t row = (2 * (int64_t)qq + (qq == p0)) * QT + (live[u] ? r[u] : 0);
+          pm[z][u] = a.part_ml[2 * row];
+          pl[z][u] = a.part_ml[2 * row + 1];
+          v[z][u] = *reinterpret_cast<const f32x4*>(a.part_o + row * D + ch);
+        }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        float top = m[u];
+#pragma unroll
+        for (int z = 0; z < Z; ++z) top = fmaxf(top, pm[z][u]);
+        const float ref = top == -INFINITY ? 0.f : top, w0 = exp_of(m[u] - ref);
+        acc[u] *= w0;
+        l[u] *= w0;
+#pragma unroll
+        for (int z = 0; z < Z; ++z) {
+          if (q + z > p1) break;
+          const float w = exp_of(pm[z][u] - ref);
+          acc[u] += w * v[z][u];
+          l[u] += w * pl[z][u];
+        }
+        m[u] = top;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (!live[u]) continue;
+      const bool empty = l[u] == 0.f;
+      acc[u] *= empty ? 0.f : 1.f / l[u];
+      const int64_t row = row0 + tok[u], hq = head0 + head[u], at = row * a.o.row + hq * a.o.head + ch;
+      if constexpr (F32) *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.out) + at) = acc[u];
+      else *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(a.out) + at) = (u32x2){pack_bf16x2(acc[u][0], acc[u][1]), pack_bf16x2(acc[u][2], acc[u][3])};
+      if (ch == 0) a.lse[hq * a.rows + row] = empty ? -INFINITY : F32 ? m[u] + logf(l[u]) : (m[u] + log2f(l[u])) * kLn2;
+    }
+  };
+  const int helpers = (p1 - p0) * kJoinWgs, me = (p - p0 - 1) * kJoinWgs + block;
+  if (helpers < GROUPS) {
+    constexpr int U = GROUPS / kJoinWgs;
+    if (p == p1) join(std::integral_constant<int, U>{}, std::integral_constant<int, 2>{}, block, kJoinWgs);
+  } else if (me < GROUPS) {
+    join(std::integral_constant<int, 1>{}, std::integral_constant<int, 8>{}, me, 0);
   }
-  const bool empty = l == 0.f;
-  acc *= empty ? 0.f : 1.f / l;
-  const int64_t at = (int64_t)(q.start + tok) * a.o.row + (int64_t)head * a.o.head + ch;
-  if constexpr (F32) *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.out) + at) = acc;
-  else *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(a.out) + at) = (u32x2){pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3])};
-  if (ch == 0) a.lse[(int64_t)head * a.rows + q.start + tok] = empty ? -INFINITY : F32 ? m + logf(l) : (m + log2f(l)) * kLn2;
 }
 
 // Tables of few tokens: a workgroup per tile, and no second launch.  Sequences whose rows of a key head fit 16 are read with the waves of a workgroup on different tokens
@@ -742,6 +787,8 @@ void cache4_chunk_split(CacheChunkArgs* a, CacheAttnArgs* narrow) {
   a->subs = (a->group + kChunkRows - 1) / kChunkRows;
   a->sub_group = (a->group + a->subs - 1) / a->subs;
   a->tile_tokens = kChunkRows / a->sub_group;
+  a->div_tokens = make_fast_div(a->tile_tokens);
+  a->div_heads = make_fast_div(a->sub_group);
   a->narrow = a->group <= kNarrowRows && a->n_seq >= 4 ? kNarrowRows : 0;
   narrow->parts = a->narrow ? (a->c.Hk < kChunkParts ? kChunkParts / a->c.Hk : 1) : 0;
   const int64_t tokens = (int64_t)a->max_blocks << a->c.log_page, heads = (int64_t)a->c.Hk * a->subs;
@@ -759,18 +806,18 @@ void cache4_chunk_split(CacheChunkArgs* a, CacheAttnArgs* narrow) {
 template <int D, int SPLIT, int NW>
 __global__ __launch_bounds__(kJoinThreads) void cache4_chunk_join_kernel(CacheChunkArgs a, CacheAttnArgs n, int wide, int each) {
   __shared__ CacheJoinLds<D, SPLIT> lds;
-  constexpr int PER = 32 * NW / (kJoinThreads / (D / 4));  // workgroups of a tile
+  constexpr int PER = kJoinWgs;
   const int i = (int)blockIdx.x - wide;
   if (i < 0) cache4_chunk_join<D, SPLIT, NW>(a, blockIdx.x / PER, blockIdx.x % PER);
-  else cache4_join_run<D, SPLIT, true>(n, lds, i / each, i % each, (int64_t)n.n_seq * each);
+  else cache4_join_run<D, SPLIT, true>(n, lds, i / each, i % each, 0);
 }
 
 template <int D, int SPLIT, int NW>
 static int launch_chunk_one(const CacheChunkArgs& args, const CacheAttnArgs& few, hipStream_t st) {
   constexpr size_t chunk_lds = ChunkLds<D>::bytes(NW), few_lds = sizeof(CacheAttnLds<D, NW>), lds = chunk_lds > few_lds ? chunk_lds : few_lds;
   static std::atomic<uint64_t> set_whole{0}, set_parts{0};
-  CacheChunkArgs a = args;
-  CacheAttnArgs n = few;
+  const CacheChunkArgs& a = args;
+  const CacheAttnArgs& n = few;
   if (a.parts == 0) {
     const auto kernel = &cache4_chunk_kernel<D, SPLIT, NW, true>;
     const int rc = allow_full_lds(reinterpret_cast<const void*>(kernel), set_whole);
@@ -786,9 +833,7 @@ static int launch_chunk_one(const CacheChunkArgs& args, const CacheAttnArgs& few
   rc = check_launch();
   if (rc != HA_OK) return rc;
   constexpr int PAR = kJoinThreads / (D / 4);
-  const int64_t rows = (int64_t)a.c.Hk * kNarrowRows;
-  n.join_few = a.n_seq * rows > (1 << 20);  // (a launch counts its threads in 32 bits)
-  const int wide = a.parts * (32 * NW / PAR), each = (int)(n.join_few ? (rows + PAR - 1) / PAR : rows);
+  const int wide = a.parts * kJoinWgs, each = a.c.Hk * (kNarrowRows / PAR);
   hipLaunchKernelGGL((cache4_chunk_join_kernel<D, SPLIT, NW>), dim3((unsigned)(wide + (a.narrow ? a.n_seq * each : 0))), dim3(kJoinThreads), 0, st, a, n, wide, each);
   return check_launch();
 }

@@ -53,9 +53,9 @@ struct CacheAttnArgs {
   int32_t* span;               // [n_seq][2]
   float* part_o;
   float* part_ml;
-  // sequences of few rows among chunks of any number (cache4_chunk.hip): rows of Q, those of a sequence, and whether the joining launch has no workgroup per row
+  // sequences of few rows among chunks of any number (cache4_chunk.hip): where their rows begin, rows of Q
   const int32_t* cu;
-  int32_t rows_all, join_few;
+  int32_t rows_all;
 };
 constexpr int kNarrowRows = 16;  // query rows of a key head that a wave keeps beside codes in registers
 int launch_cache4_attn(const CacheAttnArgs& a, int dtype, hipStream_t st);
@@ -84,8 +84,8 @@ struct CacheChunkArgs {
   int32_t parts;             // workgroups that share all work; 0: a workgroup per tile
   int32_t tiles;             // a workgroup per tile: tiles that there can be
   int32_t few_wgs;           // sums of weights: workgroups for the sequences of few rows; 0: none
-  FastDiv div_group;
-  // workspace: per workgroup, the tile that it ends of those that others began (four integers), and two tiles of sums with their references and row sums
+  FastDiv div_group, div_tokens, div_heads;  // by group, tile_tokens, sub_group
+  // workspace: per workgroup, the tile that it ends of those that others began (eight integers, sums of weights four), and two tiles of sums with their references and row sums
   int32_t* joins;
   float* part_o;
   float* part_ml;

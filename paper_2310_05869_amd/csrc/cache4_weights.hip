@@ -83,8 +83,7 @@ __global__ __launch_bounds__(64 * kWWaves, 2) void cache4_weights_kernel(CacheCh
   if (part < parts && (parts & 7) == 0) part = (part & 7) * (parts >> 3) + (part >> 3);  // a run of the line per XCD: neighbours share rows
   if (threadIdx.x == 0) a.joins[4 * part] = -1;
   if (part >= parts || total == 0) return;
-  auto part_begin = [&](int p) { return total / parts * p + total % parts * p / parts; };
-  const int64_t u0 = part_begin(part), u1 = part_begin(part + 1);
+  const int64_t u0 = run_begin(total, parts, part), u1 = run_begin(total, parts, part + 1);
   int64_t tile_first;
   int s = chunk_place(a.n_seq, before, u0, &tile_first, cost);
   WeightsSeq w = weights_seq(a, s);
@@ -92,7 +91,7 @@ __global__ __launch_bounds__(64 * kWWaves, 2) void cache4_weights_kernel(CacheCh
   int kv, k;
   {
     const int64_t head_cost = weights_upto(a, w, w.tiles), rem = u0 - tile_first;
-    kv = __builtin_amdgcn_readfirstlane((int)(rem / head_cost));
+    kv = __builtin_amdgcn_readfirstlane(whole_part(rem, head_cost));
     const int64_t in_head = rem - kv * head_cost;
     int lo = 0, hi = w.tiles;
     while (hi - lo > 1) {
@@ -361,12 +360,9 @@ __global__ __launch_bounds__(64 * kWWaves, 2) void cache4_weights_kernel(CacheCh
       } else {
         a.part_o[(2 * (int64_t)part + begins) * kWTokens + in_tile] = mine;
         if (last == nsteps && threadIdx.x == 0) {  // others began the tile: the second launch adds up
-          int p = (int)min(tile_first / (total / parts), (int64_t)part - 1);
-          while (part_begin(p) > tile_first) --p;
-          while (part_begin(p + 1) <= tile_first) ++p;
           a.joins[4 * part + 1] = kv;
           a.joins[4 * part + 2] = k;
-          a.joins[4 * part + 3] = p;
+          a.joins[4 * part + 3] = run_of(total, parts, tile_first);
           a.joins[4 * part] = s;
         }
       }
@@ -432,7 +428,7 @@ __global__ __launch_bounds__(256, SPLIT == 1 ? 3 : 2) void cache4_weights_few_ke
   const int64_t total = chunk_line(a.n_seq, lane, &before, cost);
   const int waves = (int)min((int64_t)gridDim.x * 4, total), me = blockIdx.x * 4 + wave;
   if (me >= waves) return;
-  const int64_t u0 = total / waves * me + total % waves * me / waves, u1 = total / waves * (me + 1) + total % waves * (me + 1) / waves;
+  const int64_t u0 = run_begin(total, waves, me), u1 = run_begin(total, waves, me + 1);
   int64_t at;
   int s = chunk_place(a.n_seq, before, u0, &at, cost);
   const int64_t page_bytes = (int64_t)a.c.Hk * a.c.block_bytes();
@@ -442,7 +438,7 @@ __global__ __launch_bounds__(256, SPLIT == 1 ? 3 : 2) void cache4_weights_few_ke
   FewSeq f = few_seq(a, s);
   {
     const int64_t each = each_of(f);
-    kv = __builtin_amdgcn_readfirstlane((int)((u0 - at) / each));
+    kv = __builtin_amdgcn_readfirstlane(whole_part(u0 - at, each));
     at = uniform64(at + kv * each);
   }
   for (;;) {

@@ -107,7 +107,7 @@ static size_t chunk_space(CacheChunkArgs* a, CacheAttnArgs* n, void* workspace) 
     return p;
   };
   const size_t rows = 2 * (size_t)a->parts * kChunkRows;
-  a->joins = reinterpret_cast<int32_t*>(take((size_t)a->parts * 16));
+  a->joins = reinterpret_cast<int32_t*>(take((size_t)a->parts * 32));
   a->part_o = reinterpret_cast<float*>(take(rows * a->c.d * 4));
   a->part_ml = reinterpret_cast<float*>(take(rows * 8));
   if (a->narrow && a->parts > 0) {
