@@ -291,63 +291,61 @@ __device__ __forceinline__ void cache4_chunk_run(const CacheChunkArgs& a, unsign
       if (threadIdx.x == 0) *far_flag = 0;
       __syncthreads();
 
-      // Codes are asked for two steps before they are used and their page two before that.  bf16 queries: step kt asks for K of kt + 3, V of kt + 2 and the page of kt + 4
-      // while it lays K of kt + 2 and V of kt + 1 into LDS, over K of kt and V of kt - 1, which all waves have left behind; fp32 queries have K no further than V.
-      // (Past the end the last step comes again, and is not read.)
+      // bf16 queries: step kt lays K of kt + 2 and V of kt + 1 into LDS, over K of kt and V of kt - 1, which all waves have left behind, and then asks for the codes that step
+      // kt + 1 will lay out; fp32 queries have K no further than V.  Codes have a step to come, their pages' numbers two.  (Asked for earlier, they take 13 more registers,
+      // and every reload of a spilled one waits for them: 2.8 us a step where few workgroups are the launch.  Past the end the last step comes again, and is not read.)
       const int ntiles = last - first;
       const bool live = __any(valid);  // (a wave without rows lays out its share of the tokens, no more)
       auto step_of = [&](int kt) { return first + min(kt, ntiles - 1); };
-      RawK<D> k[2];  // of even and odd steps
-      RawV<D> v[2];
+      RawK<D> k;
+      RawV<D> v;
       int pages[4];  // of steps kt ... kt + 3
       int next_page = 0;
-      auto request = [&](int kt, auto parity) {
-        constexpr int P = decltype(parity)::value;
+      auto request = [&](int kt) {
+        pages[3] = __builtin_amdgcn_readfirstlane(next_page);
         next_page = find_page(step_of(kt + 4));
-        if constexpr (!F32) load_k(step_of(kt + 3), pages[3], k[P ^ 1]);
-        else load_k(step_of(kt + 2), pages[2], k[P]);
-        load_v(step_of(kt + 2), pages[2], v[P]);
+        if constexpr (!F32) load_k(step_of(kt + 3), pages[3], k);
+        else load_k(step_of(kt + 2), pages[2], k);
+        load_v(step_of(kt + 2), pages[2], v);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) pages[i] = pages[i + 1];
       };
       auto lay_out = [&](auto parity) {  // (V is clean)
         constexpr int P = decltype(parity)::value;
-        if constexpr (!F32) store_k(P, pages[2], k[P]);
-        else store_k(P ^ 1, pages[1], k[P ^ 1]);
-        store_v(P ^ 1, v[P ^ 1]);
-      };
-      auto advance = [&]() {
-#pragma unroll
-        for (int i = 0; i < 3; ++i) pages[i] = pages[i + 1];
-        pages[3] = __builtin_amdgcn_readfirstlane(next_page);
+        if constexpr (!F32) store_k(P, pages[2], k);
+        else store_k(P ^ 1, pages[1], k);
+        store_v(P ^ 1, v);
       };
       const auto even = std::integral_constant<int, 0>{};
       const auto odd = std::integral_constant<int, 1>{};
       if (ntiles > 0) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) pages[i] = find_page(step_of(i));
+        for (int i = 0; i < 3; ++i) pages[i] = find_page(step_of(i));
+        next_page = find_page(step_of(3));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) pages[i] = __builtin_amdgcn_readfirstlane(pages[i]);
-        load_k(step_of(0), pages[0], k[0]);
-        load_v(step_of(0), pages[0], v[0]);
-        load_k(step_of(1), pages[1], k[1]);
-        load_v(step_of(1), pages[1], v[1]);
-        store_k(0, pages[0], k[0]);
-        clean_v(0, pages[0], v[0]);
-        store_v(0, v[0]);
+        for (int i = 0; i < 3; ++i) pages[i] = __builtin_amdgcn_readfirstlane(pages[i]);
+        RawK<D> k0;
+        RawV<D> v0;
+        load_k(step_of(0), pages[0], k0);
+        load_v(step_of(0), pages[0], v0);
+        load_k(step_of(1), pages[1], k);
+        load_v(step_of(1), pages[1], v);
+        store_k(0, pages[0], k0);
+        clean_v(0, pages[0], v0);
+        store_v(0, v0);
         if constexpr (!F32) {
-          load_k(step_of(2), pages[2], k[0]);
-          store_k(1, pages[1], k[1]);
+          store_k(1, pages[1], k);
+          load_k(step_of(2), pages[2], k);
         }
       }
       __syncthreads();
       if (ntiles > 0 && !live) {
         if constexpr (!F32) __syncthreads();
         auto one = [&](int kt, auto parity) {
-          constexpr int P = decltype(parity)::value;
           if (kt + 1 < ntiles) {
-            request(kt, parity);
-            clean_v(kt + 1, pages[1], v[P ^ 1]);
+            clean_v(kt + 1, pages[1], v);
             lay_out(parity);
-            advance();
+            request(kt);
           }
           __syncthreads();
         };
@@ -389,7 +387,6 @@ __device__ __forceinline__ void cache4_chunk_run(const CacheChunkArgs& a, unsign
           auto body = [&](int kt, f32x16 (&c)[2], f32x16 (&cn)[2], auto parity, auto has_next) {
             constexpr int P = decltype(parity)::value;
             constexpr bool HN = decltype(has_next)::value;
-            if constexpr (HN) request(kt, parity);
             if (__any(t_max > m + 8.f)) move_reference(t_max);
             const float shift = m == -INFINITY ? 0.f : -m;
             bf16x8 pf[4];
@@ -445,7 +442,7 @@ __device__ __forceinline__ void cache4_chunk_run(const CacheChunkArgs& a, unsign
             __builtin_amdgcn_s_setprio(0);
             if constexpr (HN) {
               mask_step(cn, kt + 1);
-              clean_v(kt + 1, pages[1], v[P ^ 1]);
+              clean_v(kt + 1, pages[1], v);
             }
             {
 #pragma unroll
@@ -465,7 +462,7 @@ __device__ __forceinline__ void cache4_chunk_run(const CacheChunkArgs& a, unsign
                 if constexpr (HN) __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);
               }
             }
-            if constexpr (HN) advance();
+            if constexpr (HN) request(kt);
             __syncthreads();
           };
           int kt = 0;
@@ -484,7 +481,6 @@ __device__ __forceinline__ void cache4_chunk_run(const CacheChunkArgs& a, unsign
           auto body = [&](int kt, auto parity) {
             constexpr int P = decltype(parity)::value;
             const bool more = kt + 1 < ntiles;
-            if (more) request(kt, parity);
             const uint32_t gone = gone_of(P);
 #pragma unroll
             for (int sub = 0; sub < 2; ++sub) {
@@ -530,9 +526,9 @@ __device__ __forceinline__ void cache4_chunk_run(const CacheChunkArgs& a, unsign
               }
             }
             if (more) {
-              clean_v(kt + 1, pages[1], v[P ^ 1]);
+              clean_v(kt + 1, pages[1], v);
               lay_out(parity);
-              advance();
+              request(kt);
             }
             __syncthreads();
           };
