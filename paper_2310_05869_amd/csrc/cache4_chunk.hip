@@ -782,7 +782,7 @@ void cache4_chunk_split(CacheChunkArgs* a, CacheAttnArgs* narrow) {
   a->tile_tokens = kChunkRows / a->sub_group;
   a->div_tokens = make_fast_div(a->tile_tokens);
   a->div_heads = make_fast_div(a->sub_group);
-  a->narrow = a->group <= kNarrowRows && a->n_seq >= 4 ? kNarrowRows : 0;
+  a->narrow = a->group <= kNarrowRows && (a->n_seq >= 4 || (int64_t)a->rows * a->group <= (int64_t)kNarrowRows * a->n_seq) ? kNarrowRows : 0;
   narrow->parts = a->narrow ? (a->c.Hk < kChunkParts ? kChunkParts / a->c.Hk : 1) : 0;
   const int64_t tokens = (int64_t)a->max_blocks << a->c.log_page, heads = (int64_t)a->c.Hk * a->subs;
   const int64_t tiles = ((int64_t)a->rows / a->tile_tokens + a->n_seq) * heads;

@@ -588,7 +588,7 @@ void cache4_weights_split(CacheChunkArgs* a) {
   a->div_group = make_fast_div(a->group);
   const int64_t tokens = (int64_t)a->max_blocks << a->c.log_page, rows = (int64_t)a->rows * a->group, steps = (rows + kWRows - 1) / kWRows;
   const int64_t heads = (int64_t)a->n_seq * a->c.Hk;
-  a->narrow = rows <= 64 || rows <= 32 * (int64_t)a->n_seq ? 0x7fffffff : a->n_seq >= 4 ? 64 : -1;
+  a->narrow = rows <= 128 || rows <= 32 * (int64_t)a->n_seq ? 0x7fffffff : a->n_seq >= 4 ? 64 : -1;
   const int64_t units = (tokens + kNUnit - 1) / kNUnit * heads * ((steps + 3) / 4 * 4);
   a->few_wgs = a->narrow < 0 ? 0 : (int32_t)(units / 4 + 1 > 768 ? 768 : units / 4 + 1);
   const int64_t runs = (tokens + kWTokens - 1) / kWTokens * heads * (steps + kWTileCost) / kWLeastRun;
