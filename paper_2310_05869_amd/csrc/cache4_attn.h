@@ -202,6 +202,8 @@ __device__ __forceinline__ void cache4_attn_run(const CacheAttnArgs& a, CacheAtt
     }
     const int limit = len - n_queries + 1 + q_tok;  // tokens that the lane's row sees
     const int all_see = len - n_queries + 1;        // that every row sees
+    // V's far groups are taken out of the product from here on (fp32 queries among chunks: everywhere; an infinity times the parts of a weight, some of them 0 or negative, is NaN)
+    const int far_from = RAGGED && F32 ? 0 : all_see;
 
     RawTile<D> raw[kTilesPerUnit];
     f32x4 o[MT];
@@ -299,7 +301,7 @@ __device__ __forceinline__ void cache4_attn_run(const CacheAttnArgs& a, CacheAtt
 
       // ---- masks: tokens behind the row's own, behind the sequence, of pages that are not there ----
       const int base = unit * kUnit;
-      bool special = base + kUnit > all_see;
+      bool special = base + kUnit > far_from;
 #pragma unroll
       for (int t = 0; t < kTilesPerUnit; ++t) special = special || !there[t];
       if (special) {
@@ -318,7 +320,7 @@ __device__ __forceinline__ void cache4_attn_run(const CacheAttnArgs& a, CacheAtt
             if constexpr (MULTI) {  // groups that are NaN or may lie past the largest number, of tokens that some rows see alone, are taken out here
               uint32_t& w = raw[t].vs[D == 128 ? i % (D / 32) : i / 2];
               const uint32_t bytes = D == 128 ? 0x01010101u : i & 1 ? 0x01010000u : 0x00000101u;
-              const uint32_t far = (((w & 0x7f7f7f7fu) + kFarSteps * 0x01010101u) & w) >> 7 & (tok >= all_see ? bytes : 0u);  // 1 in every byte from kFarScale on
+              const uint32_t far = (((w & 0x7f7f7f7fu) + kFarSteps * 0x01010101u) & w) >> 7 & (tok >= far_from ? bytes : 0u);  // 1 in every byte from kFarScale on
               w &= ~((far << 8) - far);
               taken |= far;
             }
@@ -423,7 +425,7 @@ __device__ __forceinline__ void cache4_attn_run(const CacheAttnArgs& a, CacheAtt
       const int quad = (thread & 63) >> 4, own_row = tile * kCRows + (thread & 15), own = own_row < n_rows ? own_row : 0, own_tok = own / a.group;
       const int64_t q_at = (row_first + own_tok) * a.q.row + (int64_t)(hk * a.group + own % a.group) * a.q.head + 8 * quad;
       for (int u = first + wave; u < last; u += kCWaves)
-        for (int tok = max(u * kUnit, max(all_see, 0)); tok < min(u * kUnit + kUnit, len); ++tok) {
+        for (int tok = max(u * kUnit, max(far_from, 0)); tok < min(u * kUnit + kUnit, len); ++tok) {
           const int page = blocks[tok >> log_page], at = tok & in_page;
           if ((unsigned)page >= (unsigned)a.c.n_pages) continue;
           const unsigned char* b = head_base + (int64_t)page * page_bytes;

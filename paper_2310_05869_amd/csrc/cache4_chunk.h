@@ -58,20 +58,25 @@ __device__ inline int run_of(int64_t total, int parts, int64_t x) {
 }
 
 // All sequences' work as one line: sequence s takes cost(s) >= 0 of it.  A lane sums a run of sequences; the sum is the same for all lanes, *before: what
-// precedes the lane's run.
+// precedes the lane's run.  Row starts that decrease can give the same rows to many sequences: with more rows in all than there are, there is no work.
 template <class Cost>
-__device__ inline int64_t chunk_line(int n_seq, int lane, int64_t* before, Cost&& cost) {
-  const int each = (n_seq + 63) / 64, s0 = min(n_seq, lane * each), s1 = min(n_seq, s0 + each);
+__device__ inline int64_t chunk_line(const CacheChunkArgs& a, int lane, int64_t* before, Cost&& cost) {
+  const int each = (a.n_seq + 63) / 64, s0 = min(a.n_seq, lane * each), s1 = min(a.n_seq, s0 + each);
   int64_t sum = 0;
-  for (int s = s0; s < s1; ++s) sum += cost(s);
+  float rows = 0.f;  // (exact up to 2^24, rows are at most 2^22)
+  for (int s = s0; s < s1; ++s) {
+    sum += cost(s);
+    rows += (float)chunk_seq(a, s).n;
+  }
   int64_t inc = sum;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
     const int64_t up = __shfl_up((long long)inc, o);
     if (lane >= o) inc += up;
+    rows += __shfl_xor(rows, o);
   }
   *before = inc - sum;
-  return uniform64(__shfl((long long)inc, 63));
+  return __any(rows > (float)a.rows) ? 0 : uniform64(__shfl((long long)inc, 63));
 }
 
 // The sequence at place u of the line (0 <= u < its length), and where it begins

@@ -84,7 +84,7 @@ __device__ __forceinline__ void cache4_chunk_run(const CacheChunkArgs& a, unsign
     return heads * (WHOLE ? (int64_t)T : upto(q, T));
   };
   int64_t before;
-  const int64_t total = chunk_line(a.n_seq, threadIdx.x & 63, &before, cost);
+  const int64_t total = chunk_line(a, threadIdx.x & 63, &before, cost);
   int parts = 1, part = 0;
   int64_t u0 = x, u1 = 0;
   if constexpr (WHOLE) {

@@ -167,19 +167,19 @@ def test_pages_that_are_not_there(ha, torch, tokens):
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
+@pytest.mark.parametrize("few", [False, True])   # rows of a sequence: the form for few takes them where there can be several sequences
 @pytest.mark.parametrize("tokens", [0, WIDE])
 @pytest.mark.parametrize("byte", [252, 253, 254, 255])
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("d", [64, 128])
-def test_scales_of_other_writers_count_for_the_queries_that_see_them(ha, torch, d, dtype, byte, tokens):
+def test_scales_of_other_writers_count_for_the_queries_that_see_them(ha, torch, d, dtype, byte, tokens, few):
     """V of a token in the middle of the new ones with channels 32 ... 63 at a scale of 2^125 ... 2^127 or NaN: for the rows from its own on, and no other.  (Its K is
     0, so that its weight is at most 1.)"""
     from test_gpu_cache4 import STEPS
     from test_gpu_cache4_forms import put_v
     Hq, Hk, page = 4, 2, 16
-    both = [(50, 27), (140, 30)]
+    both, at = ([(6, 60), (3, 30), (8, 150), (1, 20)], [62, 20, 155, 20]) if few else ([(50, 27), (140, 30)], [27 + 20, 30 + 90])
     Q, cache, cu, table, L, ks, vs, new, lens = a_case(ha, torch, both, Hq, Hk, d, page, dtype, tokens)
-    at = [27 + 20, 30 + 90]
     for s, pos in enumerate(at):
         slot = ints(torch, [int(table[s, pos // page]) * page + pos % page])
         k, v = ha.ha_cache4_read(cache, slot, page, dtype=torch.float32)
@@ -197,7 +197,7 @@ def test_scales_of_other_writers_count_for_the_queries_that_see_them(ha, torch, 
         put_v(bytes_[int(table[s, pos // page]), 1], page, pos % page, np.where(np.arange(d) // 32 == 1, codes, 2), scales)
         vs[s][pos, 1] = 1.0
         vs[s][pos, 1, 32:64] = np.where(np.isfinite(values[32:64]), values[32:64], 0.0)
-        first = sum(new[:s]) + pos - both[s][1]
+        first = sum(new[:s]) + max(pos - both[s][1], 0)
         sees[first:sum(new[:s + 1]), Hq // Hk:] = True
     cache.copy_(torch.from_numpy(bytes_))
     out, lse = ha.ha_cache4_attn_chunk(Q, cache, cu, table, L, page)
@@ -264,6 +264,52 @@ def test_strides_streams_and_a_workspace_kept(ha, torch):
     assert torch.equal(o2, ref) and torch.equal(l2, rl) and torch.equal(o3, ref) and torch.equal(l3, rl)
 
 
+@pytest.mark.parametrize("tokens", [0, WIDE])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d,Hq,Hk", [(64, 8, 2), (128, 3, 1), (128, 32, 2)])
+def test_few_rows_and_many_side_by_side(ha, torch, d, Hq, Hk, dtype, tokens):
+    """Sixteen rows of a key head and one more, many sequences of either, empty ones between."""
+    G = Hq // Hk
+    few = 16 // G
+    both = [(few, 200), (few + 1, 90), (0, 70), (few, 0), (40, 300), (1, 511), (0, 0), (few + 1, 0), (1, 0), (60, 3)] + [(1, n) for n in range(0, 130, 9)]
+    Q, cache, cu, table, L, ks, vs, new, lens = a_case(ha, torch, both, Hq, Hk, d, 16, dtype, tokens, pad=2)
+    T = sum(new)
+    out, lse = ha.ha_cache4_attn_chunk(Q, cache, cu, table, L, 16)
+    ref, rl, absv, werr = chunks64(host(Q)[:T], ks, vs, new)
+    check_attention(host(out)[:T], host(lse)[:, :T], ref, rl, absv, werr, dtype, max(lens))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_few_rows_behind_long_sequences(ha, torch, d):
+    """Rows whose tokens many workgroups share, in either form: joined by a group of threads, by all of a workgroup, by workgroups of several runs."""
+    for both, Hq, Hk in (([(2, 40000), (1, 3000), (1, 60), (3, 9000)], 4, 1), ([(1, 60000)] * 4, 2, 2), ([(30, 50000)], 4, 1), ([(5, 30000), (90, 20000)], 4, 2)):
+        Q, cache, cu, table, L, ks, vs, new, lens = a_case(ha, torch, both, Hq, Hk, d, 128, "bf16", seed=33)
+        out, lse = ha.ha_cache4_attn_chunk(Q, cache, cu, table, L, 128)
+        ref, rl, absv, werr = chunks64(host(Q), ks, vs, new)
+        check_attention(host(out), host(lse), ref, rl, absv, werr, "bf16", max(lens))
+
+
+def test_two_graphs_share_a_workspace(ha, torch):
+    """Nothing is kept in it: calls of other sizes, captured one by one and replayed in turn."""
+    a, b = (a_case(ha, torch, both, 8, 2, 128, 16, "bf16", seed=s) for both, s in (([(40, 2000), (1, 500), (1, 30), (1, 900)], 1), ([(3, 3000), (100, 1500)], 2)))
+    need = max(ha.ha_cache4_attn_chunk_workspace_bytes(x[1], 16, x[3].shape[0], x[0].shape[0], 8, x[3].shape[1]) for x in (a, b))
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    want = [ha.ha_cache4_attn_chunk(*x[:5], 16) for x in (a, b)]
+    out = [(torch.zeros_like(x[0]), torch.zeros(8, x[0].shape[0], device="cuda")) for x in (a, b)]
+    torch.cuda.synchronize()
+    graphs = []
+    for x, (o, l) in zip((a, b), out):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            ha.ha_cache4_attn_chunk(*x[:5], 16, out=o, lse=l, workspace=ws)
+    for which in (0, 1, 1, 0, 1):
+        for o, l in out:
+            o.zero_(), l.zero_()
+        graphs[which].replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out[which][0], want[which][0]) and torch.equal(out[which][1], want[which][1])
+
+
 def test_senseless_row_starts_stay_inside(ha, torch):
     """cu_seqlens past the rows, negative, decreasing: nothing outside the outputs is touched."""
     Hq, Hk, d, page = 4, 2, 64, 16
@@ -271,7 +317,7 @@ def test_senseless_row_starts_stay_inside(ha, torch):
         Q, cache, cu, table, L, *_ = a_case(ha, torch, [(30, 40), (20, 100), (9, 9)], Hq, Hk, d, page, "bf16", tokens)
         T = Q.shape[0]
         room = torch.full((T + 64, Hq, d), 7.0, dtype=torch.bfloat16, device="cuda")
-        for bad in ([0, 1000, 1000, 2 ** 31 - 1], [-5, 20, 10, 59], [40, 30, 20, 10], [-2 ** 31, -1, -1, 5]):
+        for bad in ([0, 1000, 1000, 2 ** 31 - 1], [-5, 20, 10, 59], [40, 30, 20, 10], [-2 ** 31, -1, -1, 5], [0, 59, 0, 59]):
             ha.ha_cache4_attn_chunk(Q, cache, ints(torch, bad), table, L, page, out=room[32:32 + T])
             assert (room[:32] == 7).all() and (room[32 + T:] == 7).all()
 

@@ -121,6 +121,34 @@ def test_a_decoding_step_by_either_attention(ha, torch):
     check(torch, weights, before, Q, lse, ks, [1] * 5, table, page, False)
 
 
+@pytest.mark.parametrize("fresh", [False, True])
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d,Hq,Hk", [(64, 8, 2), (128, 3, 1), (128, 70, 1)])
+def test_few_rows_and_many_side_by_side(ha, torch, d, Hq, Hk, dtype, fresh):
+    """Up to 64 rows of a key head and more, in one call, and sequences without any."""
+    few = max(1, 64 // (Hq // Hk))
+    both = [(few, 600), (few + 1, 90), (0, 70), (few, 0), (40, 700), (1, 511), (0, 0), (few + 1, 0), (1, 0), (300, 3)] + [(0, n) for n in range(0, 130, 19)]
+    page = 16
+    Q, cache, cu, table, L, ks, vs, new, lens = a_case(ha, torch, both, Hq, Hk, d, page, dtype, pad=2)
+    _, lse = ha.ha_cache4_attn_chunk(Q, cache, cu, table, L, page)
+    before = torch.rand(cache.shape[0], Hk, page, device="cuda")
+    weights = before.clone()
+    ha.ha_cache4_weights(Q, cache, cu, table, L, lse, weights, page, fresh=fresh)
+    check(torch, weights, before, Q, lse, ks, new, table, page, fresh)
+
+
+def test_no_rows_at_all(ha, torch):
+    """Nothing is added; fresh: what the sequences hold is 0, and nothing else."""
+    page = 16
+    Q, cache, cu, table, L, ks, vs, new, lens = a_case(ha, torch, [(0, 300), (0, 0), (0, 77)], 4, 2, 64, page, "bf16")
+    Q = Q.new_empty(0, 4, 64)   # (numpy's has other strides)
+    before = torch.rand(cache.shape[0], 2, page, device="cuda")
+    for fresh in (False, True):
+        weights = before.clone()
+        ha.ha_cache4_weights(Q, cache, cu, table, L, torch.zeros(4, 0, device="cuda"), weights, page, fresh=fresh)
+        check(torch, weights, before, Q, torch.zeros(4, 0, device="cuda"), ks, new, table, page, fresh)
+
+
 def test_the_last_rows_alone(ha, torch):
     """A prompt's last 20 rows decide: their part of Q and lse, as a call of its own."""
     page, Hq = 16, 4
@@ -182,7 +210,7 @@ def test_strides_streams_senseless_starts_and_a_graph(ha, torch):
     s.synchronize()
     assert torch.equal(a, ref) and torch.equal(b, ref)
     room = torch.zeros(cache.shape[0] + 2, Hk, page, device="cuda")
-    for bad in ([0, 1000, 1000, 2 ** 31 - 1], [-5, 20, 10, 59], [40, 30, 20, 10], [-2 ** 31, -1, -1, 5]):
+    for bad in ([0, 1000, 1000, 2 ** 31 - 1], [-5, 20, 10, 59], [40, 30, 20, 10], [-2 ** 31, -1, -1, 5], [0, 182, 0, 182]):
         ha.ha_cache4_weights(Q, cache, ints(torch, bad), table, L, lse, room[1:-1], page)
         assert (room[0] == 0).all() and (room[-1] == 0).all()
     g, w = torch.cuda.CUDAGraph(), torch.zeros_like(ref)
