@@ -455,7 +455,7 @@ template <int D>
 static int launch_evict_d(const CacheEvictArgs& a, hipStream_t st) {
   const int64_t tokens = (int64_t)a.max_blocks << a.c.log_page;
   const int heads = a.n_seq * a.c.Hk;
-  if (tokens <= 2048 || heads >= kManyHeads) return tokens <= kSmall * 32 ? launch_select<D, kSmall, true>(a, st) : launch_select<D, 1024, true>(a, st);
+  if (tokens <= 2048 || heads >= kManyHeads || heads == 0) return tokens <= kSmall * 32 ? launch_select<D, kSmall, true>(a, st) : launch_select<D, 1024, true>(a, st);
   int rc = tokens <= kSmall * 32 ? launch_select<D, kSmall, false>(a, st) : launch_select<D, 1024, false>(a, st);
   if (rc != HA_OK) return rc;
   constexpr int64_t per = kAhead * kMoveThreads / (D / 8), per_last = kAhead * kLastThreads / (D / 8);

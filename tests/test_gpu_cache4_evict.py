@@ -175,6 +175,12 @@ def test_no_pages_no_table_no_sequences(ha, torch):
     assert out.shape == (0,) and left.tolist() == [1] and F.tolist() == [2, 0, 0]
 
 
+def test_no_sequences_of_a_long_table(ha, torch):
+    cache, W, F, none = ha.alloc_cache4(3, 16, 2, 64), ha.alloc_cache4_weights(3, 16, 2), ints(torch, [2, 0, 0]), ints(torch, [])
+    out, left = ha.ha_cache4_evict(cache, W, torch.zeros(0, 5000, dtype=torch.int32, device="cuda"), none, none, F, ints(torch, [1]), 16, recent=3)
+    assert out.shape == (0,) and left.tolist() == [1] and F.tolist() == [2, 0, 0]
+
+
 def test_streams_a_workspace_kept_and_a_graph(ha, torch):
     rng = np.random.default_rng(6)
     lens, Hk, d, page = [900, 300, 77], 2, 128, 16
