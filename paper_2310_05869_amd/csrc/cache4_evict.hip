@@ -208,7 +208,10 @@ __device__ inline int select_moves(const CacheEvictArgs& a, const EvictSeq& q, i
       all_keys([&](int, const u32x4& key, int) {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (key[e] != 0 && key[e] >> shift == prefix) lds.left[atomicAdd(&lds.n_left, 1u)] = key[e];
+          if (key[e] != 0 && key[e] >> shift == prefix) {
+            const uint32_t at = atomicAdd(&lds.n_left, 1u);
+            if (at < kRanked) lds.left[at] = key[e];
+          }
       });
       __syncthreads();
       if ((int)threadIdx.x < m) {
@@ -256,7 +259,9 @@ __device__ inline int select_moves(const CacheEvictArgs& a, const EvictSeq& q, i
     gt_before += lds.gt[w];
     eq_before += lds.eq[w];
   }
+  // (Weights that change from pass to pass, of pages that sequences share against the rule, may give any order, but no place outside the list.)
   int2* moves = a.moves + ((int64_t)s * a.c.Hk + kv) * a.moves_most;
+  const uint32_t most = (uint32_t)a.moves_most;
   uint32_t gaps = 0;
   all_keys([&](int i, const u32x4& key, int page) {
     uint32_t here = 0;  // kept for certain in the upper half, equal in the lower
@@ -274,9 +279,10 @@ __device__ inline int select_moves(const CacheEvictArgs& a, const EvictSeq& q, i
       const bool more = key[e] > prefix, same = key[e] == prefix, kept = more || (same && t < want);
       const uint32_t rank = g + min(t, want);  // kept before
       // (how many stay is not known yet, so rows that move are counted from the last one)
-      if (kept && p + e >= stay) moves[stay - 1 - rank].x = slot + e;
-      const bool gap = !kept && p + e < stay;
-      if (gap) moves[p + e - rank].y = slot + e;
+      const uint32_t last = stay - 1 - rank, free = p + e - rank;
+      if (kept && p + e >= stay && last < most) moves[last].x = slot + e;
+      const bool gap = !kept && p + e < stay && free < most;
+      if (gap) moves[free].y = slot + e;
       gaps += gap;
       g += more;
       t += same;
@@ -285,7 +291,7 @@ __device__ inline int select_moves(const CacheEvictArgs& a, const EvictSeq& q, i
   gaps = wave_scan(gaps);
   if (lane == 63) atomicAdd(&lds.gaps, gaps);
   __syncthreads();
-  return (int)lds.gaps;
+  return (int)min(lds.gaps, most);
 }
 
 // A row's share of a lane: lane j of D / 8 has word j of K and of V; the first three also K's scales, V's and the weight
@@ -325,6 +331,7 @@ __device__ inline void move_rows(const CacheEvictArgs& a, int head, int count, i
   constexpr int LPR = D / 8, ROWS = NT / LPR, AHEAD = kAhead;
   const int kv = head % a.c.Hk, j = threadIdx.x % LPR;
   const int2* moves = a.moves + (int64_t)head * a.moves_most;
+  const uint32_t slots = (uint32_t)a.c.n_pages << a.c.log_page;  // (an entry that no pass wrote, see above, may be anything)
   for (int i0 = part * ROWS * AHEAD + threadIdx.x / LPR; i0 < count; i0 += parts * ROWS * AHEAD) {
     int2 m[AHEAD];
     RowPiece<D> x[AHEAD];
@@ -335,10 +342,10 @@ __device__ inline void move_rows(const CacheEvictArgs& a, int head, int count, i
     }
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u)
-      if (m[u].x >= 0) x[u] = load_piece<D>(a, kv, m[u].x, j);
+      if ((uint32_t)m[u].x < slots) x[u] = load_piece<D>(a, kv, m[u].x, j);
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u)
-      if (m[u].x >= 0 && m[u].y >= 0) store_piece<D>(a, kv, m[u].y, j, x[u]);
+      if ((uint32_t)m[u].x < slots && (uint32_t)m[u].y < slots) store_piece<D>(a, kv, m[u].y, j, x[u]);
   }
 }
 

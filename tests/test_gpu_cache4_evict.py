@@ -181,6 +181,23 @@ def test_no_sequences_of_a_long_table(ha, torch):
     assert out.shape == (0,) and left.tolist() == [1] and F.tolist() == [2, 0, 0]
 
 
+@pytest.mark.parametrize("n,blocks,keep", [(256, 300, 100), (256, 1200, 9000), (40, 1200, 9000)])
+def test_pages_that_sequences_share_against_the_rule(ha, torch, n, blocks, keep):
+    """Rows may be any, but nothing beside these pages is written, and the lengths and the stack are those of the rule."""
+    page, N = 16, blocks + 50
+    rng = np.random.default_rng(8)
+    table = torch.from_numpy(np.stack([rng.permutation(blocks) for _ in range(n)]).astype(np.int32)).cuda()
+    cache = torch.from_numpy(rng.integers(0, 256, (N, 1, page * 68), dtype=np.uint8)).cuda()
+    W = torch.rand(N, 1, page, device="cuda")
+    before, was = cache.clone(), W.clone()
+    need = ha.ha_cache4_evict_workspace_bytes(cache, page, n, blocks)
+    ws = torch.full((need + 4096,), 7, dtype=torch.uint8, device="cuda")
+    F = torch.full((N,), -1, dtype=torch.int32, device="cuda")
+    out, left = ha.ha_cache4_evict(cache, W, table, ints(torch, [blocks * page - 3] * n), ints(torch, [keep] * n), F, ints(torch, [0]), page, recent=30, workspace=ws[:need])
+    assert out.tolist() == [keep] * n and left.tolist() == [min(N, n * (blocks - -(-keep // page)))]
+    assert torch.equal(cache[blocks:], before[blocks:]) and torch.equal(W[blocks:], was[blocks:]) and bool((ws[need:] == 7).all())
+
+
 def test_streams_a_workspace_kept_and_a_graph(ha, torch):
     rng = np.random.default_rng(6)
     lens, Hk, d, page = [900, 300, 77], 2, 128, 16
