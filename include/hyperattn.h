@@ -544,7 +544,7 @@ size_t ha_cache4_weights_workspace_bytes(const ha_cache4* shape, const ha_cache4
  *   free_pages    the pages that its tokens no longer need, block_table[s][ceil(k / page) ... ceil(n / page) - 1], are put on top of the stack, sequences in order
  *   free_count_out  as ha_page_plan has them (at most n_pages)
  * block_table is not changed: lens_out tells which entries count.  A page belongs to one sequence and lies once in its row; rows from or to pages that are
- * not there are left out.  lens are taken within [0, max_blocks * page].  lens_out may be neither lens nor keep, free_count_out not free_count.
+ * not there are left out.  lens are taken within [0, max_blocks * page].  lens_out may overlap neither lens nor keep, free_count_out not free_count.
  * n_seq <= 8192, n_seq * Hk <= 2^20, n_seq * max_blocks <= 2^30, max_blocks * page <= 2^30.  weights, weights_out: 16-byte aligned.
  * workspace: device, 256-byte aligned, >= ha_cache4_evict_workspace_bytes(): four bytes for every token and key head that the table has room for; nothing in it is kept. */
 typedef struct {

@@ -147,6 +147,11 @@ def test_eviction(ha):
         p = [OK + 64 * x for x in range(10)]
         p[i] = p[j]
         assert evict(ha, p) == SHAPE, (i, j)
+    for i in (4, 5):                        # overlapping by one of their two numbers
+        for by in (-4, 4):
+            p = [OK + 64 * i for i in range(10)]
+            p[8] = p[i] + by
+            assert evict(ha, p) == SHAPE, (i, by)
     assert evict(ha, ws=None) == NULL and evict(ha, nbytes=need - 1) == WORKSPACE and evict(ha, ws=OK + 128, nbytes=need) == WORKSPACE
 
 
