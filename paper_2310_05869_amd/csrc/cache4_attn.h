@@ -117,7 +117,7 @@ struct Weights {
 // SPLIT: parts of a query number and of a weight: 1 for bf16 queries, 3 for fp32 ones (24 bits); cached values have one.
 // NW waves.  WHOLE: a workgroup per sequence, which it finishes (small tables: no second launch).  ONCE: codes are read past the caches.
 // MULTI: several queries a sequence, which see its last tokens in part.
-// bf16, four waves, d = 128, tokens shared out: held to the 168 registers of three workgroups a CU, which costs 2 spilled ones, MULTI 4 (12 and 20 bytes of scratch).
+// bf16, four waves, d = 128, tokens shared out: held to the 168 registers of three workgroups a CU, which costs MULTI a spilled one (8 bytes of scratch).
 // x, y: the workgroup's number among those that share the tokens (WHOLE: the sequence), and its key head and tile of rows.
 template <int D, int NW>
 struct CacheAttnLds {
