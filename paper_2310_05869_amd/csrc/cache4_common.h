@@ -111,8 +111,8 @@ struct CacheEvictArgs {
   int32_t* free_count_out;
   CacheGeometry c;
   int32_t n_seq, max_blocks, recent;
-  // workspace: per sequence and key head, how many rows change places, and from which slot to which
-  int32_t* counts;
+  // workspace: per sequence and key head, how many rows change places (and how many of them lie where the last ones go), and from which slot to which
+  int2* counts;
   int2* moves;
   int64_t moves_most;   // of a sequence and key head
 };

@@ -9,9 +9,9 @@
 //            tokens kept before place p, a free place p is the (p - c(p))-th, a kept token the (c(p) - c(k - r))-th that moves.  A wave has a run of places of its own,
 //            so that only 16 numbers cross the waves.
 //   move     rows of these lists, D / 8 lanes a row
-//   last     the last r rows, whose places may overlap: read, a barrier, written, some hundred at a time; beside them lengths and free pages
-// One launch, in which the workgroup that chose moves the rows too, where the sequences and key heads fill the chip or are short; three launches else, so that the rows of few heads
-// are moved by all of it.
+//   last     the last r rows, whose places may overlap: read, a barrier, written, some hundred at a time
+// One launch, in which the workgroup that chose moves the rows too, where the sequences and key heads fill the chip or are short.  Else a second launch, so that the rows of few heads
+// are moved by all of it: few last rows by the first workgroup of their head, after the rows that lie in their places; many in a third.  Lengths and free pages: a workgroup beside those that choose.
 #include <type_traits>
 
 #include "cache4_common.h"
@@ -24,6 +24,7 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 constexpr int kBins = 2048;
 constexpr int kMoveThreads = 256, kLastThreads = 1024;
 constexpr int kManyHeads = 256;  // sequences and key heads that fill the chip: a workgroup moves its own rows (64 of them, 3800 rows each: 70 us apart, 101 in one)
+constexpr int kFewLast = 512;  // last rows that move in the launch of the others (8 sequences that keep 4096 of 32768, 256 last ones: 63.6 us with one of their own, 59.4 in it)
 constexpr int kAhead = 8;  // rows that a lane has in flight
 constexpr int kSmall = 512;  // threads of a workgroup that chooses from up to 32 times as many places
 
@@ -85,13 +86,13 @@ struct SelectLds {
   uint32_t n_left;
   uint32_t scratch[NT / 64];
   uint32_t gt[NT / 64], eq[NT / 64];  // kept for certain, and equal to the limit, of every wave's places
-  uint32_t gaps;
+  uint32_t gaps, near;
   uint32_t bin, want, here;
 };
 
-// Writes the list of rows that change places and returns how many they are.  HELD: the weights are few enough to stay in registers, so many pieces of four a thread (0: they are not)
+// Writes the list of rows that change places and returns how many they are, and how many of them (the first) lie where the last rows go.  HELD: the weights are few enough to stay in registers, so many pieces of four a thread (0: they are not)
 template <int NT, int HELD>
-__device__ __forceinline__ int select_moves(const CacheEvictArgs& a, const EvictSeq& q, int s, int kv, SelectLds<NT>& lds) {
+__device__ __forceinline__ int2 select_moves(const CacheEvictArgs& a, const EvictSeq& q, int s, int kv, SelectLds<NT>& lds) {
   constexpr int NW = NT / 64, PIECES = HELD > 0 ? HELD : 8;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int from = q.n - q.r, stay = q.k - q.r;  // places that are chosen from, and how many of them
@@ -152,7 +153,7 @@ __device__ __forceinline__ int select_moves(const CacheEvictArgs& a, const Evict
   uint32_t prefix = 0, want = stay;
   for (int i = threadIdx.x; i < kCopies * kBins; i += NT) lds.hist[0][i] = 0;
   if (threadIdx.x < kRanked) lds.left[threadIdx.x] = 0;
-  if (threadIdx.x == 0) lds.n_left = lds.gaps = 0;
+  if (threadIdx.x == 0) lds.n_left = lds.gaps = lds.near = 0;
   __syncthreads();
 #pragma unroll
   for (int pass = 0; pass < 3; ++pass) {
@@ -275,13 +276,14 @@ __device__ __forceinline__ int select_moves(const CacheEvictArgs& a, const Evict
   // (Weights that change from pass to pass, of pages that sequences share against the rule, may give any order, but no place outside the list.)
   int32_t* moves = reinterpret_cast<int32_t*>(a.moves + ((int64_t)s * a.c.Hk + kv) * a.moves_most);
   const uint32_t most = (uint32_t)a.moves_most;
-  int gaps = 0;
+  int gaps = 0, near = 0;
   // (how many stay is not known yet, so rows that move are counted from the last one)
   auto list = [&](bool kept, uint32_t rank, int p, int slot) {
     const bool behind = p >= stay;
     const uint32_t at = behind ? stay - 1 - rank : p - rank;
     if (kept == behind && at < most) moves[2 * (int64_t)at + !behind] = slot;
     gaps += __popcll(__ballot(!kept && !behind));
+    near += __popcll(__ballot(kept && behind && p < q.k));
   };
   auto slot_at = [&](int page, int p) { return (unsigned)page < (unsigned)a.c.n_pages ? (page << a.c.log_page) + (p & (a.c.page - 1)) : -4; };
   if (ties) {
@@ -320,9 +322,13 @@ __device__ __forceinline__ int select_moves(const CacheEvictArgs& a, const Evict
       }
     });
   }
-  if (lane == 0) atomicAdd(&lds.gaps, (uint32_t)gaps);
+  if (lane == 0) {
+    atomicAdd(&lds.gaps, (uint32_t)gaps);
+    atomicAdd(&lds.near, (uint32_t)near);
+  }
   __syncthreads();
-  return (int)min(lds.gaps, most);
+  const uint32_t all = min(lds.gaps, most);
+  return int2{(int)all, (int)min(lds.near, all)};
 }
 
 // A row's share of a lane: lane j of D / 8 has word j of K and of V; the first three also K's scales, V's and the weight
@@ -356,20 +362,20 @@ __device__ inline void store_piece(const CacheEvictArgs& a, int kv, int slot, in
   else if (j == 2) a.weights_out[head * a.c.page + t] = __uint_as_float(x.more);
 }
 
-// Rows of the list, by workgroup `part` of `parts`: places that come free from the first on, rows that move from the last
+// Rows begin ... end - 1 of the list's `count`, by workgroup `part` of `parts`: places that come free from the first on, rows that move from the last
 template <int D, int NT>
-__device__ inline void move_rows(const CacheEvictArgs& a, int head, int count, int part, int parts) {
+__device__ inline void move_rows(const CacheEvictArgs& a, int head, int count, int begin, int end, int part, int parts) {
   constexpr int LPR = D / 8, ROWS = NT / LPR, AHEAD = kAhead;
   const int kv = head % a.c.Hk, j = threadIdx.x % LPR;
   const int2* moves = a.moves + (int64_t)head * a.moves_most;
   const uint32_t slots = (uint32_t)a.c.n_pages << a.c.log_page;  // (an entry that no pass wrote, see above, may be anything)
-  for (int i0 = part * ROWS * AHEAD + threadIdx.x / LPR; i0 < count; i0 += parts * ROWS * AHEAD) {
+  for (int i0 = begin + part * ROWS * AHEAD + threadIdx.x / LPR; i0 < end; i0 += parts * ROWS * AHEAD) {
     int2 m[AHEAD];
     RowPiece<D> x[AHEAD];
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
       const int i = i0 + u * ROWS;
-      m[u] = i < count ? int2{moves[count - 1 - i].x, moves[i].y} : int2{-1, -1};
+      m[u] = i < end ? int2{moves[count - 1 - i].x, moves[i].y} : int2{-1, -1};
     }
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u)
@@ -453,7 +459,7 @@ __global__ __launch_bounds__(NT) void cache4_select_kernel(CacheEvictArgs a) {
   }
   const int head = blockIdx.x - 1, s = head / a.c.Hk, kv = head - s * a.c.Hk;
   const EvictSeq q = evict_seq(a, s);
-  int count = 0;
+  int2 count = {0, 0};
   if (q.k < q.n && q.r < q.k) {  // (two pieces instead of eight: 3 sequences of up to 500 8.6 us, not 9.2; 64 that keep 4096 of 4160 23.1, not 23.8)
     const int from = q.n - q.r;
     count = from <= NT * 8 ? select_moves<NT, 2>(a, q, s, kv, lds) : from <= NT * 32 ? select_moves<NT, 8>(a, q, s, kv, lds) : select_moves<NT, 0>(a, q, s, kv, lds);
@@ -461,7 +467,7 @@ __global__ __launch_bounds__(NT) void cache4_select_kernel(CacheEvictArgs a) {
   if constexpr (ALL) {
     if (q.k == q.n) return;
     __syncthreads();  // (the list is written, by all waves)
-    move_rows<D, NT>(a, head, count, 0, 1);
+    move_rows<D, NT>(a, head, count.x, 0, count.x, 0, 1);
     __syncthreads();  // (rows have been read that the last ones are written over)
     move_last<D, NT>(a, q, s, kv, 0, 1);
   } else {
@@ -469,9 +475,25 @@ __global__ __launch_bounds__(NT) void cache4_select_kernel(CacheEvictArgs a) {
   }
 }
 
-template <int D>
+// LAST: the first workgroup of a sequence and key head takes its last rows, after those that lie in their places
+template <int D, bool LAST>
 __global__ __launch_bounds__(kMoveThreads) void cache4_move_kernel(CacheEvictArgs a) {
-  move_rows<D, kMoveThreads>(a, blockIdx.x, a.counts[blockIdx.x], blockIdx.y, gridDim.y);
+  const int head = blockIdx.x;
+  const int2 count = a.counts[head];
+  if constexpr (LAST) {
+    if (blockIdx.y > 0) {
+      move_rows<D, kMoveThreads>(a, head, count.x, count.y, count.x, blockIdx.y - 1, gridDim.y - 1);
+      return;
+    }
+    const int s = head / a.c.Hk, kv = head - s * a.c.Hk;
+    const EvictSeq q = evict_seq(a, s);
+    if (q.k == q.n) return;
+    move_rows<D, kMoveThreads>(a, head, count.x, 0, count.y, 0, 1);
+    __syncthreads();  // (these have been read)
+    move_last<D, kMoveThreads>(a, q, s, kv, 0, 1);
+  } else {
+    move_rows<D, kMoveThreads>(a, head, count.x, 0, count.x, blockIdx.y, gridDim.y);
+  }
 }
 
 template <int D>
@@ -501,7 +523,12 @@ static int launch_evict_d(const CacheEvictArgs& a, hipStream_t st) {
   if (rc != HA_OK) return rc;
   constexpr int64_t per = kAhead * kMoveThreads / (D / 8), per_last = kAhead * kLastThreads / (D / 8);
   const int64_t most = (a.moves_most + per - 1) / per, fill = 2048 / heads + 1;
-  hipLaunchKernelGGL(cache4_move_kernel<D>, dim3(heads, (unsigned)(most < fill ? most : fill)), dim3(kMoveThreads), 0, st, a);
+  const unsigned parts = (unsigned)(most < fill ? most : fill);
+  if (a.recent > 0 && a.recent <= kFewLast) {
+    hipLaunchKernelGGL((cache4_move_kernel<D, true>), dim3(heads, 1 + parts), dim3(kMoveThreads), 0, st, a);
+    return check_launch();
+  }
+  hipLaunchKernelGGL((cache4_move_kernel<D, false>), dim3(heads, parts), dim3(kMoveThreads), 0, st, a);
   rc = check_launch();
   if (rc != HA_OK || a.recent == 0) return rc;
   const int64_t most_last = ((int64_t)a.recent + per_last - 1) / per_last, fill_last = 512 / heads + 1;

@@ -295,7 +295,7 @@ static int evict_geometry(const ha_cache4* shape, const ha_cache4_eviction* e, C
 static size_t evict_space(const CacheEvictArgs& a, size_t* moves) {
   auto align = [](size_t x) { return (x + 255) & ~(size_t)255; };
   const size_t heads = (size_t)a.n_seq * a.c.Hk;
-  *moves = align(heads * 4);
+  *moves = align(heads * 8);
   return heads == 0 ? 0 : *moves + align(heads * (size_t)a.moves_most * 8);
 }
 
@@ -331,7 +331,7 @@ int ha_cache4_evict(void* cache, const float* weights, float* weights_out, const
   a.free_count = free_count;
   a.lens_out = lens_out;
   a.free_count_out = free_count_out;
-  a.counts = reinterpret_cast<int32_t*>(workspace);
+  a.counts = reinterpret_cast<int2*>(workspace);
   a.moves = reinterpret_cast<int2*>(reinterpret_cast<unsigned char*>(workspace) + moves);
   return launch_cache4_evict(a, (hipStream_t)stream);
 }

@@ -138,7 +138,8 @@ def test_eviction(ha, torch, case, law):
     run(ha, torch, np.random.default_rng(case), lens, keep, recent, Hk, d, page, law, apart=case % 2 == 1)
 
 
-@pytest.mark.parametrize("lens,keep,recent", [([9000, 40000], [4000, 4000], 256), ([33500, 12], [33400, 3], 3000), ([20000], [19999], 15000), ([60000], [10], 0)])
+@pytest.mark.parametrize("lens,keep,recent", [([9000, 40000], [4000, 4000], 256), ([33500, 12], [33400, 3], 3000), ([20000], [19999], 15000), ([60000], [10], 0),
+                                              ([5000, 3000, 2100], [4990, 2999, 500], 300), ([5000, 4000], [513, 3600], 512)])
 def test_long_sequences(ha, torch, lens, keep, recent):
     """More weights than a workgroup's registers hold, and more last rows than it moves at a time."""
     for law in ("heavy", "few values"):
