@@ -38,6 +38,11 @@ __device__ inline int64_t uniform64(int64_t x) {
   return (int64_t)((uint64_t)hi << 32 | lo);
 }
 
+// Attention: the line before tile t of a key head whose sequence held `held` tokens before its new ones, `tile_tokens` of these a tile and `tile_cost` for its start and end.
+__host__ __device__ constexpr int64_t chunk_upto(int held, int tile_tokens, int64_t t, int tile_cost) {
+  return t * ((int64_t)(held > 0 ? held : 0) + tile_cost) + tile_tokens * (t * (t + 1) / 2);
+}
+
 // Where run p of `parts` begins on a line.  (Rounded down from a product in double, by every workgroup alike; a division of 64 bits takes a microsecond.)
 __device__ inline int64_t run_begin(int64_t total, int parts, int p) { return p >= parts ? total : (int64_t)((double)total * ((double)p / (double)parts)); }
 

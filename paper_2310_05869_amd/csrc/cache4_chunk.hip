@@ -27,6 +27,7 @@ constexpr int kStep = 64;           // tokens of a step
 // What a tile's start and end cost a workgroup, in tokens.  (128 / 256 / 400 / 600: 64 sequences, most of one token, behind up to 16384, 32 and 8 heads, d = 128 259 / 231 / 217 / 220 us;
 // 24 of up to 200 behind up to 4096, 12 and 4 heads 58 / 55 / 55 / 57; 16 of up to 1024 behind up to 8192, 16 heads, d = 64 118 / 106 / 108 / 109.)
 constexpr int kTileCost = 320;
+static_assert(chunk_upto(0x7fffffff - 257, 1, 1, kTileCost) == 0x7fffffffll - 257 + kTileCost + 1);  // (the most tokens that a call may hold: past 32 bits)
 constexpr int kLeastRun = 256;      // tokens of the line that a workgroup takes, at least (fp32, 6 sequences of up to 150 behind up to 2000, d = 64: 512 36 us, 256 29)
 constexpr int kChunkParts = 512;    // workgroups that the chip holds at once, two per CU
 
@@ -77,7 +78,7 @@ __device__ __forceinline__ void cache4_chunk_run(const CacheChunkArgs& a, unsign
   // ---- place ----
   const int tt = a.tile_tokens, heads = a.c.Hk * a.subs;
   auto tiles_of = [&](const ChunkSeq& q) { return (int64_t)q.n * a.group <= a.narrow ? 0 : a.div_tokens.div(q.n + tt - 1); };
-  auto upto = [&](const ChunkSeq& q, int64_t t) { return t * (max(q.held, 0) + kTileCost) + tt * (t * (t + 1) / 2); };  // line before tile t of a head
+  auto upto = [&](const ChunkSeq& q, int64_t t) { return chunk_upto(q.held, tt, t, kTileCost); };  // line before tile t of a head
   auto cost = [&](int s) -> int64_t {
     const ChunkSeq q = chunk_seq(a, s);
     const int T = tiles_of(q);

@@ -120,3 +120,35 @@ def test_evictions_of_many_sequences(ha, torch):
     lens = rng.integers(0, 40, 8192)
     keep = np.where(rng.random(8192) < 0.5, rng.integers(-1, 40, 8192), 20)
     evicted.run(ha, torch, rng, [int(x) for x in lens], [int(x) for x in keep], 5, 2, 64, 16, "few values")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("page", [16, 32])
+@pytest.mark.parametrize("new", [2, 20, 32])   # 12 rows of the key head (the form for few rows), 120 (weights: the form for few rows), 192
+def test_the_longest_sequence(ha, torch, page, new, dtype):
+    """A table of the most tokens that a call may hold, nearly all of them in pages that are not there, and a length past it: held tokens and what a tile's start counts
+    for on the line of work are more than 2^31 together."""
+    Hq, Hk, d = 6, 1, 64
+    blocks = (2 ** 31 - 257) // page
+    n = blocks * page
+    assert n - new + 320 >= 2 ** 31   # (320: what a tile's start counts for)
+    rng = np.random.default_rng(5)
+    held = [0, 1, blocks // 2, blocks - 4, blocks - 3, blocks - 2, blocks - 1]
+    cache = ha.alloc_cache4(len(held), page, Hk, d)
+    dt = dtypes(torch, dtype)
+    K, V = (torch.from_numpy(rng.standard_normal((len(held) * page, Hk, d))).to(dt).cuda() for _ in range(2))
+    ha.ha_cache4_write(K, V, torch.arange(len(held) * page, dtype=torch.int32, device="cuda"), cache, page)
+    table = torch.full((1, blocks), -1, dtype=torch.int32, device="cuda")
+    table[0, torch.tensor(held, device="cuda")] = torch.arange(len(held), dtype=torch.int32, device="cuda")
+    Q = torch.from_numpy(d ** -0.25 * rng.standard_normal((new, Hq, d))).to(dt).cuda()
+    L = ints(torch, [2 ** 31 - 1])
+    cu = starts(torch, [new])
+    out, lse = ha.ha_cache4_attn_chunk(Q, cache, cu, table, L, page)
+    ks, vs = (quantised(host(x))[0] for x in (K, V))
+    # the pages that are there, one behind the other: the new tokens are the last ones of them too
+    ref, rl, absv, werr = chunks64(host(Q), [ks], [vs], [new])
+    check_attention(host(out), host(lse), ref, rl, absv, werr, dtype, len(ks))
+    w = ha.ha_cache4_weights(Q, cache, cu, table, L, lse, torch.full((len(held), Hk, page), 9.0, device="cuda"), page, fresh=True)
+    sums, bounds = weighed.weights64(host(Q), host(lse), [ks], [new])
+    got = host(w).transpose(0, 2, 1).reshape(-1, Hk)
+    assert (np.abs(got - sums[0]) <= bounds[0] + 2.0 ** -24 * sums[0]).all()
