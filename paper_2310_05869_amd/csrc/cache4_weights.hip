@@ -31,7 +31,8 @@ template <int D, int SPLIT>
 struct WeightsLds {
   static constexpr int STR = (D + 8) * 2;  // bytes per row (+16: conflict-free 16-byte row reads)
   static constexpr int PART = kWRows * STR;
-  static constexpr int BUF = SPLIT * PART + kWRows * 4;  // rows in parts, and what their exponents start from
+  static constexpr int LEFT_OUT = SPLIT * PART + kWRows * 4;
+  static constexpr int BUF = LEFT_OUT + 16;  // rows in parts, what their exponents start from, and of either half whether it has rows that give nothing
 };
 
 // A tile's place in the line.  Tile k of a sequence holds tokens 256 k ... + 255; rows are its new tokens' query heads, in steps of 64 from row 0.  The first
@@ -220,9 +221,14 @@ __global__ __launch_bounds__(64 * kWWaves, 2) void cache4_weights_kernel(CacheCh
             *reinterpret_cast<u32x4*>(to) = raw[i][0];
           }
         }
-        // a row that sees nothing has lse -inf, and gives nothing
-        if (threadIdx.x < kWRows)
-          reinterpret_cast<float*>(buf + SPLIT * L::PART)[threadIdx.x] = raw_lse == -INFINITY ? -INFINITY : F32 ? -raw_lse : -raw_lse * kLog2e;
+        // a row that sees nothing has lse -inf, and gives nothing, whatever it holds: a half with such a row takes its weights
+        // one by one (2048 queries behind 16384: 343.6 -> 346.8 us; without, a NaN there went into every token that the row sees)
+        if (threadIdx.x < kWRows) {
+          const bool none = raw_lse == -INFINITY;
+          const unsigned long long out = __ballot(none);
+          reinterpret_cast<float*>(buf + SPLIT * L::PART)[threadIdx.x] = none ? -INFINITY : F32 ? -raw_lse : -raw_lse * kLog2e;
+          if (threadIdx.x < 2) reinterpret_cast<uint32_t*>(buf + L::LEFT_OUT)[threadIdx.x] = (uint32_t)(out >> (32 * threadIdx.x));
+        }
       };
 
       if (first < last) {
@@ -234,14 +240,16 @@ __global__ __launch_bounds__(64 * kWWaves, 2) void cache4_weights_kernel(CacheCh
         __syncthreads();
       }
       const int tok0 = k * kWTokens + wave * 64, tok_end = tok0 + 64;
-      struct Half {  // scores of 32 rows, and what they are exponentiated against
+      struct Half {  // scores of 32 rows, what they are exponentiated against, and which of the rows give nothing
         f32x16 c[2];
         f32x4 shift[4];
+        uint32_t out;
       };
       auto products = [&](int step, int half, Half& x) {
         const unsigned char* buf = smem + (step & 1) * L::BUF;
 #pragma unroll
         for (int g = 0; g < 4; ++g) x.shift[g] = *reinterpret_cast<const f32x4*>(buf + SPLIT * L::PART + (32 * half + 8 * g + 4 * h) * 4);
+        x.out = reinterpret_cast<const uint32_t*>(buf + L::LEFT_OUT)[half];
 #pragma unroll
         for (int i = 0; i < 16; ++i) x.c[0][i] = x.c[1][i] = 0.f;
 #pragma unroll
@@ -278,13 +286,13 @@ __global__ __launch_bounds__(64 * kWWaves, 2) void cache4_weights_kernel(CacheCh
           }
         }
       };
-      auto plain = [&](int row0) {  // whether 32 rows are all there and all see the wave's tokens
-        return row0 + 32 <= rows && w.q.held + a.div_group.div(row0) + 1 >= tok_end;
+      auto plain = [&](const Half& x, int row0) {  // whether 32 rows are all there, all give something and all see the wave's tokens
+        return row0 + 32 <= rows && __builtin_amdgcn_readfirstlane(x.out) == 0 && w.q.held + a.div_group.div(row0) + 1 >= tok_end;
       };
       // Weights of one half beside products of the next: a slice of the vector work behind every two products, rows two products ahead.  (The order is held by hand: left to
       // itself, the compiler puts all products before all exponentials.)
       auto both = [&](const Half& x, int row0, int step, int half, Half& next) {
-        if (!plain(row0)) {
+        if (!plain(x, row0)) {
           products(step, half, next);
           add_some_weights(x, row0);
           return;
@@ -294,6 +302,7 @@ __global__ __launch_bounds__(64 * kWWaves, 2) void cache4_weights_kernel(CacheCh
         auto fragment = [&](int i, int z) {
           return *reinterpret_cast<const bf16x8*>(at + z * L::PART + (32 * ((KS * h + i) % G) + 8 * ((KS * h + i) / G)) * 2);
         };
+        next.out = reinterpret_cast<const uint32_t*>(buf + L::LEFT_OUT)[half];
         bf16x8 qf[2][SPLIT];
         __builtin_amdgcn_s_setprio(1);  // (2048 queries behind 16384: 335.4 -> 331.6 us)
 #pragma unroll
@@ -327,7 +336,7 @@ __global__ __launch_bounds__(64 * kWWaves, 2) void cache4_weights_kernel(CacheCh
         sum[1] += part[2] + part[3];
       };
       auto add = [&](const Half& x, int row0) {
-        if (plain(row0)) add_weights(x);
+        if (plain(x, row0)) add_weights(x);
         else add_some_weights(x, row0);
       };
       if (first < last) {

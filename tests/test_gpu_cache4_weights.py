@@ -227,3 +227,27 @@ def test_strides_streams_senseless_starts_and_a_graph(ha, torch):
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(w, want)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("both", [[(200, 700), (3, 90)], [(300, 2000), (2, 60), (1, 300), (40, 7), (1, 1)], [(9, 300)]])   # many rows, with few beside them, few alone
+def test_rows_left_out_give_nothing_whatever_they_hold(ha, torch, both, d, dtype):
+    """lse -inf and a row of Q of NaN, or of infinities: as if the row were zeros, in every form and wherever it lies."""
+    Hq, Hk, page = 4, 2, 16
+    Q, cache, cu, table, L, ks, vs, new, lens = a_case(ha, torch, both, Hq, Hk, d, page, dtype, WIDE, seed=11)
+    lse = ha.ha_cache4_attn_chunk(Q, cache, cu, table, L, page)[1]
+    T = Q.shape[0]
+    for left_out in ([0], [T - 1], [T // 2, T // 2 + 1], list(range(0, T, 5)), list(range(T // 3, T))):
+        for heads in ([1], [0, 1, 2, 3]):
+            q, le = Q.clone(), lse.clone()
+            for x in heads:
+                le[x, left_out] = -float("inf")
+                q[left_out, x] = 0
+            want = ha.ha_cache4_weights(q, cache, cu, table, L, le, torch.zeros(cache.shape[0], Hk, page, device="cuda"), page, fresh=True)
+            check(torch, want, torch.zeros_like(want), q, le, ks, new, table, page, True)
+            for value in (float("nan"), float("inf"), -float("inf")):
+                for x in heads:
+                    q[left_out, x] = value
+                got = ha.ha_cache4_weights(q, cache, cu, table, L, le, torch.zeros_like(want), page, fresh=True)
+                assert torch.equal(got, want), (left_out[:3], heads, value)
