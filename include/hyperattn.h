@@ -505,7 +505,7 @@ int ha_cache4_attn_form(const ha_cache4* shape, const ha_cache4_query* query, in
  * Everything else as in ha_cache4_attn: products, lens and pages, what counts for nothing, the range of results.
  * rows <= 2^22, rows * Hq <= 2^26, n_seq <= 2^16, n_seq * Hq <= 2^22, Hq % Hk == 0, Hq <= 1024, n_seq * max_blocks <= 2^30, max_blocks * page < 2^31 - 256, n_seq *
  * max_blocks * page <= 2^36.
- * workspace: device, 256-byte aligned, >= ha_cache4_attn_chunk_workspace_bytes() (at most 80 MiB; 0: none is needed, and it may be NULL); nothing in it is kept.  Same inputs, same bits. */
+ * workspace: device, 256-byte aligned, >= ha_cache4_attn_chunk_workspace_bytes() (at most 82 MiB; 0: none is needed, and it may be NULL); nothing in it is kept.  Same inputs, same bits. */
 typedef struct {
   int32_t n_seq, rows, Hq;
   int32_t dtype; /* ha_dtype of Q and out */

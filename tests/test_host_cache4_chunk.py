@@ -183,3 +183,21 @@ def test_binding_of_eviction_refuses_tensors_that_do_not_fit(ha):
             call()
     with pytest.raises(ha.HyperAttnError):
         ha.ha_cache4_evict(pages, w, table, two, two, free, one, 16, recent=-1)
+
+
+def test_the_most_workspace_is_what_the_header_says(ha):
+    """Over head counts, sequences, rows and tables up to the limits; the number is read from the header, which callers reserve by."""
+    import pathlib
+    import re
+    header = (pathlib.Path(__file__).parent.parent / "include" / "hyperattn.h").read_text()
+    for call in ("ha_cache4_attn_chunk", "ha_cache4_weights"):
+        stated, = re.findall(call + r"_workspace_bytes\(\) \(at most (\d+) MiB", header)
+        need = getattr(ha.lib(), call + "_workspace_bytes")
+        most = 0
+        for Hk in (1, 2, 8, 64, 300, 512, 513, 768, 944, 945, 1024):
+            for group in (1, 2, 16, 17, 129, 1024):
+                for n_seq in (1, 4, 64, 4096, 1 << 16):
+                    for rows in (1, 4096, 1 << 16, 1 << 22):
+                        for blocks in (1, 100, 10000):   # (sizes past a limit have no workspace: 0)
+                            most = max([most] + [need(cache(Hk=Hk, d=128, page=page), chunk(n_seq, rows, Hk * group, 0, blocks)) for page in (16, 256)])
+        assert 0 < most <= int(stated) << 20, (call, stated, most)
