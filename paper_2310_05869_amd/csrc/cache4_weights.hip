@@ -594,12 +594,17 @@ __global__ __launch_bounds__(256, SPLIT == 1 ? 3 : 2) void cache4_weights_few_ke
   }
 }
 
-// Few rows a sequence on average, or in all: the second form takes all of them.  Else it takes sequences of up to 64 rows, where there can be several.
+// Which form takes a sequence goes by its own rows of a key head: up to 48 the one for few, where there can be several sequences (64 sequences of 32, 48, 64 and 128 rows, behind up to
+// 8192, 8 key heads, few / many: 65 / 98, 76 / 84, 100 / 89, 180 / 135 us; one sequence or three: the launch for few rows costs 2.4).  The host knows the batch's rows alone; where these are few in all,
+// the form for few takes everything, in one launch instead of three (32 decoding of up to 1000: 9 / 16 us, 64 of up to 16384 77 / 81, 512 of up to 4096 166 / 172), as one sequence may
+// then have no more (63 decoding and one of n x 4 rows, behind up to 8192, 8 key heads: n = 128 51 / 65 us, 200 71 / 71, 400 114 / 82; fp32 118 / 127, 163 / 135; 511 and one of 2048 x 4: 665 / 288).
+// One sequence alone crosses earlier (behind 16384, 8 key heads, 128, 256, 512, 1024 rows: 17 / 20, 27 / 29, 46 / 39, 83 / 64; fp32, d = 64, 256 rows 32 / 24).
+constexpr int kFewRows = 48, kAllFew = 128, kAllFewShared = 1024;
 void cache4_weights_split(CacheChunkArgs* a) {
   a->div_group = make_fast_div(a->group);
   const int64_t tokens = (int64_t)a->max_blocks << a->c.log_page, rows = (int64_t)a->rows * a->group, steps = (rows + kWRows - 1) / kWRows;
   const int64_t heads = (int64_t)a->n_seq * a->c.Hk;
-  a->narrow = rows <= 128 || rows <= 32 * (int64_t)a->n_seq ? 0x7fffffff : a->n_seq >= 4 ? 64 : -1;
+  a->narrow = rows <= kAllFew || (rows <= kAllFewShared && rows <= 32 * (int64_t)a->n_seq) ? 0x7fffffff : a->n_seq >= 4 ? kFewRows : -1;
   const int64_t units = (tokens + kNUnit - 1) / kNUnit * heads * (steps < 1 ? 1 : steps * 4);
   a->few_wgs = a->narrow < 0 ? 0 : (int32_t)(units / 4 + 1 > 768 ? 768 : units / 4 + 1);
   const int64_t runs = (tokens + kWTokens - 1) / kWTokens * heads * (steps + kWTileCost) / kWLeastRun;

@@ -251,3 +251,16 @@ def test_rows_left_out_give_nothing_whatever_they_hold(ha, torch, both, d, dtype
                     q[left_out, x] = value
                 got = ha.ha_cache4_weights(q, cache, cu, table, L, le, torch.zeros_like(want), page, fresh=True)
                 assert torch.equal(got, want), (left_out[:3], heads, value)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_a_prompt_among_many_that_decode(ha, torch, dtype):
+    """Rows that are few of a sequence on average, most of them one sequence's."""
+    Hq, Hk, d, page = 8, 2, 64, 16
+    for both in ([(1, n % 50) for n in range(120)] + [(300, 500)] + [(1, n) for n in range(30)], [(1, 70)] * 60 + [(170, 30)] + [(20, 5)]):
+        Q, cache, cu, table, L, ks, vs, new, lens = a_case(ha, torch, both, Hq, Hk, d, page, dtype, pad=2, seed=12)
+        _, lse = ha.ha_cache4_attn_chunk(Q, cache, cu, table, L, page)
+        before = torch.rand(cache.shape[0], Hk, page, device="cuda")
+        weights = before.clone()
+        ha.ha_cache4_weights(Q, cache, cu, table, L, lse, weights, page)
+        check(torch, weights, before, Q, lse, ks, new, table, page, False)

@@ -201,3 +201,11 @@ def test_the_most_workspace_is_what_the_header_says(ha):
                         for blocks in (1, 100, 10000):   # (sizes past a limit have no workspace: 0)
                             most = max([most] + [need(cache(Hk=Hk, d=128, page=page), chunk(n_seq, rows, Hk * group, 0, blocks)) for page in (16, 256)])
         assert 0 < most <= int(stated) << 20, (call, stated, most)
+
+
+def test_weights_of_a_batch_of_many_rows_go_by_every_sequence(ha):
+    """The host knows the batch's rows alone: on average few of a sequence, in all as many as a prompt's, they may be one's.  (The form for few rows alone needs no workspace.)"""
+    need = ha.lib().ha_cache4_weights_workspace_bytes
+    for n_seq, rows, most in ((512, 511 + 2048, 400), (200, 199 + 600, 1000), (64, 64 * 8, 256)):
+        assert need(cache(Hk=8, d=128, page=64), chunk(n_seq, rows, 64, 0, most)) > 0, (n_seq, rows)
+    assert need(cache(Hk=8, d=128, page=64), chunk(64, 64, 32, 0, 256)) == 0   # a decoding step
