@@ -543,7 +543,10 @@ size_t ha_cache4_weights_workspace_bytes(const ha_cache4* shape, const ha_cache4
  *   lens_out[s]   k, or the length where the sequence stays as it is
  *   free_pages    the pages that its tokens no longer need, block_table[s][ceil(k / page) ... ceil(n / page) - 1], are put on top of the stack, sequences in order
  *   free_count_out  as ha_page_plan has them (at most n_pages)
- * block_table is not changed: lens_out tells which entries count.  A page belongs to one sequence and lies once in its row; rows from or to pages that are
+ * block_table is not changed: lens_out tells which entries count.  Layers whose caches lie by one block table and one stack are cut one after the other, each from the same lens,
+ * keep, recent and free_count, so that every call frees the same pages into the same places of the stack; lens_out and free_count_out, the same for all, count from the last layer
+ * on.  (With the count that a call has written, the next would put these pages there twice; with its lengths, it would keep the first tokens of its layer.)
+ * A page belongs to one sequence and lies once in its row; rows from or to pages that are
  * not there are left out.  lens are taken within [0, max_blocks * page].  lens_out may overlap neither lens nor keep, free_count_out not free_count.
  * n_seq <= 8192, n_seq * Hk <= 2^20, n_seq * max_blocks <= 2^30, max_blocks * page <= 2^30.  weights, weights_out: 16-byte aligned.
  * workspace: device, 256-byte aligned, >= ha_cache4_evict_workspace_bytes(): four bytes for every token and key head that the table has room for; nothing in it is kept. */

@@ -1074,7 +1074,8 @@ def ha_cache4_evict(cache, weights, block_table, lens, keep, free_pages, free_co
     """(lens_out, free_count_out): sequences of more than keep[s] tokens (int32 [n_seq]; < 0: all stay) keep the last `recent` of them and, for every key head, those of
     largest weight (float32 [n_pages, Hk, page], as ha_cache4_weights has them) among the others.  Rows of the cache move to the sequence's first keep[s] places, their
     weights with them (into weights_out; None: weights itself); pages that it no longer needs are put on free_pages (int32 [n_pages], changed in place; free_count
-    int32 [1]).  block_table int32 [n_seq, max_blocks] and lens int32 [n_seq] stay as they are."""
+    int32 [1]).  block_table int32 [n_seq, max_blocks] and lens int32 [n_seq] stay as they are.  Layers that share them are cut each from the same lens and free_count;
+    what comes back, the same from all, takes their places after the last layer."""
     i32, f32 = _torch().int32, _torch().float32
     sizes = _cache4(cache, page)
     if block_table.dim() != 2:

@@ -300,3 +300,34 @@ def test_a_serving_run_within_a_budget(ha, torch, d):
             np.testing.assert_array_equal(host(v[s]), h[:, 1])
     pages = torch.cat([table[s, :-(-len(held[s]) // page)] for s in range(n)] + [free[:count.item()]])
     assert sorted(pages.tolist()) == list(range(N))    # no page lost, none given twice
+
+
+def test_layers_that_share_a_table(ha, torch):
+    """Each cut from the same lengths and the same stack: every layer keeps its own heaviest tokens, and no page lies on the stack twice."""
+    rng = np.random.default_rng(9)
+    lens, keep, recent, Hk, d, page = [500, 90, 33, 0, 257], [200, 90, 7, 3, 31], 16, 2, 64, 16
+    dev = lambda x: torch.from_numpy(np.ascontiguousarray(x)).cuda()  # noqa: E731
+    _, table, free = a_pool(torch, rng, lens, Hk, d, page)
+    n_pages, spare = len(free), int((free >= 0).sum())
+    T, L, K, F, count = dev(table), ints(torch, lens), ints(torch, keep), dev(free), ints(torch, [spare])
+    results = []
+    for layer in range(3):
+        cache = rng.integers(0, 256, (n_pages, Hk, page * (d + d // 16)), dtype=np.uint8)
+        w = some_weights(rng, "heavy", (n_pages, Hk, page))
+        C, W = dev(cache), dev(w)
+        results.append(ha.ha_cache4_evict(C, W, T, L, K, F, count, page, recent=recent))
+        want_c, want_w, want_lens, freed, defined = evict64(cache, w, table, lens, keep, recent, page, d)
+        got, got_w, at = C.cpu().numpy(), W.cpu().numpy(), np.stack([row_bytes(page, d, t) for t in range(page)])
+        for p, h, t in zip(*np.nonzero(defined)):
+            np.testing.assert_array_equal(got[p, h, at[t]], want_c[p, h, at[t]])
+        np.testing.assert_array_equal(got_w[defined], want_w[defined])
+        assert results[-1][0].tolist() == want_lens and L.tolist() == lens and count.tolist() == [spare]
+    after, left = results[-1]
+    held = [int(p) for s, n in enumerate(after.tolist()) for p in table[s, :-(-n // page)]]
+    assert left.tolist() == [spare + len(freed)] and sorted(held + F[:left.item()].tolist()) == list(range(n_pages))
+    # the next step's pages are nobody else's
+    add = ints(torch, [40, 5, 1, 60, 16])
+    lens2, *_ = ha.ha_page_plan(after, add, T, F, left, page, rows=122)
+    t = T.tolist()
+    pages = [p for s, n in enumerate(lens2.tolist()) for p in t[s][:-(-n // page)]]
+    assert len(set(pages)) == len(pages) and set(pages) <= set(range(n_pages))
