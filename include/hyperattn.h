@@ -547,7 +547,8 @@ size_t ha_cache4_weights_workspace_bytes(const ha_cache4* shape, const ha_cache4
  * keep, recent and free_count, so that every call frees the same pages into the same places of the stack; lens_out and free_count_out, the same for all, count from the last layer
  * on.  (With the count that a call has written, the next would put these pages there twice; with its lengths, it would keep the first tokens of its layer.)
  * A page belongs to one sequence and lies once in its row; rows from or to pages that are
- * not there are left out.  lens are taken within [0, max_blocks * page].  lens_out may overlap neither lens nor keep, free_count_out not free_count.
+ * not there are left out.  lens are taken within [0, max_blocks * page].  lens_out and free_count_out overlap neither each other nor lens, keep
+ * and free_count (such calls are refused); nothing else that is written may overlap, but weights_out all of weights.
  * n_seq <= 8192, n_seq * Hk <= 2^20, n_seq * max_blocks <= 2^30, max_blocks * page <= 2^30.  weights, weights_out: 16-byte aligned.
  * workspace: device, 256-byte aligned, >= ha_cache4_evict_workspace_bytes(): four bytes for every token and key head that the table has room for; nothing in it is kept. */
 typedef struct {

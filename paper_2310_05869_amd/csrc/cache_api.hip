@@ -318,8 +318,10 @@ int ha_cache4_evict(void* cache, const float* weights, float* weights_out, const
   if (a.n_seq > 0 && (!lens || !keep || !lens_out || (a.max_blocks > 0 && !block_table))) return HA_ERR_NULL;
   if (any_misaligned16(cache, weights, weights_out)) return HA_ERR_ALIGN;
   if (any_misaligned4(block_table, lens, keep, free_pages) || any_misaligned4(free_count, lens_out, free_count_out)) return HA_ERR_ALIGN;
-  auto apart = [&](const int32_t* x, const int32_t* y) { return (uintptr_t)x >= (uintptr_t)(y + a.n_seq) || (uintptr_t)y >= (uintptr_t)(x + a.n_seq); };
-  if (free_count == free_count_out || !apart(lens, lens_out) || !apart(keep, lens_out)) return HA_ERR_SHAPE;  // (read by workgroups that others write ahead of)
+  auto apart = [](const int32_t* x, int32_t nx, const int32_t* y, int32_t ny) { return (uintptr_t)x >= (uintptr_t)(y + ny) || (uintptr_t)y >= (uintptr_t)(x + nx); };
+  const int32_t n = a.n_seq;  // (one workgroup writes these numbers while others, or other threads of it, read)
+  if (!apart(lens_out, n, lens, n) || !apart(lens_out, n, keep, n) || !apart(lens_out, n, free_count, 1)) return HA_ERR_SHAPE;
+  if (!apart(free_count_out, 1, lens, n) || !apart(free_count_out, 1, keep, n) || !apart(free_count_out, 1, lens_out, n) || free_count == free_count_out) return HA_ERR_SHAPE;
   if (workspace_bytes < total || ((uintptr_t)workspace & 255) != 0) return HA_ERR_WORKSPACE;
   a.cache = reinterpret_cast<unsigned char*>(cache);
   a.weights = weights;

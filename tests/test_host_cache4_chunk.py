@@ -209,3 +209,11 @@ def test_weights_of_a_batch_of_many_rows_go_by_every_sequence(ha):
     for n_seq, rows, most in ((512, 511 + 2048, 400), (200, 199 + 600, 1000), (64, 64 * 8, 256)):
         assert need(cache(Hk=8, d=128, page=64), chunk(n_seq, rows, 64, 0, most)) > 0, (n_seq, rows)
     assert need(cache(Hk=8, d=128, page=64), chunk(64, 64, 32, 0, 256)) == 0   # a decoding step
+
+
+def test_numbers_that_eviction_writes_lie_apart_from_those_it_reads(ha):
+    """Order of the pointers: 4 lens, 5 keep, 7 free_count, 8 lens_out, 9 free_count_out; two sequences."""
+    for i, j, by in ((8, 7, 0), (8, 7, -4), (9, 4, 0), (9, 4, 4), (9, 5, 0), (9, 5, 4), (9, 8, 0), (9, 8, 4)):
+        p = [OK + 64 * x for x in range(10)]
+        p[i] = p[j] + by
+        assert evict(ha, p) == SHAPE, (i, j, by)
