@@ -519,7 +519,9 @@ size_t ha_cache4_attn_chunk_workspace_bytes(const ha_cache4* shape, const ha_cac
 
 /* What attention weight the cache's tokens got from new queries: for token t of sequence s and key head h the sum, over the rows i of the sequence that see it and the query
  * heads x of h, of exp(<Q[i][x], K[t][h]> - lse[x][i]), by what ha_cache4_attn_chunk (or, with one row a sequence, ha_cache4_attn) gave as lse for the same Q, cu_seqlens,
- * block_table and lens.  Rows of part of the new tokens are taken too, as long as they are the last ones.
+ * block_table and lens.  Rows of part of the new tokens are taken too, as long as they are the last ones;
+ * the other new tokens then count as old, and without fresh what a page held before they came (another sequence's weights, perhaps) is added to.  To have part of the new tokens'
+ * rows decide and all new tokens start from 0, bring all rows, those that do not count with lse -inf.
  *   weights: float [n_pages][Hk][page], 16-byte aligned: token t's lies at weights[block_table[s][t / page]][h][t % page], as its rows do in the cache, and goes where
  *   these go.  Tokens that the rows bring (the last cu_seqlens[s + 1] - cu_seqlens[s] of lens[s]) start from 0; for the others the sum is added to what is there,
  *   or, with fresh != 0, also starts from 0.  Nothing else is touched: not what lies behind a sequence, nor pages that no sequence holds.

@@ -1049,7 +1049,7 @@ def ha_cache4_weights_workspace_bytes(cache, page, n_seq, rows, Hq, max_blocks, 
 def ha_cache4_weights(Q, cache, cu_seqlens, block_table, lens, lse, weights, page, fresh=False, workspace=None, stream=None):
     """weights (float32 [n_pages, Hk, page], changed in place): the attention weight that every token of the sequences got from their new queries is added to what
     lies at its place; tokens that the rows bring start from 0, with `fresh` all do.  Q, cu_seqlens, block_table, lens as ha_cache4_attn_chunk took them, lse as it
-    gave it (float32 [Hq, rows])."""
+    gave it (float32 [Hq, rows]); a row whose lse is -inf gives nothing."""
     torch = _torch()
     full, sizes, chunk = _chunk_call(Q, cache, cu_seqlens, block_table, page)
     rows, Hq, _ = full

@@ -264,3 +264,21 @@ def test_a_prompt_among_many_that_decode(ha, torch, dtype):
         weights = before.clone()
         ha.ha_cache4_weights(Q, cache, cu, table, L, lse, weights, page)
         check(torch, weights, before, Q, lse, ks, new, table, page, False)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows", [200, 30])
+def test_the_last_rows_alone_without_fresh(ha, torch, rows, dtype):
+    """Without the others' rows, the others' tokens count as old: what lies at their places is added to.  With them, their lse -inf, they start from 0."""
+    page, Hq, Hk, last = 16, 4, 2, 20
+    Q, cache, cu, table, L, ks, vs, new, lens = a_case(ha, torch, [(rows, 500)], Hq, Hk, 64, page, dtype)
+    _, lse = ha.ha_cache4_attn_chunk(Q, cache, cu, table, L, page)
+    before = torch.rand(cache.shape[0], Hk, page, device="cuda")
+    weights = before.clone()
+    q, l = Q[rows - last:], lse[:, rows - last:].contiguous()
+    ha.ha_cache4_weights(q, cache, ints(torch, [0, last]), table, L, l, weights, page)
+    check(torch, weights, before, q, l, ks, [last], table, page, False)
+    lse[:, :rows - last] = -float("inf")
+    weights = before.clone()
+    ha.ha_cache4_weights(Q, cache, cu, table, L, lse, weights, page)
+    check(torch, weights, before, Q, lse, ks, new, table, page, False)
