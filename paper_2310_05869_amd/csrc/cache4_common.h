@@ -98,6 +98,7 @@ void cache4_weights_split(CacheChunkArgs* a);  // sets div_group, narrow, few_wg
 constexpr int kWeightsParts = 512;             // workgroups that the chip holds at once, two per CU
 constexpr int kWeightsTokens = 256;            // of a tile
 
+constexpr int kEvictSeqs = 8192;               // of a call
 struct CacheEvictArgs {
   unsigned char* cache;
   const float* weights;

@@ -282,7 +282,7 @@ static int evict_geometry(const ha_cache4* shape, const ha_cache4_eviction* e, C
   const int rc = cache_geometry(shape, &a->c);
   if (rc != HA_OK) return rc;
   if (!e) return HA_ERR_NULL;
-  if (e->n_seq < 0 || e->n_seq > 8192 || e->max_blocks < 0 || e->recent < 0) return HA_ERR_SHAPE;
+  if (e->n_seq < 0 || e->n_seq > kEvictSeqs || e->max_blocks < 0 || e->recent < 0) return HA_ERR_SHAPE;
   if ((int64_t)e->n_seq * shape->Hk > (1 << 20) || (int64_t)e->n_seq * e->max_blocks > (1ll << 30)) return HA_ERR_SHAPE;
   if ((int64_t)e->max_blocks * shape->page > (1ll << 30)) return HA_ERR_SHAPE;
   a->n_seq = e->n_seq;
