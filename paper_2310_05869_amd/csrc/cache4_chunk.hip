@@ -25,7 +25,8 @@ typedef s16x4 __attribute__((address_space(3))) * lds_s16x4_ptr;
 
 constexpr int kStep = 64;           // tokens of a step
 // What a tile's start and end cost a workgroup, in tokens.  (128 / 256 / 400 / 600: 64 sequences, most of one token, behind up to 16384, 32 and 8 heads, d = 128 259 / 231 / 217 / 220 us;
-// 24 of up to 200 behind up to 4096, 12 and 4 heads 58 / 55 / 55 / 57; 16 of up to 1024 behind up to 8192, 16 heads, d = 64 118 / 106 / 108 / 109.)
+// 24 of up to 200 behind up to 4096, 12 and 4 heads 58 / 55 / 55 / 57; 16 of up to 1024 behind up to 8192, 16 heads, d = 64 118 / 106 / 108 / 109.  Later, 256 / 320 / 400: 64 with 8 pieces of
+// prompts 484 / 483 / 482; 24 of up to 200 77 / 76 / 75; fp32, 6 of up to 150 behind up to 4000, 8 and 2 heads, d = 128 53 / 52 / 61; one of 100 and one of 50 35 / 34 / 36.)
 constexpr int kTileCost = 320;
 static_assert(chunk_upto(0x7fffffff - 257, 1, 1, kTileCost) == 0x7fffffffll - 257 + kTileCost + 1);  // (the most tokens that a call may hold: past 32 bits)
 constexpr int kLeastRun = 256;      // tokens of the line that a workgroup takes, at least (fp32, 6 sequences of up to 150 behind up to 2000, d = 64: 512 36 us, 256 29)
@@ -775,15 +776,18 @@ __device__ __forceinline__ void cache4_chunk_join(const CacheChunkArgs& a, int p
   }
 }
 
-// Tables of few tokens: a workgroup per tile, and no second launch.  Sequences whose rows of a key head fit 16 are read with the waves of a workgroup on different tokens
-// (cache4_attn.h), where there can be several.
+// Tables of few tokens: a workgroup per tile, and no second launch (shared out -> a workgroup per tile: 64 sequences of 20 new behind up to 900, 32 and 8 heads, 50 -> 36 us, 60 of one and 4 of
+// 300 behind up to 700 51 -> 28, 17 behind 300 14.7 -> 10.2, a prompt of 1000 42 -> 30, but 60 behind 900, 8 and 2 heads, 23 -> 26; up to 2048 tokens: 60 behind 1800 23 -> 44, fp32 28 -> 74,
+// 32 of 60 behind up to 1800 72 -> 61).  Sequences whose rows of a key head fit 16 are read with the waves of a workgroup on different tokens (cache4_attn.h), where there can be several (64
+// that decode behind up to 16384 230 -> 127, 56 of them beside 8 pieces of prompts 605 -> 483, 60 beside 4 in short tables 40 -> 28, three, two of which decode behind 16000, 43 -> 28; of one and 300
+// 49.6 -> 49.0; where none has so few: 100 and 50 34.3 -> 35.4, fp32, six of up to 150, 27.3 -> 28.3).
 void cache4_chunk_split(CacheChunkArgs* a, CacheAttnArgs* narrow) {
   a->subs = (a->group + kChunkRows - 1) / kChunkRows;
   a->sub_group = (a->group + a->subs - 1) / a->subs;
   a->tile_tokens = kChunkRows / a->sub_group;
   a->div_tokens = make_fast_div(a->tile_tokens);
   a->div_heads = make_fast_div(a->sub_group);
-  a->narrow = a->group <= kNarrowRows && (a->n_seq >= 4 || (int64_t)a->rows * a->group <= (int64_t)kNarrowRows * a->n_seq) ? kNarrowRows : 0;
+  a->narrow = a->group <= kNarrowRows && (a->n_seq >= 2 || (int64_t)a->rows * a->group <= kNarrowRows) ? kNarrowRows : 0;
   narrow->parts = a->narrow ? (a->c.Hk < kChunkParts ? kChunkParts / a->c.Hk : 1) : 0;
   const int64_t tokens = (int64_t)a->max_blocks << a->c.log_page, heads = (int64_t)a->c.Hk * a->subs;
   const int64_t tiles = ((int64_t)a->rows / a->tile_tokens + a->n_seq) * heads;
