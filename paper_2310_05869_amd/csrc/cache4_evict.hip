@@ -23,8 +23,12 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kBins = 2048;
 constexpr int kMoveThreads = 256, kLastThreads = 1024;
-constexpr int kManyHeads = 256;  // sequences and key heads that fill the chip: a workgroup moves its own rows (64 of them, 3800 rows each: 70 us apart, 101 in one)
-constexpr int kFewLast = 512;  // last rows that move in the launch of the others (8 sequences that keep 4096 of 32768, 256 last ones: 63.6 us with one of their own, 59.4 in it)
+// Sequences and key heads that fill the chip: a workgroup moves its own rows.  (Launches apart / one: 64 of them, 3800 rows each, 70 / 101 us; 8 key heads, 4096 of 8192 with 128 last ones, 31, 48 and
+// 64 sequences 68 / 72, 121 / 131, 178 / 177; 4096 of 4160, 16, 28 and 64 sequences 15.4 / 12.3, 16.7 / 13.5, 24.4 / 20.7: which of both kinds it will be the host does not know.  Tables of up
+// to 2048 tokens are one launch too: 4 heads, 900 of 1900 14.9 / 14.0 us, 400 of 900 15.0 / 12.3, but 1900 of 3900 15.3 / 23.8.)
+constexpr int kManyHeads = 256;
+// Last rows that move in the launch of the others (8 sequences that keep 4096 of 32768, in a launch of their own / in it: 128 last ones 52 / 47 us, 256 53.5 / 48.6, 512 56.6 / 55.4, 1024 55.3 / 68)
+constexpr int kFewLast = 512;
 constexpr int kAhead = 8;  // rows that a lane has in flight
 constexpr int kSmall = 512;  // threads of a workgroup that chooses from up to 32 times as many places
 
