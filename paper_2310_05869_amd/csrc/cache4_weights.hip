@@ -24,8 +24,11 @@ constexpr int kWWaves = 4;
 constexpr int kWTokens = kWeightsTokens;
 static_assert(kWTokens == 64 * kWWaves);
 constexpr int kWRows = 64;              // of a step
-constexpr int kWTileCost = 2;           // what a tile's start and end cost, in steps
-constexpr int kWLeastRun = 8;           // steps that a workgroup takes, at least
+// What a tile's start and end cost, in steps.  (1 / 2 / 3 / 4: 2048 queries behind 16384, 32 and 8 heads, d = 128 347 / 343 / 338 / 334 us, fp32 1050 / 1050 / 1040 / 1029, 16 and 4 heads of d = 64,
+// fp32, 298 / 291 / 286 / 278; 64 mixed, most of one token, 280 / 286 / 288 / 290; 24 of up to 200 behind up to 4096 48 / 52 / 51 / 52.)
+constexpr int kWTileCost = 4;
+// Steps that a workgroup takes, at least.  (8 / 4 / 2: 600 queries behind 3000, 8 and 2 heads, 34 / 23 / 20 us; 200 behind 700, d = 64, 20 / 16 / 13; fp32, six of 200 46 / 34 / 28.)
+constexpr int kWLeastRun = 2;
 
 template <int D, int SPLIT>
 struct WeightsLds {
@@ -413,7 +416,7 @@ __global__ __launch_bounds__(kWTokens) void cache4_weights_join_kernel(CacheChun
 
 // ---- few rows ----
 constexpr int kNUnit = 64;       // tokens of a wave's step
-constexpr int kNStart = 3;       // what the start of a sequence and key head costs, in steps
+constexpr int kNStart = 3;       // what the start of a sequence and key head costs, in steps (0 / 3 / 8: 256 decoding behind up to 2048 16.2 / 16.3 / 18.0 us, 1000 of up to 512 21.4 / 21.8 / 23.5)
 struct FewSeq {
   ChunkSeq q;
   int rows, tiles, units;  // query rows, tiles of 16 of them, steps of 64 tokens (0: not of these)
@@ -595,10 +598,10 @@ __global__ __launch_bounds__(256, SPLIT == 1 ? 3 : 2) void cache4_weights_few_ke
 }
 
 // Which form takes a sequence goes by its own rows of a key head: up to 48 the one for few, where there can be several sequences (64 sequences of 32, 48, 64 and 128 rows, behind up to
-// 8192, 8 key heads, few / many: 65 / 98, 76 / 84, 100 / 89, 180 / 135 us; one sequence or three: the launch for few rows costs 2.4).  The host knows the batch's rows alone; where these are few in all,
-// the form for few takes everything, in one launch instead of three (32 decoding of up to 1000: 9 / 16 us, 64 of up to 16384 77 / 81, 512 of up to 4096 166 / 172), as one sequence may
-// then have no more (63 decoding and one of n x 4 rows, behind up to 8192, 8 key heads: n = 128 51 / 65 us, 200 71 / 71, 400 114 / 82; fp32 118 / 127, 163 / 135; 511 and one of 2048 x 4: 665 / 288).
-// One sequence alone crosses earlier (behind 16384, 8 key heads, 128, 256, 512, 1024 rows: 17 / 20, 27 / 29, 46 / 39, 83 / 64; fp32, d = 64, 256 rows 32 / 24).
+// 8192, 8 key heads, few / many: 65 / 95, 69 / 81, 95 / 82, 176 / 134 us; where none has so few, its launch costs 2 to 3).  The host knows the batch's rows alone; where these are few in
+// all, the form for few takes everything, in one launch instead of three (32 decoding of up to 1000: 10 / 16 us, 64 of up to 16384 77 / 80, 512 of up to 4096 166 / 172), as one sequence may
+// then have no more (63 decoding and one of n x 4 rows, behind up to 8192, 8 key heads: n = 128 51 / 58 us, 200 70 / 70, 400 114 / 82; fp32 118 / 117, 163 / 140; 511 and one of 2048 x 4: 665 / 283).
+// One sequence alone crosses earlier (behind 16384, 8 key heads, 128, 256, 512, 1024 rows: 17 / 18, 27 / 25, 45 / 39, 83 / 65; fp32, d = 64, 256 rows 33 / 17).
 constexpr int kFewRows = 48, kAllFew = 128, kAllFewShared = 1024;
 void cache4_weights_split(CacheChunkArgs* a) {
   a->div_group = make_fast_div(a->group);
