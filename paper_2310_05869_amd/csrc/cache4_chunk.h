@@ -43,6 +43,9 @@ __host__ __device__ constexpr int64_t chunk_upto(int held, int tile_tokens, int6
   return t * ((int64_t)(held > 0 ? held : 0) + tile_cost) + tile_tokens * (t * (t + 1) / 2);
 }
 
+// Scale i of a token's, as the conversions take it
+__device__ inline float scale_of(uint32_t bytes, int i) { return __uint_as_float(i < 3 ? bytes << (23 - 8 * i) : bytes >> 1); }  // (the exponent alone counts)
+
 // Where run p of `parts` begins on a line.  (Rounded down from a product in double, by every workgroup alike; a division of 64 bits takes a microsecond.)
 __device__ inline int64_t run_begin(int64_t total, int parts, int p) { return p >= parts ? total : (int64_t)((double)total * ((double)p / (double)parts)); }
 

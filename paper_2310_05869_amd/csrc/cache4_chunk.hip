@@ -56,8 +56,6 @@ struct RawV {
   std::conditional_t<D == 128, u32x4, uint32_t> sc;
 };
 
-__device__ inline float scale_of(uint32_t bytes, int i) { return __uint_as_float(i < 3 ? bytes << (23 - 8 * i) : bytes >> 1); }  // (the exponent alone counts)
-
 template <int SEL>
 __device__ inline uint32_t two_values(uint32_t w, float sc) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc, SEL));

@@ -63,8 +63,6 @@ __device__ inline int64_t weights_upto(const CacheChunkArgs& a, const WeightsSeq
   return x;
 }
 
-__device__ inline float scale_of(uint32_t bytes, int i) { return __uint_as_float(i < 3 ? bytes << (23 - 8 * i) : bytes >> 1); }  // (the exponent alone counts)
-
 // SPLIT: parts of a query number, 1 for bf16, 3 for fp32
 template <int D, int SPLIT>
 __global__ __launch_bounds__(64 * kWWaves, 2) void cache4_weights_kernel(CacheChunkArgs a) {
