@@ -3,7 +3,9 @@
 // One pass over the keys with a running reference and sum of the softmax, as in attn_mfma.hip: a wave keeps 32 query rows, S^T = K Q^T by
 // v_mfma_f32_32x32x16_bf16 over 64 tokens a step, the weights are the B operand of O^T += V^T P^T.  What differs is where tiles come from: the query
 // heads of a key head and some tokens of theirs share a workgroup (128 rows), which turns the codes of a step into bf16 once, in registers, and lays them
-// into LDS for its four waves.  Cached values are exact in bf16, so products are those of bf16 tensors.
+// into LDS for its four waves.  Cached values are exact in bf16, so products are those of bf16 tensors.  Weights of bf16 queries enter P V rounded to bf16 once, by at most 2^-8 of each (the
+// row's sum is of unrounded ones): the instruction's other operand is exact in bf16, and two parts would be twice the products.  Results lie 1.7 to 2.3e-3 from those of 64 bits, where
+// rounding them to bf16 is 1.6e-3.  Weights of fp32 queries have three parts, 24 bits.
 //   * A wave takes the K codes, V codes and scales of 16 tokens, which lie in one page: a uniform base.  v_cvt_scalef32_pk_bf16_fp4 makes two values of a
 //     byte, scale included; a lane's words become whole pieces of 16 bytes of LDS rows, because channels may lie in any order that the other
 //     operand shares: K's rows hold the page's words in their order, Q is loaded alike; V's rows hold a word's eight channels together, and

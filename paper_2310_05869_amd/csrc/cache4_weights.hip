@@ -1,7 +1,8 @@
 // What attention weight the tokens of the 4-bit cache got from new queries (ha_cache4_weights): w[t] += sum over the rows that see token t, and the query heads of
 // its key head, of exp(<q, k_t> - lse).
 //
-// A second pass over K alone, after attention has found lse: nothing is rounded, and no sum depends on the order of workgroups, which sums added up beside P V by
+// A second pass over K alone, after attention has found lse: nothing is rounded below fp32 (-lse log2 e once, up front, so that a weight's exponent is one multiply-add: 1.7e-7
+// from 64 bits where 6e-8 is the plain form's), and no sum depends on the order of workgroups, which sums added up beside P V by
 // all workgroups of a head would.  S = Q K^T has rows of Q along the matrix instructions' M, tokens along N: a lane's registers are rows of one token, whose sum
 // takes additions alone and one or two exchanges at the end.
 //   many rows   a wave keeps the K of 64 tokens as operands in registers, made from codes once, and rows of Q pass by, 64 a step, in LDS for the four waves of a
@@ -596,16 +597,18 @@ __global__ __launch_bounds__(256, SPLIT == 1 ? 3 : 2) void cache4_weights_few_ke
 }
 
 // Which form takes a sequence goes by its own rows of a key head: up to 48 the one for few, where there can be several sequences (64 sequences of 32, 48, 64 and 128 rows, behind up to
-// 8192, 8 key heads, few / many: 65 / 95, 69 / 81, 95 / 82, 176 / 134 us; where none has so few, its launch costs 2 to 3).  The host knows the batch's rows alone; where these are few in
-// all, the form for few takes everything, in one launch instead of three (32 decoding of up to 1000: 10 / 16 us, 64 of up to 16384 77 / 80, 512 of up to 4096 166 / 172), as one sequence may
-// then have no more (63 decoding and one of n x 4 rows, behind up to 8192, 8 key heads: n = 128 51 / 58 us, 200 70 / 70, 400 114 / 82; fp32 118 / 117, 163 / 140; 511 and one of 2048 x 4: 665 / 283).
+// 8192, 8 key heads, few / many: 65 / 95, 69 / 81, 95 / 82, 176 / 134 us; where none has so few, its launch costs 2 to 3).  The host knows the batch's rows and the table's tokens, no more
+// of which one sequence can have new.  Where both leave a sequence few rows, the form for few takes everything, in one launch instead of three (32 decoding of up to 1000: 10 / 16 us, 64 of
+// up to 16384 77 / 80, 176 of up to 46, most of one new token 12.7 / 25, but 300 of up to 1000, which are more rows than that, 28 / 33), as one sequence may have no more (63 decoding and one
+// of n x 4 rows, behind up to 8192, 8 key heads: n = 128 51 / 58 us, 200 70 / 70, 400 114 / 82; fp32 118 / 117, 163 / 140; 511 and one of 2048 x 4: 665 / 283).
 // One sequence alone crosses earlier (behind 16384, 8 key heads, 128, 256, 512, 1024 rows: 17 / 18, 27 / 25, 45 / 39, 83 / 65; fp32, d = 64, 256 rows 33 / 17).
 constexpr int kFewRows = 48, kAllFew = 128, kAllFewShared = 1024;
 void cache4_weights_split(CacheChunkArgs* a) {
   a->div_group = make_fast_div(a->group);
   const int64_t tokens = (int64_t)a->max_blocks << a->c.log_page, rows = (int64_t)a->rows * a->group, steps = (rows + kWRows - 1) / kWRows;
   const int64_t heads = (int64_t)a->n_seq * a->c.Hk;
-  a->narrow = rows <= kAllFew || (rows <= kAllFewShared && rows <= 32 * (int64_t)a->n_seq) ? 0x7fffffff : a->n_seq >= 4 ? kFewRows : -1;
+  const int64_t most = rows < tokens * a->group ? rows : tokens * a->group;  // of a sequence
+  a->narrow = rows <= kAllFew || (most <= kAllFewShared && rows <= 32 * (int64_t)a->n_seq) ? 0x7fffffff : a->n_seq >= 4 ? kFewRows : -1;
   const int64_t units = (tokens + kNUnit - 1) / kNUnit * heads * (steps < 1 ? 1 : steps * 4);
   a->few_wgs = a->narrow < 0 ? 0 : (int32_t)(units / 4 + 1 > 768 ? 768 : units / 4 + 1);
   const int64_t runs = (tokens + kWTokens - 1) / kWTokens * heads * (steps + kWTileCost) / kWLeastRun;

@@ -209,6 +209,7 @@ def test_weights_of_a_batch_of_many_rows_go_by_every_sequence(ha):
     for n_seq, rows, most in ((512, 511 + 2048, 400), (200, 199 + 600, 1000), (64, 64 * 8, 256)):
         assert need(cache(Hk=8, d=128, page=64), chunk(n_seq, rows, 64, 0, most)) > 0, (n_seq, rows)
     assert need(cache(Hk=8, d=128, page=64), chunk(64, 64, 32, 0, 256)) == 0   # a decoding step
+    assert need(cache(Hk=8, d=128, page=64), chunk(1000, 1000, 32, 0, 4)) == 0   # (no sequence of 256 tokens can have more new ones)
 
 
 def test_numbers_that_eviction_writes_lie_apart_from_those_it_reads(ha):
